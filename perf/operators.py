@@ -20,42 +20,42 @@ EPS = 1e-5
 def listed():
     return [
         # one serving batch of pooled rows, normalised for the next product: latency counts
-        {"name": "norm forward, serving rows", "op": "norm", "direction": "forward", "rows": 26, "cols": 128,
+        {"name": "norm forward serving rows", "op": "norm", "direction": "forward", "rows": 26, "cols": 128,
          "type": "f32", "to": "bf16"},
         # every pooled row of a Criteo-TB-shaped training batch, normalised as it leaves the embedding
-        {"name": "norm forward, pooled batch", "op": "norm", "direction": "forward", "rows": 65536 * 26, "cols": 128,
+        {"name": "norm forward pooled batch", "op": "norm", "direction": "forward", "rows": 65536 * 26, "cols": 128,
          "type": "f32", "to": "bf16"},
         # the concatenated row of all 26 tables, gradient into the embedding and into the norm's weights
-        {"name": "norm backward, concatenated", "op": "norm", "direction": "backward", "rows": 16384,
+        {"name": "norm backward concatenated", "op": "norm", "direction": "backward", "rows": 16384,
          "cols": 26 * 128, "type": "f32", "to": "f32"},
         # an odd width, 16-bit activations inside the encoder, gradient with the weights' reduction
-        {"name": "norm backward, odd width", "op": "norm", "direction": "backward", "rows": 40001, "cols": 333,
+        {"name": "norm backward odd width", "op": "norm", "direction": "backward", "rows": 40001, "cols": 333,
          "type": "bf16", "to": "bf16"},
         # dropout of one small batch's rows, odd in both sizes and cut out of a wider buffer
-        {"name": "dropout, small cut-out", "op": "dropout", "rows": 127, "cols": 129, "type": "f16", "p": 0.5,
+        {"name": "dropout small cut-out", "op": "dropout", "rows": 127, "cols": 129, "type": "f16", "p": 0.5,
          "residual": False, "gap": 31},
         # dropout of the pooled rows of a training batch in the embedding's own type
-        {"name": "dropout, pooled batch", "op": "dropout", "rows": 65536 * 26, "cols": 128, "type": "f32", "p": 0.1,
+        {"name": "dropout pooled batch", "op": "dropout", "rows": 65536 * 26, "cols": 128, "type": "f32", "p": 0.1,
          "residual": False, "gap": 0},
         # a sublayer's output dropped out and added onto the residual stream
         {"name": "dropout onto residual", "op": "dropout", "rows": 262144, "cols": 512, "type": "bf16", "p": 0.2,
          "residual": True, "gap": 0},
         # serving: the newest item of one user against a short history
-        {"name": "attention step, one user", "op": "attention", "direction": "forward", "sequences": 1, "shortest": 200,
+        {"name": "attention step one user", "op": "attention", "direction": "forward", "sequences": 1, "shortest": 200,
          "longest": 200, "queries": 1, "heads": 4, "kv_heads": 4, "dim": 64, "causal": True, "fused": False},
         # serving: the newest item of each user against long histories, shared key heads
-        {"name": "attention step, long", "op": "attention", "direction": "forward", "sequences": 48, "shortest": 512,
+        {"name": "attention step long", "op": "attention", "direction": "forward", "sequences": 48, "shortest": 512,
          "longest": 16384, "queries": 1, "heads": 16, "kv_heads": 4, "dim": 128, "causal": True, "fused": False},
         # training on packed histories of very different lengths, some of them empty
-        {"name": "attention train, histories", "op": "attention", "direction": "train", "sequences": 1024,
+        {"name": "attention train histories", "op": "attention", "direction": "train", "sequences": 1024,
          "shortest": 0, "longest": 401, "queries": 0, "heads": 4, "kv_heads": 4, "dim": 64, "causal": True,
          "fused": True},
         # prefill of long sequences
-        {"name": "attention forward, long", "op": "attention", "direction": "forward", "sequences": 3,
+        {"name": "attention forward long", "op": "attention", "direction": "forward", "sequences": 3,
          "shortest": 4096, "longest": 8192, "queries": 0, "heads": 16, "kv_heads": 4, "dim": 128, "causal": True,
          "fused": True},
         # training on long sequences, shared key heads: the largest
-        {"name": "attention train, long", "op": "attention", "direction": "train", "sequences": 4, "shortest": 2000,
+        {"name": "attention train long", "op": "attention", "direction": "train", "sequences": 4, "shortest": 2000,
          "longest": 7777, "queries": 0, "heads": 16, "kv_heads": 4, "dim": 128, "causal": True, "fused": True},
     ]
 
