@@ -387,6 +387,73 @@ pss_status pss_check_convert(int32_t direction, const void* in, void* out, int64
 pss_status pss_probe_l2(int32_t kind, void* buf, int64_t bytes, int64_t iters, int32_t ctas,
                         pss_stream stream);
 
+/*
+ * Operators of a sequence encoder over the pooled embeddings (the paper stops at
+ * the embedding; these serve a model that attends inside each history of ids).
+ * They need no handle and allocate nothing: the caller passes every buffer,
+ * all in DEVICE memory of the current device (host pointers are rejected), and
+ * the calls are asynchronous on `stream`.  A size of zero is valid and queues
+ * no work that reads or writes the empty tensors.
+ */
+
+/* Element types of these operators. */
+typedef enum { PSS_F32 = 0, PSS_BF16 = 1, PSS_F16 = 2 } pss_dtype;
+
+/*
+ * Layer norm of each row of x[rows][cols]:
+ *   mean = sum_c x / cols,   rstd = 1 / sqrt(sum_c (x - mean)^2 / cols + eps),
+ *   y = (x - mean) * rstd * weight[c] + bias[c].
+ * Rows are `x_stride` / `y_stride` elements apart (>= cols).  Statistics are
+ * fp32 (the variance from the differences, not from the squares); y is rounded
+ * once to y_type.  y may be x where types and strides are equal.
+ *   weight, bias: fp32[cols].  mean, rstd: fp32[rows], for the backward pass.
+ * cols: 1 .. 16384 (PSS_ERR_UNSUPPORTED above); eps >= 0.
+ * Errors: PSS_ERR_INVALID_ARG, PSS_ERR_UNSUPPORTED, PSS_ERR_CUDA.
+ */
+pss_status pss_layer_norm_forward(const void* x, pss_dtype x_type, int64_t x_stride,
+                                  const float* weight, const float* bias, int64_t rows,
+                                  int64_t cols, float eps, void* y, pss_dtype y_type,
+                                  int64_t y_stride, float* mean, float* rstd, pss_stream stream);
+
+/*
+ * Its backward pass, with g = grad * weight and h = (x - mean) * rstd:
+ *   dx = rstd * (g - sum_c g / cols - h * sum_c (g * h) / cols)   (type x_type),
+ *   dweight[c] = sum over rows of grad * h,   dbias[c] = sum over rows of grad.
+ * dx may be x or (equal types) grad.  dweight and dbias are overwritten; their
+ * sums run in a fixed order, so equal inputs give equal bits on one GPU model.
+ *   workspace: device memory of at least pss_layer_norm_workspace(rows, cols)
+ *   bytes, 16-byte aligned; its contents mean nothing between calls.
+ */
+int64_t pss_layer_norm_workspace(int64_t rows, int64_t cols);
+pss_status pss_layer_norm_backward(const void* grad, pss_dtype grad_type, int64_t grad_stride,
+                                   const void* x, pss_dtype x_type, int64_t x_stride,
+                                   const float* weight, const float* mean, const float* rstd,
+                                   int64_t rows, int64_t cols, void* dx, int64_t dx_stride,
+                                   float* dweight, float* dbias, void* workspace,
+                                   int64_t workspace_bytes, pss_stream stream);
+
+/*
+ * Dropout with a mask that is never stored:
+ *   y[r][c] = (keep(r*cols + c) ? x[r][c] / (1 - p') : 0)  [+ residual[r][c]].
+ * keep(e): the generator Philox4x32-10 (Salmon, Moraes, Dror & Shaw 2011) with
+ * key `seed` and counter (e / 8, offset), both 64-bit words low half first,
+ * gives four 32-bit words, i.e. eight 16-bit values (low half of each word
+ * first); e is kept when value e % 8 >= t, t = p * 65536 rounded to nearest
+ * even, and p' = t / 65536.  The mask depends on seed, offset and the logical
+ * position only, so the backward pass is the same call on the gradient,
+ * without the residual.  Calls with different offsets are independent.
+ * 16 bits a value: one generator call serves eight elements (with 32 bits a
+ * value the 16-bit types would be bound by the generator, not by memory).
+ *   p in [0, 1]; p' = 0 keeps everything, p' = 1 gives zeros (a dropped element
+ *   contributes exactly 0, whatever x holds there, also infinities and NaN).
+ *   residual: NULL, or the same type as x and y.  y may be x or residual
+ *   where the strides are equal.  Sums are fp32, rounded once.
+ */
+pss_status pss_dropout(const void* x, int64_t x_stride, const void* residual,
+                       int64_t residual_stride, int64_t rows, int64_t cols, double p,
+                       uint64_t seed, uint64_t offset, pss_dtype type, void* y, int64_t y_stride,
+                       pss_stream stream);
+
 #ifdef __cplusplus
 }
 #endif

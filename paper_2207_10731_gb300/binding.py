@@ -41,7 +41,8 @@ EXPORTS = [
     "pss_set_state", "pss_compute_locations", "pss_forward", "pss_backward_update",
     "pss_backward_grad", "pss_set_option", "pss_get_option", "pss_get_error", "pss_get_info",
     "pss_get_profile", "pss_reset_profile", "pss_status_string", "pss_grad_noalloc",
-    "pss_check_convert", "pss_probe_l2",
+    "pss_check_convert", "pss_probe_l2", "pss_layer_norm_forward", "pss_layer_norm_workspace",
+    "pss_layer_norm_backward", "pss_dropout",
 ]
 
 
@@ -79,6 +80,7 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
         lib = ctypes.CDLL(p)
         vp, i32, i64, u64, f32 = (ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64,
                                   ctypes.c_uint64, ctypes.c_float)
+        f64 = ctypes.c_double
         sigs = {
             "pss_create": [vp, i32, i32, i64, i32, i32, u64, ctypes.c_int, f32, vp, vp],
             "pss_destroy": [vp],
@@ -100,11 +102,18 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
                                  vp],
             "pss_check_convert": [i32, vp, vp, i64, vp],
             "pss_probe_l2": [i32, vp, i64, i64, i32, vp],
+            "pss_layer_norm_forward": [vp, i32, i64, vp, vp, i64, i64, f32, vp, i32, i64, vp, vp,
+                                       vp],
+            "pss_layer_norm_backward": [vp, i32, i64, vp, i32, i64, vp, vp, vp, i64, i64, vp, i64,
+                                        vp, vp, vp, i64, vp],
+            "pss_dropout": [vp, i64, vp, i64, i64, i64, f64, u64, u64, i32, vp, i64, vp],
         }
         for name, args in sigs.items():
             fn = getattr(lib, name)
             fn.argtypes = args
             fn.restype = ctypes.c_int
+        lib.pss_layer_norm_workspace.argtypes = [i64, i64]
+        lib.pss_layer_norm_workspace.restype = i64
         lib.pss_status_string.argtypes = [ctypes.c_int]
         lib.pss_status_string.restype = ctypes.c_char_p
         _lib = lib

@@ -1,0 +1,159 @@
+"""Operators of a sequence encoder over the pooled embeddings: layer norm and
+dropout (argument marshalling only, like ``binding``; the kernels
+are in libpss.so, their contracts in include/pss.h).
+
+All tensors are CUDA tensors of the current device; calls are asynchronous on
+``stream`` (default: the current stream).  Nothing is kept between calls.
+Gradients are explicit calls: there is no autograd graph here.
+"""
+from __future__ import annotations
+
+from . import binding
+
+_lib = None
+_types = None
+
+
+def _library():
+    global _lib, _types
+    if _lib is None:
+        torch = binding._torch()
+        _types = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}   # pss_dtype
+        _lib = binding.load_library()
+    return _lib
+
+
+def _stream(stream):
+    if stream is None:
+        stream = binding._torch().cuda.current_stream()
+    return stream.cuda_stream
+
+
+def _device_tensor(t, name):
+    torch = binding._torch()
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} must be on the current CUDA device")
+    return t
+
+
+def _rows(t, name, like=None, dtype=None):
+    """(rows, cols, stride) of a tensor seen as rows of its last dimension,
+    which must be dense; the leading dimensions must be one stride apart."""
+    _device_tensor(t, name)
+    if t.dtype not in _types:
+        raise TypeError(f"{name} must be float32, bfloat16 or float16, got {t.dtype}")
+    if dtype is not None and t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if like is not None and t.shape != like.shape:
+        raise ValueError(f"{name} must have shape {tuple(like.shape)}, got {tuple(t.shape)}")
+    if t.dim() == 0:
+        raise ValueError(f"{name} must have at least one dimension")
+    cols = t.shape[-1]
+    if t.is_contiguous():
+        return (t.numel() // cols if cols else 0), cols, cols
+    if cols > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{name} must be dense in its last dimension")
+    rows, stride = 1, None
+    for n, s in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):
+        if n == 1:
+            continue
+        if stride is None:
+            stride = s
+        elif s != stride * rows:
+            raise ValueError(f"{name}'s rows must be evenly spaced")
+        rows *= n
+    if t.numel() == 0:
+        return 0, cols, max(cols, 1)
+    if stride is None:
+        stride = cols
+    if stride < cols:
+        raise ValueError(f"{name}'s rows must not overlap")
+    return rows, cols, stride
+
+
+def _vector(t, n, name):
+    torch = binding._torch()
+    _device_tensor(t, name)
+    if t.dtype != torch.float32:
+        raise TypeError(f"{name} must be torch.float32, got {t.dtype}")
+    if t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous with {n} values")
+    return t.data_ptr()
+
+
+def layer_norm_forward(x, weight, bias, eps: float = 1e-5, out=None, out_dtype=None, stream=None):
+    """(y, mean, rstd) of the layer norm over x's last dimension
+    (pss_layer_norm_forward).  ``x``: float32, bfloat16 or float16, rows evenly
+    spaced; ``weight``, ``bias``: float32.  y has ``out_dtype`` (default: x's)
+    or is ``out``; mean and rstd are float32, for the backward call."""
+    lib = _library()
+    torch = binding._torch()
+    rows, cols, xs = _rows(x, "x")
+    if out is None:
+        out = torch.empty(x.shape, dtype=out_dtype or x.dtype, device=x.device)
+    elif out_dtype is not None and out.dtype != out_dtype:
+        raise TypeError(f"out must be {out_dtype}, got {out.dtype}")
+    _, _, ys = _rows(out, "out", like=x)
+    mean = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
+    rstd = torch.empty_like(mean)
+    binding._check(lib.pss_layer_norm_forward(
+        x.data_ptr(), _types[x.dtype], xs, _vector(weight, cols, "weight"),
+        _vector(bias, cols, "bias"), rows, cols, eps, out.data_ptr(), _types[out.dtype], ys,
+        mean.data_ptr(), rstd.data_ptr(), _stream(stream)), "pss_layer_norm_forward")
+    return out, mean, rstd
+
+
+def layer_norm_backward(grad, x, weight, mean, rstd, out=None, stream=None):
+    """(dx, dweight, dbias) for the upstream gradient ``grad`` of the y of
+    ``layer_norm_forward(x, weight, ...)`` (pss_layer_norm_backward).  dx has
+    x's type or is ``out``; dweight and dbias are float32."""
+    lib = _library()
+    torch = binding._torch()
+    rows, cols, xs = _rows(x, "x")
+    _, _, gs = _rows(grad, "grad", like=x)
+    if out is None:
+        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    _, _, ds = _rows(out, "out", like=x, dtype=x.dtype)
+    both = torch.empty((2, cols), dtype=torch.float32, device=x.device)
+    size = lib.pss_layer_norm_workspace(rows, cols)
+    work = torch.empty(size, dtype=torch.uint8, device=x.device)
+    binding._check(lib.pss_layer_norm_backward(
+        grad.data_ptr(), _types[grad.dtype], gs, x.data_ptr(), _types[x.dtype], xs,
+        _vector(weight, cols, "weight"), _vector(mean, rows, "mean"), _vector(rstd, rows, "rstd"),
+        rows, cols, out.data_ptr(), ds, both.data_ptr(), both.data_ptr() + 4 * cols,
+        work.data_ptr(), size, _stream(stream)), "pss_layer_norm_backward")
+    _used_on(stream, work)
+    return out, both[0], both[1]
+
+
+def _used_on(stream, *tensors):
+    """Scratch of this module that a stream other than the current one still
+    uses when the call returns: the allocator must not hand it out before."""
+    if stream is not None:
+        for t in tensors:
+            t.record_stream(stream)
+
+
+def dropout(x, p: float, seed: int, offset: int = 0, residual=None, out=None, stream=None):
+    """x with each element zeroed with probability p and the others divided by
+    1 - p, plus ``residual`` (pss_dropout).  The mask follows from (seed,
+    offset, position) alone and is not stored: the backward pass is the same
+    call on the gradient, without the residual.  seed and offset are unsigned
+    64-bit; give each call of a step an offset of its own."""
+    lib = _library()
+    torch = binding._torch()
+    rows, cols, xs = _rows(x, "x")
+    rs = 0
+    if residual is not None:
+        _, _, rs = _rows(residual, "residual", like=x, dtype=x.dtype)
+    if out is None:
+        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    _, _, ys = _rows(out, "out", like=x, dtype=x.dtype)
+    if not (0 <= seed < 2**64 and 0 <= offset < 2**64):
+        raise ValueError("seed and offset must be unsigned 64-bit integers")
+    binding._check(lib.pss_dropout(
+        x.data_ptr(), xs, None if residual is None else residual.data_ptr(), rs, rows, cols, p,
+        seed, offset, _types[x.dtype], out.data_ptr(), ys, _stream(stream)), "pss_dropout")
+    return out
