@@ -391,9 +391,9 @@ pss_status pss_probe_l2(int32_t kind, void* buf, int64_t bytes, int64_t iters, i
  * Operators of a sequence encoder over the pooled embeddings (the paper stops at
  * the embedding; these serve a model that attends inside each history of ids).
  * They need no handle and allocate nothing: the caller passes every buffer,
- * all in DEVICE memory of the current device (host pointers are rejected), and
- * the calls are asynchronous on `stream`.  A size of zero is valid and queues
- * no work that reads or writes the empty tensors.
+ * all in DEVICE memory of the current device (host pointers are rejected),
+ * and the calls are asynchronous on `stream`.  A size of zero is valid and
+ * nothing reads or writes the empty tensors.
  */
 
 /* Element types of these operators. */
@@ -453,6 +453,76 @@ pss_status pss_dropout(const void* x, int64_t x_stride, const void* residual,
                        int64_t residual_stride, int64_t rows, int64_t cols, double p,
                        uint64_t seed, uint64_t offset, pss_dtype type, void* y, int64_t y_stride,
                        pss_stream stream);
+
+/*
+ * Attention inside each sequence of a packed batch (softmax(scale q k^T) v),
+ * with grouped heads.  Sequence s owns the query rows q_offsets[s] ..
+ * q_offsets[s+1] and the key rows k_offsets[s] .. k_offsets[s+1]; its query i
+ * (of nq) sees its key j (of nk) where
+ *   causal = 0: always;      causal = 1: j <= i + nk - nq
+ * (the queries stand at the end of the sequence: nq = nk is training or a
+ * prompt, nq = 1 the step of one new token).  Query head h reads key head
+ * h / (heads / kv_heads).  A query that sees no key gives a zero row, lse =
+ * -infinity and no gradient.
+ */
+typedef struct {
+    int64_t sequences;          /* >= 0 */
+    const int64_t* q_offsets;   /* device, sequences + 1, non-decreasing, 0 .. q_tokens */
+    const int64_t* k_offsets;   /* device, sequences + 1, non-decreasing, 0 .. k_tokens;
+                                   may be q_offsets */
+    int64_t q_tokens, k_tokens; /* rows of q and of k; below 2^31 - 1024 */
+    int32_t heads, kv_heads;    /* heads = kv_heads * group, group 1 .. 128 */
+    int32_t dim;                /* values of a head: a multiple of 8, 8 .. 128 */
+    int32_t causal;             /* 0 or 1 */
+    float scale;                /* > 0, finite */
+} pss_attention_shape;
+
+/* Rows of bf16 values: element (token, head, c) at data[token * token_stride +
+ * head * head_stride + c].  16-byte aligned, strides multiples of 8 and large
+ * enough that rows do not overlap (only the stride over a size of one is free);
+ * q, k and v may be views of one buffer. */
+typedef struct {
+    void* data;
+    int64_t token_stride, head_stride;
+} pss_rows;
+
+/*
+ * out = attention (rows of q's sizes), lse[token][head] = log of the softmax's
+ * denominator (fp32, natural logarithm of sum_j exp(scale q.k_j)).
+ *   Scores, softmax statistics and sums are fp32; the probabilities enter the
+ *   second product as bf16, as its other operand v, and out is rounded once.
+ *   workspace: device, 16-byte aligned, at least
+ *   pss_attention_workspace(shape, 0) bytes (the work list, and partial sums
+ *   where few queries meet long sequences); means nothing between calls.
+ *   status: NULL or device int64[1], set to -1, to the smallest sequence with
+ *   malformed offsets (it is treated as empty; its rows are left unwritten),
+ *   or to -2 when a bounded wait gave up (the outputs are then invalid).
+ * Rows outside every sequence are left unwritten.  Equal inputs give equal
+ * bits.  A masked key or value changes nothing, also where it is infinite or
+ * NaN, and neither does another sequence's.
+ * Errors: PSS_ERR_INVALID_ARG (sizes, strides, alignment, host pointers, a
+ * small workspace), PSS_ERR_CUDA.
+ */
+int64_t pss_attention_workspace(const pss_attention_shape* shape, int32_t backward);
+pss_status pss_attention_forward(const pss_attention_shape* shape, const pss_rows* q,
+                                 const pss_rows* k, const pss_rows* v, const pss_rows* out,
+                                 float* lse, void* workspace, int64_t workspace_bytes,
+                                 int64_t* status, pss_stream stream);
+
+/*
+ * Its backward pass, for the out and lse of the forward call, with
+ *   p = exp(scale q.k - lse),  dp = grad.v,  ds = p (dp - sum_c grad out):
+ *   dq = scale sum_j ds k_j,  dk = scale sum_i ds q_i,  dv = sum_i p grad_i
+ * (dk and dv also summed over the heads that share them), overwritten.  p and
+ * ds enter their second products as bf16; sums are fp32, in a fixed order.
+ * dq, dk, dv may be views of one buffer, and may not overlap the inputs.
+ * workspace: at least pss_attention_workspace(shape, 1) bytes.
+ */
+pss_status pss_attention_backward(const pss_attention_shape* shape, const pss_rows* grad,
+                                  const pss_rows* q, const pss_rows* k, const pss_rows* v,
+                                  const pss_rows* out, const float* lse, const pss_rows* dq,
+                                  const pss_rows* dk, const pss_rows* dv, void* workspace,
+                                  int64_t workspace_bytes, int64_t* status, pss_stream stream);
 
 #ifdef __cplusplus
 }

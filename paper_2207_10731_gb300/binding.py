@@ -42,7 +42,8 @@ EXPORTS = [
     "pss_backward_grad", "pss_set_option", "pss_get_option", "pss_get_error", "pss_get_info",
     "pss_get_profile", "pss_reset_profile", "pss_status_string", "pss_grad_noalloc",
     "pss_check_convert", "pss_probe_l2", "pss_layer_norm_forward", "pss_layer_norm_workspace",
-    "pss_layer_norm_backward", "pss_dropout",
+    "pss_layer_norm_backward", "pss_dropout", "pss_attention_workspace", "pss_attention_forward",
+    "pss_attention_backward",
 ]
 
 
@@ -55,6 +56,21 @@ class PSSInfo(ctypes.Structure):
                 ("last_collision_rate", ctypes.c_double), ("A2", ctypes.c_uint64),
                 ("B2", ctypes.c_uint64), ("signed_hash", ctypes.c_int64),
                 ("circular", ctypes.c_int64), ("last_update", ctypes.c_int64)]
+
+
+class AttentionShape(ctypes.Structure):
+    """pss_attention_shape."""
+    _fields_ = [("sequences", ctypes.c_int64), ("q_offsets", ctypes.c_void_p),
+                ("k_offsets", ctypes.c_void_p), ("q_tokens", ctypes.c_int64),
+                ("k_tokens", ctypes.c_int64), ("heads", ctypes.c_int32),
+                ("kv_heads", ctypes.c_int32), ("dim", ctypes.c_int32), ("causal", ctypes.c_int32),
+                ("scale", ctypes.c_float)]
+
+
+class Rows(ctypes.Structure):
+    """pss_rows."""
+    _fields_ = [("data", ctypes.c_void_p), ("token_stride", ctypes.c_int64),
+                ("head_stride", ctypes.c_int64)]
 
 
 class PSSError(RuntimeError):
@@ -107,6 +123,8 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
             "pss_layer_norm_backward": [vp, i32, i64, vp, i32, i64, vp, vp, vp, i64, i64, vp, i64,
                                         vp, vp, vp, i64, vp],
             "pss_dropout": [vp, i64, vp, i64, i64, i64, f64, u64, u64, i32, vp, i64, vp],
+            "pss_attention_forward": [vp] * 7 + [i64, vp, vp],
+            "pss_attention_backward": [vp] * 11 + [i64, vp, vp],
         }
         for name, args in sigs.items():
             fn = getattr(lib, name)
@@ -114,6 +132,8 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
             fn.restype = ctypes.c_int
         lib.pss_layer_norm_workspace.argtypes = [i64, i64]
         lib.pss_layer_norm_workspace.restype = i64
+        lib.pss_attention_workspace.argtypes = [vp, i32]
+        lib.pss_attention_workspace.restype = i64
         lib.pss_status_string.argtypes = [ctypes.c_int]
         lib.pss_status_string.restype = ctypes.c_char_p
         _lib = lib

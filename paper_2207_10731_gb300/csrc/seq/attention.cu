@@ -1,0 +1,171 @@
+// Attention over packed sequences (pss_attention_* of pss.h): the C entry
+// points and the row-by-row kernels.
+#include <cmath>
+
+#include "attention_rows.cuh"
+
+using namespace pss;
+using namespace pss::seq;
+
+namespace {
+
+// The range of sequence s in `off`, empty where it is malformed.
+__device__ bool range_of(const int64_t* off, int64_t s, int64_t tokens, int* lo, int* hi) {
+    const int64_t a = off[s], b = off[s + 1];
+    const bool ok = a >= 0 && a <= b && b <= tokens;
+    *lo = ok ? (int)a : 0;
+    *hi = ok ? (int)b : 0;
+    return ok;
+}
+
+__global__ void __launch_bounds__(kThreads) k_attention_check(Attn a) {
+    pdl_prologue();
+    if (threadIdx.x == 0) *a.status = ~0ull;
+    __syncthreads();
+    for (int64_t s = threadIdx.x; s < a.sequences; s += kThreads) {
+        int lo, hi;
+        const bool q = range_of(a.q_off, s, a.q_tokens, &lo, &hi);
+        const bool k = range_of(a.k_off, s, a.k_tokens, &lo, &hi);
+        if (!q || !k) atomicMin(a.status, (unsigned long long)s);
+    }
+}
+
+// A warp per (row, head): rows of sequence blockIdx.y ...
+enum { FORWARD, DQ, DKV };
+template <int WHAT>
+__global__ void __launch_bounds__(kThreads) k_attention_rows(Attn a) {
+    pdl_prologue();
+    const int heads = WHAT == DKV ? a.kv_heads : a.heads;
+    for (int64_t s = blockIdx.y; s < a.sequences; s += gridDim.y) {
+        Where w;
+        const bool q = range_of(a.q_off, s, a.q_tokens, &w.q_lo, &w.q_hi);
+        const bool k = range_of(a.k_off, s, a.k_tokens, &w.k_lo, &w.k_hi);
+        if (!q || !k) continue;
+        const int lo = WHAT == DKV ? w.k_lo : w.q_lo;
+        const int64_t n = (int64_t)((WHAT == DKV ? w.k_hi : w.q_hi) - lo) * heads;
+        for (int64_t i = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5); i < n;
+             i += (int64_t)gridDim.x * kWarps) {
+            const int t = lo + (int)(i / heads), h = (int)(i % heads);
+            if (WHAT == FORWARD) forward_row(a, w, t, h);
+            if (WHAT == DQ) dq_row(a, w, t, h);
+            if (WHAT == DKV) dkv_row(a, w, t, h);
+        }
+    }
+}
+
+bool shape_ok(const pss_attention_shape* s) {
+    return s && s->sequences >= 0 && s->q_tokens >= 0 && s->k_tokens >= 0 &&
+           s->q_tokens < (int64_t(1) << 31) - 1024 && s->k_tokens < (int64_t(1) << 31) - 1024 &&
+           s->sequences < (int64_t(1) << 31) - 1024 && s->kv_heads >= 1 && s->heads >= 1 &&
+           s->heads % s->kv_heads == 0 && s->heads / s->kv_heads <= 128 && s->dim >= 8 &&
+           s->dim <= 128 && s->dim % 8 == 0 && (s->causal == 0 || s->causal == 1) &&
+           s->scale > 0.f && std::isfinite(s->scale);
+}
+
+// Checks one tensor; an empty one needs no memory.
+bool rows_ok(const pss_rows* r, int64_t tokens, int64_t heads, int64_t dim, Rows* out) {
+    if (!r) return false;
+    *out = Rows{static_cast<bf16*>(r->data), r->token_stride, r->head_stride};
+    if (tokens == 0) return true;
+    if (!device_ptr(r->data) || !aligned_to(r->data, 16)) return false;
+    const int64_t ts = r->token_stride, hs = r->head_stride;
+    if (ts < 0 || hs < 0 || ts % 8 || hs % 8) return false;
+    // rows must not overlap: the smaller stride holds a row, the larger all the others
+    if (heads == 1) return tokens == 1 || ts >= dim;
+    if (tokens == 1) return hs >= dim;
+    return hs >= dim && ts >= dim && (ts >= (heads - 1) * hs + dim || hs >= (tokens - 1) * ts + dim);
+}
+
+pss_status fill(const pss_attention_shape* s, const pss_rows* q, const pss_rows* k,
+                const pss_rows* v, const pss_rows* out, const float* lse, void* workspace,
+                int64_t workspace_bytes, int64_t* status, int backward, Attn* a) {
+    if (!shape_ok(s)) return PSS_ERR_INVALID_ARG;
+    *a = Attn{};
+    a->sequences = s->sequences;
+    a->q_off = s->q_offsets;
+    a->k_off = s->k_offsets;
+    a->q_tokens = (int)s->q_tokens;
+    a->k_tokens = (int)s->k_tokens;
+    a->heads = s->heads;
+    a->kv_heads = s->kv_heads;
+    a->group = s->heads / s->kv_heads;
+    a->dim = s->dim;
+    a->causal = s->causal;
+    a->scale = s->scale;
+    a->lse = const_cast<float*>(lse);
+    a->status = reinterpret_cast<unsigned long long*>(status);
+    if (status && !(device_ptr(status) && aligned_to(status, 8))) return PSS_ERR_INVALID_ARG;
+    if (s->sequences > 0 && (!device_ptr(s->q_offsets) || !device_ptr(s->k_offsets) ||
+                             !aligned_to(s->q_offsets, 8) || !aligned_to(s->k_offsets, 8)))
+        return PSS_ERR_INVALID_ARG;
+    if (!rows_ok(q, s->q_tokens, s->heads, s->dim, &a->q) ||
+        !rows_ok(k, s->k_tokens, s->kv_heads, s->dim, &a->k) ||
+        !rows_ok(v, s->k_tokens, s->kv_heads, s->dim, &a->v) ||
+        !rows_ok(out, s->q_tokens, s->heads, s->dim, &a->out))
+        return PSS_ERR_INVALID_ARG;
+    if (s->q_tokens > 0 && !(device_ptr(lse) && aligned_to(lse, 4))) return PSS_ERR_INVALID_ARG;
+    const int64_t need = pss_attention_workspace(s, backward);
+    if (need > 0 && (!device_ptr(workspace) || !aligned_to(workspace, 16) ||
+                     workspace_bytes < need))
+        return PSS_ERR_INVALID_ARG;
+    return PSS_OK;
+}
+
+template <int WHAT>
+cudaError_t launch_rows(const Attn& a, cudaStream_t st) {
+    const int64_t rows = (int64_t)(WHAT == DKV ? a.k_tokens : a.q_tokens) *
+                         (WHAT == DKV ? a.kv_heads : a.heads);
+    if (rows == 0 || a.sequences == 0) return cudaSuccess;
+    const int64_t y = a.sequences < 8192 ? a.sequences : 8192;
+    const int64_t x = (rows / y + kWarps) / kWarps;
+    return launch_k(k_attention_rows<WHAT>, dim3((unsigned)(x < 4096 ? x : 4096), (unsigned)y),
+                    dim3(kThreads), 0, st, a);
+}
+
+}  // namespace
+
+extern "C" int64_t pss_attention_workspace(const pss_attention_shape* s, int32_t backward) {
+    if (!shape_ok(s)) return 0;
+    (void)backward;
+    return 0;
+}
+
+extern "C" pss_status pss_attention_forward(const pss_attention_shape* shape, const pss_rows* q,
+                                            const pss_rows* k, const pss_rows* v,
+                                            const pss_rows* out, float* lse, void* workspace,
+                                            int64_t workspace_bytes, int64_t* status,
+                                            pss_stream stream) {
+    Attn a;
+    const pss_status rc =
+        fill(shape, q, k, v, out, lse, workspace, workspace_bytes, status, 0, &a);
+    if (rc != PSS_OK) return rc;
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    cudaError_t e = cudaSuccess;
+    if (status) e = launch_k(k_attention_check, dim3(1), dim3(kThreads), 0, st, a);
+    if (e == cudaSuccess) e = launch_rows<FORWARD>(a, st);
+    return status_of(e);
+}
+
+extern "C" pss_status pss_attention_backward(const pss_attention_shape* shape, const pss_rows* grad,
+                                             const pss_rows* q, const pss_rows* k,
+                                             const pss_rows* v, const pss_rows* out,
+                                             const float* lse, const pss_rows* dq,
+                                             const pss_rows* dk, const pss_rows* dv,
+                                             void* workspace, int64_t workspace_bytes,
+                                             int64_t* status, pss_stream stream) {
+    Attn a;
+    const pss_status rc =
+        fill(shape, q, k, v, out, lse, workspace, workspace_bytes, status, 1, &a);
+    if (rc != PSS_OK) return rc;
+    if (!rows_ok(grad, shape->q_tokens, a.heads, a.dim, &a.grad) ||
+        !rows_ok(dq, shape->q_tokens, a.heads, a.dim, &a.dq) ||
+        !rows_ok(dk, shape->k_tokens, a.kv_heads, a.dim, &a.dk) ||
+        !rows_ok(dv, shape->k_tokens, a.kv_heads, a.dim, &a.dv))
+        return PSS_ERR_INVALID_ARG;
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    cudaError_t e = cudaSuccess;
+    if (status) e = launch_k(k_attention_check, dim3(1), dim3(kThreads), 0, st, a);
+    if (e == cudaSuccess) e = launch_rows<DQ>(a, st);
+    if (e == cudaSuccess) e = launch_rows<DKV>(a, st);
+    return status_of(e);
+}

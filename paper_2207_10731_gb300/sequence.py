@@ -1,12 +1,14 @@
-"""Operators of a sequence encoder over the pooled embeddings: layer norm and
-dropout (argument marshalling only, like ``binding``; the kernels
-are in libpss.so, their contracts in include/pss.h).
+"""Operators of a sequence encoder over the pooled embeddings: layer norm,
+dropout and attention over packed sequences (argument marshalling only, like
+``binding``; the kernels are in libpss.so, their contracts in include/pss.h).
 
 All tensors are CUDA tensors of the current device; calls are asynchronous on
 ``stream`` (default: the current stream).  Nothing is kept between calls.
 Gradients are explicit calls: there is no autograd graph here.
 """
 from __future__ import annotations
+
+import ctypes
 
 from . import binding
 
@@ -157,3 +159,125 @@ def dropout(x, p: float, seed: int, offset: int = 0, residual=None, out=None, st
         x.data_ptr(), xs, None if residual is None else residual.data_ptr(), rs, rows, cols, p,
         seed, offset, _types[x.dtype], out.data_ptr(), ys, _stream(stream)), "pss_dropout")
     return out
+
+
+def _heads(t, name, shape=None):
+    """pss_rows of a bfloat16 tensor [tokens, heads, dim], dense in its last
+    dimension."""
+    torch = binding._torch()
+    _device_tensor(t, name)
+    if t.dtype != torch.bfloat16:
+        raise TypeError(f"{name} must be torch.bfloat16, got {t.dtype}")
+    if t.dim() != 3 or (shape is not None and tuple(t.shape) != tuple(shape)):
+        raise ValueError(f"{name} must have shape {tuple(shape) if shape else '[tokens, heads, dim]'}"
+                         f", got {tuple(t.shape)}")
+    token, head, one = t.stride()
+    if one != 1 and t.shape[2] > 1:
+        raise ValueError(f"{name} must be dense in its last dimension")
+    # the stride over a size of one means nothing
+    if t.shape[0] == 1:
+        token = 0
+    if t.shape[1] == 1:
+        head = 0
+    return binding.Rows(t.data_ptr(), token, head)
+
+
+def _offsets(t, name):
+    torch = binding._torch()
+    _device_tensor(t, name)
+    if t.dtype != torch.int64:
+        raise TypeError(f"{name} must be torch.int64, got {t.dtype}")
+    if t.dim() != 1 or t.numel() < 1 or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous with at least one entry")
+    return t
+
+
+def _attention_shape(q, k, q_offsets, kv_offsets, causal, scale):
+    _offsets(q_offsets, "q_offsets")
+    if kv_offsets is None:
+        kv_offsets = q_offsets
+    elif _offsets(kv_offsets, "kv_offsets").numel() != q_offsets.numel():
+        raise ValueError("q_offsets and kv_offsets must have the same number of entries")
+    tokens, heads, dim = q.shape
+    return binding.AttentionShape(q_offsets.numel() - 1, q_offsets.data_ptr(),
+                                  kv_offsets.data_ptr(), tokens, k.shape[0], heads, k.shape[1],
+                                  dim, int(bool(causal)), dim ** -0.5 if scale is None else scale)
+
+
+def _status(status):
+    if status is None:
+        return None
+    torch = binding._torch()
+    _device_tensor(status, "status")
+    if status.dtype != torch.int64 or status.numel() != 1:
+        raise TypeError("status must be a torch.int64 tensor of one value")
+    return status.data_ptr()
+
+
+def attention_forward(q, k, v, q_offsets, kv_offsets=None, causal: bool = True, scale=None,
+                      out=None, status=None, stream=None):
+    """(out, lse) of softmax(scale q k^T) v inside each packed sequence
+    (pss_attention_forward).
+
+    q: bfloat16 [query tokens, heads, dim]; k, v: [key tokens, kv heads, dim]
+    (views with any token and head strides that are multiples of 8; heads a
+    multiple of kv heads; dim a multiple of 8 up to 128).  Sequence s owns the
+    rows q_offsets[s] .. q_offsets[s+1] and kv_offsets[s] .. (int64, on the
+    device; kv_offsets defaults to q_offsets).  With ``causal`` the queries
+    stand at the end of their sequence: one query per sequence is the serving
+    step.  scale defaults to dim ** -0.5.  lse is float32 [query tokens,
+    heads].  ``status`` (int64, one value on the device) receives -1, the first
+    sequence with malformed offsets, or -2 if a device wait gave up."""
+    lib = _library()
+    torch = binding._torch()
+    rq, rk = _heads(q, "q"), _heads(k, "k")
+    rv = _heads(v, "v", k.shape)
+    if k.shape[2] != q.shape[2]:
+        raise ValueError(f"k must have rows of {q.shape[2]} values, got {k.shape[2]}")
+    shape = _attention_shape(q, k, q_offsets, kv_offsets, causal, scale)
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    ro = _heads(out, "out", q.shape)
+    lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
+    size = lib.pss_attention_workspace(ctypes.byref(shape), 0)
+    work = torch.empty(size, dtype=torch.uint8, device=q.device)
+    binding._check(lib.pss_attention_forward(
+        ctypes.byref(shape), ctypes.byref(rq), ctypes.byref(rk), ctypes.byref(rv),
+        ctypes.byref(ro), lse.data_ptr(), work.data_ptr(), size, _status(status),
+        _stream(stream)), "pss_attention_forward")
+    _used_on(stream, work)
+    return out, lse
+
+
+def attention_backward(grad, q, k, v, out, lse, q_offsets, kv_offsets=None, causal: bool = True,
+                       scale=None, grads=None, status=None, stream=None):
+    """(dq, dk, dv) for the upstream gradient ``grad`` of the out of
+    ``attention_forward`` (pss_attention_backward); out and lse are that
+    call's.  The gradients go to the three tensors ``grads`` if given (e.g.
+    views of one buffer for a fused projection)."""
+    lib = _library()
+    torch = binding._torch()
+    rq, rk = _heads(q, "q"), _heads(k, "k")
+    rv = _heads(v, "v", k.shape)
+    if k.shape[2] != q.shape[2]:
+        raise ValueError(f"k must have rows of {q.shape[2]} values, got {k.shape[2]}")
+    rg, ro = _heads(grad, "grad", q.shape), _heads(out, "out", q.shape)
+    shape = _attention_shape(q, k, q_offsets, kv_offsets, causal, scale)
+    if lse.shape != q.shape[:2]:
+        raise ValueError(f"lse must have shape {tuple(q.shape[:2])}, got {tuple(lse.shape)}")
+    pl = _vector(lse, lse.numel(), "lse")
+    if grads is None:
+        grads = (torch.empty(q.shape, dtype=q.dtype, device=q.device),
+                 torch.empty(k.shape, dtype=k.dtype, device=k.device),
+                 torch.empty(v.shape, dtype=v.dtype, device=v.device))
+    dq, dk, dv = grads
+    rdq, rdk, rdv = _heads(dq, "dq", q.shape), _heads(dk, "dk", k.shape), _heads(dv, "dv", v.shape)
+    size = lib.pss_attention_workspace(ctypes.byref(shape), 1)
+    work = torch.empty(size, dtype=torch.uint8, device=q.device)
+    byref = ctypes.byref
+    binding._check(lib.pss_attention_backward(
+        byref(shape), byref(rg), byref(rq), byref(rk), byref(rv), byref(ro), pl, byref(rdq),
+        byref(rdk), byref(rdv), work.data_ptr(), size, _status(status), _stream(stream)),
+        "pss_attention_backward")
+    _used_on(stream, work)
+    return dq, dk, dv
