@@ -21,7 +21,8 @@ OBJ_DIR = os.path.join(PKG, "_build")
 LIB_PATH = os.path.join(OUT_DIR, "libpss.so")
 
 SOURCES = ["pss_api.cu", "pss_kernels.cu", "pss_tiled.cu", "pss_sorted.cu", "pss_noalloc.cu",
-           "pss_probe.cu", "seq/layer_norm.cu", "seq/dropout.cu", "seq/attention.cu"]
+           "pss_probe.cu", "seq/layer_norm.cu", "seq/dropout.cu", "seq/attention.cu",
+           "seq/attention_plan.cu", "seq/attention_forward.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 

@@ -3,6 +3,8 @@
 #include <cmath>
 
 #include "attention_rows.cuh"
+#include "attention_tma.h"
+#include <cudaTypedefs.h>
 
 using namespace pss;
 using namespace pss::seq;
@@ -18,20 +20,8 @@ __device__ bool range_of(const int64_t* off, int64_t s, int64_t tokens, int* lo,
     return ok;
 }
 
-__global__ void __launch_bounds__(kThreads) k_attention_check(Attn a) {
-    pdl_prologue();
-    if (threadIdx.x == 0) *a.status = ~0ull;
-    __syncthreads();
-    for (int64_t s = threadIdx.x; s < a.sequences; s += kThreads) {
-        int lo, hi;
-        const bool q = range_of(a.q_off, s, a.q_tokens, &lo, &hi);
-        const bool k = range_of(a.k_off, s, a.k_tokens, &lo, &hi);
-        if (!q || !k) atomicMin(a.status, (unsigned long long)s);
-    }
-}
-
 // A warp per (row, head): rows of sequence blockIdx.y ...
-enum { FORWARD, DQ, DKV };
+enum { DQ, DKV };
 template <int WHAT>
 __global__ void __launch_bounds__(kThreads) k_attention_rows(Attn a) {
     pdl_prologue();
@@ -46,11 +36,18 @@ __global__ void __launch_bounds__(kThreads) k_attention_rows(Attn a) {
         for (int64_t i = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5); i < n;
              i += (int64_t)gridDim.x * kWarps) {
             const int t = lo + (int)(i / heads), h = (int)(i % heads);
-            if (WHAT == FORWARD) forward_row(a, w, t, h);
             if (WHAT == DQ) dq_row(a, w, t, h);
             if (WHAT == DKV) dkv_row(a, w, t, h);
         }
     }
+}
+
+// Work items times heads are one launch's CTAs.
+bool grids_ok(const pss_attention_shape& s) {
+    const int64_t tokens = kTile / (s.heads / s.kv_heads);
+    const int64_t most = int64_t(1) << 30;
+    return s.q_tokens / tokens + s.sequences < most / s.kv_heads &&
+           s.k_tokens / kTile + s.sequences < most / s.kv_heads;
 }
 
 bool shape_ok(const pss_attention_shape* s) {
@@ -59,7 +56,7 @@ bool shape_ok(const pss_attention_shape* s) {
            s->sequences < (int64_t(1) << 31) - 1024 && s->kv_heads >= 1 && s->heads >= 1 &&
            s->heads % s->kv_heads == 0 && s->heads / s->kv_heads <= 128 && s->dim >= 8 &&
            s->dim <= 128 && s->dim % 8 == 0 && (s->causal == 0 || s->causal == 1) &&
-           s->scale > 0.f && std::isfinite(s->scale);
+           s->scale > 0.f && std::isfinite(s->scale) && grids_ok(*s);
 }
 
 // Checks one tensor; an empty one needs no memory.
@@ -69,7 +66,8 @@ bool rows_ok(const pss_rows* r, int64_t tokens, int64_t heads, int64_t dim, Rows
     if (tokens == 0) return true;
     if (!device_ptr(r->data) || !aligned_to(r->data, 16)) return false;
     const int64_t ts = r->token_stride, hs = r->head_stride;
-    if (ts < 0 || hs < 0 || ts % 8 || hs % 8) return false;
+    const int64_t most = int64_t(1) << 39;   // strides of a tensor map: below 2^40 bytes
+    if (ts < 0 || hs < 0 || ts % 8 || hs % 8 || ts >= most || hs >= most) return false;
     // rows must not overlap: the smaller stride holds a row, the larger all the others
     if (heads == 1) return tokens == 1 || ts >= dim;
     if (tokens == 1) return hs >= dim;
@@ -111,6 +109,48 @@ pss_status fill(const pss_attention_shape* s, const pss_rows* q, const pss_rows*
     return PSS_OK;
 }
 
+// The sizes of a call's tiles and scratch, and where each part of the workspace
+// lies: a pure function of the shape, so that the size asked for beforehand is
+// the size used.  Returns the bytes.
+int64_t lay_out(const pss_attention_shape& s, bool backward, void* base, Plan* p, int* target) {
+    *p = Plan{};
+    const int group = s.heads / s.kv_heads;
+    p->tokens = kTile / group;
+    const int64_t tiles = s.q_tokens / p->tokens + s.sequences;
+    const int sms = sm_count() > 0 ? sm_count() : 1;
+    // With fewer tiles than CTAs fit the GPU, long key ranges are split into
+    // about four pieces an SM (two CTAs each, two rounds).
+    const bool split = !backward && tiles * s.kv_heads < 2 * sms;
+    *target = split ? (4 * sms + s.kv_heads - 1) / s.kv_heads : 1;
+    const int64_t slots = split ? 2 * (int64_t)*target : 0;
+    // Two query tiles to a CTA share its K and V tiles and hide each other's
+    // softmax; where sequences rarely fill two tiles, one to a CTA.
+    p->per_item =
+        !backward && !split && s.q_tokens > 2 * (int64_t)p->tokens * s.sequences ? 2 : 1;
+    const int64_t items = s.q_tokens / (p->tokens * p->per_item) + s.sequences;
+    int64_t at = 0;
+    char* b = static_cast<char*>(base);
+    auto take = [&](int64_t bytes) {
+        char* q = b + at;
+        at += (bytes + 255) / 256 * 256;
+        return q;
+    };
+    p->head = reinterpret_cast<PlanHead*>(take(sizeof(PlanHead)));
+    p->items = reinterpret_cast<Item*>(take((items + slots) * sizeof(Item)));
+    if (backward) {
+        const int64_t n = s.k_tokens / kTile + s.sequences;
+        p->key_items = reinterpret_cast<Item*>(take(n * sizeof(Item)));
+        p->most_key_items = (int)n;
+        p->stats = reinterpret_cast<float2*>(take(s.q_tokens * s.heads * 8));
+    }
+    p->joins = reinterpret_cast<Join*>(take(slots / 2 * sizeof(Join)));
+    p->partial = reinterpret_cast<float*>(take(slots * s.kv_heads * kTile * s.dim * 4));
+    p->partial_lse = reinterpret_cast<float*>(take(slots * s.kv_heads * kTile * 4));
+    p->most_items = (int)(items + slots);
+    p->most_slots = (int)slots;
+    return at;
+}
+
 template <int WHAT>
 cudaError_t launch_rows(const Attn& a, cudaStream_t st) {
     const int64_t rows = (int64_t)(WHAT == DKV ? a.k_tokens : a.q_tokens) *
@@ -126,8 +166,9 @@ cudaError_t launch_rows(const Attn& a, cudaStream_t st) {
 
 extern "C" int64_t pss_attention_workspace(const pss_attention_shape* s, int32_t backward) {
     if (!shape_ok(s)) return 0;
-    (void)backward;
-    return 0;
+    Plan p;
+    int target;
+    return lay_out(*s, backward != 0, nullptr, &p, &target);
 }
 
 extern "C" pss_status pss_attention_forward(const pss_attention_shape* shape, const pss_rows* q,
@@ -140,9 +181,11 @@ extern "C" pss_status pss_attention_forward(const pss_attention_shape* shape, co
         fill(shape, q, k, v, out, lse, workspace, workspace_bytes, status, 0, &a);
     if (rc != PSS_OK) return rc;
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-    cudaError_t e = cudaSuccess;
-    if (status) e = launch_k(k_attention_check, dim3(1), dim3(kThreads), 0, st, a);
-    if (e == cudaSuccess) e = launch_rows<FORWARD>(a, st);
+    Plan p;
+    int target;
+    lay_out(*shape, false, workspace, &p, &target);
+    cudaError_t e = launch_plan(a, p, false, target, st);
+    if (e == cudaSuccess && a.q_tokens > 0 && a.sequences > 0) e = launch_tiles_forward(a, p, st);
     return status_of(e);
 }
 
@@ -163,9 +206,43 @@ extern "C" pss_status pss_attention_backward(const pss_attention_shape* shape, c
         !rows_ok(dv, shape->k_tokens, a.kv_heads, a.dim, &a.dv))
         return PSS_ERR_INVALID_ARG;
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-    cudaError_t e = cudaSuccess;
-    if (status) e = launch_k(k_attention_check, dim3(1), dim3(kThreads), 0, st, a);
+    Plan p;
+    int target;
+    lay_out(*shape, true, workspace, &p, &target);
+    cudaError_t e = launch_plan(a, p, true, target, st);
     if (e == cudaSuccess) e = launch_rows<DQ>(a, st);
     if (e == cudaSuccess) e = launch_rows<DKV>(a, st);
     return status_of(e);
 }
+
+namespace pss {
+namespace seq {
+
+cudaError_t tile_map(CUtensorMap* map, const Rows& r, int tokens, int heads, int dim,
+                     int heads_box, int tokens_box, const void* spare) {
+    static std::atomic<void*> found{nullptr};
+    void* fn = found.load(std::memory_order_acquire);
+    if (!fn) {
+        cudaDriverEntryPointQueryResult how;
+        const cudaError_t e = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000,
+                                                               cudaEnableDefault, &how);
+        if (e != cudaSuccess) return e;
+        if (how != cudaDriverEntryPointSuccess || !fn) return cudaErrorNotSupported;
+        found.store(fn, std::memory_order_release);
+    }
+    const bool empty = tokens == 0;   // nothing is loaded; the map only has to be valid
+    // a stride over a size of one is free, but the encoder checks it
+    const int64_t row = heads == 1 ? dim : r.head, token = tokens <= 1 ? dim : r.token;
+    const cuuint64_t dims[3] = {(cuuint64_t)dim, (cuuint64_t)heads, (cuuint64_t)(empty ? 1 : tokens)};
+    const cuuint64_t strides[2] = {(cuuint64_t)row * 2, (cuuint64_t)token * 2};
+    const cuuint32_t box[3] = {64, (cuuint32_t)heads_box, (cuuint32_t)tokens_box};
+    const cuuint32_t one[3] = {1, 1, 1};
+    const CUresult rc = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(fn)(
+        map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, empty ? const_cast<void*>(spare) : r.data, dims,
+        strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+        CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return rc == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+
+}  // namespace seq
+}  // namespace pss

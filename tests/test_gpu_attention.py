@@ -171,6 +171,16 @@ def test_one_query_over_a_long_sequence(keys, heads, kv_heads, dim):
     compare(run(q, k, v, grad, nq, nk, True), q, k, v, grad, nq, nk, True)
 
 
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("group,dim", [(1, 64), (2, 128), (3, 40), (1, 104)])
+def test_as_many_tiles_as_fill_the_gpu(causal, group, dim):
+    # long and short sequences, more keys than queries and fewer, an empty one
+    nq, nk = [700, 300, 0, 513, 129, 257], [700, 450, 5, 513, 100, 0]
+    kv_heads = 64 // group
+    q, k, v, grad = inputs(nq, nk, kv_heads * group, kv_heads, dim, seed=140)
+    compare(run(q, k, v, grad, nq, nk, causal), q, k, v, grad, nq, nk, causal)
+
+
 def test_views_of_fused_buffers():
     nq = [100, 0, 37]
     heads, kv_heads, dim = 6, 2, 64
@@ -303,6 +313,21 @@ def test_malformed_offsets_are_reported_and_skipped():
         st.zero_()
         ops().attention_backward(grad, q, k, v, out, lse, off, status=st)
         assert st.item() == 1
+
+
+def test_offsets_that_overlap_stay_in_bounds():
+    # back and forth: more rows in the sequences than there are; reported, and
+    # nothing is written outside the tensors (the guard rows around them)
+    guard = torch.full((3, 80, 2, 64), 3.0, dtype=torch.bfloat16, device="cuda")
+    q, k, v, grad = inputs([60], [60], 2, 2, 64, seed=130)
+    off = torch.tensor([0, 60] * 40, dtype=torch.int64, device="cuda")
+    st = torch.zeros(1, dtype=torch.int64, device="cuda")
+    out, lse = ops().attention_forward(q, k, v, off, status=st, out=guard[0, 10:70])
+    assert st.item() == 1
+    ops().attention_backward(grad, q, k, v, out, lse, off, status=st, grads=(
+        guard[1, 10:70], guard[2, 10:70], torch.empty_like(v)))
+    assert st.item() == 1
+    assert (guard[:, :10] == 3).all() and (guard[:, 70:] == 3).all()
 
 
 def test_empty_batches():
