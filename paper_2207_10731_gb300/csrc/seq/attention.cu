@@ -2,7 +2,6 @@
 // points and the row-by-row kernels.
 #include <cmath>
 
-#include "attention_rows.cuh"
 #include "attention_tma.h"
 #include <cudaTypedefs.h>
 
@@ -11,43 +10,13 @@ using namespace pss::seq;
 
 namespace {
 
-// The range of sequence s in `off`, empty where it is malformed.
-__device__ bool range_of(const int64_t* off, int64_t s, int64_t tokens, int* lo, int* hi) {
-    const int64_t a = off[s], b = off[s + 1];
-    const bool ok = a >= 0 && a <= b && b <= tokens;
-    *lo = ok ? (int)a : 0;
-    *hi = ok ? (int)b : 0;
-    return ok;
-}
-
-// A warp per (row, head): rows of sequence blockIdx.y ...
-enum { DQ, DKV };
-template <int WHAT>
-__global__ void __launch_bounds__(kThreads) k_attention_rows(Attn a) {
-    pdl_prologue();
-    const int heads = WHAT == DKV ? a.kv_heads : a.heads;
-    for (int64_t s = blockIdx.y; s < a.sequences; s += gridDim.y) {
-        Where w;
-        const bool q = range_of(a.q_off, s, a.q_tokens, &w.q_lo, &w.q_hi);
-        const bool k = range_of(a.k_off, s, a.k_tokens, &w.k_lo, &w.k_hi);
-        if (!q || !k) continue;
-        const int lo = WHAT == DKV ? w.k_lo : w.q_lo;
-        const int64_t n = (int64_t)((WHAT == DKV ? w.k_hi : w.q_hi) - lo) * heads;
-        for (int64_t i = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5); i < n;
-             i += (int64_t)gridDim.x * kWarps) {
-            const int t = lo + (int)(i / heads), h = (int)(i % heads);
-            if (WHAT == DQ) dq_row(a, w, t, h);
-            if (WHAT == DKV) dkv_row(a, w, t, h);
-        }
-    }
-}
-
 // Work items times heads are one launch's CTAs.
 bool grids_ok(const pss_attention_shape& s) {
     const int64_t tokens = kTile / (s.heads / s.kv_heads);
     const int64_t most = int64_t(1) << 30;
     return s.q_tokens / tokens + s.sequences < most / s.kv_heads &&
-           s.k_tokens / kTile + s.sequences < most / s.kv_heads;
+           s.k_tokens / kTile + s.sequences < most / s.kv_heads &&
+           s.q_tokens < (int64_t(1) << 34) / s.heads;
 }
 
 bool shape_ok(const pss_attention_shape* s) {
@@ -151,17 +120,6 @@ int64_t lay_out(const pss_attention_shape& s, bool backward, void* base, Plan* p
     return at;
 }
 
-template <int WHAT>
-cudaError_t launch_rows(const Attn& a, cudaStream_t st) {
-    const int64_t rows = (int64_t)(WHAT == DKV ? a.k_tokens : a.q_tokens) *
-                         (WHAT == DKV ? a.kv_heads : a.heads);
-    if (rows == 0 || a.sequences == 0) return cudaSuccess;
-    const int64_t y = a.sequences < 8192 ? a.sequences : 8192;
-    const int64_t x = (rows / y + kWarps) / kWarps;
-    return launch_k(k_attention_rows<WHAT>, dim3((unsigned)(x < 4096 ? x : 4096), (unsigned)y),
-                    dim3(kThreads), 0, st, a);
-}
-
 }  // namespace
 
 extern "C" int64_t pss_attention_workspace(const pss_attention_shape* s, int32_t backward) {
@@ -210,8 +168,7 @@ extern "C" pss_status pss_attention_backward(const pss_attention_shape* shape, c
     int target;
     lay_out(*shape, true, workspace, &p, &target);
     cudaError_t e = launch_plan(a, p, true, target, st);
-    if (e == cudaSuccess) e = launch_rows<DQ>(a, st);
-    if (e == cudaSuccess) e = launch_rows<DKV>(a, st);
+    if (e == cudaSuccess && a.sequences > 0) e = launch_tiles_backward(a, p, st);
     return status_of(e);
 }
 

@@ -58,7 +58,7 @@ k_attention_forward(const __grid_constant__ CUtensorMap mq, const __grid_constan
     pdl_prologue();
     using C = Cfg<HD, NQ>;
     extern __shared__ uint8_t raw[];
-    __shared__ uint64_t q_full, full[C::kUnits], empty[C::kUnits], s_full[NQ], p_ready[NQ];
+    __shared__ uint64_t q_full, full[C::kUnits], empty[C::kUnits], s_full[NQ], p_ready[NQ], drained;
     __shared__ uint32_t tmem_at;
     __shared__ volatile int stop;
     const int item = blockIdx.x / a.kv_heads, hk = blockIdx.x - item * a.kv_heads;
@@ -84,6 +84,7 @@ k_attention_forward(const __grid_constant__ CUtensorMap mq, const __grid_constan
     if (threadIdx.x == 0) {
         stop = 0;
         bar_init(&q_full, 1);
+        bar_init(&drained, 1);
         for (int i = 0; i < C::kUnits; ++i) {
             bar_init(&full[i], 1);
             bar_init(&empty[i], 1);
@@ -176,6 +177,11 @@ k_attention_forward(const __grid_constant__ CUtensorMap mq, const __grid_constan
                 if (!ok) break;
                 tc_commit(&empty[uv % C::kUnits]);
                 if (more) tc_commit(&empty[uk % C::kUnits]);
+            }
+            if (!ok) {   // the products in flight must end before their memory is freed
+                int never = 0;
+                tc_commit(&drained);
+                bar_wait(&drained, 0, &never);
             }
         }
     } else {
@@ -281,6 +287,7 @@ k_attention_forward(const __grid_constant__ CUtensorMap mq, const __grid_constan
 #pragma unroll 1
             for (int i = 0; i < HD; i += 32) {
                 float o[32];
+                __syncwarp();
                 if (any) {
                     tmem_load32(o_at + i, o);
                     tmem_wait_load();
@@ -294,17 +301,17 @@ k_attention_forward(const __grid_constant__ CUtensorMap mq, const __grid_constan
                     o[e] *= inv;
                     odd += o[e] * 0.f;
                 }
-                if (!live) continue;
+                if (live) {
 #pragma unroll
-                for (int e = 0; e < 32; e += 8) {
-                    if (i + e >= a.dim) break;
-                    float v[8];
+                    for (int e = 0; e < 32; e += 8) {
+                        if (i + e >= a.dim) break;
+                        float v[8];
 #pragma unroll
-                    for (int x = 0; x < 8; ++x) v[x] = none ? 0.f : o[e + x];
-                    if (part) {
-                        store8(part + i + e, v);
-                    } else {
-                        store8(a.out.at(token, h) + i + e, v);
+                        for (int x = 0; x < 8; ++x) v[x] = none ? 0.f : o[e + x];
+                        if (part)
+                            store8(part + i + e, v);
+                        else
+                            store8(a.out.at(token, h) + i + e, v);
                     }
                 }
             }
