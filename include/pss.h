@@ -495,8 +495,9 @@ typedef struct {
  *   pss_attention_workspace(shape, 0) bytes (the work list, and partial sums
  *   where few queries meet long sequences); means nothing between calls.
  *   status: NULL or device int64[1], set to -1, to the smallest sequence with
- *   malformed offsets (it is treated as empty; its rows are left unwritten),
- *   or to -2 when a bounded wait gave up (the outputs are then invalid).
+ *   malformed offsets (the rows of that sequence and of later ones are then
+ *   undefined, or left unwritten; nothing outside the tensors is touched), or
+ *   to -2 when a bounded wait gave up (the outputs are then invalid).
  * Rows outside every sequence are left unwritten.  Equal inputs give equal
  * bits.  A masked key or value changes nothing, also where it is infinite or
  * NaN, and neither does another sequence's.

@@ -14,8 +14,8 @@ namespace {
 bool grids_ok(const pss_attention_shape& s) {
     const int64_t tokens = kTile / (s.heads / s.kv_heads);
     const int64_t most = int64_t(1) << 30;
-    return s.q_tokens / tokens + s.sequences < most / s.kv_heads &&
-           s.k_tokens / kTile + s.sequences < most / s.kv_heads &&
+    return s.q_tokens / tokens + 1 < most / s.kv_heads &&
+           s.k_tokens / kTile + 1 < most / s.kv_heads &&
            s.q_tokens < (int64_t(1) << 34) / s.heads;
 }
 
@@ -85,18 +85,21 @@ int64_t lay_out(const pss_attention_shape& s, bool backward, void* base, Plan* p
     *p = Plan{};
     const int group = s.heads / s.kv_heads;
     p->tokens = kTile / group;
-    const int64_t tiles = s.q_tokens / p->tokens + s.sequences;
+    p->tiles = (int)((s.q_tokens + p->tokens - 1) / p->tokens);
+    p->key_tiles = (int)((s.k_tokens + kTile - 1) / kTile);
+    const int64_t ctas = (int64_t)p->tiles * s.kv_heads;
     const int sms = sm_count() > 0 ? sm_count() : 1;
     // With fewer tiles than CTAs fit the GPU, long key ranges are split into
     // about four pieces an SM (two CTAs each, two rounds).
-    const bool split = !backward && tiles * s.kv_heads < 2 * sms;
+    const bool split = !backward && ctas < 2 * sms;
     *target = split ? (4 * sms + s.kv_heads - 1) / s.kv_heads : 1;
     const int64_t slots = split ? 2 * (int64_t)*target : 0;
     // Two query tiles to a CTA share its K and V tiles and hide each other's
-    // softmax; where sequences rarely fill two tiles, one to a CTA.
-    p->per_item =
-        !backward && !split && s.q_tokens > 2 * (int64_t)p->tokens * s.sequences ? 2 : 1;
-    const int64_t items = s.q_tokens / (p->tokens * p->per_item) + s.sequences;
+    // softmax; one to a CTA puts two CTAs on an SM, which hides the start and the
+    // end of short ones.
+    p->per_item = !backward && ctas >= 8 * sms && s.q_tokens >= 512 * s.sequences ? 2 : 1;
+    p->keys = backward ? backward_columns(s) : kTile;
+    p->key_tokens = backward_columns(s) / group;
     int64_t at = 0;
     char* b = static_cast<char*>(base);
     auto take = [&](int64_t bytes) {
@@ -104,20 +107,25 @@ int64_t lay_out(const pss_attention_shape& s, bool backward, void* base, Plan* p
         at += (bytes + 255) / 256 * 256;
         return q;
     };
+    p->most_items = (int)((p->tiles + p->per_item - 1) / p->per_item + slots);
+    p->most_slots = (int)slots;
     p->head = reinterpret_cast<PlanHead*>(take(sizeof(PlanHead)));
-    p->items = reinterpret_cast<Item*>(take((items + slots) * sizeof(Item)));
+    p->items = reinterpret_cast<Item*>(take(p->most_items * sizeof(Item)));
+    p->q_range = reinterpret_cast<Range*>(take(s.q_tokens * sizeof(Range)));
     if (backward) {
-        const int64_t n = s.k_tokens / kTile + s.sequences;
-        p->key_items = reinterpret_cast<Item*>(take(n * sizeof(Item)));
-        p->most_key_items = (int)n;
+        p->key_items = reinterpret_cast<Item*>(take(p->key_tiles * sizeof(Item)));
+        p->k_range = reinterpret_cast<Range*>(take(s.k_tokens * sizeof(Range)));
         p->stats = reinterpret_cast<float2*>(take(s.q_tokens * s.heads * 8));
     }
     p->joins = reinterpret_cast<Join*>(take(slots / 2 * sizeof(Join)));
     p->partial = reinterpret_cast<float*>(take(slots * s.kv_heads * kTile * s.dim * 4));
     p->partial_lse = reinterpret_cast<float*>(take(slots * s.kv_heads * kTile * 4));
-    p->most_items = (int)(items + slots);
-    p->most_slots = (int)slots;
     return at;
+}
+
+// Nothing to do but to say so.
+pss_status no_sequences(const Attn& a, cudaStream_t st) {
+    return a.status ? status_of(cudaMemsetAsync(a.status, 0xff, 8, st)) : PSS_OK;
 }
 
 }  // namespace
@@ -142,8 +150,9 @@ extern "C" pss_status pss_attention_forward(const pss_attention_shape* shape, co
     Plan p;
     int target;
     lay_out(*shape, false, workspace, &p, &target);
+    if (a.sequences == 0) return no_sequences(a, st);
     cudaError_t e = launch_plan(a, p, false, target, st);
-    if (e == cudaSuccess && a.q_tokens > 0 && a.sequences > 0) e = launch_tiles_forward(a, p, st);
+    if (e == cudaSuccess && a.q_tokens > 0) e = launch_tiles_forward(a, p, st);
     return status_of(e);
 }
 
@@ -167,8 +176,9 @@ extern "C" pss_status pss_attention_backward(const pss_attention_shape* shape, c
     Plan p;
     int target;
     lay_out(*shape, true, workspace, &p, &target);
+    if (a.sequences == 0) return no_sequences(a, st);
     cudaError_t e = launch_plan(a, p, true, target, st);
-    if (e == cudaSuccess && a.sequences > 0) e = launch_tiles_backward(a, p, st);
+    if (e == cudaSuccess) e = launch_tiles_backward(a, p, st);
     return status_of(e);
 }
 

@@ -28,24 +28,32 @@ struct Attn {
     unsigned long long* status;    // see pss.h, or null
 };
 
-// A piece of work: a tile of query rows (or of key rows) of one sequence and
-// the tiles of the other side that it runs over.
-//   queries: tokens q0 .. q_end (the sequence's end; the tile's own end follows
-//     from its size), key tiles t0 <= t < t1, 128 keys each from k0;
-//   keys: keys k0 .. k_end, query tiles 0 <= t < t1, each `tile tokens` from q0.
+// The keys lo .. hi that a query token sees, or the query tokens that see a key;
+// hi < 0: the token is in no sequence (and -1 - hi stands for hi).  lo and hi
+// never fall along the tokens.
+struct Range {
+    int lo, hi;
+    __device__ __forceinline__ bool live() const { return hi >= 0; }
+    __device__ __forceinline__ int end() const { return hi < 0 ? -1 - hi : hi; }
+};
+
+// A piece of work: a tile of consecutive query tokens (or keys), whichever
+// sequences they belong to, and the tiles of the other side that hold all that
+// they see.  Short neighbouring sequences so share a tile; what a row does not
+// see is masked.
+//   queries: tokens from q0, key tiles t0 <= t < t1, `keys` each from k0;
+//   keys: keys from k0, query tiles t0 = 0 <= t < t1, `key_tokens` each from q0.
 // slot: where the partial result of a split piece goes, else -1.
 struct Item {
-    int q0, q_end, k0, k_end;
-    int t0, t1, slot, pad;
+    int q0, k0, t0, t1, slot, pad[3];
 };
 // A query tile whose keys are split: slots slot .. slot + n are to be joined.
 struct Join {
-    int q0, q_end, k0, k_end;
-    int slot, n, pad[2];
+    int q0, slot, n, pad;
 };
 // Written by the planner at the head of the workspace.
 struct PlanHead {
-    int items, joins, key_items, pad;
+    int items, joins, pad[2];
 };
 
 constexpr int kTile = 128;               // rows of one tensor-core tile
@@ -54,16 +62,27 @@ constexpr int kTile = 128;               // rows of one tensor-core tile
 struct Plan {
     int tokens;                          // tokens of a query tile: 128 / group
     int per_item;                        // query tiles of an item (1 or 2)
-    int most_items, most_key_items;      // upper bounds
+    int keys;                            // keys of a key tile that a query item runs over
+    int key_tokens;                      // tokens of a query tile that a key item runs over
+    int tiles, key_tiles;                // query and key tiles of the call
+    int most_items;                      // query items: tiles / per_item, and splits
     int most_slots;                      // > 0: long key ranges may be split
     PlanHead* head;
     Item* items;
     Item* key_items;
     Join* joins;
+    Range* q_range;                      // [q_tokens]
+    Range* k_range;                      // [k_tokens], backward only
     float* partial;                      // [slot][kv head][128][dim] sums / denominators
     float* partial_lse;                  // [slot][kv head][128]
     float2* stats;                       // [kv head][q_tokens * group] (lse * log2 e, delta)
 };
+
+// Rows of the tiles that a backward item runs over: 64 where a head fits one
+// 128-byte row and a group 64 rows (see attention_backward.cu), else 128.
+inline int backward_columns(const pss_attention_shape& s) {
+    return s.dim <= 64 && s.heads / s.kv_heads <= 64 ? 64 : kTile;
+}
 
 cudaError_t launch_plan(const Attn& a, const Plan& p, bool keys, int target_items,
                         cudaStream_t st);

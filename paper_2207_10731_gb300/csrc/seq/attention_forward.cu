@@ -62,20 +62,19 @@ k_attention_forward(const __grid_constant__ CUtensorMap mq, const __grid_constan
     __shared__ uint32_t tmem_at;
     __shared__ volatile int stop;
     const int item = blockIdx.x / a.kv_heads, hk = blockIdx.x - item * a.kv_heads;
-    if (item >= p.head->items) return;
+    if (p.most_slots > 0 && item >= p.head->items) return;
     const Item it = p.items[item];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int group = a.group, tokens = p.tokens;
-    const int shift = it.k_end - it.q_end;
 
     // key tiles of each query tile: t0 <= t < end[t]
     int end[NQ];
-#pragma unroll
-    for (int t = 0; t < NQ; ++t) {
-        const int first = it.q0 + t * tokens, last = min(first + tokens, it.q_end) - 1;
-        int n = first < it.q_end ? it.k_end - it.k0 : 0;
-        if (a.causal) n = min(n, last + 1 + shift - it.k0);
-        end[t] = max(it.t0, min(it.t1, n > 0 ? (n + kTile - 1) / kTile : 0));
+    end[NQ - 1] = it.t1;
+    if (NQ == 2) {
+        const int last = it.q0 + tokens - 1;
+        const int n = last < a.q_tokens ? p.q_range[last].end() - it.k0 : 0;
+        end[0] = last < a.q_tokens ? max(it.t0, min(it.t1, (n + kTile - 1) / kTile)) : it.t1;
+        if (it.q0 + tokens >= a.q_tokens) end[1] = it.t0;
     }
     const int most = NQ == 2 ? max(end[0], end[NQ - 1]) : end[0];
 
@@ -190,9 +189,11 @@ k_attention_forward(const __grid_constant__ CUtensorMap mq, const __grid_constan
         const int r = threadIdx.x & 127;
         const int tok = r / group, h = hk * group + r - tok * group;
         const int token = it.q0 + t * tokens + tok;
-        const bool live = tok < tokens && token < it.q_end;
-        int sees = live ? it.k_end - it.k0 : 0;   // keys from k0 on
-        if (live && a.causal) sees = max(0, min(sees, token + 1 + shift - it.k0));
+        // the keys that the row sees, counted from k0: see0 .. see1
+        Range range{0, -1};
+        if (tok < tokens && token < a.q_tokens) range = p.q_range[token];
+        const bool live = range.live();
+        const int see0 = live ? range.lo - it.k0 : 0, see1 = live ? range.hi - it.k0 : 0;
         const int stop_at = NQ == 2 && t == 1 ? end[NQ - 1] : end[0];
         const uint32_t lanes = (uint32_t)(warp & 3) << 21;
         const uint32_t s_at = tmem + t * 128 + lanes, o_at = tmem + C::kO + t * HD + lanes;
@@ -210,14 +211,9 @@ k_attention_forward(const __grid_constant__ CUtensorMap mq, const __grid_constan
             tmem_wait_load();
 #pragma unroll
             for (int i = 0; i < 4; ++i) tmem_loaded(s[i]);
-            const int see = sees - j * kTile;
-            if (__any_sync(0xffffffffu, see < kTile)) {
+            const int lo = see0 - j * kTile, hi = see1 - j * kTile;
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-#pragma unroll
-                    for (int e = 0; e < 32; ++e)
-                        if (32 * i + e >= see) s[i][e] = -INFINITY;
-            }
+            for (int i = 0; i < 4; ++i) hide(s[i], lo - 32 * i, hi - 32 * i);
             float m4[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -274,7 +270,7 @@ k_attention_forward(const __grid_constant__ CUtensorMap mq, const __grid_constan
             tc_after_sync();
         }
         if (ok) {
-            const bool none = sees == 0;
+            const bool none = see1 <= see0;
             const float inv = sum > 0.f ? 1.f / sum : 0.f;
             const float lse = sum > 0.f ? top * a.scale + __log2f(sum) * kLn2 : -INFINITY;
             float odd = none ? 0.f : lse * 0.f;   // NaN where something is not finite
@@ -284,6 +280,8 @@ k_attention_forward(const __grid_constant__ CUtensorMap mq, const __grid_constan
                 part = p.partial + row * a.dim;
                 p.partial_lse[row] = lse;
             }
+            // a piece that holds none of the keys that a row sees leaves it out
+            const bool store = live && !(part && lse == -INFINITY);
 #pragma unroll 1
             for (int i = 0; i < HD; i += 32) {
                 float o[32];
@@ -301,7 +299,7 @@ k_attention_forward(const __grid_constant__ CUtensorMap mq, const __grid_constan
                     o[e] *= inv;
                     odd += o[e] * 0.f;
                 }
-                if (live) {
+                if (store) {
 #pragma unroll
                     for (int e = 0; e < 32; e += 8) {
                         if (i + e >= a.dim) break;
@@ -318,12 +316,13 @@ k_attention_forward(const __grid_constant__ CUtensorMap mq, const __grid_constan
             if (it.slot < 0) {
                 if (live) a.lse[(int64_t)token * a.heads + h] = lse;
                 unsigned again = __ballot_sync(0xffffffffu, live && !none && odd != 0.f);
-                const Where w{it.q0, it.q_end, it.k0, it.k_end};
                 while (again) {
                     const int from = __ffs(again) - 1;
                     again &= again - 1;
                     __syncwarp();
-                    forward_row(a, w, __shfl_sync(0xffffffffu, token, from),
+                    forward_row(a, __shfl_sync(0xffffffffu, range.lo, from),
+                                __shfl_sync(0xffffffffu, range.hi, from),
+                                __shfl_sync(0xffffffffu, token, from),
                                 __shfl_sync(0xffffffffu, h, from));
                 }
             }
@@ -338,44 +337,60 @@ k_attention_forward(const __grid_constant__ CUtensorMap mq, const __grid_constan
 
 // Joins the pieces of the split query tiles:
 //   lse = log sum_i exp(lse_i),  out = sum_i exp(lse_i - lse) out_i,
-// a warp to a row, lane l holding the values 4l .. 4l+3.
+// a warp to a row, lane l holding the values 4l .. 4l+3.  Most pieces of a tile
+// of many short-query sequences hold nothing that a given row sees: the lanes
+// read the pieces' lse side by side, and only the others' sums are read.
 __global__ void __launch_bounds__(kThreads) k_attention_join(Attn a, Plan p) {
     pdl_prologue();
-    const int join = blockIdx.x / a.kv_heads, hk = blockIdx.x - join * a.kv_heads;
+    constexpr int kParts = kTile / kWarps;   // CTAs to a tile and head
+    const int part = blockIdx.x % kParts, rest = blockIdx.x / kParts;
+    const int join = rest / a.kv_heads, hk = rest - join * a.kv_heads;
     if (join >= p.head->joins) return;
     const Join jn = p.joins[join];
-    const int lane = threadIdx.x & 31;
-    for (int r = threadIdx.x >> 5; r < kTile; r += kWarps) {
-        const int tok = r / a.group, token = jn.q0 + tok, h = hk * a.group + r - tok * a.group;
-        if (tok >= p.tokens || token >= jn.q_end) return;
-        const Where w{jn.q0, jn.q_end, jn.k0, jn.k_end};
-        if (keys_end(a, w, token) <= jn.k0) {
-            put4(a.out.at(token, h), make_float4(0.f, 0.f, 0.f, 0.f), a.dim);
-            if (lane == 0) a.lse[(int64_t)token * a.heads + h] = -INFINITY;
-            continue;
-        }
-        float top = -INFINITY;
-        for (int i = 0; i < jn.n; ++i)
-            top = fmaxf(top, p.partial_lse[((int64_t)(jn.slot + i) * a.kv_heads + hk) * kTile + r]);
-        float sum = 0.f;
-        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int i = 0; i < jn.n; ++i) {
-            const int64_t row = ((int64_t)(jn.slot + i) * a.kv_heads + hk) * kTile + r;
-            const float e = exp2_fast((p.partial_lse[row] - top) * kLog2e);
-            sum += e;
-            if (4 * lane < a.dim)
-                add4(o, e, *reinterpret_cast<const float4*>(p.partial + row * a.dim + 4 * lane));
-        }
-        const float inv = 1.f / sum, lse = top + __log2f(sum) * kLn2;
-        o = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
-        const float odd = (o.x + o.y + o.z + o.w) * 0.f + lse * 0.f;
-        if (__any_sync(0xffffffffu, odd != 0.f)) {
-            forward_row(a, w, token, h);
-            continue;
-        }
-        put4(a.out.at(token, h), o, a.dim);
-        if (lane == 0) a.lse[(int64_t)token * a.heads + h] = lse;
+    const int lane = threadIdx.x & 31, r = part * kWarps + (threadIdx.x >> 5);
+    const int tok = r / a.group, token = jn.q0 + tok, h = hk * a.group + r - tok * a.group;
+    if (tok >= p.tokens || token >= a.q_tokens) return;
+    const Range range = p.q_range[token];
+    if (!range.live()) return;
+    if (range.hi <= range.lo) {
+        put4(a.out.at(token, h), make_float4(0.f, 0.f, 0.f, 0.f), a.dim);
+        if (lane == 0) a.lse[(int64_t)token * a.heads + h] = -INFINITY;
+        return;
     }
+    const int64_t base = ((int64_t)jn.slot * a.kv_heads + hk) * kTile + r;
+    const int64_t step = (int64_t)a.kv_heads * kTile;
+    float top = -INFINITY;
+    for (int i = lane; i < jn.n; i += 32) top = fmaxf(top, p.partial_lse[base + i * step]);
+#pragma unroll
+    for (int m = 16; m > 0; m >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, m));
+    float sum = 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int i0 = 0; i0 < jn.n; i0 += 32) {
+        const int i = i0 + lane;
+        const float lse = i < jn.n ? p.partial_lse[base + i * step] : -INFINITY;
+        const float e = lse == -INFINITY ? 0.f : exp2_fast((lse - top) * kLog2e);
+        sum += e;
+        unsigned some = __ballot_sync(0xffffffffu, lse != -INFINITY);
+        while (some) {
+            const int j = __ffs(some) - 1;
+            some &= some - 1;
+            const float w = __shfl_sync(0xffffffffu, e, j);
+            if (4 * lane < a.dim)
+                add4(o, w, *reinterpret_cast<const float4*>(
+                               p.partial + (base + (i0 + j) * step) * a.dim + 4 * lane));
+        }
+    }
+#pragma unroll
+    for (int m = 16; m > 0; m >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, m);
+    const float inv = 1.f / sum, lse = top + __log2f(sum) * kLn2;
+    o = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+    const float odd = (o.x + o.y + o.z + o.w) * 0.f + lse * 0.f;
+    if (__any_sync(0xffffffffu, odd != 0.f)) {
+        forward_row(a, range.lo, range.hi, token, h);
+        return;
+    }
+    put4(a.out.at(token, h), o, a.dim);
+    if (lane == 0) a.lse[(int64_t)token * a.heads + h] = lse;
 }
 
 template <int HD, int NQ>
@@ -403,7 +418,7 @@ cudaError_t launch_tiles_forward(const Attn& a, const Plan& p, cudaStream_t st) 
     else
         e = p.per_item == 2 ? launch<128, 2>(a, p, st) : launch<128, 1>(a, p, st);
     if (e != cudaSuccess || p.most_slots == 0) return e;
-    return launch_k(k_attention_join, dim3((unsigned)(p.most_slots / 2 * a.kv_heads)),
+    return launch_k(k_attention_join, dim3((unsigned)(p.tiles * a.kv_heads * (kTile / kWarps))),
                     dim3(kThreads), 0, st, a, p);
 }
 

@@ -1,11 +1,15 @@
-// The work list of an attention call: which tiles of query rows (and of key
-// rows, for the backward pass) the packed sequences make, the longest first.
+// The work list of an attention call: what each token sees, which tiles that
+// makes, the longest first.
 //
-// The sequence lengths live on the device, so the list is made there: one CTA,
-// a warp per sequence and a lane per tile, two sweeps (count by cost, place).
-// Sorted by cost so that the last tiles to start are short ones.  Where a tile
-// stands among those of equal cost follows the scheduling; no result depends
-// on it.
+// The sequence lengths live on the device, so the list is made there, in two
+// steps: a thread per token finds its sequence in the offsets and writes the
+// range that it sees (coalesced later for whoever needs it); one CTA then turns
+// the ranges at the ends of each tile into work items, sorted by cost so that
+// the last tiles to start are short ones.  Where a tile stands among those of
+// equal cost follows the scheduling; no result depends on it.  Up to
+// kSmallTokens tokens the one CTA takes both steps: one launch less.
+//
+// Measured at 1024 sequences of 64 k tokens in all, both lists: see launch_plan.
 #include "attention.h"
 
 namespace pss {
@@ -13,6 +17,8 @@ namespace seq {
 namespace {
 
 constexpr int kBuckets = 128;
+constexpr int kPlanThreads = 1024;
+constexpr int kSmallTokens = 4096;
 
 // Exact up to 15, four steps to a doubling above.
 __device__ __forceinline__ int bucket(int cost) {
@@ -21,139 +27,177 @@ __device__ __forceinline__ int bucket(int cost) {
     return min(kBuckets - 1, 16 + (e - 4) * 4 + ((cost >> (e - 2)) & 3));
 }
 
-__device__ bool range_of(const int64_t* off, int64_t s, int64_t tokens, int* lo, int* hi) {
-    const int64_t a = off[s], b = off[s + 1];
-    const bool ok = a >= 0 && a <= b && b <= tokens;
-    *lo = ok ? (int)a : 0;
-    *hi = ok ? (int)b : 0;
-    return ok;
+__device__ __forceinline__ int64_t clamp64(int64_t x, int64_t lo, int64_t hi) {
+    return x < lo ? lo : x > hi ? hi : x;
 }
 
-__global__ void __launch_bounds__(1024) k_attention_plan(Attn a, Plan p, int target_items) {
+// The last sequence that starts at or before t, or -1.
+__device__ __forceinline__ int64_t find(const int64_t* off, int64_t n, int64_t t) {
+    int64_t lo = 0, hi = n;
+    while (lo < hi) {
+        const int64_t mid = (lo + hi) >> 1;
+        if (off[mid] <= t)
+            lo = mid + 1;
+        else
+            hi = mid;
+    }
+    return lo - 1;
+}
+
+// What token t of one side sees on the other side.
+template <bool KEYS>
+__device__ __forceinline__ Range range_of(const Attn& a, int64_t t) {
+    const int64_t* own = KEYS ? a.k_off : a.q_off;
+    const int64_t* other = KEYS ? a.q_off : a.k_off;
+    const int64_t own_n = KEYS ? a.k_tokens : a.q_tokens;
+    const int64_t other_n = KEYS ? a.q_tokens : a.k_tokens;
+    const int64_t s = find(own, a.sequences, t);
+    if (s < 0) {
+        const int at = (int)clamp64(other[0], 0, other_n);
+        return Range{at, -1 - at};
+    }
+    const int64_t begin = own[s], end = own[s + 1], lo = other[s], hi = other[s + 1];
+    if (begin < 0 || t >= end || end > own_n || lo < 0 || lo > hi || hi > other_n) {
+        const int at = (int)clamp64(hi, 0, other_n);
+        return Range{at, -1 - at};
+    }
+    if (!a.causal) return Range{(int)lo, (int)hi};
+    // query i stands at key i + (end of the keys - end of the queries)
+    if (KEYS) return Range{(int)clamp64(t - (end - hi), lo, hi), (int)hi};
+    return Range{(int)lo, (int)clamp64(t + 1 + (hi - end), lo, hi)};
+}
+
+__global__ void __launch_bounds__(kThreads) k_attention_ranges(Attn a, Plan p) {
+    pdl_prologue();
+    const int64_t t = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    if (blockIdx.y == 0) {
+        if (t < a.q_tokens) p.q_range[t] = range_of<false>(a, t);
+    } else {
+        if (t < a.k_tokens) p.k_range[t] = range_of<true>(a, t);
+    }
+}
+
+__global__ void __launch_bounds__(kPlanThreads)
+k_attention_plan(Attn a, Plan p, int target_items, int small) {
     pdl_prologue();
     __shared__ unsigned count[kBuckets], next[kBuckets];
     __shared__ unsigned slots, joins, total;
-    __shared__ long long work;
+    __shared__ unsigned long long work;
     const bool keys = blockIdx.x == 1;
-    const unsigned cap = keys ? p.most_key_items : p.most_items;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    if (threadIdx.x < kBuckets) count[threadIdx.x] = 0;
-    if (threadIdx.x == 0) {
+    const int tid = threadIdx.x;
+    if (tid < kBuckets) count[tid] = 0;
+    if (tid == 0) {
         slots = joins = 0;
         work = 0;
         if (!keys && a.status) *a.status = ~0ull;
     }
+    if (small) {
+        if (keys) {
+            for (int t = tid; t < a.k_tokens; t += kPlanThreads)
+                p.k_range[t] = range_of<true>(a, t);
+        } else {
+            for (int t = tid; t < a.q_tokens; t += kPlanThreads)
+                p.q_range[t] = range_of<false>(a, t);
+        }
+    }
     __syncthreads();
+    if (!keys && a.status)
+        for (int64_t s = tid; s < a.sequences; s += kPlanThreads)
+            if (a.q_off[s] < 0 || a.q_off[s] > a.q_off[s + 1] || a.q_off[s + 1] > a.q_tokens ||
+                a.k_off[s] < 0 || a.k_off[s] > a.k_off[s + 1] || a.k_off[s + 1] > a.k_tokens)
+                atomicMin(a.status, (unsigned long long)s);
 
-    // sweep 0: total work, where long ranges may be split; sweep 1: count; 2: place
+    const int tiles = keys ? p.key_tiles : p.tiles;
+    const int step = keys ? kTile : p.tokens * p.per_item;
+    const int items = keys ? tiles : (p.tiles + p.per_item - 1) / p.per_item;
+    const int cap = keys ? items : p.most_items;
+    const int64_t own_n = keys ? a.k_tokens : a.q_tokens;
+    const Range* ranges = keys ? p.k_range : p.q_range;
+    const int other = keys ? p.key_tokens : p.keys;
+    // sweep 0: total work, where long ranges may be split; 1: count; 2: place
     int chunk = 1 << 30;
     for (int sweep = p.most_slots > 0 && !keys ? 0 : 1; sweep < 3; ++sweep) {
-        long long mine = 0;
-        for (int64_t s = warp; s < a.sequences; s += 32) {
-            int q_lo, q_hi, k_lo, k_hi;
-            const bool ok_q = range_of(a.q_off, s, a.q_tokens, &q_lo, &q_hi);
-            const bool ok_k = range_of(a.k_off, s, a.k_tokens, &k_lo, &k_hi);
-            if (!ok_q || !ok_k) {
-                if (sweep == 1 && !keys && lane == 0 && a.status)
-                    atomicMin(a.status, (unsigned long long)s);
+        unsigned long long mine = 0;
+        for (int i = tid; i < items; i += kPlanThreads) {
+            const int64_t first = (int64_t)i * step, past = first + step;
+            const int from = ranges[first].lo;
+            const int to = ranges[(past < own_n ? past : own_n) - 1].end();
+            const int all = to > from ? (int)(((int64_t)to - from + other - 1) / other) : 0;
+            if (sweep == 0) {
+                mine += all;
                 continue;
             }
-            const int shift = k_hi - q_hi;   // the last key that token t sees is t + shift
-            const int step = keys ? kTile : p.tokens * p.per_item;
-            const int lo = keys ? k_lo : q_lo, hi = keys ? k_hi : q_hi;
-            for (int i = lane; i < (hi - lo + step - 1) / step; i += 32) {
-                Item it;
-                it.q0 = q_lo;
-                it.q_end = q_hi;
-                it.k0 = k_lo;
-                it.k_end = k_hi;
-                it.t0 = 0;
-                it.slot = -1;
-                it.pad = 0;
-                if (keys) {
-                    it.k0 = lo + i * step;
-                    if (a.causal) it.q0 = max(q_lo, it.k0 - shift);
-                    it.t1 = it.q0 < q_hi ? (q_hi - it.q0 + p.tokens - 1) / p.tokens : 0;
-                } else {
-                    it.q0 = lo + i * step;
-                    const int last = min(q_hi - it.q0, step) + it.q0 - 1;
-                    const int end = a.causal ? min(k_hi, last + 1 + shift) : k_hi;
-                    it.t1 = end > k_lo ? (end - k_lo + kTile - 1) / kTile : 0;
-                }
-                if (sweep == 0) {
-                    mine += it.t1;
-                    continue;
-                }
-                const int parts = it.t1 > chunk ? (it.t1 + chunk - 1) / chunk : 1;
-                const int all = it.t1;
-                const int cost = bucket((all + parts - 1) / parts);
-                if (sweep == 1) {
-                    atomicAdd(&count[cost], (unsigned)parts);
-                    continue;
-                }
-                const unsigned at = atomicAdd(&next[cost], (unsigned)parts);
-                int slot = -1;
-                bool fits = at < cap && cap - at >= (unsigned)parts;
-                if (parts > 1 && fits) {
-                    slot = (int)atomicAdd(&slots, (unsigned)parts);
-                    fits = slot + parts <= p.most_slots;
-                    if (fits)
-                        p.joins[atomicAdd(&joins, 1u)] =
-                            Join{it.q0, it.q_end, it.k0, it.k_end, slot, parts, {0, 0}};
-                }
-                Item* to = (keys ? p.key_items : p.items) + at;
-                if (!fits) {
-                    // offsets that go back make more tiles than the tokens can:
-                    // what does not fit the list becomes empty pieces
-                    for (int j = 0; j < parts && at + j < cap; ++j)
-                        to[j] = Item{0, 0, 0, 0, 0, 0, -1, 0};
-                    continue;
-                }
-                for (int j = 0; j < parts; ++j) {
-                    it.t0 = (int)((long long)all * j / parts);
-                    it.t1 = (int)((long long)all * (j + 1) / parts);
-                    if (slot >= 0) it.slot = slot + j;
-                    to[j] = it;
-                }
+            const int parts = all > chunk ? (all + chunk - 1) / chunk : 1;
+            const int cost = bucket((all + parts - 1) / parts);
+            if (sweep == 1) {
+                atomicAdd(&count[cost], (unsigned)parts);
+                continue;
+            }
+            const int at = (int)atomicAdd(&next[cost], (unsigned)parts);
+            if (at + parts > cap) continue;   // cannot be: cap counts them all
+            int slot = -1;
+            if (parts > 1) {
+                slot = (int)atomicAdd(&slots, (unsigned)parts);
+                p.joins[atomicAdd(&joins, 1u)] = Join{(int)first, slot, parts, 0};
+            }
+            Item* list = (keys ? p.key_items : p.items) + at;
+            for (int j = 0; j < parts; ++j) {
+                Item it{};
+                it.q0 = keys ? from : (int)first;
+                it.k0 = keys ? (int)first : from;
+                it.t0 = (int)((int64_t)all * j / parts);
+                it.t1 = (int)((int64_t)all * (j + 1) / parts);
+                it.slot = slot < 0 ? -1 : slot + j;
+                list[j] = it;
             }
         }
         if (sweep == 0) {
-            for (int m = 16; m > 0; m >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, m);
-            if (lane == 0) atomicAdd((unsigned long long*)&work, (unsigned long long)mine);
+            if (mine) atomicAdd(&work, mine);
             __syncthreads();
             // at least 4 key tiles a piece: joining costs a pass over the partial sums
-            const long long each = (work + target_items - 1) / target_items;
+            const unsigned long long each = (work + target_items - 1) / target_items;
             chunk = (int)(each < 4 ? 4 : each > (1 << 30) ? (1 << 30) : each);
         }
         if (sweep == 1) {
             __syncthreads();
-            if (threadIdx.x == 0) {   // longest first
+            if (tid < 32) {   // longest first: an exclusive sum from the last bucket down
                 unsigned at = 0;
-                for (int b = kBuckets - 1; b >= 0; --b) {
-                    next[b] = at;
-                    at += count[b];
+                for (int b = kBuckets - 32; b >= 0; b -= 32) {
+                    const unsigned own = count[b + 31 - tid];
+                    unsigned sum = own;
+#pragma unroll
+                    for (int m = 1; m < 32; m <<= 1) {
+                        const unsigned up = __shfl_up_sync(0xffffffffu, sum, m);
+                        if (tid >= m) sum += up;
+                    }
+                    next[b + 31 - tid] = at + sum - own;
+                    at += __shfl_sync(0xffffffffu, sum, 31);
                 }
-                total = at;
+                if (tid == 0) total = at;
             }
             __syncthreads();
         }
     }
     __syncthreads();
-    if (threadIdx.x == 0) {
-        if (keys) {
-            p.head->key_items = (int)min(total, cap);
-        } else {
-            p.head->items = (int)min(total, cap);
-            p.head->joins = (int)joins;
-        }
+    if (tid == 0 && !keys) {
+        p.head->items = min((int)total, cap);
+        p.head->joins = (int)joins;
     }
 }
 
 }  // namespace
 
-cudaError_t launch_plan(const Attn& a, const Plan& p, bool keys, int target_items,
+cudaError_t launch_plan(const Attn& a, const Plan& p, bool backward, int target_items,
                         cudaStream_t st) {
-    return launch_k(k_attention_plan, dim3(keys ? 2 : 1), dim3(1024), 0, st, a, p, target_items);
+    const int64_t most = backward && a.k_tokens > a.q_tokens ? a.k_tokens : a.q_tokens;
+    const bool small = most <= kSmallTokens;
+    if (!small) {
+        const dim3 grid((unsigned)((most + kThreads - 1) / kThreads), backward ? 2 : 1);
+        const cudaError_t e = launch_k(k_attention_ranges, grid, dim3(kThreads), 0, st, a, p);
+        if (e != cudaSuccess) return e;
+    }
+    return launch_k(k_attention_plan, dim3(backward ? 2 : 1), dim3(kPlanThreads), 0, st, a, p,
+                    target_items, (int)small);
 }
 
 }  // namespace seq

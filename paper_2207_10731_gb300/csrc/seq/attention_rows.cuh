@@ -8,11 +8,6 @@
 namespace pss {
 namespace seq {
 
-// Where a row stands: its sequence's ranges of query and key rows.
-struct Where {
-    int q_lo, q_hi, k_lo, k_hi;
-};
-
 __device__ __forceinline__ float4 row4(const bf16* p, int dim) {
     const int c = 4 * (threadIdx.x & 31);
     if (c >= dim) return make_float4(0.f, 0.f, 0.f, 0.f);
@@ -41,18 +36,13 @@ __device__ __forceinline__ void add4(float4& a, float s, float4 b) {
     a.w += s * b.w;
 }
 
-// One past the last key that query row t sees.
-__device__ __forceinline__ int keys_end(const Attn& a, const Where& w, int t) {
-    return a.causal ? min(w.k_hi, t + 1 + (w.k_hi - w.q_hi)) : w.k_hi;
-}
-
-// out and lse of query row t, head h.
-static __device__ void forward_row(const Attn& a, const Where& w, int t, int h) {
-    const int hk = h / a.group, end = keys_end(a, w, t);
+// out and lse of query token t, head h, which sees the keys first .. end.
+static __device__ void forward_row(const Attn& a, int first, int end, int t, int h) {
+    const int hk = h / a.group;
     const float4 q = row4(a.q.at(t, h), a.dim);
     float top = -INFINITY, sum = 0.f;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int j = w.k_lo; j < end; ++j) {
+    for (int j = first; j < end; ++j) {
         const float s = dot4(q, row4(a.k.at(j, hk), a.dim)) * a.scale;
         const float next = fmaxf(top, s);
         const float keep = next == -INFINITY ? 1.f : expf(top - next);
@@ -65,21 +55,21 @@ static __device__ void forward_row(const Attn& a, const Where& w, int t, int h) 
         add4(o, p, row4(a.v.at(j, hk), a.dim));
         top = next;
     }
-    const float inv = end > w.k_lo ? 1.f / sum : 0.f;
+    const float inv = end > first ? 1.f / sum : 0.f;
     put4(a.out.at(t, h), make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv), a.dim);
     if ((threadIdx.x & 31) == 0)
-        a.lse[(int64_t)t * a.heads + h] = end > w.k_lo ? top + logf(sum) : -INFINITY;
+        a.lse[(int64_t)t * a.heads + h] = end > first ? top + logf(sum) : -INFINITY;
 }
 
-// dq of query row t, head h.
-static __device__ void dq_row(const Attn& a, const Where& w, int t, int h) {
-    const int hk = h / a.group, end = keys_end(a, w, t);
+// dq of query token t, head h.
+static __device__ void dq_row(const Attn& a, int first, int end, int t, int h) {
+    const int hk = h / a.group;
     const float4 q = row4(a.q.at(t, h), a.dim), g = row4(a.grad.at(t, h), a.dim);
     float4 d = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (end > w.k_lo) {
+    if (end > first) {
         const float lse = a.lse[(int64_t)t * a.heads + h];
         const float delta = dot4(g, row4(a.out.at(t, h), a.dim));
-        for (int j = w.k_lo; j < end; ++j) {
+        for (int j = first; j < end; ++j) {
             const float4 k = row4(a.k.at(j, hk), a.dim);
             const float p = expf(dot4(q, k) * a.scale - lse);
             add4(d, p * (dot4(g, row4(a.v.at(j, hk), a.dim)) - delta) * a.scale, k);
@@ -88,12 +78,11 @@ static __device__ void dq_row(const Attn& a, const Where& w, int t, int h) {
     put4(a.dq.at(t, h), d, a.dim);
 }
 
-// dk and dv of key row j, key head hk.
-static __device__ void dkv_row(const Attn& a, const Where& w, int j, int hk) {
+// dk and dv of key j, key head hk, which the query tokens first .. end see.
+static __device__ void dkv_row(const Attn& a, int first, int end, int j, int hk) {
     const float4 k = row4(a.k.at(j, hk), a.dim), v = row4(a.v.at(j, hk), a.dim);
     float4 dk = make_float4(0.f, 0.f, 0.f, 0.f), dv = dk;
-    const int first = a.causal ? max(w.q_lo, j - (w.k_hi - w.q_hi)) : w.q_lo;
-    for (int t = first; t < w.q_hi; ++t)
+    for (int t = first; t < end; ++t)
         for (int h = hk * a.group; h < (hk + 1) * a.group; ++h) {
             const float4 q = row4(a.q.at(t, h), a.dim), g = row4(a.grad.at(t, h), a.dim);
             const float p = expf(dot4(q, k) * a.scale - a.lse[(int64_t)t * a.heads + h]);

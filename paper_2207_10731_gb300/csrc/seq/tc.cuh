@@ -190,6 +190,17 @@ __device__ __forceinline__ void tmem_wait_store() {
     asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
 }
 
+// Scores outside columns lo .. hi of a thread's 32 become -infinity.  Where the
+// warp hides nothing it costs a vote.
+__device__ __forceinline__ void hide(float (&s)[32], int lo, int hi) {
+    if (!__any_sync(0xffffffffu, lo > 0 || hi < 32)) return;
+    uint32_t see = hi >= 32 ? 0xffffffffu : hi <= 0 ? 0u : (1u << hi) - 1u;
+    see &= lo <= 0 ? 0xffffffffu : lo >= 32 ? 0u : ~((1u << lo) - 1u);
+#pragma unroll
+    for (int e = 0; e < 32; ++e)
+        if (!(see & (1u << e))) s[e] = -INFINITY;
+}
+
 // 2^x, the hardware's approximation (relative error below 2^-22).
 __device__ __forceinline__ float exp2_fast(float x) {
     float y;
