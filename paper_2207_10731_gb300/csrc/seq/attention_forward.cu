@@ -9,8 +9,8 @@
 // units; rows past a tensor's end arrive as zeros, rows of a neighbouring
 // sequence are masked.
 //
-// Roles: one warp loads, one thread issues the products, four warps per query
-// tile do the softmax, a thread to a row (tensor-memory lane).  With two tiles
+// Roles: one warp loads, one thread per query tile issues its products, four
+// warps per tile do the softmax, a thread to a row (tensor-memory lane).  With two tiles
 // to a CTA (NQ = 2) one tile's softmax runs under the other's products and both
 // read the same K and V from shared memory; with one (NQ = 1) two CTAs share
 // an SM.  P overwrites S in tensor memory, as bf16, and is the first operand of
@@ -45,22 +45,27 @@ struct Cfg {
     static constexpr int kUnit = kHalves * 16384;                      // one K or V tile
     static constexpr int kUnits = HD == 128 ? (NQ == 2 ? 4 : 2) : (NQ == 2 ? 8 : 4);
     static constexpr int kQ = NQ * kUnit;
-    static constexpr int kSmem = kQ + kUnits * kUnit + 1024;           // + alignment
+    static constexpr int kSmem = kQ + kUnits * kUnit;
     static constexpr int kCols = NQ == 2 ? 512 : 256;                  // tensor-memory columns
     static constexpr int kO = NQ * 128;                                // O's first column
-    static constexpr int kThreads = NQ * 128 + 64;
+    // NQ = 2: three whole warpgroups, so that the two of the softmax can take
+    // registers from the third (set_registers)
+    static constexpr int kThreads = NQ == 2 ? 384 : 192;
 };
 
 template <int HD, int NQ>
 __global__ void __launch_bounds__(Cfg<HD, NQ>::kThreads, NQ == 1 ? 2 : 1)
 k_attention_forward(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk,
-                    const __grid_constant__ CUtensorMap mv, Attn a, Plan p) {
+                    const __grid_constant__ CUtensorMap mv, const __grid_constant__ CUtensorMap mo,
+                    Attn a, Plan p) {
     pdl_prologue();
     using C = Cfg<HD, NQ>;
-    extern __shared__ uint8_t raw[];
-    __shared__ uint64_t q_full, full[C::kUnits], empty[C::kUnits], s_full[NQ], p_ready[NQ], drained;
+    extern __shared__ __align__(1024) uint8_t smem[];
+    __shared__ uint64_t q_full, full[C::kUnits], empty[C::kUnits], s_full[NQ], p_ready[NQ],
+        drained[NQ], turn[2];
     __shared__ uint32_t tmem_at;
     __shared__ volatile int stop;
+    __shared__ bool keep[NQ][kTile];   // rows to be stored
     const int item = blockIdx.x / a.kv_heads, hk = blockIdx.x - item * a.kv_heads;
     if (p.most_slots > 0 && item >= p.head->items) return;
     const Item it = p.items[item];
@@ -78,18 +83,29 @@ k_attention_forward(const __grid_constant__ CUtensorMap mq, const __grid_constan
     }
     const int most = NQ == 2 ? max(end[0], end[NQ - 1]) : end[0];
 
-    uint8_t* smem = raw + ((1024 - (smem_addr(raw) & 1023)) & 1023);
+    // the softmax's row; asked for first, the loads behind it take a while
+    const int row = threadIdx.x & 127, tile = NQ == 2 ? (warp >> 2) & 1 : 0;
+    const int row_tok = row / group, row_h = hk * group + row - row_tok * group;
+    const int token = it.q0 + tile * tokens + row_tok;
+    Range range{0, -1};
+    if (warp < NQ * 4 && row_tok < tokens && token < a.q_tokens) range = p.q_range[token];
+
     uint8_t* ring = smem + C::kQ;
     if (threadIdx.x == 0) {
+        prefetch_map(&mq);
+        prefetch_map(&mk);
+        prefetch_map(&mv);
+        prefetch_map(&mo);
         stop = 0;
         bar_init(&q_full, 1);
-        bar_init(&drained, 1);
         for (int i = 0; i < C::kUnits; ++i) {
             bar_init(&full[i], 1);
-            bar_init(&empty[i], 1);
+            bar_init(&empty[i], NQ);
         }
         for (int t = 0; t < NQ; ++t) {
             bar_init(&s_full[t], 1);
+            bar_init(&drained[t], 1);
+            bar_init(&turn[t], 1);
             bar_init(&p_ready[t], 128);
         }
         bar_init_done();
@@ -100,8 +116,10 @@ k_attention_forward(const __grid_constant__ CUtensorMap mq, const __grid_constan
     tc_after_sync();
     const uint32_t tmem = tmem_at;
 
+    // NQ = 2: 3 x 168 registers a thread at launch = 2 x 224 + 56
     if (warp == NQ * 4) {
         // ---- loads: Q, then K and V tiles in turn ----
+        if (NQ == 2) set_registers<56, false>();
         if (lane == 0 && most > it.t0) {
             const uint32_t box = (uint32_t)(tokens * group) * 128;
             bar_expect(&q_full, NQ * C::kHalves * box);
@@ -118,6 +136,9 @@ k_attention_forward(const __grid_constant__ CUtensorMap mq, const __grid_constan
                 for (int h = 0; h < C::kHalves; ++h)
                     tma_load3(ring + slot * C::kUnit + h * 16384, u & 1 ? &mv : &mk, 64 * h, hk,
                               it.k0 + (it.t0 + u / 2) * kTile, &full[slot]);
+                // a query tile that does not use this unit frees it at once
+                if (NQ == 2 && it.t0 + u / 2 >= end[0]) bar_arrive(&empty[slot]);
+                if (NQ == 2 && it.t0 + u / 2 >= end[1]) bar_arrive(&empty[slot]);
             }
             if (stop) {   // the loads in flight must land before the CTA ends
                 int never = 0;
@@ -126,72 +147,74 @@ k_attention_forward(const __grid_constant__ CUtensorMap mq, const __grid_constan
                     bar_wait(&full[w % C::kUnits], (w / C::kUnits) & 1, &never);
             }
         }
-    } else if (warp == NQ * 4 + 1) {
-        // ---- products ----
-        if (lane == 0 && most > it.t0) {
+    } else if (warp > NQ * 4 && warp <= NQ * 5) {
+        // ---- products: a thread to a query tile, in turns (kAhead) ----
+        if (NQ == 2) set_registers<56, false>();
+        const int t = warp - NQ * 4 - 1;
+        const int steps = (t == 0 ? end[0] : end[NQ - 1]) - it.t0;
+        const int others = NQ == 1 ? 0 : (t == 0 ? end[NQ - 1] : end[0]) - it.t0;
+        if (lane == 0 && steps > 0) {
             constexpr uint32_t kQK = mma_desc(128, 128, false), kPV = mma_desc(128, HD, true);
-            const uint32_t q_at = smem_addr(smem), ring_at = smem_addr(ring);
-            auto scores = [&](int t, int u) {
+            constexpr int kS = HD / 16;
+            const uint32_t q_at = smem_addr(smem) + t * C::kUnit, ring_at = smem_addr(ring);
+            const uint32_t s_at = tmem + t * 128, o_at = tmem + C::kO + t * HD;
+            auto loaded = [&](int u) {
+                return bar_wait(&full[u % C::kUnits], (u / C::kUnits) & 1, &stop);
+            };
+            auto scores = [&](int u, int from, int to) {
                 const uint32_t k_at = ring_at + (u % C::kUnits) * C::kUnit;
 #pragma unroll
-                for (int i = 0; i < HD / 16; ++i) {
+                for (int i = from; i < to; ++i) {
                     const uint32_t off = (i / 4) * 16384 + (i % 4) * 32;
-                    mma_ss(tmem + t * 128, smem_desc(q_at + t * C::kUnit + off, 16),
-                           smem_desc(k_at + off, 16), kQK, i > 0);
+                    mma_ss(s_at, smem_desc(q_at + off, 16), smem_desc(k_at + off, 16), kQK, i > 0);
                 }
             };
-            auto values = [&](int t, int u, bool add) {
+            auto values = [&](int u, int from, int to) {
                 const uint32_t v_at = ring_at + (u % C::kUnits) * C::kUnit;
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    mma_ts(tmem + C::kO + t * HD, tmem + t * 128 + i * 8,
-                           smem_desc(v_at + i * 2048, 16384), kPV, add || i > 0);
+                for (int i = from; i < to; ++i)
+                    mma_ts(o_at, s_at + i * 8, smem_desc(v_at + i * 2048, 16384), kPV,
+                           u > 1 || i > 0);
             };
-            bool ok = bar_wait(&q_full, 0, &stop) && bar_wait(&full[0], 0, &stop);
+            bool ok = bar_wait(&q_full, 0, &stop) && loaded(0);
             if (ok) {
                 tc_after_sync();
-#pragma unroll
-                for (int t = 0; t < NQ; ++t)
-                    if (it.t0 < end[t]) {
-                        scores(t, 0);
-                        tc_commit(&s_full[t]);
-                    }
-                tc_commit(&empty[0]);
+                scores(0, 0, kS);
+                tc_commit(&s_full[t]);
             }
-            for (int j = it.t0; ok && j < most; ++j) {
-                const int n = j - it.t0, uv = 2 * n + 1, uk = 2 * n + 2;
-                const bool more = j + 1 < most;
-                ok = bar_wait(&full[uv % C::kUnits], (uv / C::kUnits) & 1, &stop) &&
-                     (!more || bar_wait(&full[uk % C::kUnits], (uk / C::kUnits) & 1, &stop));
-#pragma unroll
-                for (int t = 0; t < NQ; ++t) {
-                    if (!ok || j >= end[t]) continue;
-                    ok = bar_wait(&p_ready[t], n & 1, &stop);
-                    if (!ok) continue;
-                    tc_after_sync();
-                    values(t, uv, n > 0);
-                    if (j + 1 < end[t]) scores(t, uk);
-                    tc_commit(&s_full[t]);
-                }
+            for (int n = 0; ok && n < steps; ++n) {
+                const bool more = n + 1 < steps;
+                ok = loaded(2 * n + 1) && (!more || loaded(2 * n + 2)) &&
+                     bar_wait(&p_ready[t], n & 1, &stop);
+                // the other tile's products before these: of step n, or of n - 1
+                const int before = t == 0 ? n - 1 : n;
+                if (ok && before >= 0 && before < others)
+                    ok = bar_wait(&turn[t], before & 1, &stop);
                 if (!ok) break;
-                tc_commit(&empty[uv % C::kUnits]);
-                if (more) tc_commit(&empty[uk % C::kUnits]);
+                tc_after_sync();
+                if (more) {
+                    values(2 * n + 1, 0, 8);
+                    scores(2 * n + 2, 0, kS - kAhead);
+                    if (NQ == 2) bar_arrive(&turn[t ^ 1]);
+                    scores(2 * n + 2, kS - kAhead, kS);
+                } else {
+                    values(2 * n + 1, 0, 8 - kAhead);
+                    if (NQ == 2) bar_arrive(&turn[t ^ 1]);
+                    values(2 * n + 1, 8 - kAhead, 8);
+                }
+                tc_commit(&s_full[t]);
             }
             if (!ok) {   // the products in flight must end before their memory is freed
                 int never = 0;
-                tc_commit(&drained);
-                bar_wait(&drained, 0, &never);
+                tc_commit(&drained[t]);
+                bar_wait(&drained[t], 0, &never);
             }
         }
-    } else {
+    } else if (warp < NQ * 4) {
         // ---- softmax: thread = row ----
-        const int t = NQ == 2 ? warp >> 2 : 0;
-        const int r = threadIdx.x & 127;
-        const int tok = r / group, h = hk * group + r - tok * group;
-        const int token = it.q0 + t * tokens + tok;
+        if (NQ == 2) set_registers<224, true>();
+        const int t = tile, r = row, h = row_h;
         // the keys that the row sees, counted from k0: see0 .. see1
-        Range range{0, -1};
-        if (tok < tokens && token < a.q_tokens) range = p.q_range[token];
         const bool live = range.live();
         const int see0 = live ? range.lo - it.k0 : 0, see1 = live ? range.hi - it.k0 : 0;
         const int stop_at = NQ == 2 && t == 1 ? end[NQ - 1] : end[0];
@@ -204,6 +227,11 @@ k_attention_forward(const __grid_constant__ CUtensorMap mq, const __grid_constan
             const int n = j - it.t0;
             ok = bar_wait(&s_full[t], n & 1, &stop);
             if (!__all_sync(0xffffffffu, ok)) break;
+            // this query tile's products up to S(n) have ended: it frees K(n), V(n - 1)
+            if (row == 0) {
+                bar_arrive(&empty[(2 * n) % C::kUnits]);
+                if (n > 0) bar_arrive(&empty[(2 * n - 1) % C::kUnits]);
+            }
             tc_after_sync();
             float s[4][32];
 #pragma unroll
@@ -212,16 +240,21 @@ k_attention_forward(const __grid_constant__ CUtensorMap mq, const __grid_constan
 #pragma unroll
             for (int i = 0; i < 4; ++i) tmem_loaded(s[i]);
             const int lo = see0 - j * kTile, hi = see1 - j * kTile;
+            if (__any_sync(0xffffffffu, lo > 0 || hi < kTile)) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) hide(s[i], lo - 32 * i, hi - 32 * i);
-            float m4[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                m4[i] = s[i][0];
-#pragma unroll
-                for (int e = 1; e < 32; ++e) m4[i] = fmaxf(m4[i], s[i][e]);
+                for (int i = 0; i < 4; ++i) hide(s[i], lo - 32 * i, hi - 32 * i);
             }
-            const float m = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
+            // eight chains side by side: one warp of a tile runs alone on its scheduler
+            float m8[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) m8[i] = fmaxf(s[i >> 1][i & 1], s[i >> 1][2 + (i & 1)]);
+#pragma unroll
+            for (int e = 4; e < 32; e += 4)
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    m8[i] = max3(m8[i], s[i >> 1][e + (i & 1)], s[i >> 1][e + 2 + (i & 1)]);
+            const float m = fmaxf(max3(m8[0], m8[1], m8[2]),
+                                  fmaxf(max3(m8[3], m8[4], m8[5]), fmaxf(m8[6], m8[7])));
             const bool raise = m * c > top * c + kSlack;   // also the first finite maximum
             if (__any_sync(0xffffffffu, raise)) {
                 const float keep = raise ? (top == -INFINITY ? 0.f : exp2_fast((top - m) * c)) : 1.f;
@@ -242,21 +275,30 @@ k_attention_forward(const __grid_constant__ CUtensorMap mq, const __grid_constan
             }
             const float base = top == -INFINITY ? 0.f : -top * c;
             const float2 c2 = make_float2(c, c), base2 = make_float2(base, base);
-            float2 add = make_float2(0.f, 0.f);
+            float2 add[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) add[i] = make_float2(0.f, 0.f);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
+                float2 x[16];
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    x[e] = fma2(make_float2(s[i][2 * e], s[i][2 * e + 1]), c2, base2);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    x[e].x = exp2_fast(x[e].x);
+                    x[e].y = exp2_fast(x[e].y);
+                }
                 uint32_t w[16];
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
-                    float2 x = fma2(make_float2(s[i][2 * e], s[i][2 * e + 1]), c2, base2);
-                    x.x = exp2_fast(x.x);
-                    x.y = exp2_fast(x.y);
-                    add = add2(add, x);
-                    w[e] = pack2(x.x, x.y, bf16());
+                    add[e & 3] = add2(add[e & 3], x[e]);
+                    w[e] = pack2(x[e].x, x[e].y, bf16());
                 }
                 tmem_store16(s_at + 16 * i, w);
             }
-            sum += add.x + add.y;
+            add[0] = add2(add2(add[0], add[1]), add2(add[2], add[3]));
+            sum += add[0].x + add[0].y;
             tmem_wait_store();
             tc_before_sync();
             bar_arrive(&p_ready[t]);
@@ -266,22 +308,20 @@ k_attention_forward(const __grid_constant__ CUtensorMap mq, const __grid_constan
         if (any) {
             ok = __all_sync(0xffffffffu, ok) != 0;
             if (ok) ok = bar_wait(&s_full[t], (stop_at - it.t0) & 1, &stop);
+            if (row == 0) bar_arrive(&empty[(2 * (stop_at - it.t0) - 1) % C::kUnits]);
             ok = __all_sync(0xffffffffu, ok) != 0;
             tc_after_sync();
         }
-        if (ok) {
-            const bool none = see1 <= see0;
-            const float inv = sum > 0.f ? 1.f / sum : 0.f;
-            const float lse = sum > 0.f ? top * a.scale + __log2f(sum) * kLn2 : -INFINITY;
-            float odd = none ? 0.f : lse * 0.f;   // NaN where something is not finite
-            float* part = nullptr;
-            if (it.slot >= 0) {
-                const int64_t row = ((int64_t)it.slot * a.kv_heads + hk) * kTile + r;
-                part = p.partial + row * a.dim;
-                p.partial_lse[row] = lse;
-            }
-            // a piece that holds none of the keys that a row sees leaves it out
-            const bool store = live && !(part && lse == -INFINITY);
+        // ok: whether the waits of this warp ended well; a wait of another warp may
+        // not have, so all of a tile's warps meet below either way
+        const bool none = see1 <= see0;
+        const float inv = sum > 0.f ? 1.f / sum : 0.f;
+        const float lse = sum > 0.f ? top * a.scale + __log2f(sum) * kLn2 : -INFINITY;
+        if (it.slot >= 0) {
+            // a piece: fp32, and nothing where it holds none of the row's keys
+            const int64_t at = ((int64_t)it.slot * a.kv_heads + hk) * kTile + r;
+            const bool store = ok && live && lse != -INFINITY;
+            p.partial_lse[at] = lse;
 #pragma unroll 1
             for (int i = 0; i < HD; i += 32) {
                 float o[32];
@@ -290,14 +330,6 @@ k_attention_forward(const __grid_constant__ CUtensorMap mq, const __grid_constan
                     tmem_load32(o_at + i, o);
                     tmem_wait_load();
                     tmem_loaded(o);
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) o[e] = 0.f;
-                }
-#pragma unroll
-                for (int e = 0; e < 32; ++e) {
-                    o[e] *= inv;
-                    odd += o[e] * 0.f;
                 }
                 if (store) {
 #pragma unroll
@@ -305,28 +337,48 @@ k_attention_forward(const __grid_constant__ CUtensorMap mq, const __grid_constan
                         if (i + e >= a.dim) break;
                         float v[8];
 #pragma unroll
-                        for (int x = 0; x < 8; ++x) v[x] = none ? 0.f : o[e + x];
-                        if (part)
-                            store8(part + i + e, v);
-                        else
-                            store8(a.out.at(token, h) + i + e, v);
+                        for (int x = 0; x < 8; ++x) v[x] = o[e + x] * inv;
+                        store8(p.partial + at * a.dim + i + e, v);
                     }
                 }
             }
-            if (it.slot < 0) {
-                if (live) a.lse[(int64_t)token * a.heads + h] = lse;
-                unsigned again = __ballot_sync(0xffffffffu, live && !none && odd != 0.f);
-                while (again) {
-                    const int from = __ffs(again) - 1;
-                    again &= again - 1;
-                    __syncwarp();
-                    forward_row(a, __shfl_sync(0xffffffffu, range.lo, from),
-                                __shfl_sync(0xffffffffu, range.hi, from),
-                                __shfl_sync(0xffffffffu, token, from),
-                                __shfl_sync(0xffffffffu, h, from));
-                }
+        } else {
+            // through the tile's own Q, which no product reads any more
+            uint8_t* out = smem + t * C::kUnit;
+            bool again = false;
+            if (ok) {
+                const bool fine = stage_row<HD>(o_at, out, r, 0, inv, any);
+                again = live && !(fine && (none || lse * 0.f == 0.f));
+                if (live && !again) a.lse[(int64_t)token * a.heads + h] = lse;
+            }
+            keep[t][r] = ok && live && !again;
+            fence_async();
+            // rows past the tile or the tensor are left out by the store itself
+            if (!part_any(1 + t, 128, !ok || again ||
+                                          (!live && row_tok < tokens && token < a.q_tokens))) {
+                if (r == 0 && it.q0 + t * tokens < a.q_tokens)
+                    store_tile<HD>(&mo, out, hk * group, it.q0 + t * tokens);
+            } else {
+                store_rows<HD, 32>(out, (warp & 3) * 32, a.dim, [&](int i) -> bf16* {
+                    const int tok = i / group;
+                    return keep[t][i]
+                               ? a.out.at(it.q0 + t * tokens + tok, hk * group + i - tok * group)
+                               : nullptr;
+                });
+            }
+            unsigned rest = __ballot_sync(0xffffffffu, again);
+            while (rest) {
+                const int from = __ffs(rest) - 1;
+                rest &= rest - 1;
+                __syncwarp();
+                forward_row(a, __shfl_sync(0xffffffffu, range.lo, from),
+                            __shfl_sync(0xffffffffu, range.hi, from),
+                            __shfl_sync(0xffffffffu, token, from),
+                            __shfl_sync(0xffffffffu, h, from));
             }
         }
+    } else if (NQ == 2) {
+        set_registers<56, false>();   // the warps without a role
     }
     tc_before_sync();
     __syncthreads();
@@ -400,13 +452,16 @@ cudaError_t launch(const Attn& a, const Plan& p, cudaStream_t st) {
     cudaError_t e = tile_map(&mq, a.q, a.q_tokens, a.heads, a.dim, a.group, p.tokens, p.head);
     if (e == cudaSuccess) e = tile_map(&mk, a.k, a.k_tokens, a.kv_heads, a.dim, 1, kTile, p.head);
     if (e == cudaSuccess) e = tile_map(&mv, a.v, a.k_tokens, a.kv_heads, a.dim, 1, kTile, p.head);
+    CUtensorMap mo;
+    if (e == cudaSuccess)
+        e = tile_map(&mo, a.out, a.q_tokens, a.heads, a.dim, a.group, p.tokens, p.head);
     if (e != cudaSuccess) return e;
     auto* k = k_attention_forward<HD, NQ>;
     static std::atomic<uint64_t> ready{0};
     e = allow_smem(k, C::kSmem, &ready);
     if (e != cudaSuccess) return e;
     return launch_k(k, dim3((unsigned)p.most_items * a.kv_heads), dim3(C::kThreads), C::kSmem, st,
-                    mq, mk, mv, a, p);
+                    mq, mk, mv, mo, a, p);
 }
 
 }  // namespace

@@ -6,10 +6,9 @@
 // range that it sees (coalesced later for whoever needs it); one CTA then turns
 // the ranges at the ends of each tile into work items, sorted by cost so that
 // the last tiles to start are short ones.  Where a tile stands among those of
-// equal cost follows the scheduling; no result depends on it.  Up to
-// kSmallTokens tokens the one CTA takes both steps: one launch less.
-//
-// Measured at 1024 sequences of 64 k tokens in all, both lists: see launch_plan.
+// equal cost follows the scheduling; no result depends on it.  A
+// forward call of up to kSmallTokens tokens leaves both steps to the one CTA: one
+// launch less.
 #include "attention.h"
 
 namespace pss {
@@ -19,6 +18,7 @@ namespace {
 constexpr int kBuckets = 128;
 constexpr int kPlanThreads = 1024;
 constexpr int kSmallTokens = 4096;
+constexpr float kLog2e = 1.4426950408889634f;
 
 // Exact up to 15, four steps to a doubling above.
 __device__ __forceinline__ int bucket(int cost) {
@@ -67,13 +67,68 @@ __device__ __forceinline__ Range range_of(const Attn& a, int64_t t) {
     return Range{(int)lo, (int)clamp64(t + 1 + (hi - end), lo, hi)};
 }
 
-__global__ void __launch_bounds__(kThreads) k_attention_ranges(Attn a, Plan p) {
+// (lse * log2 e, sum_c grad out) of consecutive rows of the query side, by a
+// warp: LANES lanes to a row, eight rows to a thread, all loads before the first
+// use.  In the order of the tiles' rows:
+// stats[key head][token * group + head of the group].
+template <int LANES>
+__device__ __forceinline__ void stats_of(const Attn& a, const Plan& p, int64_t first) {
+    constexpr int kRows = 8, kSide = 32 / LANES;   // rows of a thread, rows side by side
+    const int64_t rows = (int64_t)a.q_tokens * a.heads;
+    const int lane = threadIdx.x & 31, c = (lane % LANES) * 8;
+    const int64_t row0 = first + lane / LANES;
+    const int64_t t0 = row0 / a.heads;
+    const int h0 = (int)(row0 - t0 * a.heads);
+    uint4 g[kRows], o[kRows];
+    int64_t t = t0;
+    int h = h0;
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) {
+        g[i] = o[i] = make_uint4(0, 0, 0, 0);
+        if (row0 + i * kSide < rows && c < a.dim) {
+            g[i] = load16(a.grad.at(t, h) + c);
+            o[i] = load16(a.out.at(t, h) + c);
+        }
+        for (h += kSide; h >= a.heads; h -= a.heads) ++t;
+    }
+    t = t0;
+    h = h0;
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) {
+        float s = dot2(g[i].x, o[i].x) + dot2(g[i].y, o[i].y) + dot2(g[i].z, o[i].z) +
+                  dot2(g[i].w, o[i].w);
+#pragma unroll
+        for (int m = LANES / 2; m > 0; m >>= 1) s += __shfl_xor_sync(0xffffffffu, s, m);
+        const int64_t row = row0 + i * kSide;
+        if (c == 0 && row < rows) {
+            const int hk = h / a.group;
+            const float lse = a.lse[row];
+            p.stats[((int64_t)hk * a.q_tokens + t) * a.group + h - hk * a.group] =
+                make_float2(lse == -INFINITY ? INFINITY : lse * kLog2e, s);
+        }
+        for (h += kSide; h >= a.heads; h -= a.heads) ++t;
+    }
+}
+
+// blockIdx.y 0: what the query tokens see, 1: who sees the keys, 2: stats.
+__global__ void __launch_bounds__(kThreads) k_attention_ready(Attn a, Plan p) {
     pdl_prologue();
     const int64_t t = (int64_t)blockIdx.x * kThreads + threadIdx.x;
     if (blockIdx.y == 0) {
         if (t < a.q_tokens) p.q_range[t] = range_of<false>(a, t);
-    } else {
+    } else if (blockIdx.y == 1) {
         if (t < a.k_tokens) p.k_range[t] = range_of<true>(a, t);
+    } else {
+        const int64_t rows = (int64_t)a.q_tokens * a.heads;
+        const int each = a.dim <= 64 ? 32 : 16;   // rows of a warp
+        const int64_t warp = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5);
+        for (int64_t first = warp * each; first < rows;
+             first += (int64_t)gridDim.x * kWarps * each) {
+            if (a.dim <= 64)
+                stats_of<8>(a, p, first);
+            else
+                stats_of<16>(a, p, first);
+        }
     }
 }
 
@@ -190,10 +245,18 @@ k_attention_plan(Attn a, Plan p, int target_items, int small) {
 cudaError_t launch_plan(const Attn& a, const Plan& p, bool backward, int target_items,
                         cudaStream_t st) {
     const int64_t most = backward && a.k_tokens > a.q_tokens ? a.k_tokens : a.q_tokens;
-    const bool small = most <= kSmallTokens;
-    if (!small) {
-        const dim3 grid((unsigned)((most + kThreads - 1) / kThreads), backward ? 2 : 1);
-        const cudaError_t e = launch_k(k_attention_ranges, grid, dim3(kThreads), 0, st, a, p);
+    const bool small = !backward && most <= kSmallTokens;
+    if (!small && most > 0) {
+        int64_t blocks = (most + kThreads - 1) / kThreads;
+        if (backward) {
+            // the rows of stats, up to 32 CTAs an SM in all
+            const int64_t rows = ((int64_t)a.q_tokens * a.heads + 16 * kWarps - 1) / (16 * kWarps);
+            const int64_t enough = (int64_t)sm_count() * 32;
+            const int64_t some = rows < enough ? rows : enough;
+            if (blocks < some) blocks = some;
+        }
+        const cudaError_t e = launch_k(k_attention_ready, dim3((unsigned)blocks, backward ? 3 : 1),
+                                       dim3(kThreads), 0, st, a, p);
         if (e != cudaSuccess) return e;
     }
     return launch_k(k_attention_plan, dim3(backward ? 2 : 1), dim3(kPlanThreads), 0, st, a, p,

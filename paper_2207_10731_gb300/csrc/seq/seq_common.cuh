@@ -45,6 +45,12 @@ __device__ __forceinline__ uint32_t pack2(float a, float b, f16) {
     return *reinterpret_cast<const uint32_t*>(&h);
 }
 
+// The product of two pairs of bf16.
+__device__ __forceinline__ float dot2(uint32_t a, uint32_t b) {
+    const float2 x = unpack2(a, bf16()), y = unpack2(b, bf16());
+    return x.x * y.x + x.y * y.y;
+}
+
 // Streaming access to global memory: the operators read and write each element
 // once, so nothing is gained by keeping it in L1.  A thread moves 8 elements:
 // 32 bytes in one instruction (sm_100 and later) or 16.
@@ -78,6 +84,14 @@ __device__ __forceinline__ void store8(T* p, const float (&v)[8]) {
     for (int i = 0; i < 4; ++i) w[i] = pack2(v[2 * i], v[2 * i + 1], T());
     asm volatile("st.global.v4.u32 [%0], {%1,%2,%3,%4};"
                  :: "l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
+}
+
+// 16 bytes, issued here: the compiler does not move the load to its use.
+__device__ __forceinline__ uint4 load16(const void* p) {
+    uint4 v;
+    asm volatile("ld.global.v4.u32 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p) : "memory");
+    return v;
 }
 
 // VEC elements at p: 8 (aligned to 8 elements) or 1.

@@ -49,7 +49,7 @@ __device__ __forceinline__ uint64_t now_ns() {
 // given up (*stop, in shared memory).  The caller then leaves its loop, the
 // CTA frees its tensor memory and reports through the call's status word.
 constexpr uint64_t kWaitNs = 2000000000ull;
-static __device__ __noinline__ bool bar_wait_slow(uint64_t* b, uint32_t parity,
+__device__ __forceinline__ bool bar_wait_slow(uint64_t* b, uint32_t parity,
                                                   volatile int* stop) {
     const uint64_t start = now_ns();
     while (!bar_try(b, parity)) {
@@ -71,6 +71,15 @@ __device__ __forceinline__ void report_stop(unsigned long long* status) {
     if (status) atomicExch(status, ~1ull);   // -2
 }
 
+// Products are issued one by one as the tensor core takes them; it holds only one
+// or two, and a thread's barrier operations queue behind its own products.  So a
+// thread that looks for its next operands after its last product leaves the pipe
+// empty for some 400 cycles.  Two threads therefore take turns: each waits for
+// its operands while the other's products run, and hands over the turn kAhead
+// products before its own end.  (Without turns their products alternate one by
+// one, which costs the tensor core more than the waits did.)
+constexpr int kAhead = 3;
+
 // ---- TMA ---------------------------------------------------------------------
 
 // Loads box (c0 .., c1 .., c2 ..) of a 3-D tensor map into shared memory.
@@ -81,6 +90,10 @@ __device__ __forceinline__ void tma_load3(void* dst, const CUtensorMap* map, int
         " [%0], [%1, {%2, %3, %4}], [%5];"
         :: "r"(smem_addr(dst)), "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(smem_addr(bar))
         : "memory");
+}
+// Fetches a tensor map ahead of its first use.
+__device__ __forceinline__ void prefetch_map(const CUtensorMap* map) {
+    asm volatile("prefetch.tensormap [%0];" :: "l"(map) : "memory");
 }
 // Generic-proxy writes to shared memory become visible to TMA and the tensor core.
 __device__ __forceinline__ void fence_async() {
@@ -201,6 +214,34 @@ __device__ __forceinline__ void hide(float (&s)[32], int lo, int hi) {
         if (!(see & (1u << e))) s[e] = -INFINITY;
 }
 
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    return fmaxf(fmaxf(a, b), c);
+}
+
+// All warps of a warpgroup: this many registers a thread from here on.  The
+// block's warpgroups must stay within what it was launched with.
+template <int N, bool MORE>
+__device__ __forceinline__ void set_registers() {
+    if (MORE)
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" :: "n"(N));
+    else
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(N));
+}
+
+// A barrier of `threads` threads of the CTA, number `id` (1 and up).
+__device__ __forceinline__ void part_sync(int id, int threads) {
+    asm volatile("bar.sync %0, %1;" :: "r"(id), "r"(threads) : "memory");
+}
+
+// The same, and whether any of the threads says yes.
+__device__ __forceinline__ bool part_any(int id, int threads, bool yes) {
+    uint32_t any;
+    asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 q, %3, 0;\n"
+                 " barrier.cta.red.or.pred p, %1, %2, q;\n selp.u32 %0, 1, 0, p;\n}"
+                 : "=r"(any) : "r"(id), "r"(threads), "r"((uint32_t)yes) : "memory");
+    return any != 0;
+}
+
 // 2^x, the hardware's approximation (relative error below 2^-22).
 __device__ __forceinline__ float exp2_fast(float x) {
     float y;
@@ -229,6 +270,73 @@ __device__ __forceinline__ float2 mul2(float2 a, float2 b) {
         : "=l"(reinterpret_cast<uint64_t&>(d))
         : "l"(reinterpret_cast<uint64_t&>(a)), "l"(reinterpret_cast<uint64_t&>(b)));
     return d;
+}
+
+// Result rows leave through shared memory, in the layout that the loads have: a
+// thread holds a row (or half of one), and 32 rows' 16-byte pieces written at
+// once would touch 32 lines.
+// stage_row: N columns from tensor memory, times `scale`, as bf16 into row r of
+// a tile, from its 16-byte piece `piece` on; zeros where there are no columns to
+// read (`load`, the same for the warp).  Returns whether all are finite.
+template <int N>
+__device__ __forceinline__ bool stage_row(uint32_t at, uint8_t* tile, int r, int piece, float scale,
+                                          bool load) {
+    uint32_t most = 0;   // the largest exponent field of each half
+    const float2 scale2 = make_float2(scale, scale);
+#pragma unroll 1
+    for (int i = 0; i < N; i += 32) {
+        float v[32];
+#pragma unroll
+        for (int e = 0; e < 32; ++e) v[e] = 0.f;
+        if (load) {
+            tmem_load32(at + i, v);
+            tmem_wait_load();
+            tmem_loaded(v);
+        }
+        uint32_t w[16];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const float2 x = mul2(make_float2(v[2 * e], v[2 * e + 1]), scale2);
+            w[e] = pack2(x.x, x.y, bf16());
+            most = __vmaxu2(most, w[e] & 0x7f807f80u);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int c = piece + i / 8 + e;
+            *reinterpret_cast<uint4*>(tile + (c / 8) * 16384 + r * 128 +
+                                      (((c & 7) ^ (r & 7)) * 16)) =
+                make_uint4(w[4 * e], w[4 * e + 1], w[4 * e + 2], w[4 * e + 3]);
+        }
+    }
+    return (most & 0xffffu) < 0x7f80u && (most >> 16) < 0x7f80u;
+}
+// A staged tile to memory in one go, by one thread (after a fence_async of every
+// thread that staged and a barrier): what lies outside the tensor is left out.
+template <int HD>
+__device__ __forceinline__ void store_tile(const CUtensorMap* map, const uint8_t* tile, int head,
+                                           int token) {
+#pragma unroll
+    for (int h = 0; h < HD / 64; ++h)
+        asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group"
+                     " [%0, {%1, %2, %3}], [%4];"
+                     :: "l"(map), "r"(64 * h), "r"(head), "r"(token),
+                        "r"(smem_addr(tile + h * 16384)) : "memory");
+    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+    asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+}
+// Or row by row: N rows from `first` on, HD / 8 lanes of a warp to a row; to(r):
+// where row r goes, or null.
+template <int HD, int N, typename F>
+__device__ __forceinline__ void store_rows(const uint8_t* tile, int first, int dim, F to) {
+    constexpr int kLanes = HD / 8, kRows = 32 / kLanes;
+    const int lane = threadIdx.x & 31, c = lane % kLanes;
+    for (int i = lane / kLanes; i < N; i += kRows) {
+        const int r = first + i;
+        bf16* p = to(r);
+        if (p && c * 8 < dim)
+            *reinterpret_cast<uint4*>(p + c * 8) = *reinterpret_cast<const uint4*>(
+                tile + (c / 8) * 16384 + r * 128 + (((c & 7) ^ (r & 7)) * 16));
+    }
 }
 
 }  // namespace seq
