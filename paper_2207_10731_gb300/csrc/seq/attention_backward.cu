@@ -21,9 +21,9 @@
 //   dKV: P(n) over S, dS(n) over dP:
 //        dS(n) | dV += P(n) dO(n), S(n+1);   P(n+1) | dK += dS(n) Q(n), dP(n+1).
 // So the first operand's tiles (K of dQ, Q of dKV) live for three steps and
-// have three buffers, the others two.  No product signals that a buffer is
-// free: the elementwise warps do, when they see S or dP of a later step, which
-// the tensor core finished after it.
+// have three buffers, the others two.  Most buffers are freed by the elementwise
+// warps, when they see S or dP of a later step, which the tensor core finished
+// after it; K of dQ, which is wanted again soonest, by its last product.
 //
 // What a row does not see gets S = -infinity, hence P = 0; a row that sees
 // nothing has L = +infinity.  Non-finite rows are computed again by the
@@ -60,10 +60,12 @@ struct Cfg {
     static constexpr int kA = 3, kB = 2;                       // buffers of the two rings
     static constexpr int kSmem = 2 * kTileBytes + (kA + kB) * kUnit;
     static constexpr int kCtas = TN == 64 && HD == 64 ? 2 : 1; // to an SM
-    // threads that issue products, in turns (kAhead); where two CTAs share the SM
-    // the other one's products fill the gaps, and registers are short
+    // dK, dV: threads that issue products, in turns (kAhead); where two CTAs share
+    // the SM the other one's products fill the gaps, and registers are short.  dQ
+    // has one long run of products a step: one thread (two were 16 % slower).
     static constexpr int kIssuers = kCtas == 2 ? 1 : 2;
-    static constexpr int kThreads = kCompute + 32 + 32 * kIssuers;
+    static constexpr int kThreads = kCompute + 64;
+    static constexpr int kThreadsKV = kCompute + 32 + 32 * kIssuers;
     static constexpr int kCols = kCtas == 2 ? 256 : 512;       // tensor-memory columns
     static constexpr int kChunks = TN / 64;                    // a thread's columns / 32
 };
@@ -72,7 +74,7 @@ struct Cfg {
 template <int TN>
 struct Shared {
     uint64_t resident, a_full[3], a_empty[3], b_full[2], b_empty[2];
-    uint64_t s_full[2], dp_full, p_ready, ds_ready[2], stats_full[2], stats_free[2], done, turn[2];
+    uint64_t s_full[2], dp_full, p_ready, ds_ready, stats_full[2], stats_free[2], done, turn[2];
     union alignas(16) {
         struct {
             float lse[2][TN], delta[2][TN];   // dK, dV
@@ -179,11 +181,8 @@ k_attention_dq(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
         for (int i = 0; i < C::kB; ++i) bar_init(&sh.b_full[i], 1), bar_init(&sh.b_empty[i], 1);
         for (int i = 0; i < 2; ++i) bar_init(&sh.s_full[i], 1);
         bar_init(&sh.dp_full, 1);
-        // two: dS(n + 1) can be there before both issuing threads have seen dS(n)
-        for (int i = 0; i < 2; ++i) bar_init(&sh.ds_ready[i], kCompute);
-        bar_init(&sh.done, C::kIssuers);
-        bar_init(&sh.turn[0], 1);
-        bar_init(&sh.turn[1], 1);
+        bar_init(&sh.ds_ready, kCompute);
+        bar_init(&sh.done, 1);
         bar_init_done();
     }
     if (warp == 0) tmem_alloc(&sh.tmem, C::kCols);
@@ -222,12 +221,11 @@ k_attention_dq(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
                 if (n < n_tiles) bar_wait(&sh.a_full[n % C::kA], (n / C::kA) & 1, &never);
             }
         }
-    } else if (warp >= 9) {
+    } else if (warp == 9) {
         // ---- products ----
         if (lane == 0 && n_tiles > 0) {
             const uint32_t q_at = smem_addr(smem), g_at = q_at + C::kTileBytes;
             const uint32_t a_at = smem_addr(ring_a), b_at = smem_addr(ring_b);
-            constexpr int kS = HD / 16;
             auto a_buf = [&](int n) { return a_at + (n % C::kA) * C::kUnit; };
             auto b_buf = [&](int n) { return b_at + (n % C::kB) * C::kUnit; };
             auto s_buf = [&](int n) { return tmem + (n & 1) * TN; };
@@ -237,54 +235,34 @@ k_attention_dq(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
             auto have_b = [&](int n) {
                 return bar_wait(&sh.b_full[n % C::kB], (n / C::kB) & 1, stop);
             };
-            // turn i is handed over by the other thread's step n
-            auto my_turn = [&](int i, int n) {
-                return C::kIssuers == 1 || n < 0 || bar_wait(&sh.turn[i], n & 1, stop);
-            };
-            auto hand_over = [&](int i) {
-                if (C::kIssuers == 2) bar_arrive(&sh.turn[i]);
-            };
-            const bool x = C::kIssuers == 1 || warp == 9, y = C::kIssuers == 1 || warp == 10;
-            bool ok = bar_wait(&sh.resident, 0, stop);
-            if (ok && y && (ok = have_a(0))) {
+            bool ok = bar_wait(&sh.resident, 0, stop) && have_a(0) && have_b(0) &&
+                      (n_tiles == 1 || have_a(1));
+            if (ok) {
                 tc_after_sync();
                 mma_rows<HD, TN>(s_buf(0), q_at, a_buf(0));
                 tc_commit(&sh.s_full[0]);
-            }
-            if (ok && x && (ok = have_b(0))) {
-                tc_after_sync();
                 mma_rows<HD, TN>(dp_at, g_at, b_buf(0));
                 tc_commit(&sh.dp_full);
-            }
-            if (ok && y && n_tiles > 1 && (ok = have_a(1))) {
-                mma_rows<HD, TN>(s_buf(1), q_at, a_buf(1));
-                tc_commit(&sh.s_full[1]);
+                if (n_tiles > 1) {
+                    mma_rows<HD, TN>(s_buf(1), q_at, a_buf(1));
+                    tc_commit(&sh.s_full[1]);
+                }
             }
             for (int n = 0; ok && n < n_tiles; ++n) {
                 const bool more = n + 1 < n_tiles, more2 = n + 2 < n_tiles;
-                if (!(ok = (!x || !more || have_b(n + 1)) && (!y || !more2 || have_a(n + 2)) &&
-                           bar_wait(&sh.ds_ready[n & 1], (n >> 1) & 1, stop)))
+                if (!(ok = (!more || have_b(n + 1)) && bar_wait(&sh.ds_ready, n & 1, stop)))
                     break;
-                if (x && more) {   // dP(n) was read before dS(n) was announced
-                    if (!(ok = my_turn(0, n - 1))) break;
-                    tc_after_sync();
-                    mma_rows<HD, TN>(dp_at, g_at, b_buf(n + 1), 0, kS - kAhead);
-                    hand_over(1);
-                    mma_rows<HD, TN>(dp_at, g_at, b_buf(n + 1), kS - kAhead, kS);
+                tc_after_sync();
+                if (more) {   // dP(n) was read before dS(n) was announced
+                    mma_rows<HD, TN>(dp_at, g_at, b_buf(n + 1));
                     tc_commit(&sh.dp_full);
                 }
-                if (y) {
-                    if (!(ok = my_turn(1, more ? n : -1))) break;
-                    tc_after_sync();
-                    mma_columns<HD, TN>(dq_at, s_buf(n), a_buf(n), n > 0);
-                    if (more2) {
-                        mma_rows<HD, TN>(s_buf(n), q_at, a_buf(n + 2), 0, kS - kAhead);
-                        hand_over(0);
-                        mma_rows<HD, TN>(s_buf(n), q_at, a_buf(n + 2), kS - kAhead, kS);
-                        tc_commit(&sh.s_full[n & 1]);
-                    } else {
-                        hand_over(0);
-                    }
+                mma_columns<HD, TN>(dq_at, s_buf(n), a_buf(n), n > 0);
+                tc_commit(&sh.a_empty[n % C::kA]);
+                if (more2) {
+                    if (!(ok = have_a(n + 2))) break;
+                    mma_rows<HD, TN>(s_buf(n), q_at, a_buf(n + 2));
+                    tc_commit(&sh.s_full[n & 1]);
                 }
             }
             tc_commit(&sh.done);
@@ -307,8 +285,6 @@ k_attention_dq(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
         for (int n = 0; n < n_tiles; ++n) {
             ok = ok && bar_wait(&sh.s_full[n & 1], (n >> 1) & 1, stop);
             ok = __all_sync(0xffffffffu, ok) != 0;
-            // S(n) came after dQ(n - 2): that K may be overwritten
-            if (threadIdx.x == 0 && n >= 2) bar_arrive(&sh.a_empty[(n - 2) % C::kA]);
             tc_after_sync();
             float s[C::kChunks][32], d[C::kChunks][32];
             const uint32_t s_at = tmem + (n & 1) * TN + half * (TN / 2) + lanes;
@@ -363,7 +339,7 @@ k_attention_dq(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
             store_bf16(s_at, d);
             tmem_wait_store();
             tc_before_sync();
-            bar_arrive(&sh.ds_ready[n & 1]);
+            bar_arrive(&sh.ds_ready);
             if (!ok) break;
         }
         if (n_tiles == 1 && live && half == 0) p.stats[at_stats] = st;   // for dK and dV
@@ -410,7 +386,7 @@ k_attention_dq(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
 }
 
 template <int HD, int TN>
-__global__ void __launch_bounds__(Cfg<HD, TN>::kThreads, Cfg<HD, TN>::kCtas)
+__global__ void __launch_bounds__(Cfg<HD, TN>::kThreadsKV, Cfg<HD, TN>::kCtas)
 k_attention_dkv(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mg,
                 const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv,
                 const __grid_constant__ CUtensorMap mdk, const __grid_constant__ CUtensorMap mdv,
@@ -447,7 +423,7 @@ k_attention_dkv(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
         bar_init(&sh.s_full[0], 1);
         bar_init(&sh.dp_full, 1);
         bar_init(&sh.p_ready, kCompute);
-        bar_init(&sh.ds_ready[0], kCompute);
+        bar_init(&sh.ds_ready, kCompute);
         for (int i = 0; i < 2; ++i) {
             bar_init(&sh.stats_full[i], 32);
             bar_init(&sh.stats_free[i], kCompute);
@@ -460,7 +436,7 @@ k_attention_dkv(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
     // rows that no load writes (TN is not a multiple of the group) enter the
     // products as zeros
     for (int i = threadIdx.x; i < (C::kA + C::kB) * C::kHalves * (TN - rows) * 8;
-         i += C::kThreads) {
+         i += C::kThreadsKV) {
         const int slab = i / ((TN - rows) * 8), at = i - slab * (TN - rows) * 8;
         reinterpret_cast<uint4*>(ring_a + slab * C::kSlab + rows * 128)[at] =
             make_uint4(0, 0, 0, 0);
@@ -576,7 +552,7 @@ k_attention_dkv(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
                 }
                 if (y) {   // dK += dS(n) Q(n), then dP(n + 1) over dS(n)
                     if (!(ok = have_a(n) && (!more || have_b(n + 1)) &&
-                               bar_wait(&sh.ds_ready[0], n & 1, stop) && my_turn(1, n)))
+                               bar_wait(&sh.ds_ready, n & 1, stop) && my_turn(1, n)))
                         break;
                     tc_after_sync();
                     mma_columns<HD, TN>(dk_at, dp_at, a_buf(n), n > 0);
@@ -675,7 +651,7 @@ k_attention_dkv(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
             store_bf16(d_at, d);
             tmem_wait_store();
             tc_before_sync();
-            bar_arrive(&sh.ds_ready[0]);
+            bar_arrive(&sh.ds_ready);
         }
         // ---- epilogue: the first four warps stage dV, the others dK ----
         const bool any = n_tiles > 0;
@@ -751,8 +727,8 @@ cudaError_t launch(const Attn& a, const Plan& p, cudaStream_t st) {
         keys(&mx, a.dk, kTile);
         keys(&my, a.dv, kTile);
         if (e == cudaSuccess)
-            e = launch_k(dkv, dim3((unsigned)p.key_tiles * a.kv_heads), dim3(C::kThreads), kSmem,
-                         st, mq, mg, mk, mv, mx, my, a, p);
+            e = launch_k(dkv, dim3((unsigned)p.key_tiles * a.kv_heads), dim3(C::kThreadsKV),
+                         kSmem, st, mq, mg, mk, mv, mx, my, a, p);
     }
     return e;
 }

@@ -68,12 +68,12 @@ __device__ __forceinline__ Range range_of(const Attn& a, int64_t t) {
 }
 
 // (lse * log2 e, sum_c grad out) of consecutive rows of the query side, by a
-// warp: LANES lanes to a row, eight rows to a thread, all loads before the first
+// warp: LANES lanes to a row, four rows to a thread, all loads before the first
 // use.  In the order of the tiles' rows:
 // stats[key head][token * group + head of the group].
 template <int LANES>
 __device__ __forceinline__ void stats_of(const Attn& a, const Plan& p, int64_t first) {
-    constexpr int kRows = 8, kSide = 32 / LANES;   // rows of a thread, rows side by side
+    constexpr int kRows = 4, kSide = 32 / LANES;   // rows of a thread, rows side by side
     const int64_t rows = (int64_t)a.q_tokens * a.heads;
     const int lane = threadIdx.x & 31, c = (lane % LANES) * 8;
     const int64_t row0 = first + lane / LANES;
@@ -120,7 +120,7 @@ __global__ void __launch_bounds__(kThreads) k_attention_ready(Attn a, Plan p) {
         if (t < a.k_tokens) p.k_range[t] = range_of<true>(a, t);
     } else {
         const int64_t rows = (int64_t)a.q_tokens * a.heads;
-        const int each = a.dim <= 64 ? 32 : 16;   // rows of a warp
+        const int each = a.dim <= 64 ? 16 : 8;   // rows of a warp
         const int64_t warp = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5);
         for (int64_t first = warp * each; first < rows;
              first += (int64_t)gridDim.x * kWarps * each) {
@@ -250,7 +250,7 @@ cudaError_t launch_plan(const Attn& a, const Plan& p, bool backward, int target_
         int64_t blocks = (most + kThreads - 1) / kThreads;
         if (backward) {
             // the rows of stats, up to 32 CTAs an SM in all
-            const int64_t rows = ((int64_t)a.q_tokens * a.heads + 16 * kWarps - 1) / (16 * kWarps);
+            const int64_t rows = ((int64_t)a.q_tokens * a.heads + 8 * kWarps - 1) / (8 * kWarps);
             const int64_t enough = (int64_t)sm_count() * 32;
             const int64_t some = rows < enough ? rows : enough;
             if (blocks < some) blocks = some;
