@@ -58,21 +58,6 @@ class PSSInfo(ctypes.Structure):
                 ("circular", ctypes.c_int64), ("last_update", ctypes.c_int64)]
 
 
-class AttentionShape(ctypes.Structure):
-    """pss_attention_shape."""
-    _fields_ = [("sequences", ctypes.c_int64), ("q_offsets", ctypes.c_void_p),
-                ("k_offsets", ctypes.c_void_p), ("q_tokens", ctypes.c_int64),
-                ("k_tokens", ctypes.c_int64), ("heads", ctypes.c_int32),
-                ("kv_heads", ctypes.c_int32), ("dim", ctypes.c_int32), ("causal", ctypes.c_int32),
-                ("scale", ctypes.c_float)]
-
-
-class Rows(ctypes.Structure):
-    """pss_rows."""
-    _fields_ = [("data", ctypes.c_void_p), ("token_stride", ctypes.c_int64),
-                ("head_stride", ctypes.c_int64)]
-
-
 class PSSError(RuntimeError):
     def __init__(self, status: int, what: str):
         self.status = status

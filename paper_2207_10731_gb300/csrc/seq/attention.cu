@@ -185,18 +185,40 @@ extern "C" pss_status pss_attention_backward(const pss_attention_shape* shape, c
 namespace pss {
 namespace seq {
 
+namespace {
+
+// A driver function, looked up once.
+void* driver_call(const char* name, std::atomic<void*>* found) {
+    void* fn = found->load(std::memory_order_acquire);
+    if (fn) return fn;
+    cudaDriverEntryPointQueryResult how;
+    if (cudaGetDriverEntryPointByVersion(name, &fn, 12000, cudaEnableDefault, &how) !=
+            cudaSuccess ||
+        how != cudaDriverEntryPointSuccess) {
+        cudaGetLastError();
+        return nullptr;
+    }
+    found->store(fn, std::memory_order_release);
+    return fn;
+}
+
+}  // namespace
+
+bool device_ptr(const void* p) {
+    static std::atomic<void*> found{nullptr};
+    void* fn = driver_call("cuPointerGetAttribute", &found);
+    CUmemorytype type;
+    return p && fn &&
+           reinterpret_cast<PFN_cuPointerGetAttribute_v4000>(fn)(
+               &type, CU_POINTER_ATTRIBUTE_MEMORY_TYPE, (CUdeviceptr)p) == CUDA_SUCCESS &&
+           type == CU_MEMORYTYPE_DEVICE;
+}
+
 cudaError_t tile_map(CUtensorMap* map, const Rows& r, int tokens, int heads, int dim,
                      int heads_box, int tokens_box, const void* spare) {
     static std::atomic<void*> found{nullptr};
-    void* fn = found.load(std::memory_order_acquire);
-    if (!fn) {
-        cudaDriverEntryPointQueryResult how;
-        const cudaError_t e = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000,
-                                                               cudaEnableDefault, &how);
-        if (e != cudaSuccess) return e;
-        if (how != cudaDriverEntryPointSuccess || !fn) return cudaErrorNotSupported;
-        found.store(fn, std::memory_order_release);
-    }
+    void* fn = driver_call("cuTensorMapEncodeTiled", &found);
+    if (!fn) return cudaErrorNotSupported;
     const bool empty = tokens == 0;   // nothing is loaded; the map only has to be valid
     // a stride over a size of one is free, but the encoder checks it
     const int64_t row = heads == 1 ? dim : r.head, token = tokens <= 1 ? dim : r.token;

@@ -23,7 +23,9 @@ struct Params {
     int64_t n, cols;               // n = rows * cols elements
     uint64_t inv;                  // floor((2^64 - 1) / d), d of the division below
     int64_t xs, rs, ys;            // row strides
-    uint32_t key0, key1, off0, off1, threshold;
+    uint32_t key0, key1, off0, off1;
+    uint32_t below;                // (threshold << 16) - 1
+    bool all;                      // the threshold is 0
     float scale;
 };
 
@@ -47,9 +49,17 @@ __device__ __forceinline__ void philox(uint64_t counter, const Params& p, uint32
         k1 += 0xBB67AE85u;
     }
 }
-__device__ __forceinline__ bool kept(const uint32_t (&c)[4], int i, uint32_t threshold) {
+// Whether 16-bit value i is at least the threshold: the value in the upper half
+// of a word against the last word below the threshold's.
+__device__ __forceinline__ bool kept(const uint32_t (&c)[4], int i, const Params& p) {
     const uint32_t w = c[i >> 1];
-    return ((i & 1) ? w >> 16 : w & 0xffffu) >= threshold;
+    return ((i & 1) ? w : w << 16) > p.below || p.all;
+}
+// A dropped element is left out before the product, which would keep a NaN.
+template <bool RES>
+__device__ __forceinline__ float dropped(bool keep, float v, float scale, float add) {
+    const float t = keep ? v : 0.f;
+    return RES ? fmaf(t, scale, add) : t * scale;
 }
 
 // s / d for s < 2^63, inv = floor((2^64 - 1) / d): umulhi gives the quotient or
@@ -71,7 +81,7 @@ __device__ __forceinline__ int64_t divide(int64_t s, int64_t d, uint64_t inv, in
 enum { FLAT, ROWS, SINGLE };
 
 template <typename T, int MODE, bool RES>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, 4)
 k_dropout(const T* x, const T* res, T* y, Params p) {
     pdl_prologue();
     const int64_t whole = MODE == SINGLE ? 0 : p.n / 8;
@@ -102,10 +112,8 @@ k_dropout(const T* x, const T* res, T* y, Params p) {
             philox((uint64_t)g, p, c);
             if (g < whole) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    v[u][i] = kept(c, i, p.threshold) ? v[u][i] * p.scale : 0.f;
-                    if (RES) v[u][i] += add[u][i];
-                }
+                for (int i = 0; i < 8; ++i)
+                    v[u][i] = dropped<RES>(kept(c, i, p), v[u][i], p.scale, add[u][i]);
                 store8(y + row[u] * p.ys + at[u], v[u]);
                 continue;
             }
@@ -114,9 +122,9 @@ k_dropout(const T* x, const T* res, T* y, Params p) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 if (8 * g + i >= p.n) break;
-                float o = kept(c, i, p.threshold) ? load_f32(x[r * p.xs + k]) * p.scale : 0.f;
-                if (RES) o += load_f32(res[r * p.rs + k]);
-                y[r * p.ys + k] = round_to<T>(o);
+                y[r * p.ys + k] = round_to<T>(
+                    dropped<RES>(kept(c, i, p), load_f32(x[r * p.xs + k]), p.scale,
+                                 RES ? load_f32(res[r * p.rs + k]) : 0.f));
                 if (++k == p.cols && MODE == SINGLE) {
                     k = 0;
                     ++r;
@@ -160,8 +168,10 @@ extern "C" pss_status pss_dropout(const void* x, int64_t x_stride, const void* r
     q.key1 = (uint32_t)(seed >> 32);
     q.off0 = (uint32_t)offset;
     q.off1 = (uint32_t)(offset >> 32);
-    q.threshold = (uint32_t)std::nearbyint(p * 65536.0);
-    q.scale = q.threshold < 65536u ? (float)(65536.0 / (65536.0 - q.threshold)) : 0.f;
+    const uint32_t threshold = (uint32_t)std::nearbyint(p * 65536.0);
+    q.below = (uint32_t)(((uint64_t)threshold << 16) - 1);
+    q.all = threshold == 0;
+    q.scale = threshold < 65536u ? (float)(65536.0 / (65536.0 - threshold)) : 0.f;
     const bool packed = rows == 1 || (x_stride == cols && y_stride == cols &&
                                       (!residual || residual_stride == cols));
     const bool bases = aligned_to(x, 8 * size) && aligned_to(y, 8 * size) &&

@@ -55,14 +55,49 @@ __device__ __forceinline__ float row_sum(float v, int lanes, float* slot) {
 }
 
 // How the rows are spread over threads: `lanes` threads to a row, each with
-// CH vectors of VEC elements, vector c of thread t at (c*lanes + t)*VEC.
+// CH vectors of VEC elements, vector c of thread t at (c*lanes + t)*VEC - shift.
+// shift > 0: rows do not start at a multiple of 8 elements.  Row r starts
+// (shift0 + r*step) % 8 past one, and a thread only meets rows a multiple of 8
+// apart (RAGGED), so its vectors stay aligned and its columns the same; a row's
+// ends are moved one by one.
 struct Shape {
     int64_t rows;
     int cols, lanes, log2_lanes;   // log2_lanes: for lanes <= 32
     int groups;                    // rows of a CTA at a time
+    int shift0, step;              // RAGGED
 };
+enum { ALIGNED, RAGGED };          // 8 elements at a time, or VEC = 1 (ALIGNED)
 
-template <typename TX, typename TY, int VEC, int CH>
+// The thread's place in its row: VEC-element vector c at at(c).
+template <int VEC, int MODE>
+struct Place {
+    int t, group, shift;
+    __device__ __forceinline__ Place(const Shape& sh) {
+        const bool wide = sh.lanes > 32;
+        t = wide ? threadIdx.x : threadIdx.x & (sh.lanes - 1);
+        group = wide ? 0 : threadIdx.x >> sh.log2_lanes;
+        const int first = (blockIdx.x * sh.groups + group) & 7;
+        shift = MODE == RAGGED ? (sh.shift0 + first * sh.step) & 7 : 0;
+    }
+    __device__ __forceinline__ int at(const Shape& sh, int c) const {
+        return (c * sh.lanes + t) * VEC - shift;
+    }
+};
+// Whether the 7 elements before and after row r are between the tensor's first
+// and last; otherwise (the first and last rows) they must not be touched.
+__device__ __forceinline__ bool inner(const Shape& sh, int64_t r, int64_t stride) {
+    return r * stride >= 7 && (sh.rows - 1 - r) * stride >= 7;
+}
+// Whether element e of n exists; a vector that exists at all holds only such
+// elements unless the rows are ragged.
+template <int MODE>
+__device__ __forceinline__ bool inside(int e, int n, bool vector) {
+    return MODE == RAGGED ? (unsigned)e < (unsigned)n : vector;
+}
+
+// Weight and bias stay in registers where these reach: not with 1024 threads,
+// which have 64 each.
+template <typename TX, typename TY, int VEC, int CH, int MODE>
 __global__ void __launch_bounds__(max_threads<VEC, CH>(1024))
 k_layer_norm_forward(const TX* x, int64_t xs, const float* __restrict__ weight,
                      const float* __restrict__ bias, TY* y, int64_t ys,
@@ -70,37 +105,36 @@ k_layer_norm_forward(const TX* x, int64_t xs, const float* __restrict__ weight,
                      float eps) {
     pdl_prologue();
     __shared__ float slots[2][32];
-    const bool wide = sh.lanes > 32;
-    const int t = wide ? threadIdx.x : threadIdx.x & (sh.lanes - 1);
-    const int group = wide ? 0 : threadIdx.x >> sh.log2_lanes;
+    const Place<VEC, MODE> place(sh);
     const float inv_n = 1.f / (float)sh.cols;
-    // weight and bias stay in registers where these reach (64 with 1024 threads)
     constexpr bool kKeep = max_threads<VEC, CH>(1024) == 256;
     float w[kKeep ? CH : 1][VEC], b[kKeep ? CH : 1][VEC];
     bool in[CH];
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-        const int at = (c * sh.lanes + t) * VEC;
+        const int at = place.at(sh, c);
         in[c] = at < sh.cols;
 #pragma unroll
         for (int i = 0; i < VEC; ++i) {
             if (!kKeep) continue;
-            w[kKeep ? c : 0][i] = in[c] ? weight[at + i] : 0.f;
-            b[kKeep ? c : 0][i] = in[c] ? bias[at + i] : 0.f;
+            const bool use = inside<MODE>(at + i, sh.cols, in[c]);
+            w[kKeep ? c : 0][i] = use ? weight[at + i] : 0.f;
+            b[kKeep ? c : 0][i] = use ? bias[at + i] : 0.f;
         }
     }
     // the trip count is the same for every thread of the CTA (shuffles and
     // barriers inside); rows past the end are computed from zeros and dropped
     for (int64_t r0 = (int64_t)blockIdx.x * sh.groups; r0 < sh.rows;
          r0 += (int64_t)gridDim.x * sh.groups) {
-        const int64_t r = r0 + group;
+        const int64_t r = r0 + place.group;
         const bool live = r < sh.rows;
         float v[CH][VEC];
         float s = 0.f;
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
             if (live && in[c]) {
-                load_vec(x + r * xs + (c * sh.lanes + t) * VEC, v[c]);
+                load_part(x + r * xs, place.at(sh, c), sh.cols,
+                          MODE == ALIGNED || inner(sh, r, xs), v[c]);
             } else {
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) v[c][i] = 0.f;
@@ -109,7 +143,8 @@ k_layer_norm_forward(const TX* x, int64_t xs, const float* __restrict__ weight,
 #pragma unroll
         for (int c = 0; c < CH; ++c)
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) s += v[c][i];
+            for (int i = 0; i < VEC; ++i)
+                if (inside<MODE>(place.at(sh, c) + i, sh.cols, true)) s += v[c][i];
         const float mean = row_sum(s, sh.lanes, slots[0]) * inv_n;
         s = 0.f;
 #pragma unroll
@@ -117,22 +152,25 @@ k_layer_norm_forward(const TX* x, int64_t xs, const float* __restrict__ weight,
 #pragma unroll
             for (int i = 0; i < VEC; ++i) {
                 v[c][i] -= mean;
-                s += in[c] ? v[c][i] * v[c][i] : 0.f;
+                if (inside<MODE>(place.at(sh, c) + i, sh.cols, in[c])) s += v[c][i] * v[c][i];
             }
         const float rstd = 1.f / sqrtf(row_sum(s, sh.lanes, slots[1]) * inv_n + eps);
         if (live) {
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
                 if (!in[c]) continue;
-                const int at = (c * sh.lanes + t) * VEC;
+                const int at = place.at(sh, c);
                 float o[VEC];
 #pragma unroll
-                for (int i = 0; i < VEC; ++i)
-                    o[i] = v[c][i] * rstd * (kKeep ? w[kKeep ? c : 0][i] : weight[at + i]) +
-                           (kKeep ? b[kKeep ? c : 0][i] : bias[at + i]);
-                store_vec(y + r * ys + at, o);
+                for (int i = 0; i < VEC; ++i) {
+                    const bool use = kKeep || inside<MODE>(at + i, sh.cols, true);
+                    const float wi = kKeep ? w[kKeep ? c : 0][i] : use ? weight[at + i] : 0.f;
+                    const float bi = kKeep ? b[kKeep ? c : 0][i] : use ? bias[at + i] : 0.f;
+                    o[i] = v[c][i] * rstd * wi + bi;
+                }
+                store_part(y + r * ys, at, sh.cols, o);
             }
-            if (t == 0) {
+            if (place.t == 0) {
                 mean_out[r] = mean;
                 rstd_out[r] = rstd;
             }
@@ -140,78 +178,132 @@ k_layer_norm_forward(const TX* x, int64_t xs, const float* __restrict__ weight,
     }
 }
 
-// SMEM: the column sums live in shared memory (2 * cols floats, each touched
-// by its one thread) instead of registers, for rows of more than 8192 columns:
-// 1024 threads leave 64 registers each.
-template <typename TG, typename TX, int VEC, int CH, bool SMEM>
-__global__ void __launch_bounds__(max_threads<VEC, CH>(SMEM ? 1024 : 512))
-k_layer_norm_backward(const TG* grad, int64_t gs, const TX* x,
-                      int64_t xs, const float* __restrict__ weight,
-                      const float* __restrict__ mean_in, const float* __restrict__ rstd_in,
-                      TX* dx, int64_t ds, float* __restrict__ partial, Shape sh) {
-    pdl_prologue();
-    extern __shared__ float sums[];
-    __shared__ float slots[2][32];
-    const bool wide = sh.lanes > 32;
-    const int t = wide ? threadIdx.x : threadIdx.x & (sh.lanes - 1);
-    const int group = wide ? 0 : threadIdx.x >> sh.log2_lanes;
-    const float inv_n = 1.f / (float)sh.cols;
-    // the weights stay in registers where these reach
-    constexpr bool kKeep = !SMEM && (VEC > 1 || CH < 16);
-    float w[kKeep ? CH : 1][VEC], dw[SMEM ? 1 : CH][VEC], db[SMEM ? 1 : CH][VEC];
-    bool in[CH];
+// A thread's part of one row of the backward pass as it comes from memory.
+template <typename TG, typename TX, int VEC, int CH>
+struct Row;
+template <typename TG, typename TX, int CH>
+struct Row<TG, TX, 8, CH> {
+    Raw8<TX> x[CH];
+    Raw8<TG> g[CH];
+    template <int MODE>
+    __device__ __forceinline__ void load(const TX* xr, const TG* gr, bool live, bool whole,
+                                         const bool (&in)[CH], const Place<8, MODE>& place,
+                                         const Shape& sh) {
 #pragma unroll
-    for (int c = 0; c < CH; ++c) {
-        const int at = (c * sh.lanes + t) * VEC;
-        in[c] = at < sh.cols;
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-            if (SMEM) {
-                if (in[c]) sums[at + i] = sums[sh.cols + at + i] = 0.f;
+        for (int c = 0; c < CH; ++c) {
+            if (live && in[c]) {
+                x[c] = load_raw_part(xr, place.at(sh, c), sh.cols, whole);
+                g[c] = load_raw_part(gr, place.at(sh, c), sh.cols, whole);
             } else {
-                if (kKeep) w[kKeep ? c : 0][i] = in[c] ? weight[at + i] : 0.f;
-                dw[SMEM ? 0 : c][i] = db[SMEM ? 0 : c][i] = 0.f;
+                x[c] = Raw8<TX>{};
+                g[c] = Raw8<TG>{};
             }
         }
     }
-    for (int64_t r0 = (int64_t)blockIdx.x * sh.groups; r0 < sh.rows;
-         r0 += (int64_t)gridDim.x * sh.groups) {
-        const int64_t r = r0 + group;
-        const bool live = r < sh.rows;
-        float h[CH][VEC], g[CH][VEC];
-        float mean = 0.f, rstd = 0.f;
-        if (live) {
-            mean = mean_in[r];
-            rstd = rstd_in[r];
-        }
+    __device__ __forceinline__ void get(int c, float (&h)[8], float (&d)[8]) const {
+        unpack(x[c], h);
+        unpack(g[c], d);
+    }
+};
+template <typename TG, typename TX, int CH>
+struct Row<TG, TX, 1, CH> {
+    float x[CH], g[CH];
+    template <int MODE>
+    __device__ __forceinline__ void load(const TX* xr, const TG* gr, bool live, bool,
+                                         const bool (&in)[CH], const Place<1, MODE>& place,
+                                         const Shape& sh) {
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
-            const int at = (c * sh.lanes + t) * VEC;
-            if (live && in[c]) {
-                load_vec(x + r * xs + at, h[c]);
-                load_vec(grad + r * gs + at, g[c]);
-            } else {
+            const bool use = live && in[c];
+            x[c] = use ? load_f32(xr[place.at(sh, c)]) : 0.f;
+            g[c] = use ? load_f32(gr[place.at(sh, c)]) : 0.f;
+        }
+    }
+    __device__ __forceinline__ void get(int c, float (&h)[1], float (&d)[1]) const {
+        h[0] = x[c];
+        d[0] = g[c];
+    }
+};
+
+// A row's loads are issued before the row in front of it is worked on: between
+// its loads and its store a row waits for two reductions, and the rows of the
+// two or three CTAs that the column sums leave room for do not cover that.
+// SUMS: where the columns' sums are kept: in registers, or in shared memory (2 *
+// cols floats, each touched by its one thread) for rows of more than 8192
+// columns, where 1024 threads leave 64 registers each.  (Shared memory for
+// shorter rows: 302 instead of 138 us at 16384 x 3328, for bank conflicts.)
+enum { REGISTERS, SHARED };
+template <typename TG, typename TX, int VEC, int CH, int MODE, int SUMS>
+__global__ void __launch_bounds__(max_threads<VEC, CH>(SUMS == SHARED ? 1024 : 512))
+k_layer_norm_backward(const TG* grad, int64_t gs, const TX* x, int64_t xs,
+                      const float* __restrict__ weight, const float* __restrict__ mean_in,
+                      const float* __restrict__ rstd_in, TX* dx, int64_t ds,
+                      float* __restrict__ partial, Shape sh) {
+    pdl_prologue();
+    extern __shared__ float sums[];
+    __shared__ float slots[2][32];
+    constexpr bool kShared = SUMS == SHARED;
+    const Place<VEC, MODE> place(sh);
+    const float inv_n = 1.f / (float)sh.cols;
+    // the weights stay in registers where these reach
+    constexpr bool kKeep = !kShared && VEC * CH < 16;
+    float w[kKeep ? CH : 1][VEC], dw[kShared ? 1 : CH][VEC], db[kShared ? 1 : CH][VEC];
+    bool in[CH];
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) h[c][i] = g[c][i] = 0.f;
+    for (int c = 0; c < CH; ++c) {
+        const int at = place.at(sh, c);
+        in[c] = at < sh.cols;
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+            const bool use = inside<MODE>(at + i, sh.cols, in[c]);
+            if (kShared) {
+                if (use) sums[at + i] = sums[sh.cols + at + i] = 0.f;
+            } else {
+                if (kKeep) w[kKeep ? c : 0][i] = use ? weight[at + i] : 0.f;
+                dw[kShared ? 0 : c][i] = db[kShared ? 0 : c][i] = 0.f;
             }
         }
+    }
+    const int64_t step = (int64_t)gridDim.x * sh.groups;
+    const int64_t first = (int64_t)blockIdx.x * sh.groups + place.group;
+    Row<TG, TX, VEC, CH> next;
+    float next_mean = 0.f, next_rstd = 0.f;
+    auto fetch = [&](int64_t r) {
+        const bool live = r < sh.rows;
+        const bool whole = MODE == ALIGNED || (inner(sh, r, xs) && inner(sh, r, gs));
+        next.load(x + r * xs, grad + r * gs, live, whole, in, place, sh);
+        next_mean = live ? mean_in[r] : 0.f;
+        next_rstd = live ? rstd_in[r] : 0.f;
+    };
+    if (!kShared) fetch(first);
+    for (int64_t r0 = (int64_t)blockIdx.x * sh.groups; r0 < sh.rows; r0 += step) {
+        const int64_t r = r0 + place.group;
+        const bool live = r < sh.rows;
+        if (kShared) fetch(r);   // no registers for two rows
+        const Row<TG, TX, VEC, CH> row = next;
+        const float mean = next_mean, rstd = next_rstd;
+        if (!kShared && r0 + step < sh.rows) fetch(r + step);
+        float h[CH][VEC], g[CH][VEC];
+#pragma unroll
+        for (int c = 0; c < CH; ++c) row.get(c, h[c], g[c]);
         float s = 0.f, sh_ = 0.f;
 #pragma unroll
         for (int c = 0; c < CH; ++c)
 #pragma unroll
             for (int i = 0; i < VEC; ++i) {
-                const int at = (c * sh.lanes + t) * VEC + i;
-                const bool use = live && in[c];
+                const int at = place.at(sh, c) + i;
+                const bool use = live && inside<MODE>(at, sh.cols, in[c]);
                 h[c][i] = use ? (h[c][i] - mean) * rstd : 0.f;
-                if (SMEM) {
+                if (MODE == RAGGED && !use) g[c][i] = 0.f;   // another row's
+                if (kShared) {
                     if (use) {
                         sums[at] += g[c][i] * h[c][i];
                         sums[sh.cols + at] += g[c][i];
                         g[c][i] *= weight[at];
                     }
                 } else {
-                    dw[SMEM ? 0 : c][i] += g[c][i] * h[c][i];
-                    db[SMEM ? 0 : c][i] += g[c][i];
+                    dw[kShared ? 0 : c][i] += g[c][i] * h[c][i];
+                    db[kShared ? 0 : c][i] += g[c][i];
                     if (kKeep)
                         g[c][i] *= w[kKeep ? c : 0][i];
                     else if (use)
@@ -229,34 +321,21 @@ k_layer_norm_backward(const TG* grad, int64_t gs, const TX* x,
                 float o[VEC];
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) o[i] = (g[c][i] - s - h[c][i] * sh_) * rstd;
-                store_vec(dx + r * ds + (c * sh.lanes + t) * VEC, o);
+                store_part(dx + r * ds, place.at(sh, c), sh.cols, o);
             }
         }
     }
     // the CTA's partial row: [2][cols] at blockIdx.x
     float* out = partial + (int64_t)blockIdx.x * 2 * sh.cols;
-    if (SMEM) {
+    if (sh.lanes > 32) {
 #pragma unroll
         for (int c = 0; c < CH; ++c)
 #pragma unroll
             for (int i = 0; i < VEC; ++i) {
-                const int at = (c * sh.lanes + t) * VEC + i;
-                if (in[c]) {
-                    out[at] = sums[at];
-                    out[sh.cols + at] = sums[sh.cols + at];
-                }
-            }
-        return;
-    }
-    if (wide) {
-#pragma unroll
-        for (int c = 0; c < CH; ++c)
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) {
-                const int at = (c * sh.lanes + t) * VEC + i;
-                if (in[c]) {
-                    out[at] = dw[SMEM ? 0 : c][i];
-                    out[sh.cols + at] = db[SMEM ? 0 : c][i];
+                const int at = place.at(sh, c) + i;
+                if (inside<MODE>(at, sh.cols, in[c])) {
+                    out[at] = kShared ? sums[at] : dw[kShared ? 0 : c][i];
+                    out[sh.cols + at] = kShared ? sums[sh.cols + at] : db[kShared ? 0 : c][i];
                 }
             }
         return;
@@ -266,10 +345,10 @@ k_layer_norm_backward(const TG* grad, int64_t gs, const TX* x,
     for (int c = 0; c < CH; ++c)
 #pragma unroll
         for (int i = 0; i < VEC; ++i) {
-            const int at = (c * sh.lanes + t) * VEC + i;
-            if (in[c]) {
-                sums[(group * 2) * sh.cols + at] = dw[SMEM ? 0 : c][i];
-                sums[(group * 2 + 1) * sh.cols + at] = db[SMEM ? 0 : c][i];
+            const int at = place.at(sh, c) + i;
+            if (inside<MODE>(at, sh.cols, in[c])) {
+                sums[(place.group * 2) * sh.cols + at] = dw[kShared ? 0 : c][i];
+                sums[(place.group * 2 + 1) * sh.cols + at] = db[kShared ? 0 : c][i];
             }
         }
     __syncthreads();
@@ -302,22 +381,24 @@ k_layer_norm_columns(const float* __restrict__ partial, int parts, int cols,
 }
 
 // Threads to a row and vectors to a thread.
-//   most: the largest CH of this vector width.  A row within one warp's reach
+//   most: the largest CH of this vector width; extra: elements that a ragged
+//   row's first vector may hold in front of it.  A row within one warp's reach
 //   (32 * most vectors) takes the fewest lanes that hold it with one vector
 //   each, up to 32; a longer row takes a CTA.
 struct Split {
     int lanes, log2_lanes, ch, threads, groups;
 };
-Split split_row(int cols, int vec, int most, int cta) {
+Split split_row(int cols, int vec, int most, int extra) {
+    constexpr int kCta = 256;
     Split s;
-    const int vecs = (cols + vec - 1) / vec;
+    const int vecs = (cols + extra + vec - 1) / vec;
     if (vecs <= 32 * most) {
         s.lanes = 1;
         s.log2_lanes = 0;
         while (s.lanes < 32 && s.lanes < vecs) s.lanes *= 2, ++s.log2_lanes;
         s.ch = (vecs + s.lanes - 1) / s.lanes;
-        s.threads = cta;
-        s.groups = cta / s.lanes;
+        s.threads = kCta;
+        s.groups = kCta / s.lanes;
     } else {
         s.ch = most;
         s.lanes = ((vecs + most - 1) / most + 31) / 32 * 32;
@@ -328,13 +409,24 @@ Split split_row(int cols, int vec, int most, int cta) {
     return s;
 }
 
-// CTAs of the backward pass: as many partial rows as `per_sm` CTAs on every SM
-// write.  Two for long rows: their partial rows (8 bytes a column) are then a
-// few percent of the traffic.
-int backward_ctas(int64_t rows, int groups, int per_sm, int sms) {
-    const int64_t need = (rows + groups - 1) / groups;
-    const int64_t most = (int64_t)per_sm * sms;
-    return (int)(need < most ? (need > 0 ? need : 1) : most);
+// How a call's rows lie: 8 elements at a time where every row starts at a
+// multiple of 8, or where all tensors' rows start equally far past one.
+enum { VECTORS, SHIFTED, SINGLE };
+struct Lie {
+    int how, shift0, step;
+};
+template <int N>
+Lie rows_lie(int64_t cols, const void* const (&p)[N], const int64_t (&stride)[N],
+             const int (&type)[N]) {
+    bool aligned = cols % 8 == 0, same = true;
+    for (int i = 0; i < N; ++i) {
+        const size_t size = dtype_size(type[i]);
+        aligned = aligned && aligned8(p[i], stride[i], size);
+        same = same && past8(p[i], size) == past8(p[0], dtype_size(type[0])) &&
+               stride[i] % 8 == stride[0] % 8;
+    }
+    return Lie{aligned ? VECTORS : same ? SHIFTED : SINGLE,
+               past8(p[0], dtype_size(type[0])), (int)(stride[0] % 8)};
 }
 
 constexpr int kBackwardPerSm = 4;
@@ -347,33 +439,44 @@ int resident(K kernel, int threads, size_t smem, int most) {
     return n < 1 ? 1 : n < most ? n : most;
 }
 
-template <typename TX, typename TY, int VEC, int CH>
-cudaError_t launch_forward(const TX* x, int64_t xs, const float* w, const float* b, TY* y,
-                           int64_t ys, float* mean, float* rstd, int64_t rows, int cols,
-                           const Split& s, float eps, cudaStream_t st) {
-    auto* k = k_layer_norm_forward<TX, TY, VEC, CH>;
-    const Shape sh{rows, cols, s.lanes, s.log2_lanes, s.groups};
+// CTAs of a launch; with RAGGED a CTA's rows have to be a multiple of 8 apart.
+template <typename F>
+int ctas_of(int64_t rows, const Split& s, F per_sm, int mode) {
     const int64_t need = (rows + s.groups - 1) / s.groups;
-    const int64_t most = (int64_t)sm_count() * resident(k, s.threads, 0, 32);
-    return launch_k(k, dim3((unsigned)(need < most ? need : most)), dim3(s.threads), 0, st, x, xs,
-                    w, b, y, ys, mean, rstd, sh, eps);
+    if (need <= sm_count()) return (int)need;   // a small call does not ask how many fit
+    int64_t most = (int64_t)per_sm() * sm_count();
+    if (need <= most) return (int)need;
+    if (mode == RAGGED) most -= most % 8;
+    return (int)(most > 0 ? most : need < 8 ? need : 8);
 }
 
-template <typename TG, typename TX, int VEC, int CH, bool SMEM>
+template <typename TX, typename TY, int VEC, int CH, int MODE>
+cudaError_t launch_forward(const TX* x, int64_t xs, const float* w, const float* b, TY* y,
+                           int64_t ys, float* mean, float* rstd, int64_t rows, int cols,
+                           const Split& s, const Lie& lie, float eps, cudaStream_t st) {
+    auto* k = k_layer_norm_forward<TX, TY, VEC, CH, MODE>;
+    const Shape sh{rows, cols, s.lanes, s.log2_lanes, s.groups, lie.shift0, lie.step};
+    const int ctas = ctas_of(rows, s, [&] { return resident(k, s.threads, 0, 32); }, MODE);
+    return launch_k(k, dim3(ctas), dim3(s.threads), 0, st, x, xs, w, b, y, ys, mean, rstd, sh,
+                    eps);
+}
+
+template <typename TG, typename TX, int VEC, int CH, int MODE, int SUMS>
 cudaError_t launch_backward(const TG* g, int64_t gs, const TX* x, int64_t xs, const float* w,
                             const float* mean, const float* rstd, TX* dx, int64_t ds,
                             float* dw, float* db, float* partial, int64_t rows, int cols,
-                            const Split& s, cudaStream_t st) {
-    auto* k = k_layer_norm_backward<TG, TX, VEC, CH, SMEM>;
-    const size_t smem = SMEM ? (size_t)8 * cols : s.lanes <= 32 ? (size_t)s.groups * 8 * cols : 0;
+                            const Split& s, const Lie& lie, cudaStream_t st) {
+    auto* k = k_layer_norm_backward<TG, TX, VEC, CH, MODE, SUMS>;
+    const size_t smem =
+        SUMS == SHARED ? (size_t)8 * cols : s.lanes <= 32 ? (size_t)s.groups * 8 * cols : 0;
     if (smem > 48 * 1024) {
         const cudaError_t e =
             cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
         if (e != cudaSuccess) return e;
     }
-    const Shape sh{rows, cols, s.lanes, s.log2_lanes, s.groups};
-    const int ctas =
-        backward_ctas(rows, s.groups, resident(k, s.threads, smem, kBackwardPerSm), sm_count());
+    const Shape sh{rows, cols, s.lanes, s.log2_lanes, s.groups, lie.shift0, lie.step};
+    const int ctas = ctas_of(
+        rows, s, [&] { return resident(k, s.threads, smem, kBackwardPerSm); }, MODE);
     cudaError_t e = launch_k(k, dim3(ctas), dim3(s.threads), smem, st, g, gs, x, xs, w, mean, rstd,
                              dx, ds, partial, sh);
     if (e != cudaSuccess) return e;
@@ -401,27 +504,30 @@ extern "C" pss_status pss_layer_norm_forward(const void* x, pss_dtype x_type, in
         !aligned_to(rstd, 4))
         return PSS_ERR_INVALID_ARG;
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-    const bool wide = cols % 8 == 0 && aligned8(x, x_stride, dtype_size(x_type)) &&
-                      aligned8(y, y_stride, dtype_size(y_type));
+    const Lie lie = rows_lie<2>(cols, {x, y}, {x_stride, y_stride}, {x_type, y_type});
     return status_of(with_type(x_type, [&](auto tx) {
         return with_type(y_type, [&](auto ty) {
             using TX = decltype(tx);
             using TY = decltype(ty);
-            auto go = [&](auto vec, auto ch, const Split& s) {
-                return launch_forward<TX, TY, decltype(vec)::value, decltype(ch)::value>(
+            auto go = [&](auto vec, auto ch, auto mode, const Split& s) {
+                return launch_forward<TX, TY, decltype(vec)::value, decltype(ch)::value,
+                                      decltype(mode)::value>(
                     static_cast<const TX*>(x), x_stride, weight, bias, static_cast<TY*>(y),
-                    y_stride, mean, rstd, rows, (int)cols, s, eps, st);
+                    y_stride, mean, rstd, rows, (int)cols, s, lie, eps, st);
             };
-            if (wide) {
-                const Split s = split_row((int)cols, 8, 2, 256);
-                return s.ch <= 1 ? go(Int<8>(), Int<1>(), s) : go(Int<8>(), Int<2>(), s);
+            if (lie.how == VECTORS) {
+                const Split s = split_row((int)cols, 8, 2, 0);
+                return s.ch <= 1 ? go(Int<8>(), Int<1>(), Int<ALIGNED>(), s)
+                                 : go(Int<8>(), Int<2>(), Int<ALIGNED>(), s);
             }
-            const Split s = split_row((int)cols, 1, 16, 256);
-            return s.ch <= 2   ? go(Int<1>(), Int<2>(), s)
-                   : s.ch <= 4 ? go(Int<1>(), Int<4>(), s)
-                   : s.ch <= 8 ? go(Int<1>(), Int<8>(), s)
-                   : s.ch <= 12 ? go(Int<1>(), Int<12>(), s)
-                                : go(Int<1>(), Int<16>(), s);
+            if (lie.how == SHIFTED && cols <= kMaxCols - 8) {
+                const Split s = split_row((int)cols, 8, 2, 7);
+                return s.ch <= 1 ? go(Int<8>(), Int<1>(), Int<RAGGED>(), s)
+                                 : go(Int<8>(), Int<2>(), Int<RAGGED>(), s);
+            }
+            const Split s = split_row((int)cols, 1, 16, 0);
+            return s.ch <= 4 ? go(Int<1>(), Int<4>(), Int<ALIGNED>(), s)
+                             : go(Int<1>(), Int<16>(), Int<ALIGNED>(), s);
         });
     }));
 }
@@ -457,33 +563,38 @@ extern "C" pss_status pss_layer_norm_backward(
         !aligned_to(rstd, 4) || !aligned_to(workspace, 16) ||
         workspace_bytes < pss_layer_norm_workspace(rows, cols))
         return PSS_ERR_INVALID_ARG;
-    const bool wide = cols % 8 == 0 && aligned8(x, x_stride, dtype_size(x_type)) &&
-                      aligned8(dx, dx_stride, dtype_size(x_type)) &&
-                      aligned8(grad, grad_stride, dtype_size(grad_type));
+    const Lie lie = rows_lie<3>(cols, {x, grad, dx}, {x_stride, grad_stride, dx_stride},
+                                {x_type, grad_type, x_type});
     return status_of(with_type(grad_type, [&](auto tg) {
         return with_type(x_type, [&](auto tx) {
             using TG = decltype(tg);
             using TX = decltype(tx);
-            auto go = [&](auto vec, auto ch, auto smem, const Split& s) {
+            auto go = [&](auto vec, auto ch, auto mode, auto sums, const Split& s) {
                 return launch_backward<TG, TX, decltype(vec)::value, decltype(ch)::value,
-                                       decltype(smem)::value != 0>(
+                                       decltype(mode)::value, decltype(sums)::value>(
                     static_cast<const TG*>(grad), grad_stride, static_cast<const TX*>(x), x_stride,
                     weight, mean, rstd, static_cast<TX*>(dx), dx_stride, dweight, dbias,
-                    static_cast<float*>(workspace), rows, (int)cols, s, st);
+                    static_cast<float*>(workspace), rows, (int)cols, s, lie, st);
             };
-            const bool smem = cols > 8192;
-            if (wide) {
-                const Split s = split_row((int)cols, 8, 2, 256);
-                return s.ch <= 1 ? go(Int<8>(), Int<1>(), Int<0>(), s)
-                       : smem    ? go(Int<8>(), Int<2>(), Int<1>(), s)
-                                 : go(Int<8>(), Int<2>(), Int<0>(), s);
+            if (lie.how == VECTORS) {
+                const Split s = split_row((int)cols, 8, 2, 0);
+                return s.ch <= 1 ? go(Int<8>(), Int<1>(), Int<ALIGNED>(), Int<REGISTERS>(), s)
+                       : s.threads > 512
+                           ? go(Int<8>(), Int<2>(), Int<ALIGNED>(), Int<SHARED>(), s)
+                           : go(Int<8>(), Int<2>(), Int<ALIGNED>(), Int<REGISTERS>(), s);
             }
-            const Split s = split_row((int)cols, 1, 16, 256);
-            return s.ch <= 4   ? go(Int<1>(), Int<4>(), Int<0>(), s)
-                   : s.ch <= 8 ? go(Int<1>(), Int<8>(), Int<0>(), s)
-                   : s.ch <= 12 ? go(Int<1>(), Int<12>(), Int<0>(), s)
-                   : smem      ? go(Int<1>(), Int<16>(), Int<1>(), s)
-                               : go(Int<1>(), Int<16>(), Int<0>(), s);
+            if (lie.how == SHIFTED && cols <= kMaxCols - 8) {
+                const Split s = split_row((int)cols, 8, 2, 7);
+                return s.ch <= 1 ? go(Int<8>(), Int<1>(), Int<RAGGED>(), Int<REGISTERS>(), s)
+                       : s.threads > 512
+                           ? go(Int<8>(), Int<2>(), Int<RAGGED>(), Int<SHARED>(), s)
+                           : go(Int<8>(), Int<2>(), Int<RAGGED>(), Int<REGISTERS>(), s);
+            }
+            const Split s = split_row((int)cols, 1, 16, 0);
+            return s.ch <= 4 ? go(Int<1>(), Int<4>(), Int<ALIGNED>(), Int<REGISTERS>(), s)
+                   : s.threads > 512
+                       ? go(Int<1>(), Int<16>(), Int<ALIGNED>(), Int<SHARED>(), s)
+                       : go(Int<1>(), Int<16>(), Int<ALIGNED>(), Int<REGISTERS>(), s);
         });
     }));
 }

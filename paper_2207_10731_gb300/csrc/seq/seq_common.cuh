@@ -86,6 +86,47 @@ __device__ __forceinline__ void store8(T* p, const float (&v)[8]) {
                  :: "l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
 }
 
+// 8 elements as they are in memory, to be unpacked when they are needed.
+template <typename T>
+struct Raw8 {
+    uint32_t w[2 * sizeof(T)];
+};
+__device__ __forceinline__ Raw8<float> load_raw(const float* p) {
+    Raw8<float> r;
+    asm volatile("ld.global.L1::no_allocate.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(r.w[0]), "=r"(r.w[1]), "=r"(r.w[2]), "=r"(r.w[3]), "=r"(r.w[4]),
+                   "=r"(r.w[5]), "=r"(r.w[6]), "=r"(r.w[7])
+                 : "l"(p) : "memory");
+    return r;
+}
+template <typename T>
+__device__ __forceinline__ Raw8<T> load_raw(const T* p) {
+    Raw8<T> r;
+    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(r.w[0]), "=r"(r.w[1]), "=r"(r.w[2]), "=r"(r.w[3]) : "l"(p) : "memory");
+    return r;
+}
+__device__ __forceinline__ void unpack(const Raw8<float>& r, float (&v)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(r.w[i]);
+}
+template <typename T>
+__device__ __forceinline__ void unpack(const Raw8<T>& r, float (&v)[8]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 f = unpack2(r.w[i], T());
+        v[2 * i] = f.x;
+        v[2 * i + 1] = f.y;
+    }
+}
+__device__ __forceinline__ void set_raw(Raw8<float>& r, int i, float v) {
+    r.w[i] = __float_as_uint(v);
+}
+template <typename T>
+__device__ __forceinline__ void set_raw(Raw8<T>& r, int i, T v) {
+    reinterpret_cast<T*>(r.w)[i] = v;
+}
+
 // 16 bytes, issued here: the compiler does not move the load to its use.
 __device__ __forceinline__ uint4 load16(const void* p) {
     uint4 v;
@@ -94,35 +135,58 @@ __device__ __forceinline__ uint4 load16(const void* p) {
     return v;
 }
 
-// VEC elements at p: 8 (aligned to 8 elements) or 1.
+// Elements at .. at + 8 of a row of n, at < 0 and at + 8 > n allowed.  Where
+// `whole` says that memory on both sides of the row may be read (it is another
+// row's, or lies between rows), the vector is read as it is, and the caller
+// leaves out what is not the row's; else its elements one by one, zeros outside.
 template <typename T>
-__device__ __forceinline__ void load_vec(const T* p, float (&v)[8]) { load8(p, v); }
+__device__ __forceinline__ Raw8<T> load_raw_part(const T* row, int at, int n, bool whole) {
+    if (whole || (at >= 0 && at + 8 <= n)) return load_raw(row + at);
+    Raw8<T> r;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        set_raw(r, i, (unsigned)(at + i) < (unsigned)n ? row[at + i] : round_to<T>(0.f));
+    return r;
+}
 template <typename T>
-__device__ __forceinline__ void load_vec(const T* p, float (&v)[1]) { v[0] = load_f32(*p); }
+__device__ __forceinline__ void load_part(const T* row, int at, int n, bool whole, float (&v)[8]) {
+    unpack(load_raw_part(row, at, n, whole), v);
+}
 template <typename T>
-__device__ __forceinline__ void store_vec(T* p, const float (&v)[8]) { store8(p, v); }
+__device__ __forceinline__ void store_part(T* row, int at, int n, const float (&v)[8]) {
+    if (at >= 0 && at + 8 <= n) {
+        store8(row + at, v);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if ((unsigned)(at + i) < (unsigned)n) row[at + i] = round_to<T>(v[i]);
+    }
+}
 template <typename T>
-__device__ __forceinline__ void store_vec(T* p, const float (&v)[1]) { *p = round_to<T>(v[0]); }
+__device__ __forceinline__ void load_part(const T* row, int at, int n, bool whole, float (&v)[1]) {
+    v[0] = load_f32(row[at]);
+}
+template <typename T>
+__device__ __forceinline__ void store_part(T* row, int at, int n, const float (&v)[1]) {
+    row[at] = round_to<T>(v[0]);
+}
 
 // ---- host side -----------------------------------------------------------
 
 inline size_t dtype_size(int t) { return t == PSS_F32 ? 4 : 2; }
 inline bool dtype_ok(int t) { return t == PSS_F32 || t == PSS_BF16 || t == PSS_F16; }
 
-// Whether p is memory that the kernels of the current device may use.
-inline bool device_ptr(const void* p) {
-    cudaPointerAttributes a;
-    if (!p || cudaPointerGetAttributes(&a, p) != cudaSuccess) {
-        cudaGetLastError();
-        return false;
-    }
-    return a.type == cudaMemoryTypeDevice || a.type == cudaMemoryTypeManaged;
-}
+// Whether p is memory that the kernels of the current device may use.  Asked of
+// the driver: a call checks up to ten pointers, and the runtime's
+// cudaPointerGetAttributes collects all attributes of each.
+bool device_ptr(const void* p);
 
 // Whether rows of `size`-byte elements may be moved 8 elements at a time.
 inline bool aligned8(const void* p, int64_t stride, size_t size) {
     return ((uintptr_t)p % (8 * size)) == 0 && stride % 8 == 0;
 }
+// How many elements p stands past a multiple of 8 elements.
+inline int past8(const void* p, size_t size) { return (int)((uintptr_t)p / size % 8); }
 inline bool aligned_to(const void* p, size_t n) { return ((uintptr_t)p % n) == 0; }
 
 inline int sm_count() {

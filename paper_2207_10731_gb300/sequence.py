@@ -3,41 +3,45 @@ dropout and attention over packed sequences (argument marshalling only, like
 ``binding``; the kernels are in libpss.so, their contracts in include/pss.h).
 
 All tensors are CUDA tensors of the current device; calls are asynchronous on
-``stream`` (default: the current stream).  Nothing is kept between calls.
-Gradients are explicit calls: there is no autograd graph here.
+``stream`` (a keyword of each; default: the current stream), to which the
+results belong.  Nothing is kept between calls.  Gradients are explicit calls:
+there is no autograd graph here.
 """
 from __future__ import annotations
 
-import ctypes
+import functools
+import struct
+import threading
 
 from . import binding
 
-_lib = None
-_types = None
+_lib = torch = None
+_types = {}
+_local = threading.local()
+# pss_attention_shape, then up to ten pss_rows
+_SHAPE = struct.Struct("5q4if4x")
+_ROWS = struct.Struct("Pqq")
 
 
 def _library():
-    global _lib, _types
+    global _lib, torch
     if _lib is None:
         torch = binding._torch()
-        _types = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}   # pss_dtype
+        torch.cuda.init()
+        _types.update({torch.float32: 0, torch.bfloat16: 1, torch.float16: 2})   # pss_dtype
         _lib = binding.load_library()
     return _lib
 
 
-def _stream(stream):
-    if stream is None:
-        stream = binding._torch().cuda.current_stream()
-    return stream.cuda_stream
+def _stream():
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
 
 
 def _device_tensor(t, name):
-    torch = binding._torch()
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
-    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+    if t.get_device() != torch._C._cuda_getDevice():
         raise ValueError(f"{name} must be on the current CUDA device")
-    return t
 
 
 def _rows(t, name, like=None, dtype=None):
@@ -48,17 +52,21 @@ def _rows(t, name, like=None, dtype=None):
         raise TypeError(f"{name} must be float32, bfloat16 or float16, got {t.dtype}")
     if dtype is not None and t.dtype != dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
-    if like is not None and t.shape != like.shape:
-        raise ValueError(f"{name} must have shape {tuple(like.shape)}, got {tuple(t.shape)}")
-    if t.dim() == 0:
+    shape = t.shape
+    if like is not None and shape != like.shape:
+        raise ValueError(f"{name} must have shape {tuple(like.shape)}, got {tuple(shape)}")
+    if not shape:
         raise ValueError(f"{name} must have at least one dimension")
-    cols = t.shape[-1]
+    cols = shape[-1]
     if t.is_contiguous():
         return (t.numel() // cols if cols else 0), cols, cols
-    if cols > 1 and t.stride(-1) != 1:
+    strides = t.stride()
+    if cols > 1 and strides[-1] != 1:
         raise ValueError(f"{name} must be dense in its last dimension")
+    if t.numel() == 0:
+        return 0, cols, max(cols, 1)
     rows, stride = 1, None
-    for n, s in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):
+    for n, s in zip(reversed(shape[:-1]), reversed(strides[:-1])):
         if n == 1:
             continue
         if stride is None:
@@ -66,8 +74,6 @@ def _rows(t, name, like=None, dtype=None):
         elif s != stride * rows:
             raise ValueError(f"{name}'s rows must be evenly spaced")
         rows *= n
-    if t.numel() == 0:
-        return 0, cols, max(cols, 1)
     if stride is None:
         stride = cols
     if stride < cols:
@@ -76,7 +82,6 @@ def _rows(t, name, like=None, dtype=None):
 
 
 def _vector(t, n, name):
-    torch = binding._torch()
     _device_tensor(t, name)
     if t.dtype != torch.float32:
         raise TypeError(f"{name} must be torch.float32, got {t.dtype}")
@@ -85,13 +90,26 @@ def _vector(t, n, name):
     return t.data_ptr()
 
 
-def layer_norm_forward(x, weight, bias, eps: float = 1e-5, out=None, out_dtype=None, stream=None):
+def _on_stream(call):
+    """Runs ``call`` with ``stream`` as the current stream, so that what it
+    allocates belongs to the stream that uses it."""
+    @functools.wraps(call)
+    def run(*args, stream=None, **kwargs):
+        if stream is None:
+            return call(*args, **kwargs)
+        _library()
+        with torch.cuda.stream(stream):
+            return call(*args, **kwargs)
+    return run
+
+
+@_on_stream
+def layer_norm_forward(x, weight, bias, eps: float = 1e-5, out=None, out_dtype=None):
     """(y, mean, rstd) of the layer norm over x's last dimension
     (pss_layer_norm_forward).  ``x``: float32, bfloat16 or float16, rows evenly
     spaced; ``weight``, ``bias``: float32.  y has ``out_dtype`` (default: x's)
     or is ``out``; mean and rstd are float32, for the backward call."""
     lib = _library()
-    torch = binding._torch()
     rows, cols, xs = _rows(x, "x")
     if out is None:
         out = torch.empty(x.shape, dtype=out_dtype or x.dtype, device=x.device)
@@ -103,20 +121,20 @@ def layer_norm_forward(x, weight, bias, eps: float = 1e-5, out=None, out_dtype=N
     binding._check(lib.pss_layer_norm_forward(
         x.data_ptr(), _types[x.dtype], xs, _vector(weight, cols, "weight"),
         _vector(bias, cols, "bias"), rows, cols, eps, out.data_ptr(), _types[out.dtype], ys,
-        mean.data_ptr(), rstd.data_ptr(), _stream(stream)), "pss_layer_norm_forward")
+        mean.data_ptr(), rstd.data_ptr(), _stream()), "pss_layer_norm_forward")
     return out, mean, rstd
 
 
-def layer_norm_backward(grad, x, weight, mean, rstd, out=None, stream=None):
+@_on_stream
+def layer_norm_backward(grad, x, weight, mean, rstd, out=None):
     """(dx, dweight, dbias) for the upstream gradient ``grad`` of the y of
     ``layer_norm_forward(x, weight, ...)`` (pss_layer_norm_backward).  dx has
     x's type or is ``out``; dweight and dbias are float32."""
     lib = _library()
-    torch = binding._torch()
     rows, cols, xs = _rows(x, "x")
     _, _, gs = _rows(grad, "grad", like=x)
     if out is None:
-        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        out = torch.empty_like(x, memory_format=torch.contiguous_format)
     _, _, ds = _rows(out, "out", like=x, dtype=x.dtype)
     both = torch.empty((2, cols), dtype=torch.float32, device=x.device)
     size = lib.pss_layer_norm_workspace(rows, cols)
@@ -125,65 +143,67 @@ def layer_norm_backward(grad, x, weight, mean, rstd, out=None, stream=None):
         grad.data_ptr(), _types[grad.dtype], gs, x.data_ptr(), _types[x.dtype], xs,
         _vector(weight, cols, "weight"), _vector(mean, rows, "mean"), _vector(rstd, rows, "rstd"),
         rows, cols, out.data_ptr(), ds, both.data_ptr(), both.data_ptr() + 4 * cols,
-        work.data_ptr(), size, _stream(stream)), "pss_layer_norm_backward")
-    _used_on(stream, work)
+        work.data_ptr(), size, _stream()), "pss_layer_norm_backward")
     return out, both[0], both[1]
 
 
-def _used_on(stream, *tensors):
-    """Scratch of this module that a stream other than the current one still
-    uses when the call returns: the allocator must not hand it out before."""
-    if stream is not None:
-        for t in tensors:
-            t.record_stream(stream)
-
-
-def dropout(x, p: float, seed: int, offset: int = 0, residual=None, out=None, stream=None):
+@_on_stream
+def dropout(x, p: float, seed: int, offset: int = 0, residual=None, out=None):
     """x with each element zeroed with probability p and the others divided by
     1 - p, plus ``residual`` (pss_dropout).  The mask follows from (seed,
     offset, position) alone and is not stored: the backward pass is the same
     call on the gradient, without the residual.  seed and offset are unsigned
     64-bit; give each call of a step an offset of its own."""
     lib = _library()
-    torch = binding._torch()
     rows, cols, xs = _rows(x, "x")
     rs = 0
     if residual is not None:
         _, _, rs = _rows(residual, "residual", like=x, dtype=x.dtype)
     if out is None:
-        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        out = torch.empty_like(x, memory_format=torch.contiguous_format)
     _, _, ys = _rows(out, "out", like=x, dtype=x.dtype)
     if not (0 <= seed < 2**64 and 0 <= offset < 2**64):
         raise ValueError("seed and offset must be unsigned 64-bit integers")
     binding._check(lib.pss_dropout(
         x.data_ptr(), xs, None if residual is None else residual.data_ptr(), rs, rows, cols, p,
-        seed, offset, _types[x.dtype], out.data_ptr(), ys, _stream(stream)), "pss_dropout")
+        seed, offset, _types[x.dtype], out.data_ptr(), ys, _stream()), "pss_dropout")
     return out
 
 
 def _heads(t, name, shape=None):
-    """pss_rows of a bfloat16 tensor [tokens, heads, dim], dense in its last
-    dimension."""
-    torch = binding._torch()
+    """(data, token stride, head stride) of a bfloat16 tensor [tokens, heads,
+    dim], dense in its last dimension."""
     _device_tensor(t, name)
     if t.dtype != torch.bfloat16:
         raise TypeError(f"{name} must be torch.bfloat16, got {t.dtype}")
-    if t.dim() != 3 or (shape is not None and tuple(t.shape) != tuple(shape)):
+    own = t.shape
+    if len(own) != 3 or (shape is not None and own != shape):
         raise ValueError(f"{name} must have shape {tuple(shape) if shape else '[tokens, heads, dim]'}"
-                         f", got {tuple(t.shape)}")
+                         f", got {tuple(own)}")
     token, head, one = t.stride()
-    if one != 1 and t.shape[2] > 1:
+    if one != 1 and own[2] > 1:
         raise ValueError(f"{name} must be dense in its last dimension")
     # the stride over a size of one means nothing
-    if t.shape[0] == 1:
-        token = 0
-    if t.shape[1] == 1:
-        head = 0
-    return binding.Rows(t.data_ptr(), token, head)
+    return t.data_ptr(), token if own[0] != 1 else 0, head if own[1] != 1 else 0
+
+
+def _structs(shape, *rows):
+    """Addresses of the structures of one call, in a buffer of this thread that
+    the library reads before it returns."""
+    buffer = getattr(_local, "buffer", None)
+    if buffer is None:
+        buffer = _local.buffer = bytearray(_SHAPE.size + 10 * _ROWS.size)
+        _local.at = binding.ctypes.addressof(binding.ctypes.c_char.from_buffer(buffer))
+    _SHAPE.pack_into(buffer, 0, *shape)
+    at, where = _SHAPE.size, [_local.at]
+    for r in rows:
+        _ROWS.pack_into(buffer, at, *r)
+        where.append(_local.at + at)
+        at += _ROWS.size
+    return where
 
 
 def _offsets(t, name):
-    torch = binding._torch()
     _device_tensor(t, name)
     if t.dtype != torch.int64:
         raise TypeError(f"{name} must be torch.int64, got {t.dtype}")
@@ -199,23 +219,24 @@ def _attention_shape(q, k, q_offsets, kv_offsets, causal, scale):
     elif _offsets(kv_offsets, "kv_offsets").numel() != q_offsets.numel():
         raise ValueError("q_offsets and kv_offsets must have the same number of entries")
     tokens, heads, dim = q.shape
-    return binding.AttentionShape(q_offsets.numel() - 1, q_offsets.data_ptr(),
-                                  kv_offsets.data_ptr(), tokens, k.shape[0], heads, k.shape[1],
-                                  dim, int(bool(causal)), dim ** -0.5 if scale is None else scale)
+    if k.shape[2] != dim:
+        raise ValueError(f"k must have rows of {dim} values, got {k.shape[2]}")
+    return (q_offsets.numel() - 1, q_offsets.data_ptr(), kv_offsets.data_ptr(), tokens, k.shape[0],
+            heads, k.shape[1], dim, int(bool(causal)), dim ** -0.5 if scale is None else scale)
 
 
 def _status(status):
     if status is None:
         return None
-    torch = binding._torch()
     _device_tensor(status, "status")
     if status.dtype != torch.int64 or status.numel() != 1:
         raise TypeError("status must be a torch.int64 tensor of one value")
     return status.data_ptr()
 
 
+@_on_stream
 def attention_forward(q, k, v, q_offsets, kv_offsets=None, causal: bool = True, scale=None,
-                      out=None, status=None, stream=None):
+                      out=None, status=None):
     """(out, lse) of softmax(scale q k^T) v inside each packed sequence
     (pss_attention_forward).
 
@@ -229,38 +250,29 @@ def attention_forward(q, k, v, q_offsets, kv_offsets=None, causal: bool = True, 
     heads].  ``status`` (int64, one value on the device) receives -1, the first
     sequence with malformed offsets, or -2 if a device wait gave up."""
     lib = _library()
-    torch = binding._torch()
-    rq, rk = _heads(q, "q"), _heads(k, "k")
-    rv = _heads(v, "v", k.shape)
-    if k.shape[2] != q.shape[2]:
-        raise ValueError(f"k must have rows of {q.shape[2]} values, got {k.shape[2]}")
+    rq, rk, rv = _heads(q, "q"), _heads(k, "k"), _heads(v, "v", k.shape)
     shape = _attention_shape(q, k, q_offsets, kv_offsets, causal, scale)
     if out is None:
         out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    ro = _heads(out, "out", q.shape)
+    at = _structs(shape, rq, rk, rv, _heads(out, "out", q.shape))
     lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
-    size = lib.pss_attention_workspace(ctypes.byref(shape), 0)
+    size = lib.pss_attention_workspace(at[0], 0)
     work = torch.empty(size, dtype=torch.uint8, device=q.device)
-    binding._check(lib.pss_attention_forward(
-        ctypes.byref(shape), ctypes.byref(rq), ctypes.byref(rk), ctypes.byref(rv),
-        ctypes.byref(ro), lse.data_ptr(), work.data_ptr(), size, _status(status),
-        _stream(stream)), "pss_attention_forward")
-    _used_on(stream, work)
+    binding._check(lib.pss_attention_forward(*at, lse.data_ptr(), work.data_ptr(), size,
+                                             _status(status), _stream()),
+                   "pss_attention_forward")
     return out, lse
 
 
+@_on_stream
 def attention_backward(grad, q, k, v, out, lse, q_offsets, kv_offsets=None, causal: bool = True,
-                       scale=None, grads=None, status=None, stream=None):
+                       scale=None, grads=None, status=None):
     """(dq, dk, dv) for the upstream gradient ``grad`` of the out of
     ``attention_forward`` (pss_attention_backward); out and lse are that
     call's.  The gradients go to the three tensors ``grads`` if given (e.g.
     views of one buffer for a fused projection)."""
     lib = _library()
-    torch = binding._torch()
-    rq, rk = _heads(q, "q"), _heads(k, "k")
-    rv = _heads(v, "v", k.shape)
-    if k.shape[2] != q.shape[2]:
-        raise ValueError(f"k must have rows of {q.shape[2]} values, got {k.shape[2]}")
+    rq, rk, rv = _heads(q, "q"), _heads(k, "k"), _heads(v, "v", k.shape)
     rg, ro = _heads(grad, "grad", q.shape), _heads(out, "out", q.shape)
     shape = _attention_shape(q, k, q_offsets, kv_offsets, causal, scale)
     if lse.shape != q.shape[:2]:
@@ -271,13 +283,11 @@ def attention_backward(grad, q, k, v, out, lse, q_offsets, kv_offsets=None, caus
                  torch.empty(k.shape, dtype=k.dtype, device=k.device),
                  torch.empty(v.shape, dtype=v.dtype, device=v.device))
     dq, dk, dv = grads
-    rdq, rdk, rdv = _heads(dq, "dq", q.shape), _heads(dk, "dk", k.shape), _heads(dv, "dv", v.shape)
-    size = lib.pss_attention_workspace(ctypes.byref(shape), 1)
+    at = _structs(shape, rg, rq, rk, rv, ro, _heads(dq, "dq", q.shape), _heads(dk, "dk", k.shape),
+                  _heads(dv, "dv", v.shape))
+    size = lib.pss_attention_workspace(at[0], 1)
     work = torch.empty(size, dtype=torch.uint8, device=q.device)
-    byref = ctypes.byref
-    binding._check(lib.pss_attention_backward(
-        byref(shape), byref(rg), byref(rq), byref(rk), byref(rv), byref(ro), pl, byref(rdq),
-        byref(rdk), byref(rdv), work.data_ptr(), size, _status(status), _stream(stream)),
-        "pss_attention_backward")
-    _used_on(stream, work)
+    binding._check(lib.pss_attention_backward(*at[:6], pl, *at[6:], work.data_ptr(), size,
+                                              _status(status), _stream()),
+                   "pss_attention_backward")
     return dq, dk, dv

@@ -215,3 +215,27 @@ def test_refusals():
     with pytest.raises(binding.PSSError) as e:
         fwd(big, big[0], big[0])
     assert e.value.status == binding.PSS_ERR_UNSUPPORTED
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,cols", [(1, 5), (2, 3), (9, 13), (300, 333), (130, 1001), (40, 8191), (20, 12001)])
+def test_odd_rows_read_nothing_of_their_neighbours(kind, rows, cols):
+    # every row between NaN rows and NaN margins: only its own values may count
+    wide = torch.full((2 * rows + 1, cols), float("nan"), dtype=TYPES[kind], device="cuda")
+    x = wide[1::2]
+    x.copy_(normal(31, rows, cols).to(TYPES[kind]))
+    gwide = torch.full_like(wide, float("nan"))
+    g = gwide[1::2]
+    g.copy_(normal(32, rows, cols).to(TYPES[kind]))
+    w, c = normal(33, cols), normal(34, cols)
+    out = torch.full_like(wide, 5.0)
+    y, mean, rstd = ops().layer_norm_forward(x, w, c, out=out[1::2])
+    ref, _, _, bound, _, _ = reference(x, w, c, 1e-5)
+    check(y, ref, bound, "y")
+    assert (out[::2] == 5).all()
+    want = backward_reference(g, x, w, mean, rstd)
+    dx, dw, db = ops().layer_norm_backward(g, x, w, mean, rstd, out=out[1::2])
+    check(dx, want[0], want[3], "dx")
+    check(dw, want[1], want[4], "dweight")
+    check(db, want[2], want[5], "dbias")
+    assert (out[::2] == 5).all()
