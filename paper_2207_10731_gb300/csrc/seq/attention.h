@@ -57,6 +57,7 @@ struct PlanHead {
 };
 
 constexpr int kTile = 128;               // rows of one tensor-core tile
+constexpr int kLeastPiece = 4;           // key tiles of a piece of a split range, at least
 
 // Sizes of a call's work list and scratch, from what the host knows.
 struct Plan {

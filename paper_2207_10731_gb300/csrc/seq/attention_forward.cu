@@ -411,27 +411,49 @@ __global__ void __launch_bounds__(kThreads) k_attention_join(Attn a, Plan p) {
     }
     const int64_t base = ((int64_t)jn.slot * a.kv_heads + hk) * kTile + r;
     const int64_t step = (int64_t)a.kv_heads * kTile;
-    float top = -INFINITY;
-    for (int i = lane; i < jn.n; i += 32) top = fmaxf(top, p.partial_lse[base + i * step]);
+    // the pieces' lse, 32 at a time a lane each; the first 128 stay in registers
+    constexpr int kHeld = 4;
+    float held[kHeld], top = -INFINITY;
+#pragma unroll
+    for (int x = 0; x < kHeld; ++x) {
+        const int i = 32 * x + lane;
+        held[x] = i < jn.n ? p.partial_lse[base + i * step] : -INFINITY;
+        top = fmaxf(top, held[x]);
+    }
+    for (int i = 32 * kHeld + lane; i < jn.n; i += 32)
+        top = fmaxf(top, p.partial_lse[base + i * step]);
 #pragma unroll
     for (int m = 16; m > 0; m >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, m));
     float sum = 0.f;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int i0 = 0; i0 < jn.n; i0 += 32) {
-        const int i = i0 + lane;
-        const float lse = i < jn.n ? p.partial_lse[base + i * step] : -INFINITY;
+    auto add_pieces = [&](int i0, float lse) {
         const float e = lse == -INFINITY ? 0.f : exp2_fast((lse - top) * kLog2e);
         sum += e;
         unsigned some = __ballot_sync(0xffffffffu, lse != -INFINITY);
         while (some) {
-            const int j = __ffs(some) - 1;
-            some &= some - 1;
-            const float w = __shfl_sync(0xffffffffu, e, j);
-            if (4 * lane < a.dim)
-                add4(o, w, *reinterpret_cast<const float4*>(
-                               p.partial + (base + (i0 + j) * step) * a.dim + 4 * lane));
+            // four pieces' sums in flight; a missing one is read as the first, times 0
+            float w[4];
+            float4 v[4];
+            const int j0 = __ffs(some) - 1;
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                const int j = some ? __ffs(some) - 1 : j0;
+                w[x] = some ? __shfl_sync(0xffffffffu, e, j) : 0.f;
+                some &= some - 1;
+                v[x] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (4 * lane < a.dim)
+                    v[x] = *reinterpret_cast<const float4*>(
+                        p.partial + (base + (i0 + j) * step) * a.dim + 4 * lane);
+            }
+#pragma unroll
+            for (int x = 0; x < 4; ++x) add4(o, w[x], v[x]);
         }
-    }
+    };
+#pragma unroll
+    for (int x = 0; x < kHeld; ++x)
+        if (32 * x < jn.n) add_pieces(32 * x, held[x]);
+    for (int i0 = 32 * kHeld; i0 < jn.n; i0 += 32)
+        add_pieces(i0, i0 + lane < jn.n ? p.partial_lse[base + (i0 + lane) * step] : -INFINITY);
 #pragma unroll
     for (int m = 16; m > 0; m >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, m);
     const float inv = 1.f / sum, lse = top + __log2f(sum) * kLn2;

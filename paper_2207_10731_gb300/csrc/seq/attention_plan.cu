@@ -18,6 +18,7 @@ namespace {
 constexpr int kBuckets = 128;
 constexpr int kPlanThreads = 1024;
 constexpr int kSmallTokens = 4096;
+constexpr int kSmallSequences = 1024, kSmallItems = 1024;
 constexpr float kLog2e = 1.4426950408889634f;
 
 // Exact up to 15, four steps to a doubling above.
@@ -44,11 +45,12 @@ __device__ __forceinline__ int64_t find(const int64_t* off, int64_t n, int64_t t
     return lo - 1;
 }
 
-// What token t of one side sees on the other side.
+// What token t of one side sees on the other side; the offsets may be copies.
 template <bool KEYS>
-__device__ __forceinline__ Range range_of(const Attn& a, int64_t t) {
-    const int64_t* own = KEYS ? a.k_off : a.q_off;
-    const int64_t* other = KEYS ? a.q_off : a.k_off;
+__device__ __forceinline__ Range range_of(const Attn& a, int64_t t, const int64_t* q_off,
+                                          const int64_t* k_off) {
+    const int64_t* own = KEYS ? k_off : q_off;
+    const int64_t* other = KEYS ? q_off : k_off;
     const int64_t own_n = KEYS ? a.k_tokens : a.q_tokens;
     const int64_t other_n = KEYS ? a.q_tokens : a.k_tokens;
     const int64_t s = find(own, a.sequences, t);
@@ -115,9 +117,9 @@ __global__ void __launch_bounds__(kThreads) k_attention_ready(Attn a, Plan p) {
     pdl_prologue();
     const int64_t t = (int64_t)blockIdx.x * kThreads + threadIdx.x;
     if (blockIdx.y == 0) {
-        if (t < a.q_tokens) p.q_range[t] = range_of<false>(a, t);
+        if (t < a.q_tokens) p.q_range[t] = range_of<false>(a, t, a.q_off, a.k_off);
     } else if (blockIdx.y == 1) {
-        if (t < a.k_tokens) p.k_range[t] = range_of<true>(a, t);
+        if (t < a.k_tokens) p.k_range[t] = range_of<true>(a, t, a.q_off, a.k_off);
     } else {
         const int64_t rows = (int64_t)a.q_tokens * a.heads;
         const int each = a.dim <= 64 ? 16 : 8;   // rows of a warp
@@ -138,6 +140,8 @@ k_attention_plan(Attn a, Plan p, int target_items, int small) {
     __shared__ unsigned count[kBuckets], next[kBuckets];
     __shared__ unsigned slots, joins, total;
     __shared__ unsigned long long work;
+    __shared__ int64_t offsets[2][kSmallSequences];
+    __shared__ int from_of[kSmallItems], tiles_of[kSmallItems];
     const bool keys = blockIdx.x == 1;
     const int tid = threadIdx.x;
     if (tid < kBuckets) count[tid] = 0;
@@ -147,13 +151,19 @@ k_attention_plan(Attn a, Plan p, int target_items, int small) {
         if (!keys && a.status) *a.status = ~0ull;
     }
     if (small) {
-        if (keys) {
-            for (int t = tid; t < a.k_tokens; t += kPlanThreads)
-                p.k_range[t] = range_of<true>(a, t);
-        } else {
-            for (int t = tid; t < a.q_tokens; t += kPlanThreads)
-                p.q_range[t] = range_of<false>(a, t);
+        // the search's steps wait on one another: in shared memory where it fits
+        const int64_t *q_off = a.q_off, *k_off = a.k_off;
+        if (a.sequences < kSmallSequences) {
+            for (int i = tid; i <= a.sequences; i += kPlanThreads) {
+                offsets[0][i] = q_off[i];
+                offsets[1][i] = k_off[i];
+            }
+            __syncthreads();
+            q_off = offsets[0];
+            k_off = offsets[1];
         }
+        for (int t = tid; t < a.q_tokens; t += kPlanThreads)
+            p.q_range[t] = range_of<false>(a, t, q_off, k_off);
     }
     __syncthreads();
     if (!keys && a.status)
@@ -169,39 +179,62 @@ k_attention_plan(Attn a, Plan p, int target_items, int small) {
     const int64_t own_n = keys ? a.k_tokens : a.q_tokens;
     const Range* ranges = keys ? p.k_range : p.q_range;
     const int other = keys ? p.key_tokens : p.keys;
+    // the key range of item i: its first key and its tiles
+    auto span = [&](int i, int* from) {
+        const int64_t first = (int64_t)i * step, past = first + step;
+        *from = ranges[first].lo;
+        const int to = ranges[(past < own_n ? past : own_n) - 1].end();
+        return to > *from ? (int)(((int64_t)to - *from + other - 1) / other) : 0;
+    };
+    const bool kept = items <= kSmallItems;   // asked for once instead of every sweep
+    if (kept) {
+        for (int i = tid; i < items; i += kPlanThreads) tiles_of[i] = span(i, &from_of[i]);
+        __syncthreads();
+    }
     // sweep 0: total work, where long ranges may be split; 1: count; 2: place
+    const bool split = p.most_slots > 0 && !keys;
     int chunk = 1 << 30;
-    for (int sweep = p.most_slots > 0 && !keys ? 0 : 1; sweep < 3; ++sweep) {
+    for (int sweep = split ? 0 : 1; sweep < 3; ++sweep) {
         unsigned long long mine = 0;
-        for (int i = tid; i < items; i += kPlanThreads) {
-            const int64_t first = (int64_t)i * step, past = first + step;
-            const int from = ranges[first].lo;
-            const int to = ranges[(past < own_n ? past : own_n) - 1].end();
-            const int all = to > from ? (int)(((int64_t)to - from + other - 1) / other) : 0;
+        // a thread to an item; a warp where an item may have many pieces
+        const int lane = tid & 31;
+        const bool wide = split && sweep == 2;
+        for (int i = wide ? tid >> 5 : tid; i < items; i += wide ? 32 : kPlanThreads) {
+            int from;
+            const int all = kept ? tiles_of[i] : span(i, &from);
+            if (kept) from = from_of[i];
             if (sweep == 0) {
                 mine += all;
                 continue;
             }
             const int parts = all > chunk ? (all + chunk - 1) / chunk : 1;
-            const int cost = bucket((all + parts - 1) / parts);
+            const int each = all / parts, rest = all - each * parts;
+            const int cost = bucket(each + (rest > 0));
             if (sweep == 1) {
                 atomicAdd(&count[cost], (unsigned)parts);
                 continue;
             }
-            const int at = (int)atomicAdd(&next[cost], (unsigned)parts);
-            if (at + parts > cap) continue;   // cannot be: cap counts them all
-            int slot = -1;
-            if (parts > 1) {
-                slot = (int)atomicAdd(&slots, (unsigned)parts);
-                p.joins[atomicAdd(&joins, 1u)] = Join{(int)first, slot, parts, 0};
+            int at = 0, slot = -1;
+            if (!wide || lane == 0) {
+                at = (int)atomicAdd(&next[cost], (unsigned)parts);
+                if (parts > 1) {
+                    slot = (int)atomicAdd(&slots, (unsigned)parts);
+                    if (slot + parts <= p.most_slots)   // else: cannot be
+                        p.joins[atomicAdd(&joins, 1u)] = Join{i * step, slot, parts, 0};
+                }
             }
+            if (wide) {
+                at = __shfl_sync(0xffffffffu, at, 0);
+                slot = __shfl_sync(0xffffffffu, slot, 0);
+            }
+            if (at + parts > cap || (slot >= 0 && slot + parts > p.most_slots)) continue;
             Item* list = (keys ? p.key_items : p.items) + at;
-            for (int j = 0; j < parts; ++j) {
+            for (int j = wide ? lane : 0; j < parts; j += wide ? 32 : 1) {
                 Item it{};
-                it.q0 = keys ? from : (int)first;
-                it.k0 = keys ? (int)first : from;
-                it.t0 = (int)((int64_t)all * j / parts);
-                it.t1 = (int)((int64_t)all * (j + 1) / parts);
+                it.q0 = keys ? from : i * step;
+                it.k0 = keys ? i * step : from;
+                it.t0 = j * each + min(j, rest);
+                it.t1 = it.t0 + each + (j < rest);
                 it.slot = slot < 0 ? -1 : slot + j;
                 list[j] = it;
             }
@@ -209,9 +242,11 @@ k_attention_plan(Attn a, Plan p, int target_items, int small) {
         if (sweep == 0) {
             if (mine) atomicAdd(&work, mine);
             __syncthreads();
-            // at least 4 key tiles a piece: joining costs a pass over the partial sums
-            const unsigned long long each = (work + target_items - 1) / target_items;
-            chunk = (int)(each < 4 ? 4 : each > (1 << 30) ? (1 << 30) : each);
+            // at most target_items pieces (every tile may end in a short one), and not
+            // shorter than kLeastPiece: joining costs a pass over the partial sums
+            const unsigned long long whole = max(1, target_items - items);
+            const unsigned long long each = (work + whole - 1) / whole;
+            chunk = (int)(each < kLeastPiece ? kLeastPiece : each > (1 << 30) ? (1 << 30) : each);
         }
         if (sweep == 1) {
             __syncthreads();
