@@ -44,6 +44,13 @@ constexpr float kLog2e = 1.4426950408889634f;
 // below 2^-150, and the factor is taken off exactly at the end.  (A dO above
 // 2^104 makes that row infinite, and it is computed by its definition.)
 constexpr float kLift = 24.f, kUnlift = 1.f / 16777216.f;
+// The dQ kernel's second product takes dS as the sum of two bf16 for heads up to
+// 64, where the products wait for the elementwise work anyway, and for heads of
+// 128 in items of up to this many keys.  dQ's error against 64 bits is then 1.2
+// to 1.4 times that of rounding dQ once instead of 1.6 (packed histories: 229
+// instead of 221 us for the whole pass); on long rows of 128, where one part
+// gives 1.4, it would cost a third more products.
+constexpr int kTwiceKeys = 1024;
 constexpr int kCompute = 256;   // threads of the elementwise work
 
 // HD: values of a head, padded; TN: rows of the tiles that an item runs over,
@@ -121,6 +128,18 @@ __device__ __forceinline__ void mma_columns(uint32_t d, uint32_t a, uint32_t b_a
                smem_desc(b_at + i * 2048, TN * 128), kDesc, add || i > 0);
 }
 
+// Values less what their rounding to bf16 keeps.
+template <int N>
+__device__ __forceinline__ void bf16_rest(float (&v)[N][32]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int e = 0; e < 32; e += 2) {
+            const float2 kept = unpack2(pack2(v[i][e], v[i][e + 1], bf16()), bf16());
+            v[i][e] -= kept.x;
+            v[i][e + 1] -= kept.y;
+        }
+}
 // Packs values to bf16 and stores them over the columns at `at`.
 template <int N>
 __device__ __forceinline__ void store_bf16(uint32_t at, const float (&v)[N][32]) {
@@ -155,6 +174,9 @@ k_attention_dq(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
     const Item it = p.items[item];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int group = a.group, tokens = p.tokens, n_tiles = it.t1;
+    // rows of few keys have the largest dS and feel the rounding of both dS and
+    // out (in delta) most
+    const bool twice = HD == 64 || n_tiles * TN <= kTwiceKeys;
 
     // the thread's row and what it sees; asked for before the loads begin
     const int r = (warp & 3) * 32 + lane, tok = r / group, h = hk * group + r - tok * group;
@@ -258,6 +280,7 @@ k_attention_dq(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
                     tc_commit(&sh.dp_full);
                 }
                 mma_columns<HD, TN>(dq_at, s_buf(n), a_buf(n), n > 0);
+                if (twice) mma_columns<HD, TN>(dq_at, s_buf(n) + TN / 4, a_buf(n), true);
                 tc_commit(&sh.a_empty[n % C::kA]);
                 if (more2) {
                     if (!(ok = have_a(n + 2))) break;
@@ -281,6 +304,7 @@ k_attention_dq(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
         const uint32_t lanes = (uint32_t)(warp & 3) << 21;
         const float c = a.scale * kLog2e;
         const float2 c2 = make_float2(c, c), l2 = make_float2(-st.x, -st.x);
+        float2 ds_sum = make_float2(0.f, 0.f);
         bool ok = true;
         for (int n = 0; n < n_tiles; ++n) {
             ok = ok && bar_wait(&sh.s_full[n & 1], (n >> 1) & 1, stop);
@@ -324,7 +348,8 @@ k_attention_dq(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
                                    make_float2(d[i][e], d[i][e + 1]), sum);
                 sh.part[half][r] = sum.x + sum.y;
                 part_sync(1, kCompute);
-                st.y = sh.part[0][r] + sh.part[1][r];
+                const float delta = sh.part[0][r] + sh.part[1][r];
+                if (isfinite(delta)) st.y = delta;   // a masked dp may not be
             }
             const float2 d2 = make_float2(-st.y, -st.y);
 #pragma unroll
@@ -336,13 +361,32 @@ k_attention_dq(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
                     d[i][e] = x.x;
                     d[i][e + 1] = x.y;
                 }
+            if (n_tiles > 1) {
+#pragma unroll
+                for (int i = 0; i < C::kChunks; ++i)
+#pragma unroll
+                    for (int e = 0; e < 32; e += 2)
+                        ds_sum = add2(ds_sum, make_float2(d[i][e], d[i][e + 1]));
+            }
             store_bf16(s_at, d);
+            if (twice) {
+                bf16_rest(d);
+                store_bf16(s_at + TN / 4, d);
+            }
             tmem_wait_store();
             tc_before_sync();
             bar_arrive(&sh.ds_ready);
             if (!ok) break;
         }
-        if (n_tiles == 1 && live && half == 0) p.stats[at_stats] = st;   // for dK and dV
+        // For dK and dV: with sum_j p = 1, sum_j ds is what delta was short of for
+        // out's rounding to bf16.
+        if (n_tiles > 1) {
+            sh.part[half][r] = ds_sum.x + ds_sum.y;
+            part_sync(1, kCompute);
+            const float rest = sh.part[0][r] + sh.part[1][r];
+            if (isfinite(rest)) st.y += rest;
+        }
+        if (ok && live && see1 > see0 && half == 0) p.stats[at_stats] = st;
         // ---- epilogue: each half stages its half of the columns ----
         const bool any = n_tiles > 0;
         ok = ok && (!any || bar_wait(&sh.done, 0, stop));
