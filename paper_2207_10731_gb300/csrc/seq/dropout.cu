@@ -23,30 +23,29 @@ struct Params {
     int64_t n, cols;               // n = rows * cols elements
     uint64_t inv;                  // floor((2^64 - 1) / d), d of the division below
     int64_t xs, rs, ys;            // row strides
-    uint32_t key0, key1, off0, off1;
+    uint32_t off0, off1;
+    uint32_t key[10][2];           // of each round
     uint32_t below;                // (threshold << 16) - 1
     bool all;                      // the threshold is 0
     float scale;
 };
 
 // The generator of Salmon, Moraes, Dror & Shaw, "Parallel random numbers: as
-// easy as 1, 2, 3" (SC 2011), 4x32 bits, 10 rounds.
+// easy as 1, 2, 3" (SC 2011), 4x32 bits, 10 rounds;
+// the rounds' keys come with the launch, as constants.
 __device__ __forceinline__ void philox(uint64_t counter, const Params& p, uint32_t (&c)[4]) {
     c[0] = (uint32_t)counter;
     c[1] = (uint32_t)(counter >> 32);
     c[2] = p.off0;
     c[3] = p.off1;
-    uint32_t k0 = p.key0, k1 = p.key1;
 #pragma unroll
     for (int r = 0; r < 10; ++r) {
         const uint64_t a = (uint64_t)c[0] * 0xD2511F53u;
         const uint64_t b = (uint64_t)c[2] * 0xCD9E8D57u;
-        c[0] = (uint32_t)(b >> 32) ^ c[1] ^ k0;
+        c[0] = (uint32_t)(b >> 32) ^ c[1] ^ p.key[r][0];
         c[1] = (uint32_t)b;
-        c[2] = (uint32_t)(a >> 32) ^ c[3] ^ k1;
+        c[2] = (uint32_t)(a >> 32) ^ c[3] ^ p.key[r][1];
         c[3] = (uint32_t)a;
-        k0 += 0x9E3779B9u;
-        k1 += 0xBB67AE85u;
     }
 }
 // Whether 16-bit value i is at least the threshold: the value in the upper half
@@ -164,8 +163,10 @@ extern "C" pss_status pss_dropout(const void* x, int64_t x_stride, const void* r
     q.xs = x_stride;
     q.rs = residual_stride;
     q.ys = y_stride;
-    q.key0 = (uint32_t)seed;
-    q.key1 = (uint32_t)(seed >> 32);
+    for (uint32_t r = 0; r < 10; ++r) {
+        q.key[r][0] = (uint32_t)seed + r * 0x9E3779B9u;
+        q.key[r][1] = (uint32_t)(seed >> 32) + r * 0xBB67AE85u;
+    }
     q.off0 = (uint32_t)offset;
     q.off1 = (uint32_t)(offset >> 32);
     const uint32_t threshold = (uint32_t)std::nearbyint(p * 65536.0);
