@@ -86,34 +86,43 @@ k_dropout(const T* x, const T* res, T* y, Params p) {
     const int64_t whole = MODE == SINGLE ? 0 : p.n / 8;
     const int64_t groups = (p.n + 7) / 8;
     const int64_t step = (int64_t)gridDim.x * kThreads;
-    // two groups a turn, their loads first: twice the bytes in flight
-    for (int64_t g0 = (int64_t)blockIdx.x * kThreads + threadIdx.x; g0 < groups; g0 += 2 * step) {
-        float v[2][8], add[2][8];
-        int64_t row[2], at[2];
+    // several groups a turn, their loads first and kept as they came: 64 bytes a
+    // thread and tensor in flight
+    constexpr int kGroups = sizeof(T) == 4 ? 2 : 4;
+    for (int64_t g0 = (int64_t)blockIdx.x * kThreads + threadIdx.x; g0 < groups;
+         g0 += kGroups * step) {
+        Raw8<T> in[kGroups], add[RES ? kGroups : 1];
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
+        for (int u = 0; u < kGroups; ++u) {
             const int64_t g = g0 + u * step;
-            row[u] = 0;
-            at[u] = 8 * g;
             if (g >= whole) continue;
+            int64_t row = 0, at = 8 * g;
             if (MODE == ROWS) {
-                row[u] = divide(g, p.cols / 8, p.inv, &at[u]);
-                at[u] *= 8;
+                row = divide(g, p.cols / 8, p.inv, &at);
+                at *= 8;
             }
-            load8(x + row[u] * p.xs + at[u], v[u]);
-            if (RES) load8(res + row[u] * p.rs + at[u], add[u]);
+            in[u] = load_raw(x + row * p.xs + at);
+            if (RES) add[RES ? u : 0] = load_raw(res + row * p.rs + at);
         }
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
+        for (int u = 0; u < kGroups; ++u) {
             const int64_t g = g0 + u * step;
             if (g >= groups) continue;
             uint32_t c[4];
             philox((uint64_t)g, p, c);
             if (g < whole) {
+                int64_t row = 0, at = 8 * g;
+                if (MODE == ROWS) {
+                    row = divide(g, p.cols / 8, p.inv, &at);
+                    at *= 8;
+                }
+                float v[8], w[8];
+                unpack(in[u], v);
+                if (RES) unpack(add[RES ? u : 0], w);
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
-                    v[u][i] = dropped<RES>(kept(c, i, p), v[u][i], p.scale, add[u][i]);
-                store8(y + row[u] * p.ys + at[u], v[u]);
+                    v[i] = dropped<RES>(kept(c, i, p), v[i], p.scale, RES ? w[i] : 0.f);
+                store8(y + row * p.ys + at, v);
                 continue;
             }
             int64_t r = 0, k = 8 * g;
@@ -136,7 +145,7 @@ k_dropout(const T* x, const T* res, T* y, Params p) {
 template <typename T, int MODE, bool RES>
 cudaError_t launch(const void* x, const void* res, void* y, const Params& p, cudaStream_t st) {
     auto* k = k_dropout<T, MODE, RES>;
-    const int64_t blocks = ((p.n + 7) / 8 + 2 * kThreads - 1) / (2 * kThreads);
+    const int64_t blocks = ((p.n + 7) / 8 + kThreads - 1) / kThreads;
     const int64_t most = (int64_t)sm_count() * 16;
     return launch_k(k, dim3((unsigned)(blocks < most ? blocks : most)), dim3(kThreads), 0, st,
                     static_cast<const T*>(x), static_cast<const T*>(res), static_cast<T*>(y), p);
