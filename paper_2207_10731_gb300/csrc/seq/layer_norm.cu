@@ -95,6 +95,33 @@ __device__ __forceinline__ bool inside(int e, int n, bool vector) {
     return MODE == RAGGED ? (unsigned)e < (unsigned)n : vector;
 }
 
+// A thread's part of one row of a tensor, as it comes from memory.
+template <typename T, int VEC, int CH>
+struct Part;
+template <typename T, int CH>
+struct Part<T, 8, CH> {
+    Raw8<T> v[CH];
+    template <int MODE>
+    __device__ __forceinline__ void load(const T* row, bool live, bool whole, const bool (&in)[CH],
+                                         const Place<8, MODE>& place, const Shape& sh) {
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
+            v[c] = live && in[c] ? load_raw_part(row, place.at(sh, c), sh.cols, whole) : Raw8<T>{};
+    }
+    __device__ __forceinline__ void get(int c, float (&to)[8]) const { unpack(v[c], to); }
+};
+template <typename T, int CH>
+struct Part<T, 1, CH> {
+    float v[CH];
+    template <int MODE>
+    __device__ __forceinline__ void load(const T* row, bool live, bool, const bool (&in)[CH],
+                                         const Place<1, MODE>& place, const Shape& sh) {
+#pragma unroll
+        for (int c = 0; c < CH; ++c) v[c] = live && in[c] ? load_f32(row[place.at(sh, c)]) : 0.f;
+    }
+    __device__ __forceinline__ void get(int c, float (&to)[1]) const { to[0] = v[c]; }
+};
+
 // Weight and bias stay in registers where these reach: not with 1024 threads,
 // which have 64 each.
 template <typename TX, typename TY, int VEC, int CH, int MODE>
@@ -122,24 +149,26 @@ k_layer_norm_forward(const TX* x, int64_t xs, const float* __restrict__ weight,
             b[kKeep ? c : 0][i] = use ? bias[at + i] : 0.f;
         }
     }
-    // the trip count is the same for every thread of the CTA (shuffles and
-    // barriers inside); rows past the end are computed from zeros and dropped
-    for (int64_t r0 = (int64_t)blockIdx.x * sh.groups; r0 < sh.rows;
-         r0 += (int64_t)gridDim.x * sh.groups) {
+    // The next row's loads are issued before this row is worked on, where the
+    // registers reach.  The trip count is the same for every thread of the CTA
+    // (shuffles and barriers inside); rows past the end are computed from zeros
+    // and dropped.
+    const int64_t step = (int64_t)gridDim.x * sh.groups;
+    Part<TX, VEC, CH> next;
+    auto fetch = [&](int64_t r) {
+        next.load(x + r * xs, r < sh.rows, MODE == ALIGNED || inner(sh, r, xs), in, place, sh);
+    };
+    if (kKeep) fetch((int64_t)blockIdx.x * sh.groups + place.group);
+    for (int64_t r0 = (int64_t)blockIdx.x * sh.groups; r0 < sh.rows; r0 += step) {
         const int64_t r = r0 + place.group;
         const bool live = r < sh.rows;
+        if (!kKeep) fetch(r);
+        const Part<TX, VEC, CH> part = next;
+        if (kKeep && r0 + step < sh.rows) fetch(r + step);
         float v[CH][VEC];
         float s = 0.f;
 #pragma unroll
-        for (int c = 0; c < CH; ++c) {
-            if (live && in[c]) {
-                load_part(x + r * xs, place.at(sh, c), sh.cols,
-                          MODE == ALIGNED || inner(sh, r, xs), v[c]);
-            } else {
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) v[c][i] = 0.f;
-            }
-        }
+        for (int c = 0; c < CH; ++c) part.get(c, v[c]);
 #pragma unroll
         for (int c = 0; c < CH; ++c)
 #pragma unroll
@@ -177,53 +206,6 @@ k_layer_norm_forward(const TX* x, int64_t xs, const float* __restrict__ weight,
         }
     }
 }
-
-// A thread's part of one row of the backward pass as it comes from memory.
-template <typename TG, typename TX, int VEC, int CH>
-struct Row;
-template <typename TG, typename TX, int CH>
-struct Row<TG, TX, 8, CH> {
-    Raw8<TX> x[CH];
-    Raw8<TG> g[CH];
-    template <int MODE>
-    __device__ __forceinline__ void load(const TX* xr, const TG* gr, bool live, bool whole,
-                                         const bool (&in)[CH], const Place<8, MODE>& place,
-                                         const Shape& sh) {
-#pragma unroll
-        for (int c = 0; c < CH; ++c) {
-            if (live && in[c]) {
-                x[c] = load_raw_part(xr, place.at(sh, c), sh.cols, whole);
-                g[c] = load_raw_part(gr, place.at(sh, c), sh.cols, whole);
-            } else {
-                x[c] = Raw8<TX>{};
-                g[c] = Raw8<TG>{};
-            }
-        }
-    }
-    __device__ __forceinline__ void get(int c, float (&h)[8], float (&d)[8]) const {
-        unpack(x[c], h);
-        unpack(g[c], d);
-    }
-};
-template <typename TG, typename TX, int CH>
-struct Row<TG, TX, 1, CH> {
-    float x[CH], g[CH];
-    template <int MODE>
-    __device__ __forceinline__ void load(const TX* xr, const TG* gr, bool live, bool,
-                                         const bool (&in)[CH], const Place<1, MODE>& place,
-                                         const Shape& sh) {
-#pragma unroll
-        for (int c = 0; c < CH; ++c) {
-            const bool use = live && in[c];
-            x[c] = use ? load_f32(xr[place.at(sh, c)]) : 0.f;
-            g[c] = use ? load_f32(gr[place.at(sh, c)]) : 0.f;
-        }
-    }
-    __device__ __forceinline__ void get(int c, float (&h)[1], float (&d)[1]) const {
-        h[0] = x[c];
-        d[0] = g[c];
-    }
-};
 
 // A row's loads are issued before the row in front of it is worked on: between
 // its loads and its store a row waits for two reductions, and the rows of the
@@ -266,12 +248,14 @@ k_layer_norm_backward(const TG* grad, int64_t gs, const TX* x, int64_t xs,
     }
     const int64_t step = (int64_t)gridDim.x * sh.groups;
     const int64_t first = (int64_t)blockIdx.x * sh.groups + place.group;
-    Row<TG, TX, VEC, CH> next;
+    Part<TX, VEC, CH> next_x;
+    Part<TG, VEC, CH> next_g;
     float next_mean = 0.f, next_rstd = 0.f;
     auto fetch = [&](int64_t r) {
         const bool live = r < sh.rows;
         const bool whole = MODE == ALIGNED || (inner(sh, r, xs) && inner(sh, r, gs));
-        next.load(x + r * xs, grad + r * gs, live, whole, in, place, sh);
+        next_x.load(x + r * xs, live, whole, in, place, sh);
+        next_g.load(grad + r * gs, live, whole, in, place, sh);
         next_mean = live ? mean_in[r] : 0.f;
         next_rstd = live ? rstd_in[r] : 0.f;
     };
@@ -280,12 +264,16 @@ k_layer_norm_backward(const TG* grad, int64_t gs, const TX* x, int64_t xs,
         const int64_t r = r0 + place.group;
         const bool live = r < sh.rows;
         if (kShared) fetch(r);   // no registers for two rows
-        const Row<TG, TX, VEC, CH> row = next;
+        const Part<TX, VEC, CH> part_x = next_x;
+        const Part<TG, VEC, CH> part_g = next_g;
         const float mean = next_mean, rstd = next_rstd;
         if (!kShared && r0 + step < sh.rows) fetch(r + step);
         float h[CH][VEC], g[CH][VEC];
 #pragma unroll
-        for (int c = 0; c < CH; ++c) row.get(c, h[c], g[c]);
+        for (int c = 0; c < CH; ++c) {
+            part_x.get(c, h[c]);
+            part_g.get(c, g[c]);
+        }
         float s = 0.f, sh_ = 0.f;
 #pragma unroll
         for (int c = 0; c < CH; ++c)

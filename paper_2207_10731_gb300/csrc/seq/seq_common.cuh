@@ -54,24 +54,6 @@ __device__ __forceinline__ float dot2(uint32_t a, uint32_t b) {
 // Streaming access to global memory: the operators read and write each element
 // once, so nothing is gained by keeping it in L1.  A thread moves 8 elements:
 // 32 bytes in one instruction (sm_100 and later) or 16.
-__device__ __forceinline__ void load8(const float* p, float (&v)[8]) {
-    asm volatile("ld.global.L1::no_allocate.v8.f32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
-                 : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]),
-                   "=f"(v[6]), "=f"(v[7])
-                 : "l"(p) : "memory");
-}
-template <typename T>
-__device__ __forceinline__ void load8(const T* p, float (&v)[8]) {
-    uint32_t w[4];
-    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
-                 : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "l"(p) : "memory");
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const float2 f = unpack2(w[i], T());
-        v[2 * i] = f.x;
-        v[2 * i + 1] = f.y;
-    }
-}
 __device__ __forceinline__ void store8(float* p, const float (&v)[8]) {
     asm volatile("st.global.v8.f32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
                  :: "l"(p), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]),
@@ -149,10 +131,6 @@ __device__ __forceinline__ Raw8<T> load_raw_part(const T* row, int at, int n, bo
     return r;
 }
 template <typename T>
-__device__ __forceinline__ void load_part(const T* row, int at, int n, bool whole, float (&v)[8]) {
-    unpack(load_raw_part(row, at, n, whole), v);
-}
-template <typename T>
 __device__ __forceinline__ void store_part(T* row, int at, int n, const float (&v)[8]) {
     if (at >= 0 && at + 8 <= n) {
         store8(row + at, v);
@@ -161,10 +139,6 @@ __device__ __forceinline__ void store_part(T* row, int at, int n, const float (&
         for (int i = 0; i < 8; ++i)
             if ((unsigned)(at + i) < (unsigned)n) row[at + i] = round_to<T>(v[i]);
     }
-}
-template <typename T>
-__device__ __forceinline__ void load_part(const T* row, int at, int n, bool whole, float (&v)[1]) {
-    v[0] = load_f32(row[at]);
 }
 template <typename T>
 __device__ __forceinline__ void store_part(T* row, int at, int n, const float (&v)[1]) {
