@@ -386,7 +386,8 @@ k_attention_dq(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
             const float rest = sh.part[0][r] + sh.part[1][r];
             if (isfinite(rest)) st.y += rest;
         }
-        if (ok && live && see1 > see0 && half == 0) p.stats[at_stats] = st;
+        // Tokens in no sequence get L = +infinity: their rows may hold anything.
+        if (ok && half == 0 && tok < tokens && token < a.q_tokens) p.stats[at_stats] = st;
         // ---- epilogue: each half stages its half of the columns ----
         const bool any = n_tiles > 0;
         ok = ok && (!any || bar_wait(&sh.done, 0, stop));

@@ -316,7 +316,9 @@ k_attention_forward(const __grid_constant__ CUtensorMap mq, const __grid_constan
         // not have, so all of a tile's warps meet below either way
         const bool none = see1 <= see0;
         const float inv = sum > 0.f ? 1.f / sum : 0.f;
-        const float lse = sum > 0.f ? top * a.scale + __log2f(sum) * kLn2 : -INFINITY;
+        const float lse = sum > 0.f    ? top * a.scale + __log2f(sum) * kLn2
+                          : sum == 0.f ? -INFINITY
+                                       : NAN;
         if (it.slot >= 0) {
             // a piece: fp32, and nothing where it holds none of the row's keys
             const int64_t at = ((int64_t)it.slot * a.kv_heads + hk) * kTile + r;

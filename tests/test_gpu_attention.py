@@ -268,6 +268,61 @@ def test_gradient_against_differences():
         assert abs(mine - slope) <= room
 
 
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_a_seen_bad_key_is_not_lost_in_a_split_range(bad):
+    # one query over a long sequence, its keys split into pieces: a piece whose
+    # sum is not finite must not pass for one that holds nothing
+    q, k, v, _ = inputs([1, 1], [6000, 3000], 2, 1, 64, seed=150)
+    clean, _ = run(q, k, v, None, [1, 1], [6000, 3000], True)
+    k[4321] = bad
+    out, lse = run(q, k, v, None, [1, 1], [6000, 3000], True)
+    score = (q[0].double() @ k[4321, 0].double()) * 0.125
+    for h in range(2):
+        if score[h] == -math.inf:   # the key's weight is zero
+            assert torch.isfinite(out[0, h]).all() and torch.isfinite(lse[0, h])
+        else:
+            assert out[0, h].isnan().all() and not torch.isfinite(lse[0, h])
+    assert torch.equal(out[1], clean[1])
+    # a value that is not finite, of a key with some weight
+    k[4321] = 0
+    v[4321, 0, 3] = bad
+    out, _ = run(q, k, v, None, [1, 1], [6000, 3000], True)
+    assert not torch.isfinite(out[0, :, 3]).any()
+    assert torch.isfinite(out[0, :, 4]).all() and torch.equal(out[1], clean[1])
+
+
+def test_tokens_outside_every_sequence_are_left_alone():
+    n = 300
+    q, k, v, grad = inputs([n], [n], 4, 2, 64, seed=160)
+    off = torch.tensor([7, 40, 40, 190, 250], dtype=torch.int64, device="cuda")
+    outside = torch.ones(n, dtype=torch.bool, device="cuda")
+    outside[7:250] = False
+    for t in (q, k, v, grad):   # what they hold does not matter
+        t[outside] = float("nan")
+    places = [torch.full_like(t, 7.0) for t in (q, q, k, v)]
+    out, lse = ops().attention_forward(q, k, v, off, out=places[0])
+    out[outside] = float("nan")
+    lse[outside] = float("nan")
+    ops().attention_backward(grad, q, k, v, out, lse, off, grads=places[1:])
+    for p in places[1:]:
+        assert (p[outside] == 7).all()
+    lens = [33, 0, 150, 60]
+    inner = [t[7:250] for t in (q, k, v, grad)]
+    compare([t[7:250] for t in (out, lse, *places[1:])], *inner, lens, lens, True)
+
+
+@pytest.mark.parametrize("heads,dim", [(1, 8), (2, 96)])
+def test_thousands_of_sequences(heads, dim):
+    # more than the planner keeps in shared memory, and more tiles (150 k tokens of
+    # one head: 1170)
+    lens = [(37 * i) % 101 for i in range(3000)]
+    lens[1500] = 700
+    if heads > 1:
+        lens = [n % 7 for n in lens]
+    q, k, v, grad = inputs(lens, lens, heads, 1, dim, seed=170)
+    compare(run(q, k, v, grad, lens, lens, True), q, k, v, grad, lens, lens, True)
+
+
 def test_equal_inputs_give_equal_bits_and_other_streams():
     nq = [400, 0, 3, 129, 700]
     q, k, v, grad = inputs(nq, nq, 8, 2, 64, seed=100)
