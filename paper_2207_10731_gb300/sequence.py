@@ -9,7 +9,6 @@ there is no autograd graph here.
 """
 from __future__ import annotations
 
-import functools
 import struct
 import threading
 
@@ -33,21 +32,32 @@ def _library():
     return _lib
 
 
-def _stream():
-    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+def _under(stream, call, *args, **kwargs):
+    """The call with ``stream`` as the current stream, so that what it allocates
+    belongs to the stream that uses it."""
+    _library()
+    with torch.cuda.stream(stream):
+        return call(*args, **kwargs)
 
 
-def _device_tensor(t, name):
+def _device():
+    """The current device, with the library loaded."""
+    if _lib is None:
+        _library()
+    return torch._C._cuda_getDevice()
+
+
+def _tensor(t, name, device):
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
-    if t.get_device() != torch._C._cuda_getDevice():
+    if t.get_device() != device:
         raise ValueError(f"{name} must be on the current CUDA device")
 
 
-def _rows(t, name, like=None, dtype=None):
+def _rows(t, name, device, like=None, dtype=None):
     """(rows, cols, stride) of a tensor seen as rows of its last dimension,
     which must be dense; the leading dimensions must be one stride apart."""
-    _device_tensor(t, name)
+    _tensor(t, name, device)
     if t.dtype not in _types:
         raise TypeError(f"{name} must be float32, bfloat16 or float16, got {t.dtype}")
     if dtype is not None and t.dtype != dtype:
@@ -81,8 +91,8 @@ def _rows(t, name, like=None, dtype=None):
     return rows, cols, stride
 
 
-def _vector(t, n, name):
-    _device_tensor(t, name)
+def _vector(t, n, name, device):
+    _tensor(t, name, device)
     if t.dtype != torch.float32:
         raise TypeError(f"{name} must be torch.float32, got {t.dtype}")
     if t.numel() != n or not t.is_contiguous():
@@ -90,90 +100,93 @@ def _vector(t, n, name):
     return t.data_ptr()
 
 
-def _on_stream(call):
-    """Runs ``call`` with ``stream`` as the current stream, so that what it
-    allocates belongs to the stream that uses it."""
-    @functools.wraps(call)
-    def run(*args, stream=None, **kwargs):
-        if stream is None:
-            return call(*args, **kwargs)
-        _library()
-        with torch.cuda.stream(stream):
-            return call(*args, **kwargs)
-    return run
-
-
-@_on_stream
-def layer_norm_forward(x, weight, bias, eps: float = 1e-5, out=None, out_dtype=None):
+def layer_norm_forward(x, weight, bias, eps: float = 1e-5, out=None, out_dtype=None, stream=None):
     """(y, mean, rstd) of the layer norm over x's last dimension
     (pss_layer_norm_forward).  ``x``: float32, bfloat16 or float16, rows evenly
     spaced; ``weight``, ``bias``: float32.  y has ``out_dtype`` (default: x's)
     or is ``out``; mean and rstd are float32, for the backward call."""
-    lib = _library()
-    rows, cols, xs = _rows(x, "x")
+    if stream is not None:
+        return _under(stream, layer_norm_forward, x, weight, bias, eps, out, out_dtype)
+    device = _device()
+    rows, cols, xs = _rows(x, "x", device)
     if out is None:
         out = torch.empty(x.shape, dtype=out_dtype or x.dtype, device=x.device)
-    elif out_dtype is not None and out.dtype != out_dtype:
-        raise TypeError(f"out must be {out_dtype}, got {out.dtype}")
-    _, _, ys = _rows(out, "out", like=x)
+        if out.dtype not in _types:
+            raise TypeError(f"out_dtype must be float32, bfloat16 or float16, got {out.dtype}")
+        ys = cols
+    else:
+        if out_dtype is not None and out.dtype != out_dtype:
+            raise TypeError(f"out must be {out_dtype}, got {out.dtype}")
+        _, _, ys = _rows(out, "out", device, like=x)
     mean = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
     rstd = torch.empty_like(mean)
-    binding._check(lib.pss_layer_norm_forward(
-        x.data_ptr(), _types[x.dtype], xs, _vector(weight, cols, "weight"),
-        _vector(bias, cols, "bias"), rows, cols, eps, out.data_ptr(), _types[out.dtype], ys,
-        mean.data_ptr(), rstd.data_ptr(), _stream()), "pss_layer_norm_forward")
+    rc = _lib.pss_layer_norm_forward(
+        x.data_ptr(), _types[x.dtype], xs, _vector(weight, cols, "weight", device),
+        _vector(bias, cols, "bias", device), rows, cols, eps, out.data_ptr(), _types[out.dtype], ys,
+        mean.data_ptr(), rstd.data_ptr(), torch._C._cuda_getCurrentRawStream(device))
+    if rc:
+        binding._check(rc, "pss_layer_norm_forward")
     return out, mean, rstd
 
 
-@_on_stream
-def layer_norm_backward(grad, x, weight, mean, rstd, out=None):
+def layer_norm_backward(grad, x, weight, mean, rstd, out=None, stream=None):
     """(dx, dweight, dbias) for the upstream gradient ``grad`` of the y of
     ``layer_norm_forward(x, weight, ...)`` (pss_layer_norm_backward).  dx has
     x's type or is ``out``; dweight and dbias are float32."""
-    lib = _library()
-    rows, cols, xs = _rows(x, "x")
-    _, _, gs = _rows(grad, "grad", like=x)
+    if stream is not None:
+        return _under(stream, layer_norm_backward, grad, x, weight, mean, rstd, out)
+    device = _device()
+    rows, cols, xs = _rows(x, "x", device)
+    _, _, gs = _rows(grad, "grad", device, like=x)
     if out is None:
-        out = torch.empty_like(x, memory_format=torch.contiguous_format)
-    _, _, ds = _rows(out, "out", like=x, dtype=x.dtype)
+        out, ds = torch.empty_like(x, memory_format=torch.contiguous_format), cols
+    else:
+        _, _, ds = _rows(out, "out", device, like=x, dtype=x.dtype)
     both = torch.empty((2, cols), dtype=torch.float32, device=x.device)
-    size = lib.pss_layer_norm_workspace(rows, cols)
+    size = _lib.pss_layer_norm_workspace(rows, cols)
     work = torch.empty(size, dtype=torch.uint8, device=x.device)
-    binding._check(lib.pss_layer_norm_backward(
+    rc = _lib.pss_layer_norm_backward(
         grad.data_ptr(), _types[grad.dtype], gs, x.data_ptr(), _types[x.dtype], xs,
-        _vector(weight, cols, "weight"), _vector(mean, rows, "mean"), _vector(rstd, rows, "rstd"),
-        rows, cols, out.data_ptr(), ds, both.data_ptr(), both.data_ptr() + 4 * cols,
-        work.data_ptr(), size, _stream()), "pss_layer_norm_backward")
+        _vector(weight, cols, "weight", device), _vector(mean, rows, "mean", device),
+        _vector(rstd, rows, "rstd", device), rows, cols, out.data_ptr(), ds, both.data_ptr(),
+        both.data_ptr() + 4 * cols, work.data_ptr(), size,
+        torch._C._cuda_getCurrentRawStream(device))
+    if rc:
+        binding._check(rc, "pss_layer_norm_backward")
     return out, both[0], both[1]
 
 
-@_on_stream
-def dropout(x, p: float, seed: int, offset: int = 0, residual=None, out=None):
+def dropout(x, p: float, seed: int, offset: int = 0, residual=None, out=None, stream=None):
     """x with each element zeroed with probability p and the others divided by
     1 - p, plus ``residual`` (pss_dropout).  The mask follows from (seed,
     offset, position) alone and is not stored: the backward pass is the same
     call on the gradient, without the residual.  seed and offset are unsigned
     64-bit; give each call of a step an offset of its own."""
-    lib = _library()
-    rows, cols, xs = _rows(x, "x")
-    rs = 0
+    if stream is not None:
+        return _under(stream, dropout, x, p, seed, offset, residual, out)
+    device = _device()
+    rows, cols, xs = _rows(x, "x", device)
+    more, rs = None, 0
     if residual is not None:
-        _, _, rs = _rows(residual, "residual", like=x, dtype=x.dtype)
+        _, _, rs = _rows(residual, "residual", device, like=x, dtype=x.dtype)
+        more = residual.data_ptr()
     if out is None:
-        out = torch.empty_like(x, memory_format=torch.contiguous_format)
-    _, _, ys = _rows(out, "out", like=x, dtype=x.dtype)
+        out, ys = torch.empty_like(x, memory_format=torch.contiguous_format), cols
+    else:
+        _, _, ys = _rows(out, "out", device, like=x, dtype=x.dtype)
     if not (0 <= seed < 2**64 and 0 <= offset < 2**64):
         raise ValueError("seed and offset must be unsigned 64-bit integers")
-    binding._check(lib.pss_dropout(
-        x.data_ptr(), xs, None if residual is None else residual.data_ptr(), rs, rows, cols, p,
-        seed, offset, _types[x.dtype], out.data_ptr(), ys, _stream()), "pss_dropout")
+    rc = _lib.pss_dropout(x.data_ptr(), xs, more, rs, rows, cols, p, seed, offset, _types[x.dtype],
+                          out.data_ptr(), ys, torch._C._cuda_getCurrentRawStream(device))
+    if rc:
+        binding._check(rc, "pss_dropout")
     return out
 
 
-def _heads(t, name, shape=None):
+def _heads(t, name, device, shape=None):
     """(data, token stride, head stride) of a bfloat16 tensor [tokens, heads,
     dim], dense in its last dimension."""
-    _device_tensor(t, name)
+    _tensor(t, name, device)
     if t.dtype != torch.bfloat16:
         raise TypeError(f"{name} must be torch.bfloat16, got {t.dtype}")
     own = t.shape
@@ -187,24 +200,32 @@ def _heads(t, name, shape=None):
     return t.data_ptr(), token if own[0] != 1 else 0, head if own[1] != 1 else 0
 
 
+def _made(t):
+    """The same of a tensor made here."""
+    _, heads, dim = t.shape
+    return t.data_ptr(), heads * dim if t.shape[0] != 1 else 0, dim if heads != 1 else 0
+
+
 def _structs(shape, *rows):
     """Addresses of the structures of one call, in a buffer of this thread that
     the library reads before it returns."""
-    buffer = getattr(_local, "buffer", None)
-    if buffer is None:
-        buffer = _local.buffer = bytearray(_SHAPE.size + 10 * _ROWS.size)
-        _local.at = binding.ctypes.addressof(binding.ctypes.c_char.from_buffer(buffer))
+    try:
+        buffer, start = _local.buffer
+    except AttributeError:
+        buffer = bytearray(_SHAPE.size + 10 * _ROWS.size)
+        start = binding.ctypes.addressof(binding.ctypes.c_char.from_buffer(buffer))
+        _local.buffer = buffer, start
     _SHAPE.pack_into(buffer, 0, *shape)
-    at, where = _SHAPE.size, [_local.at]
+    at, where = _SHAPE.size, [start]
     for r in rows:
         _ROWS.pack_into(buffer, at, *r)
-        where.append(_local.at + at)
+        where.append(start + at)
         at += _ROWS.size
     return where
 
 
-def _offsets(t, name):
-    _device_tensor(t, name)
+def _offsets(t, name, device):
+    _tensor(t, name, device)
     if t.dtype != torch.int64:
         raise TypeError(f"{name} must be torch.int64, got {t.dtype}")
     if t.dim() != 1 or t.numel() < 1 or not t.is_contiguous():
@@ -212,31 +233,31 @@ def _offsets(t, name):
     return t
 
 
-def _attention_shape(q, k, q_offsets, kv_offsets, causal, scale):
-    _offsets(q_offsets, "q_offsets")
+def _attention_shape(q, k, q_offsets, kv_offsets, causal, scale, device):
+    n = _offsets(q_offsets, "q_offsets", device).numel()
     if kv_offsets is None:
         kv_offsets = q_offsets
-    elif _offsets(kv_offsets, "kv_offsets").numel() != q_offsets.numel():
+    elif _offsets(kv_offsets, "kv_offsets", device).numel() != n:
         raise ValueError("q_offsets and kv_offsets must have the same number of entries")
     tokens, heads, dim = q.shape
-    if k.shape[2] != dim:
-        raise ValueError(f"k must have rows of {dim} values, got {k.shape[2]}")
-    return (q_offsets.numel() - 1, q_offsets.data_ptr(), kv_offsets.data_ptr(), tokens, k.shape[0],
-            heads, k.shape[1], dim, int(bool(causal)), dim ** -0.5 if scale is None else scale)
+    k_tokens, kv_heads, k_dim = k.shape
+    if k_dim != dim:
+        raise ValueError(f"k must have rows of {dim} values, got {k_dim}")
+    return (n - 1, q_offsets.data_ptr(), kv_offsets.data_ptr(), tokens, k_tokens, heads, kv_heads,
+            dim, 1 if causal else 0, dim ** -0.5 if scale is None else scale)
 
 
-def _status(status):
+def _status(status, device):
     if status is None:
         return None
-    _device_tensor(status, "status")
+    _tensor(status, "status", device)
     if status.dtype != torch.int64 or status.numel() != 1:
         raise TypeError("status must be a torch.int64 tensor of one value")
     return status.data_ptr()
 
 
-@_on_stream
 def attention_forward(q, k, v, q_offsets, kv_offsets=None, causal: bool = True, scale=None,
-                      out=None, status=None):
+                      out=None, status=None, stream=None):
     """(out, lse) of softmax(scale q k^T) v inside each packed sequence
     (pss_attention_forward).
 
@@ -249,45 +270,60 @@ def attention_forward(q, k, v, q_offsets, kv_offsets=None, causal: bool = True, 
     step.  scale defaults to dim ** -0.5.  lse is float32 [query tokens,
     heads].  ``status`` (int64, one value on the device) receives -1, the first
     sequence with malformed offsets, or -2 if a device wait gave up."""
-    lib = _library()
-    rq, rk, rv = _heads(q, "q"), _heads(k, "k"), _heads(v, "v", k.shape)
-    shape = _attention_shape(q, k, q_offsets, kv_offsets, causal, scale)
+    if stream is not None:
+        return _under(stream, attention_forward, q, k, v, q_offsets, kv_offsets, causal, scale, out,
+                      status)
+    device = _device()
+    rq, rk, rv = _heads(q, "q", device), _heads(k, "k", device), _heads(v, "v", device, k.shape)
+    shape = _attention_shape(q, k, q_offsets, kv_offsets, causal, scale, device)
     if out is None:
         out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    at = _structs(shape, rq, rk, rv, _heads(out, "out", q.shape))
+        ro = _made(out)
+    else:
+        ro = _heads(out, "out", device, q.shape)
+    at = _structs(shape, rq, rk, rv, ro)
     lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
-    size = lib.pss_attention_workspace(at[0], 0)
+    size = _lib.pss_attention_workspace(at[0], 0)
     work = torch.empty(size, dtype=torch.uint8, device=q.device)
-    binding._check(lib.pss_attention_forward(*at, lse.data_ptr(), work.data_ptr(), size,
-                                             _status(status), _stream()),
-                   "pss_attention_forward")
+    rc = _lib.pss_attention_forward(*at, lse.data_ptr(), work.data_ptr(), size,
+                                    _status(status, device),
+                                    torch._C._cuda_getCurrentRawStream(device))
+    if rc:
+        binding._check(rc, "pss_attention_forward")
     return out, lse
 
 
-@_on_stream
 def attention_backward(grad, q, k, v, out, lse, q_offsets, kv_offsets=None, causal: bool = True,
-                       scale=None, grads=None, status=None):
+                       scale=None, grads=None, status=None, stream=None):
     """(dq, dk, dv) for the upstream gradient ``grad`` of the out of
     ``attention_forward`` (pss_attention_backward); out and lse are that
     call's.  The gradients go to the three tensors ``grads`` if given (e.g.
     views of one buffer for a fused projection)."""
-    lib = _library()
-    rq, rk, rv = _heads(q, "q"), _heads(k, "k"), _heads(v, "v", k.shape)
-    rg, ro = _heads(grad, "grad", q.shape), _heads(out, "out", q.shape)
-    shape = _attention_shape(q, k, q_offsets, kv_offsets, causal, scale)
+    if stream is not None:
+        return _under(stream, attention_backward, grad, q, k, v, out, lse, q_offsets, kv_offsets,
+                      causal, scale, grads, status)
+    device = _device()
+    rq, rk, rv = _heads(q, "q", device), _heads(k, "k", device), _heads(v, "v", device, k.shape)
+    rg, ro = _heads(grad, "grad", device, q.shape), _heads(out, "out", device, q.shape)
+    shape = _attention_shape(q, k, q_offsets, kv_offsets, causal, scale, device)
     if lse.shape != q.shape[:2]:
         raise ValueError(f"lse must have shape {tuple(q.shape[:2])}, got {tuple(lse.shape)}")
-    pl = _vector(lse, lse.numel(), "lse")
+    pl = _vector(lse, lse.numel(), "lse", device)
     if grads is None:
-        grads = (torch.empty(q.shape, dtype=q.dtype, device=q.device),
-                 torch.empty(k.shape, dtype=k.dtype, device=k.device),
-                 torch.empty(v.shape, dtype=v.dtype, device=v.device))
-    dq, dk, dv = grads
-    at = _structs(shape, rg, rq, rk, rv, ro, _heads(dq, "dq", q.shape), _heads(dk, "dk", k.shape),
-                  _heads(dv, "dv", v.shape))
-    size = lib.pss_attention_workspace(at[0], 1)
+        dq = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        dk = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+        dv = torch.empty(v.shape, dtype=v.dtype, device=v.device)
+        to = _made(dq), _made(dk), _made(dv)
+    else:
+        dq, dk, dv = grads
+        to = (_heads(dq, "dq", device, q.shape), _heads(dk, "dk", device, k.shape),
+              _heads(dv, "dv", device, v.shape))
+    at = _structs(shape, rg, rq, rk, rv, ro, *to)
+    size = _lib.pss_attention_workspace(at[0], 1)
     work = torch.empty(size, dtype=torch.uint8, device=q.device)
-    binding._check(lib.pss_attention_backward(*at[:6], pl, *at[6:], work.data_ptr(), size,
-                                              _status(status), _stream()),
-                   "pss_attention_backward")
+    rc = _lib.pss_attention_backward(*at[:6], pl, *at[6:], work.data_ptr(), size,
+                                     _status(status, device),
+                                     torch._C._cuda_getCurrentRawStream(device))
+    if rc:
+        binding._check(rc, "pss_attention_backward")
     return dq, dk, dv

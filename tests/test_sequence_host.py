@@ -53,7 +53,7 @@ def test_structures_match_the_header():
     assert size == sequence._ROWS.size == 24 and fields == [(0, 8), (8, 8), (16, 8)]
     # each tensor of a call has its place in the buffer
     assert sequence._structs((1, 0, 0, 2, 3, 4, 4, 64, 1, 0.5), (16, 8, 8), (32, 8, 8))[1:] == \
-        [sequence._local.at + 64, sequence._local.at + 88]
+        [sequence._local.buffer[1] + 64, sequence._local.buffer[1] + 88]
 
 
 def test_refusals_before_any_device_work(lib):
