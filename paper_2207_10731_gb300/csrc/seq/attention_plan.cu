@@ -298,9 +298,10 @@ cudaError_t launch_plan(const Attn& a, const Plan& p, bool backward, int target_
     auto blocks = [](int64_t n, int64_t each) { return (int)((n + each - 1) / each); };
     Roles r{backward ? 2 : 1, 0, blocks(a.q_tokens, kPlanThreads)};
     if (backward) {
-        // up to 16 CTAs an SM in all, 8 or 16 rows a warp and turn
+        // one CTA an SM fits, which then loops over its rows: new CTAs would each wait for
+        // their first loads
         const int rows = blocks((int64_t)a.q_tokens * a.heads, 8 * (kPlanThreads / 32));
-        const int most = sm_count() * 16;
+        const int most = sm_count();
         r.stats = rows < most ? rows : most;
     }
     const int keys = backward ? blocks(a.k_tokens, kPlanThreads) : 0;
