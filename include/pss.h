@@ -500,7 +500,9 @@ typedef struct {
  *   to -2 when a bounded wait gave up (the outputs are then invalid).
  * Rows outside every sequence are left unwritten.  Equal inputs give equal
  * bits.  A masked key or value changes nothing, also where it is infinite or
- * NaN, and neither does another sequence's.
+ * NaN, and neither does another sequence's.  (Rows that come out infinite or NaN
+ * are computed a second time, one key after the other: right, and some hundred
+ * times slower.)
  * Errors: PSS_ERR_INVALID_ARG (sizes, strides, alignment, host pointers, a
  * small workspace), PSS_ERR_CUDA.
  */

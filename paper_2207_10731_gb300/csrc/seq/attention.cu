@@ -152,7 +152,12 @@ extern "C" pss_status pss_attention_forward(const pss_attention_shape* shape, co
     int target;
     lay_out(*shape, false, workspace, &p, &target);
     if (a.sequences == 0) return no_sequences(a, st);
-    cudaError_t e = launch_plan(a, p, false, target, st);
+    // A few tiles of a few sequences need no list: their order does not matter, and
+    // a CTA's two short searches cost less than a launch (1 user x 200 keys: 27 us a
+    // call with the list, 22 without).  The status word is the list's business.
+    p.direct = !status && p.most_slots == 0 && p.per_item == 1 && a.sequences <= 64 &&
+               p.tiles * a.kv_heads <= sm_count();
+    cudaError_t e = p.direct ? cudaSuccess : launch_plan(a, p, false, target, st);
     if (e == cudaSuccess && a.q_tokens > 0) e = launch_tiles_forward(a, p, st);
     return status_of(e);
 }

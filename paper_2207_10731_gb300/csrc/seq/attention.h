@@ -37,6 +37,47 @@ struct Range {
     __device__ __forceinline__ int end() const { return hi < 0 ? -1 - hi : hi; }
 };
 
+__device__ __forceinline__ int64_t clamp64(int64_t x, int64_t lo, int64_t hi) {
+    return x < lo ? lo : x > hi ? hi : x;
+}
+
+// The last sequence that starts at or before t, or -1.
+__device__ __forceinline__ int64_t find(const int64_t* off, int64_t n, int64_t t) {
+    int64_t lo = 0, hi = n;
+    while (lo < hi) {
+        const int64_t mid = (lo + hi) >> 1;
+        if (off[mid] <= t)
+            lo = mid + 1;
+        else
+            hi = mid;
+    }
+    return lo - 1;
+}
+
+// What token t of one side sees on the other side; the offsets may be copies.
+template <bool KEYS>
+__device__ __forceinline__ Range range_of(const Attn& a, int64_t t, const int64_t* q_off,
+                                          const int64_t* k_off) {
+    const int64_t* own = KEYS ? k_off : q_off;
+    const int64_t* other = KEYS ? q_off : k_off;
+    const int64_t own_n = KEYS ? a.k_tokens : a.q_tokens;
+    const int64_t other_n = KEYS ? a.q_tokens : a.k_tokens;
+    const int64_t s = find(own, a.sequences, t);
+    if (s < 0) {
+        const int at = (int)clamp64(other[0], 0, other_n);
+        return Range{at, -1 - at};
+    }
+    const int64_t begin = own[s], end = own[s + 1], lo = other[s], hi = other[s + 1];
+    if (begin < 0 || t >= end || end > own_n || lo < 0 || lo > hi || hi > other_n) {
+        const int at = (int)clamp64(hi, 0, other_n);
+        return Range{at, -1 - at};
+    }
+    if (!a.causal) return Range{(int)lo, (int)hi};
+    // query i stands at key i + (end of the keys - end of the queries)
+    if (KEYS) return Range{(int)clamp64(t - (end - hi), lo, hi), (int)hi};
+    return Range{(int)lo, (int)clamp64(t + 1 + (hi - end), lo, hi)};
+}
+
 // A piece of work: a tile of consecutive query tokens (or keys), whichever
 // sequences they belong to, and the tiles of the other side that hold all that
 // they see.  Short neighbouring sequences so share a tile; what a row does not
@@ -68,6 +109,7 @@ struct Plan {
     int tiles, key_tiles;                // query and key tiles of the call
     int most_items;                      // query items: tiles / per_item, and splits
     int most_slots;                      // > 0: long key ranges may be split
+    bool direct;                         // no list: each CTA works its item out itself
     PlanHead* head;
     Item* items;
     Item* key_items;

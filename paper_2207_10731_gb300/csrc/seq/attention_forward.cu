@@ -68,9 +68,20 @@ k_attention_forward(const __grid_constant__ CUtensorMap mq, const __grid_constan
     __shared__ bool keep[NQ][kTile];   // rows to be stored
     const int item = blockIdx.x / a.kv_heads, hk = blockIdx.x - item * a.kv_heads;
     if (p.most_slots > 0 && item >= p.head->items) return;
-    const Item it = p.items[item];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int group = a.group, tokens = p.tokens;
+    Item it;
+    if (NQ == 1 && p.direct) {
+        it.q0 = item * tokens;
+        it.k0 = range_of<false>(a, it.q0, a.q_off, a.k_off).lo;
+        const int last = min(it.q0 + tokens, a.q_tokens) - 1;
+        const int keys = range_of<false>(a, last, a.q_off, a.k_off).end() - it.k0;
+        it.t0 = 0;
+        it.t1 = keys > 0 ? (keys + kTile - 1) / kTile : 0;
+        it.slot = -1;
+    } else {
+        it = p.items[item];
+    }
 
     // key tiles of each query tile: t0 <= t < end[t]
     int end[NQ];
@@ -88,7 +99,9 @@ k_attention_forward(const __grid_constant__ CUtensorMap mq, const __grid_constan
     const int row_tok = row / group, row_h = hk * group + row - row_tok * group;
     const int token = it.q0 + tile * tokens + row_tok;
     Range range{0, -1};
-    if (warp < NQ * 4 && row_tok < tokens && token < a.q_tokens) range = p.q_range[token];
+    if (warp < NQ * 4 && row_tok < tokens && token < a.q_tokens)
+        range = NQ == 1 && p.direct ? range_of<false>(a, token, a.q_off, a.k_off)
+                                    : p.q_range[token];
 
     uint8_t* ring = smem + C::kQ;
     if (threadIdx.x == 0) {

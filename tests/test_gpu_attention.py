@@ -148,6 +148,19 @@ def test_lengths_and_masks(lens, causal, heads, kv_heads, dim):
     compare(run(q, k, v, grad, nq, nk, causal), q, k, v, grad, nq, nk, causal)
 
 
+@pytest.mark.parametrize("lens", ["one token", "one row", "short", "around a tile", "more queries than keys"])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("heads,kv_heads,dim", [(1, 1, 64), (6, 2, 128)])
+def test_small_calls_without_a_status_word(lens, causal, heads, kv_heads, dim):
+    # no work list is made for these: the same results, bit for bit
+    nq, nk = LENS[lens]
+    q, k, v, _ = inputs(nq, nk, heads, kv_heads, dim, seed=180)
+    got = run(q, k, v, None, nq, nk, causal, status=False)
+    compare(got, q, k, v, None, nq, nk, causal)
+    listed = run(q, k, v, None, nq, nk, causal)
+    assert torch.equal(got[0], listed[0]) and torch.equal(got[1], listed[1])
+
+
 @pytest.mark.parametrize("dim", [8, 16, 24, 32, 40, 56, 64, 72, 80, 96, 112, 120, 128])
 @pytest.mark.parametrize("heads,kv_heads", [(2, 2), (5, 1)])
 def test_dims(dim, heads, kv_heads):
