@@ -497,7 +497,8 @@ typedef struct {
  *   status: NULL or device int64[1], set to -1, to the smallest sequence with
  *   malformed offsets (the rows of that sequence and of later ones are then
  *   undefined, or left unwritten; nothing outside the tensors is touched), or
- *   to -2 when a bounded wait gave up (the outputs are then invalid).
+ *   to -2 when a wait inside a kernel gave up after 2 s (its tile's rows were
+ *   then computed one at a time).
  * Rows outside every sequence are left unwritten.  Equal inputs give equal
  * bits.  A masked key or value changes nothing, also where it is infinite or
  * NaN, and neither does another sequence's.  (Rows that come out infinite or NaN

@@ -26,8 +26,8 @@
 // after it; K of dQ, which is wanted again soonest, by its last product.
 //
 // What a row does not see gets S = -infinity, hence P = 0; a row that sees
-// nothing has L = +infinity.  Non-finite rows are computed again by the
-// definition, as in the forward pass.
+// nothing has L = +infinity.  Rows that are not finite, or whose tile did not
+// come to its end, are computed again by the definition, as in the forward pass.
 #include <atomic>
 
 #include "attention_rows.cuh"
@@ -100,6 +100,18 @@ __device__ __forceinline__ void load_tile(uint8_t* to, int slab, const CUtensorM
 #pragma unroll
     for (int h = 0; h < HD / 64; ++h)
         tma_load3(to + h * slab, map, 64 * h, head, token, bar);
+}
+
+// The loads (na and nb tiles of the rings) must land before the CTA ends, also
+// where nobody waits for them.
+template <typename C, int TN>
+__device__ __forceinline__ void loads_landed(Shared<TN>& sh, int na, int nb) {
+    int never = 0;
+    bar_wait(&sh.resident, 0, &never);
+    for (int m = max(0, na - C::kA); m < na; ++m)
+        bar_wait(&sh.a_full[m % C::kA], (m / C::kA) & 1, &never);
+    for (int m = max(0, nb - C::kB); m < nb; ++m)
+        bar_wait(&sh.b_full[m % C::kB], (m / C::kB) & 1, &never);
 }
 
 // D = A B^T: 128 and TN rows of HD values in shared memory.
@@ -221,27 +233,21 @@ k_attention_dq(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
             bar_expect(&sh.resident, 2 * box);
             load_tile<HD>(smem, 16384, &mq, hk * group, it.q0, &sh.resident);
             load_tile<HD>(smem + C::kTileBytes, 16384, &mg, hk * group, it.q0, &sh.resident);
-            int n = 0;
-            for (; n < n_tiles; ++n) {
+            int na = 0, nb = 0;
+            for (int n = 0; n < n_tiles; ++n) {
                 const int sa = n % C::kA, sb = n % C::kB;
                 if (n >= C::kA && !bar_wait(&sh.a_empty[sa], (n / C::kA - 1) & 1, stop)) break;
                 bar_expect(&sh.a_full[sa], C::kUnit);
                 load_tile<HD>(ring_a + sa * C::kUnit, C::kSlab, &mk, hk, it.k0 + n * TN,
                               &sh.a_full[sa]);
+                ++na;
                 if (n >= C::kB && !bar_wait(&sh.b_empty[sb], (n / C::kB - 1) & 1, stop)) break;
                 bar_expect(&sh.b_full[sb], C::kUnit);
                 load_tile<HD>(ring_b + sb * C::kUnit, C::kSlab, &mv, hk, it.k0 + n * TN,
                               &sh.b_full[sb]);
+                ++nb;
             }
-            if (*stop) {   // the loads in flight must land before the CTA ends
-                int never = 0;
-                bar_wait(&sh.resident, 0, &never);
-                for (int m = max(0, n - C::kA); m < n; ++m)
-                    bar_wait(&sh.a_full[m % C::kA], (m / C::kA) & 1, &never);
-                for (int m = max(0, n - C::kB); m < n; ++m)
-                    bar_wait(&sh.b_full[m % C::kB], (m / C::kB) & 1, &never);
-                if (n < n_tiles) bar_wait(&sh.a_full[n % C::kA], (n / C::kA) & 1, &never);
-            }
+            loads_landed<C>(sh, na, nb);
         }
     } else if (warp == 9) {
         // ---- products ----
@@ -288,11 +294,11 @@ k_attention_dq(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
                     tc_commit(&sh.s_full[n & 1]);
                 }
             }
+            // the products must end before their memory is freed, also where the
+            // other warps have given up
+            int never = 0;
             tc_commit(&sh.done);
-            if (!ok) {   // the products in flight must end before their memory is freed
-                int never = 0;
-                bar_wait(&sh.done, 0, &never);
-            }
+            bar_wait(&sh.done, 0, &never);
         }
     } else {
         // ---- P and dS: thread = half a row ----
@@ -380,14 +386,14 @@ k_attention_dq(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
         }
         // For dK and dV: with sum_j p = 1, sum_j ds is what delta was short of for
         // out's rounding to bf16.
+        if (n_tiles > 1) sh.part[half][r] = ds_sum.x + ds_sum.y;
+        const bool lost = part_any(1, kCompute, !ok);
         if (n_tiles > 1) {
-            sh.part[half][r] = ds_sum.x + ds_sum.y;
-            part_sync(1, kCompute);
             const float rest = sh.part[0][r] + sh.part[1][r];
             if (isfinite(rest)) st.y += rest;
         }
         // Tokens in no sequence get L = +infinity: their rows may hold anything.
-        if (ok && half == 0 && tok < tokens && token < a.q_tokens) p.stats[at_stats] = st;
+        if (!lost && half == 0 && tok < tokens && token < a.q_tokens) p.stats[at_stats] = st;
         // ---- epilogue: each half stages its half of the columns ----
         const bool any = n_tiles > 0;
         ok = ok && (!any || bar_wait(&sh.done, 0, stop));
@@ -412,8 +418,8 @@ k_attention_dq(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
                            : a.dq.at(it.q0 + t, hk * group + i - t * group);
             });
         }
-        unsigned rest = __ballot_sync(0xffffffffu, ok && half == 0 && live &&
-                                                       (sh.bad[0][r] | sh.bad[1][r]));
+        unsigned rest =
+            __ballot_sync(0xffffffffu, half == 0 && live && (sh.bad[0][r] | sh.bad[1][r]));
         while (rest) {
             const int from = __ffs(rest) - 1;
             rest &= rest - 1;
@@ -538,14 +544,7 @@ k_attention_dkv(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
             }
             bar_arrive(&sh.stats_full[b]);
         }
-        if (lane == 0 && *stop) {   // the loads in flight must land before the CTA ends
-            int never = 0;
-            if (n_tiles > 0) bar_wait(&sh.resident, 0, &never);
-            for (int m = max(0, na - C::kA); m < na; ++m)
-                bar_wait(&sh.a_full[m % C::kA], (m / C::kA) & 1, &never);
-            for (int m = max(0, nb - C::kB); m < nb; ++m)
-                bar_wait(&sh.b_full[m % C::kB], (m / C::kB) & 1, &never);
-        }
+        if (lane == 0 && n_tiles > 0) loads_landed<C>(sh, na, nb);
     } else if (warp >= 9) {
         // ---- products ----
         if (lane == 0 && n_tiles > 0) {
@@ -611,11 +610,11 @@ k_attention_dkv(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
                     }
                 }
             }
+            // the products must end before their memory is freed, also where the
+            // other warps have given up
+            int never = 0;
             tc_commit(&sh.done);
-            if (!ok) {   // the products in flight must end before their memory is freed
-                int never = 0;
-                bar_wait(&sh.done, 0, &never);
-            }
+            bar_wait(&sh.done, 0, &never);
         }
     } else {
         // ---- P and dS, transposed: thread = half of a key's row ----
@@ -719,8 +718,8 @@ k_attention_dkv(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
                            : (half == 0 ? a.dv : a.dk).at(it.k0 + i, hk);
             });
         }
-        unsigned rest = __ballot_sync(
-            0xffffffffu, ok && half == 0 && live && (sh.bad[0][r] | sh.bad[1][r]));
+        unsigned rest =
+            __ballot_sync(0xffffffffu, half == 0 && live && (sh.bad[0][r] | sh.bad[1][r]));
         while (rest) {
             const int from = __ffs(rest) - 1;
             rest &= rest - 1;

@@ -24,7 +24,8 @@
 //
 // A row whose result is not finite is computed again by its definition
 // (attention_rows.cuh): a product with a zero probability takes up an
-// infinite or NaN value behind the mask, the definition does not.
+// infinite or NaN value behind the mask, the definition does not.  So is a row
+// whose tile did not come to its end (a wait gave up).
 #include <atomic>
 
 #include "attention_rows.cuh"
@@ -153,12 +154,11 @@ k_attention_forward(const __grid_constant__ CUtensorMap mq, const __grid_constan
                 if (NQ == 2 && it.t0 + u / 2 >= end[0]) bar_arrive(&empty[slot]);
                 if (NQ == 2 && it.t0 + u / 2 >= end[1]) bar_arrive(&empty[slot]);
             }
-            if (stop) {   // the loads in flight must land before the CTA ends
-                int never = 0;
-                bar_wait(&q_full, 0, &never);
-                for (int w = max(0, u - C::kUnits); w < u; ++w)
-                    bar_wait(&full[w % C::kUnits], (w / C::kUnits) & 1, &never);
-            }
+            // the loads must land before the CTA ends, also where nobody waits for them
+            int never = 0;
+            bar_wait(&q_full, 0, &never);
+            for (int w = max(0, u - C::kUnits); w < u; ++w)
+                bar_wait(&full[w % C::kUnits], (w / C::kUnits) & 1, &never);
         }
     } else if (warp > NQ * 4 && warp <= NQ * 5) {
         // ---- products: a thread to a query tile, in turns (kAhead) ----
@@ -217,11 +217,11 @@ k_attention_forward(const __grid_constant__ CUtensorMap mq, const __grid_constan
                 }
                 tc_commit(&s_full[t]);
             }
-            if (!ok) {   // the products in flight must end before their memory is freed
-                int never = 0;
-                tc_commit(&drained[t]);
-                bar_wait(&drained[t], 0, &never);
-            }
+            // the products must end before their memory is freed, also where the
+            // softmax has given up
+            int never = 0;
+            tc_commit(&drained[t]);
+            bar_wait(&drained[t], 0, &never);
         }
     } else if (warp < NQ * 4) {
         // ---- softmax: thread = row ----
@@ -329,7 +329,9 @@ k_attention_forward(const __grid_constant__ CUtensorMap mq, const __grid_constan
         // not have, so all of a tile's warps meet below either way
         const bool none = see1 <= see0;
         const float inv = sum > 0.f ? 1.f / sum : 0.f;
-        const float lse = sum > 0.f    ? top * a.scale + __log2f(sum) * kLn2
+        // a row whose waits gave up counts as not finite
+        const float lse = !ok          ? NAN
+                          : sum > 0.f  ? top * a.scale + __log2f(sum) * kLn2
                           : sum == 0.f ? -INFINITY
                                        : NAN;
         if (it.slot >= 0) {
@@ -360,13 +362,10 @@ k_attention_forward(const __grid_constant__ CUtensorMap mq, const __grid_constan
         } else {
             // through the tile's own Q, which no product reads any more
             uint8_t* out = smem + t * C::kUnit;
-            bool again = false;
-            if (ok) {
-                const bool fine = stage_row<HD>(o_at, out, r, 0, inv, any);
-                again = live && !(fine && (none || lse * 0.f == 0.f));
-                if (live && !again) a.lse[(int64_t)token * a.heads + h] = lse;
-            }
-            keep[t][r] = ok && live && !again;
+            const bool fine = ok && stage_row<HD>(o_at, out, r, 0, inv, any);
+            const bool again = live && !(fine && (none || lse * 0.f == 0.f));
+            if (live && !again) a.lse[(int64_t)token * a.heads + h] = lse;
+            keep[t][r] = live && !again;
             fence_async();
             // rows past the tile or the tensor are left out by the store itself
             if (!part_any(1 + t, 128, !ok || again ||
