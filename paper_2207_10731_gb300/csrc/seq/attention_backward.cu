@@ -396,7 +396,8 @@ k_attention_dq(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
         if (!lost && half == 0 && tok < tokens && token < a.q_tokens) p.stats[at_stats] = st;
         // ---- epilogue: each half stages its half of the columns ----
         const bool any = n_tiles > 0;
-        ok = ok && (!any || bar_wait(&sh.done, 0, stop));
+        // (an issuing thread that gave up has announced its end, too)
+        ok = ok && (!any || (bar_wait(&sh.done, 0, stop) && !*stop));
         ok = __all_sync(0xffffffffu, ok) != 0;
         tc_after_sync();
         bool fine = true;
@@ -699,7 +700,8 @@ k_attention_dkv(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
         }
         // ---- epilogue: the first four warps stage dV, the others dK ----
         const bool any = n_tiles > 0;
-        ok = ok && (!any || bar_wait(&sh.done, 0, stop));
+        // (an issuing thread that gave up has announced its end, too)
+        ok = ok && (!any || (bar_wait(&sh.done, 0, stop) && !*stop));
         ok = __all_sync(0xffffffffu, ok) != 0;
         tc_after_sync();
         bool fine = true;
