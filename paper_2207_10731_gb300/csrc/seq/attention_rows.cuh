@@ -46,7 +46,8 @@ static __device__ void forward_row(const Attn& a, int first, int end, int t, int
         const float s = dot4(q, row4(a.k.at(j, hk), a.dim)) * a.scale;
         const float next = fmaxf(top, s);
         const float keep = next == -INFINITY ? 1.f : expf(top - next);
-        const float p = next == -INFINITY ? 0.f : expf(s - next);
+        // no weight for a score of -infinity; a NaN, which fmaxf passes over, goes on
+        const float p = s == -INFINITY ? 0.f : expf(s - next);
         sum = sum * keep + p;
         o.x *= keep;
         o.y *= keep;
