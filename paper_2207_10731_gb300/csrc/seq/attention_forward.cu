@@ -324,6 +324,11 @@ k_attention_forward(const __grid_constant__ CUtensorMap mq, const __grid_constan
             if (row == 0) bar_arrive(&empty[(2 * (stop_at - it.t0) - 1) % C::kUnits]);
             ok = __all_sync(0xffffffffu, ok) != 0;
             tc_after_sync();
+        } else if (most > it.t0) {
+            // the other tile has keys, so this tile's Q is on its way to where the zero
+            // rows are about to be staged
+            ok = bar_wait(&q_full, 0, &stop);
+            ok = __all_sync(0xffffffffu, ok) != 0;
         }
         // ok: whether the waits of this warp ended well; a wait of another warp may
         // not have, so all of a tile's warps meet below either way
