@@ -27,7 +27,7 @@
 //
 // What a row does not see gets S = -infinity, hence P = 0; a row that sees
 // nothing has L = +infinity.  Rows that are not finite, or whose tile did not
-// come to its end, are computed again by the definition, as in the forward pass.
+// come to its end, are computed again (attention_rows.cuh), as in the forward pass.
 #include <atomic>
 
 #include "attention_rows.cuh"
@@ -42,7 +42,7 @@ constexpr float kLog2e = 1.4426950408889634f;
 // A key that every query nearly ignores has a gradient of the size of its P, so
 // the dK, dV kernel takes P and dS times 2^24: what exp2 flushes to zero is then
 // below 2^-150, and the factor is taken off exactly at the end.  (A dO above
-// 2^104 makes that row infinite, and it is computed by its definition.)
+// 2^104 makes that row infinite, and it is computed again without the factor.)
 constexpr float kLift = 24.f, kUnlift = 1.f / 16777216.f;
 // The dQ kernel's second product takes dS as the sum of two bf16 for heads up to
 // 64, where the products wait for the elementwise work anyway, and for heads of
@@ -176,7 +176,8 @@ template <int HD, int TN>
 __global__ void __launch_bounds__(Cfg<HD, TN>::kThreads, Cfg<HD, TN>::kCtas)
 k_attention_dq(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mg,
                const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv,
-               const __grid_constant__ CUtensorMap mdq, Attn a, Plan p) {
+               const __grid_constant__ CUtensorMap mdq, const __grid_constant__ Attn a,
+               const __grid_constant__ Plan p) {
     pdl_prologue();
     using C = Cfg<HD, TN>;
     extern __shared__ __align__(1024) uint8_t smem[];
@@ -419,16 +420,10 @@ k_attention_dq(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
                            : a.dq.at(it.q0 + t, hk * group + i - t * group);
             });
         }
-        unsigned rest =
-            __ballot_sync(0xffffffffu, half == 0 && live && (sh.bad[0][r] | sh.bad[1][r]));
-        while (rest) {
-            const int from = __ffs(rest) - 1;
-            rest &= rest - 1;
-            __syncwarp();
-            dq_row(a, __shfl_sync(0xffffffffu, range.lo, from),
-                   __shfl_sync(0xffffffffu, range.hi, from),
-                   __shfl_sync(0xffffffffu, token, from), __shfl_sync(0xffffffffu, h, from));
-        }
+        // the two warps that hold a row's halves take 16 of their 32 rows each
+        const bool again = live && (sh.bad[0][r] | sh.bad[1][r]);
+        if (__any_sync(0xffffffffu, again))
+            dq_rows<HD>(a, hk, token, h, range.lo, range.hi, again, st, half);
     }
     tc_before_sync();
     __syncthreads();
@@ -442,7 +437,7 @@ __global__ void __launch_bounds__(Cfg<HD, TN>::kThreadsKV, Cfg<HD, TN>::kCtas)
 k_attention_dkv(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mg,
                 const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv,
                 const __grid_constant__ CUtensorMap mdk, const __grid_constant__ CUtensorMap mdv,
-                Attn a, Plan p) {
+                const __grid_constant__ Attn a, const __grid_constant__ Plan p) {
     pdl_prologue();
     using C = Cfg<HD, TN>;
     extern __shared__ __align__(1024) uint8_t smem[];
@@ -715,20 +710,15 @@ k_attention_dkv(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
             if (r == 0) store_tile<HD>(half == 0 ? &mdv : &mdk, tile, hk, it.k0);
         } else {
             store_rows<HD, 32>(tile, (warp & 3) * 32, a.dim, [&](int i) -> bf16* {
-                return sh.bad[0][i] | sh.bad[1][i]
-                           ? nullptr
-                           : (half == 0 ? a.dv : a.dk).at(it.k0 + i, hk);
+                return sh.bad[half][i] ? nullptr : (half == 0 ? a.dv : a.dk).at(it.k0 + i, hk);
             });
         }
-        unsigned rest =
-            __ballot_sync(0xffffffffu, half == 0 && live && (sh.bad[0][r] | sh.bad[1][r]));
-        while (rest) {
-            const int from = __ffs(rest) - 1;
-            rest &= rest - 1;
-            __syncwarp();
-            dkv_row(a, __shfl_sync(0xffffffffu, range.lo, from),
-                    __shfl_sync(0xffffffffu, range.hi, from),
-                    __shfl_sync(0xffffffffu, key, from), hk);
+        const bool again = live && sh.bad[half][r];
+        if (__any_sync(0xffffffffu, again)) {
+            if (half == 0)
+                dkv_rows<HD, false>(a, p.stats, hk, key, range.lo, range.hi, again);
+            else
+                dkv_rows<HD, true>(a, p.stats, hk, key, range.lo, range.hi, again);
         }
     }
     tc_before_sync();

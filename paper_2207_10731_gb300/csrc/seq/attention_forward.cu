@@ -22,10 +22,10 @@
 // of tile j, then S of tile j + 1" makes one barrier say both that S is ready
 // and that O may be touched.
 //
-// A row whose result is not finite is computed again by its definition
-// (attention_rows.cuh): a product with a zero probability takes up an
-// infinite or NaN value behind the mask, the definition does not.  So is a row
-// whose tile did not come to its end (a wait gave up).
+// A row (or a piece of one) whose result is not finite is computed again
+// (attention_rows.cuh): a product with a zero probability takes up an infinite or
+// NaN value behind the mask.  So is a row whose tile did not come to its end (a
+// wait gave up).
 #include <atomic>
 
 #include "attention_rows.cuh"
@@ -58,7 +58,7 @@ template <int HD, int NQ>
 __global__ void __launch_bounds__(Cfg<HD, NQ>::kThreads, NQ == 1 ? 2 : 1)
 k_attention_forward(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk,
                     const __grid_constant__ CUtensorMap mv, const __grid_constant__ CUtensorMap mo,
-                    Attn a, Plan p) {
+                    const __grid_constant__ Attn a, const __grid_constant__ Plan p) {
     pdl_prologue();
     using C = Cfg<HD, NQ>;
     extern __shared__ __align__(1024) uint8_t smem[];
@@ -341,9 +341,11 @@ k_attention_forward(const __grid_constant__ CUtensorMap mq, const __grid_constan
                                        : NAN;
         if (it.slot >= 0) {
             // a piece: fp32, and nothing where it holds none of the row's keys
-            const int64_t at = ((int64_t)it.slot * a.kv_heads + hk) * kTile + r;
-            const bool store = ok && live && lse != -INFINITY;
-            p.partial_lse[at] = lse;
+            const int from = max(see0, it.t0 * kTile), to = min(see1, it.t1 * kTile);
+            const bool some = live && to > from;
+            const int64_t first = ((int64_t)it.slot * a.kv_heads + hk) * kTile + (warp & 3) * 32;
+            float* sums = p.partial + (first + lane) * a.dim;
+            float odd = 0.f;   // NaN where a value is not finite
 #pragma unroll 1
             for (int i = 0; i < HD; i += 32) {
                 float o[32];
@@ -353,17 +355,26 @@ k_attention_forward(const __grid_constant__ CUtensorMap mq, const __grid_constan
                     tmem_wait_load();
                     tmem_loaded(o);
                 }
-                if (store) {
+                if (ok && some) {
 #pragma unroll
                     for (int e = 0; e < 32; e += 8) {
                         if (i + e >= a.dim) break;
                         float v[8];
 #pragma unroll
-                        for (int x = 0; x < 8; ++x) v[x] = o[e + x] * inv;
-                        store8(p.partial + at * a.dim + i + e, v);
+                        for (int x = 0; x < 8; ++x) {
+                            v[x] = o[e + x] * inv;
+                            odd = fmaf(v[x], 0.f, odd);
+                        }
+                        store8(sums + i + e, v);
                     }
                 }
             }
+            const bool again = some && !(ok && odd == 0.f && lse * 0.f == 0.f);
+            if (!again) p.partial_lse[first + lane] = some ? lse : -INFINITY;
+            __syncwarp();
+            if (__any_sync(0xffffffffu, again))
+                forward_rows<HD>(a, hk, token, h, it.k0 + from, it.k0 + to, again,
+                                 p.partial + first * a.dim, p.partial_lse + first);
         } else {
             // through the tile's own Q, which no product reads any more
             uint8_t* out = smem + t * C::kUnit;
@@ -385,16 +396,8 @@ k_attention_forward(const __grid_constant__ CUtensorMap mq, const __grid_constan
                                : nullptr;
                 });
             }
-            unsigned rest = __ballot_sync(0xffffffffu, again);
-            while (rest) {
-                const int from = __ffs(rest) - 1;
-                rest &= rest - 1;
-                __syncwarp();
-                forward_row(a, __shfl_sync(0xffffffffu, range.lo, from),
-                            __shfl_sync(0xffffffffu, range.hi, from),
-                            __shfl_sync(0xffffffffu, token, from),
-                            __shfl_sync(0xffffffffu, h, from));
-            }
+            if (__any_sync(0xffffffffu, again))
+                forward_rows<HD>(a, hk, token, h, range.lo, range.hi, again, nullptr, nullptr);
         }
     } else if (NQ == 2) {
         set_registers<56, false>();   // the warps without a role
@@ -404,6 +407,22 @@ k_attention_forward(const __grid_constant__ CUtensorMap mq, const __grid_constan
     tc_after_sync();
     if (warp == 0) tmem_free(tmem, C::kCols);
     if (threadIdx.x == 0 && stop) report_stop(a.status);
+}
+
+// The values 4l .. 4l+3 of a row are lane l's.
+__device__ __forceinline__ void put4(bf16* p, float4 v, int dim) {
+    const int c = 4 * (threadIdx.x & 31);
+    if (c >= dim) return;
+    uint2 w;
+    w.x = pack2(v.x, v.y, bf16());
+    w.y = pack2(v.z, v.w, bf16());
+    *reinterpret_cast<uint2*>(p + c) = w;
+}
+__device__ __forceinline__ void add4(float4& a, float s, float4 b) {
+    a.x += s * b.x;
+    a.y += s * b.y;
+    a.z += s * b.z;
+    a.w += s * b.w;
 }
 
 // Joins the pieces of the split query tiles:
@@ -477,11 +496,6 @@ __global__ void __launch_bounds__(kThreads) k_attention_join(Attn a, Plan p) {
     for (int m = 16; m > 0; m >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, m);
     const float inv = 1.f / sum, lse = top + __log2f(sum) * kLn2;
     o = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
-    const float odd = (o.x + o.y + o.z + o.w) * 0.f + lse * 0.f;
-    if (__any_sync(0xffffffffu, odd != 0.f)) {
-        forward_row(a, range.lo, range.hi, token, h);
-        return;
-    }
     put4(a.out.at(token, h), o, a.dim);
     if (lane == 0) a.lse[(int64_t)token * a.heads + h] = lse;
 }

@@ -47,7 +47,7 @@ __device__ __forceinline__ uint64_t now_ns() {
 
 // Every wait ends: after kWaitNs, or as soon as another wait of the CTA has
 // given up (*stop, in shared memory).  The caller then leaves its loop, the CTA
-// lets its loads and products end, computes its rows by their definition, frees
+// lets its loads and products end, computes its rows another way, frees
 // its tensor memory and reports through the call's status word.
 constexpr uint64_t kWaitNs = 2000000000ull;
 __device__ __forceinline__ bool bar_wait_slow(uint64_t* b, uint32_t parity,
