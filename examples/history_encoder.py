@@ -101,18 +101,22 @@ class HistoryEncoder:
 
     def serve(self, ids, offsets):
         """Logits of each history's newest item: one query per user over the
-        keys and values of the whole history."""
+        keys and values of the whole history.  NaN for an empty history, which
+        has no newest item."""
+        some = offsets.diff() > 0
+        if ids.numel() == 0:
+            return torch.full(some.shape, float("nan"), device="cuda")
         h = self.embed(ids, offsets)
         y, _, _ = sequence.layer_norm_forward(h, self.w["norm"], self.w["norm_bias"],
                                               out_dtype=torch.bfloat16)
-        newest = offsets[1:] - 1
+        newest = (offsets[1:] - 1).clamp_(min=0)   # an empty history's is another's: not used
         q, k, v = self._split(y @ self.w["qkv"].bfloat16())
         steps = torch.arange(newest.numel() + 1, device="cuda")
         out, _ = sequence.attention_forward(q[newest], k, v, steps, offsets)
         o = out.reshape(newest.numel(), -1) @ self.w["out"].bfloat16()
         h2 = o.float() + h[newest]
         z, _, _ = sequence.layer_norm_forward(h2, self.w["last"], self.w["last_bias"])
-        return z @ self.w["head"]
+        return torch.where(some, z @ self.w["head"], float("nan"))
 
 
 def histories(seed, users=256, items=1000, longest=64):

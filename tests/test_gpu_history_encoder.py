@@ -67,3 +67,31 @@ def test_a_step_takes_the_formulas_gradient():
         grad, want = m / 0.1, w[name].grad
         # bf16 operands: 2^-8 of each of a handful of factors
         assert (grad - want).norm() <= 0.03 * want.norm(), name
+
+
+def test_an_empty_history_is_served_as_one():
+    ex = example()
+    model = ex.HistoryEncoder(seed=7)
+    ids, offsets, _ = ex.histories(9, users=20, longest=30)
+    want = model.serve(ids, offsets)
+    # users without items first, between, last and in a row
+    at = [0, 0, 5, 5, 11, 20]
+    ends = offsets.tolist()
+    with_empty, full = [0], []
+    for user in range(20):
+        for _ in range(at.count(user)):
+            with_empty.append(ends[user])
+            full.append(False)
+        with_empty.append(ends[user + 1])
+        full.append(True)
+    with_empty.append(ends[-1])
+    full.append(False)
+    full = torch.tensor(full, device="cuda")
+    got = model.serve(ids, torch.tensor(with_empty, device="cuda"))
+    # nobody else's item answers for a user who has none
+    assert got[~full].isnan().all()
+    # the same rows through the same products, but other tiles and row counts
+    assert (got[full] - want).abs().max() <= 0.05 * want.abs().max()
+    # nobody has any
+    none = torch.zeros(4, dtype=torch.int64, device="cuda")
+    assert model.serve(ids[:0], none).isnan().all() and model.serve(ids[:0], none).shape == (3,)
