@@ -405,6 +405,9 @@ k_attention_dq(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
         if (ok)
             fine = stage_row<HD / 2>(dq_at + half * (HD / 2) + lanes, smem, r, half * (HD / 16),
                                      a.scale, any);
+        // rows that hold no token (128 is not a multiple of the group) come from what shared
+        // memory held before
+        fine = fine || tok >= tokens;
         // a row that is not to be stored now: dead, or to be computed again
         sh.bad[half][r] = !ok || !live || !fine;
         fence_async();

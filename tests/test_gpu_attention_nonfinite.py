@@ -201,3 +201,19 @@ def test_what_is_not_finite_does_not_hold_the_gpu(where, dim):
     odd = time()
     print(f"\ndim {dim}, {where}: clean {clean:.3f} ms, not finite {odd:.3f} ms")
     assert odd < 50 * clean
+
+
+@pytest.mark.parametrize("group,dim", [(3, 64), (5, 128), (12, 128), (65, 40)])
+def test_what_shared_memory_held_before_does_not_matter(group, dim):
+    # tiles whose 128 rows the group does not divide: the rows over hold what the CTA
+    # before left, here NaN
+    n = [300, 20, 150]
+    x = inputs(n, n, 2 * group, 2, dim, seed=295)
+    want = run(*x, n, n, True, status=False)
+    odd = [torch.full_like(y, float("nan")) for y in inputs([4096], [4096], 2 * 4, 2, dim)]
+    off = offsets([4096])
+    for _ in range(3):
+        out, lse = sequence.attention_forward(*odd[:3], off)
+        sequence.attention_backward(odd[3], *odd[:3], out, lse, off)
+        got = run(*x, n, n, True, status=False)
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
