@@ -441,7 +441,9 @@ pss_status pss_layer_norm_backward(const void* grad, pss_dtype grad_type, int64_
  * first); e is kept when value e % 8 >= t, t = p * 65536 rounded to nearest
  * even, and p' = t / 65536.  The mask depends on seed, offset and the logical
  * position only, so the backward pass is the same call on the gradient,
- * without the residual.  Calls with different offsets are independent.
+ * without the residual.  Calls with different offsets are independent.  seed and
+ * offset are values of the call: a captured graph repeats its mask at every
+ * replay, so a training step that is captured once needs its dropout outside.
  * 16 bits a value: one generator call serves eight elements (with 32 bits a
  * value the 16-bit types would be bound by the generator, not by memory).
  *   p in [0, 1]; p' = 0 keeps everything, p' = 1 gives zeros (a dropped element
@@ -495,13 +497,14 @@ typedef struct {
  *   pss_attention_workspace(shape, 0) bytes (the work list, and partial sums
  *   where few queries meet long sequences); means nothing between calls.
  *   status: NULL or device int64[1], set to -1, to the smallest sequence with
- *   malformed offsets (the rows of that sequence and of later ones are then
- *   undefined, or left unwritten; nothing outside the tensors is touched), or
+ *   malformed offsets (any row may then be undefined or left unwritten, since rows
+ *   find their sequence by bisection; nothing outside the tensors is touched), or
  *   to -2 when a wait inside a kernel gave up after 2 s (its tile's rows were
  *   then computed another way).
  * Rows outside every sequence are left unwritten.  Equal inputs give equal
- * bits.  A masked key or value changes nothing, also where it is infinite or
- * NaN, and neither does another sequence's.  (Rows that come out infinite or NaN are
+ * bits.  A masked key or value reaches no result, also where it is infinite or
+ * NaN, and neither does another sequence's: the rows that do not see it are as
+ * near to the definition as always, if not equal to the last bit.  (Rows that come out infinite or NaN are
  * computed a second time, without the tiles: a call on nothing but NaN takes about
  * twice its time, the dearest known, values that are all NaN under finite scores, 17
  * times.)
@@ -520,7 +523,9 @@ pss_status pss_attention_forward(const pss_attention_shape* shape, const pss_row
  *   dq = scale sum_j ds k_j,  dk = scale sum_i ds q_i,  dv = sum_i p grad_i
  * (dk and dv also summed over the heads that share them), overwritten.  p and
  * ds enter their second products as bf16; sums are fp32, in a fixed order.
- * dq, dk, dv may be views of one buffer, and may not overlap the inputs.
+ * dq, dk, dv may be views of one buffer, and may not overlap the inputs.  Rows
+ * outside every sequence are left unwritten; what the inputs hold there does not
+ * matter.
  * workspace: at least pss_attention_workspace(shape, 1) bytes.
  */
 pss_status pss_attention_backward(const pss_attention_shape* shape, const pss_rows* grad,

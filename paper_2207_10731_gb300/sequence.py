@@ -161,7 +161,8 @@ def dropout(x, p: float, seed: int, offset: int = 0, residual=None, out=None, st
     1 - p, plus ``residual`` (pss_dropout).  The mask follows from (seed,
     offset, position) alone and is not stored: the backward pass is the same
     call on the gradient, without the residual.  seed and offset are unsigned
-    64-bit; give each call of a step an offset of its own."""
+    64-bit; give each call of a step an offset of its own.  Both are values of
+    the call: a captured CUDA graph repeats its mask at every replay."""
     if stream is not None:
         return _under(stream, dropout, x, p, seed, offset, residual, out)
     device = _device()
@@ -269,7 +270,9 @@ def attention_forward(q, k, v, q_offsets, kv_offsets=None, causal: bool = True, 
     stand at the end of their sequence: one query per sequence is the serving
     step.  scale defaults to dim ** -0.5.  lse is float32 [query tokens,
     heads].  ``status`` (int64, one value on the device) receives -1, the first
-    sequence with malformed offsets, or -2 if a device wait gave up."""
+    sequence with malformed offsets (no result is defined then), or -2 if a
+    device wait gave up.  Rows outside every sequence are left as they are, in
+    results made here whatever the memory held."""
     if stream is not None:
         return _under(stream, attention_forward, q, k, v, q_offsets, kv_offsets, causal, scale, out,
                       status)
@@ -298,7 +301,8 @@ def attention_backward(grad, q, k, v, out, lse, q_offsets, kv_offsets=None, caus
     """(dq, dk, dv) for the upstream gradient ``grad`` of the out of
     ``attention_forward`` (pss_attention_backward); out and lse are that
     call's.  The gradients go to the three tensors ``grads`` if given (e.g.
-    views of one buffer for a fused projection)."""
+    views of one buffer for a fused projection).  Rows outside every sequence
+    are left as they are, as in the forward call."""
     if stream is not None:
         return _under(stream, attention_backward, grad, q, k, v, out, lse, q_offsets, kv_offsets,
                       causal, scale, grads, status)
