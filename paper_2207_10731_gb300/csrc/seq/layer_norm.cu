@@ -11,7 +11,7 @@
 // two reductions and written once.  A row is shared by `lanes` threads: a
 // power of two up to 32 (several rows to a warp for the embedding's short
 // rows, all within shuffles), or a whole CTA for rows above one warp's
-// registers (two barriers a reduction, hidden by the SM's other CTAs).  The
+// registers (a barrier a reduction, hidden by the SM's other CTAs).  The
 // variance is taken from the differences in registers: the textbook
 // sum(x^2) - mean^2 would cancel for rows far from zero.
 //
@@ -122,8 +122,11 @@ struct Part<T, 1, CH> {
     __device__ __forceinline__ void get(int c, float (&to)[1]) const { to[0] = v[c]; }
 };
 
-// Weight and bias stay in registers where these reach: not with 1024 threads,
-// which have 64 each.
+// Weight and bias stay in registers, and the next row's loads ahead, where the
+// instantiation's threads are at most 256: the one with the largest CH is bounded at
+// 1024 threads, 64 registers each, and so does without also for rows of 257 columns
+// and more that take fewer threads (262144 x 512 bf16: 258 us, 31 % of the copy
+// bandwidth, where 262144 x 256 takes 65).
 template <typename TX, typename TY, int VEC, int CH, int MODE>
 __global__ void __launch_bounds__(max_threads<VEC, CH>(1024))
 k_layer_norm_forward(const TX* x, int64_t xs, const float* __restrict__ weight,
