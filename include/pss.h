@@ -501,6 +501,7 @@ typedef struct {
  *   find their sequence by bisection; nothing outside the tensors is touched), or
  *   to -2 when a wait inside a kernel gave up after 2 s (its tile's rows were
  *   then computed another way).
+ * out may not overlap the inputs.
  * Rows outside every sequence are left unwritten.  Equal inputs give equal
  * bits.  A masked key or value reaches no result, also where it is infinite or
  * NaN, and neither does another sequence's: the rows that do not see it are as

@@ -52,6 +52,9 @@ struct Cfg {
     // NQ = 2: three whole warpgroups, so that the two of the softmax can take
     // registers from the third (set_registers)
     static constexpr int kThreads = NQ == 2 ? 384 : 192;
+    // registers a thread that the launch has to bring for the split
+    static constexpr int kMore = 224, kLess = 56;
+    static constexpr int kLaunch = NQ == 2 ? (2 * kMore + kLess) / 3 : 0;
 };
 
 template <int HD, int NQ>
@@ -130,10 +133,10 @@ k_attention_forward(const __grid_constant__ CUtensorMap mq, const __grid_constan
     tc_after_sync();
     const uint32_t tmem = tmem_at;
 
-    // NQ = 2: 3 x 168 registers a thread at launch = 2 x 224 + 56
+    // NQ = 2: 3 x 168 registers a thread at launch = 2 x 224 + 56 (kLaunch)
     if (warp == NQ * 4) {
         // ---- loads: Q, then K and V tiles in turn ----
-        if (NQ == 2) set_registers<56, false>();
+        if (NQ == 2) set_registers<C::kLess, false>();
         if (lane == 0 && most > it.t0) {
             const uint32_t box = (uint32_t)(tokens * group) * 128;
             bar_expect(&q_full, NQ * C::kHalves * box);
@@ -162,7 +165,7 @@ k_attention_forward(const __grid_constant__ CUtensorMap mq, const __grid_constan
         }
     } else if (warp > NQ * 4 && warp <= NQ * 5) {
         // ---- products: a thread to a query tile, in turns (kAhead) ----
-        if (NQ == 2) set_registers<56, false>();
+        if (NQ == 2) set_registers<C::kLess, false>();
         const int t = warp - NQ * 4 - 1;
         const int steps = (t == 0 ? end[0] : end[NQ - 1]) - it.t0;
         const int others = NQ == 1 ? 0 : (t == 0 ? end[NQ - 1] : end[0]) - it.t0;
@@ -225,7 +228,7 @@ k_attention_forward(const __grid_constant__ CUtensorMap mq, const __grid_constan
         }
     } else if (warp < NQ * 4) {
         // ---- softmax: thread = row ----
-        if (NQ == 2) set_registers<224, true>();
+        if (NQ == 2) set_registers<C::kMore, true>();
         const int t = tile, r = row, h = row_h;
         // the keys that the row sees, counted from k0: see0 .. see1
         const bool live = range.live();
@@ -400,7 +403,7 @@ k_attention_forward(const __grid_constant__ CUtensorMap mq, const __grid_constan
                 forward_rows<HD>(a, hk, token, h, range.lo, range.hi, again, nullptr, nullptr);
         }
     } else if (NQ == 2) {
-        set_registers<56, false>();   // the warps without a role
+        set_registers<C::kLess, false>();   // the warps without a role
     }
     tc_before_sync();
     __syncthreads();
@@ -513,7 +516,7 @@ cudaError_t launch(const Attn& a, const Plan& p, cudaStream_t st) {
     if (e != cudaSuccess) return e;
     auto* k = k_attention_forward<HD, NQ>;
     static std::atomic<uint64_t> ready{0};
-    e = allow_smem(k, C::kSmem, &ready);
+    e = allow_smem(k, C::kSmem, &ready, C::kLaunch);
     if (e != cudaSuccess) return e;
     return launch_k(k, dim3((unsigned)p.most_items * a.kv_heads), dim3(C::kThreads), C::kSmem, st,
                     mq, mk, mv, mo, a, p);

@@ -15,14 +15,23 @@ namespace seq {
 cudaError_t tile_map(CUtensorMap* map, const Rows& r, int tokens, int heads, int dim,
                      int heads_box, int tokens_box, const void* spare);
 
-// Raises a kernel's dynamic shared-memory limit, once per device.
+// Raises a kernel's dynamic shared-memory limit, once per device.  least_registers:
+// what a kernel that splits its registers among its warpgroups was counted with; built
+// with fewer a thread it would wait for them for ever, so it is not launched then.
 template <typename K>
-cudaError_t allow_smem(K* kernel, int bytes, std::atomic<uint64_t>* ready) {
+cudaError_t allow_smem(K* kernel, int bytes, std::atomic<uint64_t>* ready,
+                       int least_registers = 0) {
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
     const uint64_t bit = 1ull << (dev & 63);
     if (ready->load(std::memory_order_acquire) & bit) return cudaSuccess;
+    if (least_registers > 0) {
+        cudaFuncAttributes built;
+        e = cudaFuncGetAttributes(&built, kernel);
+        if (e != cudaSuccess) return e;
+        if (built.numRegs < least_registers) return cudaErrorInvalidConfiguration;
+    }
     e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (e == cudaSuccess) ready->fetch_or(bit, std::memory_order_release);
     return e;

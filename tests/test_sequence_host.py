@@ -94,3 +94,17 @@ def test_refusals_before_any_device_work(lib):
     assert rc == bad and size > 0             # host memory
     assert lib.pss_attention_forward(*[None] * 7, 0, None, None) == bad
     assert lib.pss_attention_backward(*[None] * 11, 0, None, None) == bad
+
+
+def test_a_register_split_is_checked_before_its_kernel_is_launched():
+    # a warpgroup that asks for more registers than the launch brought waits for ever
+    kernels = {f: open(os.path.join(SEQ, f)).read() for f in os.listdir(SEQ)}
+    users = {f for f, src in kernels.items() if "set_registers<C::" in src}
+    assert users == {"attention_forward.cu"}
+    src = kernels["attention_forward.cu"]
+    assert not re.search(r"set_registers<\d", src)
+    more, less = map(int, re.search(r"kMore = (\d+), kLess = (\d+)", src).groups())
+    # the launch's registers are a whole number a thread, and at most what 384 threads can have
+    assert (2 * more + less) % 3 == 0 and (2 * more + less) // 3 <= 65536 // 384 // 8 * 8
+    assert "allow_smem(k, C::kSmem, &ready, C::kLaunch)" in src
+    assert "built.numRegs < least_registers" in kernels["attention_tma.h"]
