@@ -36,8 +36,8 @@ def listed():
          "dense": "out", "gap": 0},
         # gradients of the product that reads the concatenated row of all 26 tables: few outputs, a long sum over tokens
         {"name": "linear backward concatenated", "op": "linear", "direction": "backward", "tokens": 65536,
-         "in": 26 * 128, "out": 512, "type": "bf16", "activation": "relu", "bias": True, "residual": False, "keep": False,
-         "dense": "in", "gap": 0},
+         "in": 26 * 128, "out": 512, "type": "bf16", "activation": "relu", "bias": True, "residual": False,
+         "keep": False, "dense": "in", "gap": 0},
         # the newest items of eight users between two blocks: latency counts
         {"name": "norm serving rows", "op": "norm", "direction": "forward", "rows": 8, "cols": 1024, "type": "bf16",
          "stream": "bf16", "post": True, "pre": True, "gate": "none", "scale": 1.0, "gap": 0},
