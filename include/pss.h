@@ -535,6 +535,85 @@ pss_status pss_attention_backward(const pss_attention_shape* shape, const pss_ro
                                   const pss_rows* dk, const pss_rows* dv, void* workspace,
                                   int64_t workspace_bytes, int64_t* status, pss_stream stream);
 
+/*
+ * Rows of a dense table [rows][cols] by id, scaled (for what is not hashed: positions,
+ * small tables, vocabularies):
+ *   out[t] = scale * weight[ids[t]],   rounded once to out_type.
+ * An id outside 0 .. rows - 1 (say -1, for padding) gives a zero row and no gradient.
+ *   ids: int64[tokens].  weight_stride, out_stride: elements between rows (>= cols).
+ *   status: NULL or device int64[1], set to the smallest position whose id is
+ *   outside the table, or -1.
+ * tokens, rows below 2^31 - 1024; cols up to 2^20 (PSS_ERR_UNSUPPORTED above); scale
+ * finite.  out may not overlap the weight.
+ */
+pss_status pss_embedding_forward(const void* weight, pss_dtype weight_type, int64_t weight_stride,
+                                 int64_t rows, int64_t cols, const int64_t* ids, int64_t tokens,
+                                 float scale, void* out, pss_dtype out_type, int64_t out_stride,
+                                 int64_t* status, pss_stream stream);
+
+/*
+ * Its gradient, overwriting all of dweight[rows][cols]:
+ *   dweight[v] = scale * sum over t with ids[t] = v of grad[t]    (zeros where there is none).
+ * Sums are fp32, in an order that follows from the ids alone (positions sorted by id):
+ * equal inputs give equal bits; rounded once to dweight_type.
+ *   workspace: device, 16-byte aligned, at least pss_embedding_workspace(tokens, rows,
+ *   cols) bytes; means nothing between calls.
+ * dweight may not overlap grad.
+ */
+int64_t pss_embedding_workspace(int64_t tokens, int64_t rows, int64_t cols);
+pss_status pss_embedding_backward(const void* grad, pss_dtype grad_type, int64_t grad_stride,
+                                  const int64_t* ids, int64_t tokens, float scale, int64_t rows,
+                                  int64_t cols, void* dweight, pss_dtype dweight_type,
+                                  int64_t dweight_stride, void* workspace,
+                                  int64_t workspace_bytes, int64_t* status, pss_stream stream);
+
+/*
+ * What lies between two blocks of an encoder, in one pass: root-mean-square norm of a
+ * block's output x, gated and scaled onto the residual stream, and the norm that the
+ * next block reads.  For rows of `cols` values and r(v) = 1 / sqrt(sum_c v^2 / cols + eps):
+ *   u = x r(x) post_weight                     (u = x where post_weight is NULL),
+ *   total = residual + scale * sigmoid(gate) * u          (gates = 0: without the gate),
+ *   y = total r(total) pre_weight              (no y where pre_weight is NULL).
+ *   x, gate, y: `type`; residual, total: stream_type, which is `type` or PSS_F32.
+ *   gate: logits; gates = 1: one to a row (gate_stride elements apart), 2: one to a value.
+ *   post_weight, pre_weight: fp32[cols].  post_rstd = r(x), pre_rstd = r(total): fp32[rows],
+ *   for the backward pass (unused without the norm).
+ * Sums are fp32; total and y are each rounded once (y is the norm of the unrounded total).
+ * total may be residual and y may be x where the strides are equal; other overlaps are
+ * undefined.  cols: 1 .. 16384 (PSS_ERR_UNSUPPORTED above); eps >= 0; scale finite.
+ */
+pss_status pss_residual_norm_forward(const void* x, pss_dtype type, int64_t x_stride,
+                                     const void* residual, pss_dtype stream_type,
+                                     int64_t residual_stride, const void* gate, int32_t gates,
+                                     int64_t gate_stride, const float* post_weight,
+                                     const float* pre_weight, int64_t rows, int64_t cols,
+                                     float scale, float eps, void* total, int64_t total_stride,
+                                     void* y, int64_t y_stride, float* post_rstd, float* pre_rstd,
+                                     pss_stream stream);
+
+/*
+ * Its backward pass, for the gradients of total (NULL: zero) and y, from x, total, gate and
+ * both rstd of the forward call: with that = total r(total), xhat = x r(x), s = sigmoid(gate),
+ *   g = grad_y pre_weight,   d = grad_total + r(total) (g - that sum_c(g that) / cols),
+ *   dresidual = d,           dgate = scale d u s (1 - s)  (gates = 1: summed over the row),
+ *   e = scale d s,  h = e post_weight,  dx = r(x) (h - xhat sum_c(h xhat) / cols),
+ *   dpre_weight = sum over rows of grad_y that,  dpost_weight = sum over rows of e xhat.
+ * Tensors of a norm or gate that is not there are not touched; nor is x without the first
+ * norm and the gate.  dresidual may be grad_total, dx may be x or grad_y and dgate may be gate, where
+ * the strides are equal.  The weights' sums run in a fixed order.
+ *   workspace: device, 16-byte aligned, at least pss_residual_norm_workspace(rows, cols) bytes.
+ */
+int64_t pss_residual_norm_workspace(int64_t rows, int64_t cols);
+pss_status pss_residual_norm_backward(
+    const void* grad_total, int64_t grad_total_stride, const void* grad_y, int64_t grad_y_stride,
+    const void* x, pss_dtype type, int64_t x_stride, const void* total, pss_dtype stream_type,
+    int64_t total_stride, const void* gate, int32_t gates, int64_t gate_stride,
+    const float* post_weight, const float* pre_weight, const float* post_rstd,
+    const float* pre_rstd, int64_t rows, int64_t cols, float scale, void* dx, int64_t dx_stride,
+    void* dresidual, int64_t dresidual_stride, void* dgate, int64_t dgate_stride,
+    float* dpost_weight, float* dpre_weight, void* workspace, int64_t workspace_bytes,
+    pss_stream stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -43,7 +43,9 @@ EXPORTS = [
     "pss_get_profile", "pss_reset_profile", "pss_status_string", "pss_grad_noalloc",
     "pss_check_convert", "pss_probe_l2", "pss_layer_norm_forward", "pss_layer_norm_workspace",
     "pss_layer_norm_backward", "pss_dropout", "pss_attention_workspace", "pss_attention_forward",
-    "pss_attention_backward",
+    "pss_attention_backward", "pss_embedding_forward", "pss_embedding_workspace",
+    "pss_embedding_backward", "pss_residual_norm_forward", "pss_residual_norm_workspace",
+    "pss_residual_norm_backward",
 ]
 
 
@@ -110,6 +112,14 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
             "pss_dropout": [vp, i64, vp, i64, i64, i64, f64, u64, u64, i32, vp, i64, vp],
             "pss_attention_forward": [vp] * 7 + [i64, vp, vp],
             "pss_attention_backward": [vp] * 11 + [i64, vp, vp],
+            "pss_embedding_forward": [vp, i32, i64, i64, i64, vp, i64, f32, vp, i32, i64, vp, vp],
+            "pss_embedding_backward": [vp, i32, i64, vp, i64, f32, i64, i64, vp, i32, i64, vp, i64,
+                                       vp, vp],
+            "pss_residual_norm_forward": [vp, i32, i64, vp, i32, i64, vp, i32, i64, vp, vp, i64,
+                                          i64, f32, f32, vp, i64, vp, i64, vp, vp, vp],
+            "pss_residual_norm_backward": [vp, i64, vp, i64, vp, i32, i64, vp, i32, i64, vp, i32,
+                                           i64, vp, vp, vp, vp, i64, i64, f32, vp, i64, vp, i64,
+                                           vp, i64, vp, vp, vp, i64, vp],
         }
         for name, args in sigs.items():
             fn = getattr(lib, name)
@@ -117,6 +127,10 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
             fn.restype = ctypes.c_int
         lib.pss_layer_norm_workspace.argtypes = [i64, i64]
         lib.pss_layer_norm_workspace.restype = i64
+        lib.pss_embedding_workspace.argtypes = [i64, i64, i64]
+        lib.pss_embedding_workspace.restype = i64
+        lib.pss_residual_norm_workspace.argtypes = [i64, i64]
+        lib.pss_residual_norm_workspace.restype = i64
         lib.pss_attention_workspace.argtypes = [vp, i32]
         lib.pss_attention_workspace.restype = i64
         lib.pss_status_string.argtypes = [ctypes.c_int]

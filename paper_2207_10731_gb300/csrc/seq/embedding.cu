@@ -1,0 +1,540 @@
+// Rows of a dense table by id, and their gradient (pss_embedding_* of pss.h).
+//
+// Forward:  out[t] = scale * weight[ids[t]].
+// Backward: dweight[v] = scale * sum over t with ids[t] = v of grad[t].
+//
+// Both are bound by memory.  Backward, the token positions are sorted by id, stable
+// (one CTA's bitonic sort up to kSmall tokens, else the radix sort of the shared
+// array's backward), so that each row of the table is summed by one group of threads
+// in the order of the tokens and stored once, rows without a token as zeros: no
+// atomics, and equal inputs give equal bits.  A popular id's run would be one group's
+// long chain: runs are cut at multiples of kChunk sorted places, the pieces that lie
+// wholly in a run are summed beforehand side by side, kChunk of these again, and the
+// row's group adds head, pieces and tail.
+#include <cmath>
+
+#include "seq_common.cuh"
+
+using namespace pss;
+using namespace pss::seq;
+
+namespace {
+
+constexpr int kPer = 8;          // values of a row that a thread holds
+constexpr int kChunk = 64;       // sorted places of a piece, and pieces of a large piece
+constexpr int kLarge = kChunk * kChunk;
+constexpr int kSmall = 4096;     // tokens that one CTA sorts
+constexpr int kSortThreads = 1024;
+constexpr uint32_t kNone = 0xffffffffu;
+
+// How a row is spread: `lanes` threads (a power of two up to 32) to a block of 8 * lanes
+// values, `blocks` blocks to a row.
+struct Spread {
+    int log2_lanes, blocks, cols;
+};
+
+// The 8 values that a thread holds of block b: consecutive ones (VECTOR: rows start at
+// multiples of 8 elements), else every lanes'th.
+template <bool VECTOR>
+struct Piece {
+    int at, step, cols;
+    __device__ __forceinline__ Piece(const Spread& s, int block) {
+        const int lanes = 1 << s.log2_lanes, lane = threadIdx.x & (lanes - 1);
+        cols = s.cols;
+        step = VECTOR ? 1 : lanes;
+        at = block * kPer * lanes + (VECTOR ? kPer * lane : lane);
+    }
+    __device__ __forceinline__ bool any() const { return at < cols; }
+    template <typename T>
+    __device__ __forceinline__ Raw8<T> load(const T* row) const {
+        if constexpr (VECTOR) {
+            return load_raw(row + at);
+        } else {
+            Raw8<T> r;
+#pragma unroll
+            for (int i = 0; i < kPer; ++i)
+                set_raw(r, i, at + i * step < cols ? row[at + i * step] : round_to<T>(0.f));
+            return r;
+        }
+    }
+    template <typename T>
+    __device__ __forceinline__ void store(T* row, const float (&v)[kPer]) const {
+        if constexpr (VECTOR) {
+            store8(row + at, v);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kPer; ++i)
+                if (at + i * step < cols) row[at + i * step] = round_to<T>(v[i]);
+        }
+    }
+};
+
+// A group's number and the block of its row's values.
+__device__ __forceinline__ int64_t group_of(const Spread& s, int* block) {
+    const int64_t g = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) >> s.log2_lanes;
+    if (s.blocks == 1) {
+        *block = 0;
+        return g;
+    }
+    const int64_t of = g / s.blocks;
+    *block = (int)(g - of * s.blocks);
+    return of;
+}
+
+__device__ __forceinline__ void note_outside(unsigned long long* status, int64_t t) {
+    if (status) atomicMin(status, (unsigned long long)t);
+}
+
+// U tokens to a group, all their loads in flight.
+template <typename TW, typename TO, bool VECTOR, int U>
+__global__ void __launch_bounds__(kThreads)
+k_embedding_forward(const TW* __restrict__ weight, int64_t ws, int64_t rows,
+                    const int64_t* __restrict__ ids, int64_t tokens, float scale, TO* out,
+                    int64_t os, unsigned long long* status, Spread s) {
+    pdl_prologue();
+    int block;
+    const int64_t t0 = group_of(s, &block) * U;
+    const Piece<VECTOR> piece(s, block);
+    if (!piece.any() || t0 >= tokens) return;
+    int64_t id[U];
+    Raw8<TW> raw[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) id[u] = t0 + u < tokens ? ids[t0 + u] : -1;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const bool in = (uint64_t)id[u] < (uint64_t)rows;
+        raw[u] = in ? piece.load(weight + id[u] * ws) : Raw8<TW>{};
+        if (!in && piece.at == 0 && t0 + u < tokens) note_outside(status, t0 + u);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        if (t0 + u >= tokens) break;
+        float v[kPer];
+        unpack(raw[u], v);
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) v[i] *= scale;
+        piece.store(out + (t0 + u) * os, v);
+    }
+}
+
+// ---- sorting -----------------------------------------------------------------
+
+// The radix sort's input: each token's id (kNone: outside the table) and place.
+__global__ void __launch_bounds__(kThreads)
+k_embedding_keys(const int64_t* __restrict__ ids, int64_t tokens, int64_t rows, uint32_t* keys,
+                 uint32_t* places, uint32_t* done, unsigned long long* status) {
+    pdl_prologue();
+    const int64_t t = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    if (t == 0) *done = 0u;
+    if (t >= tokens) return;
+    const int64_t id = ids[t];
+    const bool in = (uint64_t)id < (uint64_t)rows;
+    if (!in) note_outside(status, t);
+    keys[t] = in ? (uint32_t)id : kNone;
+    places[t] = (uint32_t)t;
+}
+
+// Up to kSmall tokens in one CTA's shared memory: id << 32 | place, all different, so
+// that any sort of them is stable.
+__global__ void __launch_bounds__(kSortThreads)
+k_embedding_sort(const int64_t* __restrict__ ids, int tokens, int size, int64_t rows,
+                 unsigned long long* __restrict__ sorted, unsigned long long* __restrict__ count,
+                 unsigned long long* status) {
+    pdl_prologue();
+    __shared__ unsigned long long e[kSmall];
+    __shared__ int valid;
+    if (threadIdx.x == 0) valid = 0;
+    __syncthreads();
+    int mine = 0;
+    for (int t = threadIdx.x; t < size; t += kSortThreads) {
+        unsigned long long v = ~0ull;
+        if (t < tokens) {
+            const int64_t id = ids[t];
+            if ((uint64_t)id < (uint64_t)rows) {
+                v = ((unsigned long long)id << 32) | (unsigned)t;
+                ++mine;
+            } else {
+                note_outside(status, t);
+            }
+        }
+        e[t] = v;
+    }
+    if (mine) atomicAdd(&valid, mine);
+    __syncthreads();
+    for (int k = 2; k <= size; k *= 2)
+        for (int j = k / 2; j > 0; j /= 2) {
+            for (int i = threadIdx.x; i < size / 2; i += kSortThreads) {
+                const int a = 2 * i - (i & (j - 1)), b = a + j;
+                const unsigned long long x = e[a], y = e[b];
+                if ((x > y) == ((a & k) == 0)) {
+                    e[a] = y;
+                    e[b] = x;
+                }
+            }
+            __syncthreads();
+        }
+    for (int t = threadIdx.x; t < valid; t += kSortThreads) sorted[t] = e[t];
+    if (threadIdx.x == 0) *count = (unsigned long long)valid;
+}
+
+// ---- sums --------------------------------------------------------------------
+
+__device__ __forceinline__ uint32_t key_of(unsigned long long e) { return (uint32_t)(e >> 32); }
+
+__device__ __forceinline__ void add_to(float (&sum)[kPer], const float (&v)[kPer]) {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) sum[i] += v[i];
+}
+
+// A group to a piece of kChunk sorted places that belong to one id: its sum in fp32.
+// Other pieces are left alone (and never read).
+template <typename TG, bool VECTOR>
+__global__ void __launch_bounds__(kThreads)
+k_embedding_pieces(const TG* __restrict__ grad, int64_t gs,
+                   const unsigned long long* __restrict__ sorted,
+                   const unsigned long long* __restrict__ count, float* __restrict__ sums,
+                   int64_t sums_stride, Spread s) {
+    pdl_prologue();
+    int block;
+    const int64_t c = group_of(s, &block), i0 = c * kChunk;
+    const Piece<VECTOR> piece(s, block);
+    if (!piece.any() || i0 + kChunk > (int64_t)*count ||
+        key_of(sorted[i0]) != key_of(sorted[i0 + kChunk - 1]))
+        return;
+    constexpr int U = 8;
+    float sum[kPer] = {};
+    for (int i = 0; i < kChunk; i += U) {
+        Raw8<TG> raw[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) raw[u] = piece.load(grad + (uint32_t)sorted[i0 + i + u] * gs);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            float v[kPer];
+            unpack(raw[u], v);
+            add_to(sum, v);
+        }
+    }
+    piece.store(sums + c * sums_stride, sum);
+}
+
+// kChunk pieces of one id again.
+template <bool VECTOR>
+__global__ void __launch_bounds__(kThreads)
+k_embedding_large_pieces(const float* __restrict__ sums, int64_t sums_stride,
+                         const unsigned long long* __restrict__ sorted,
+                         const unsigned long long* __restrict__ count, float* __restrict__ large,
+                         Spread s) {
+    pdl_prologue();
+    int block;
+    const int64_t c = group_of(s, &block), i0 = c * kLarge;
+    const Piece<VECTOR> piece(s, block);
+    if (!piece.any() || i0 + kLarge > (int64_t)*count ||
+        key_of(sorted[i0]) != key_of(sorted[i0 + kLarge - 1]))
+        return;
+    constexpr int U = 8;
+    float sum[kPer] = {};
+    for (int i = 0; i < kChunk; i += U) {
+        Raw8<float> raw[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) raw[u] = piece.load(sums + (c * kChunk + i + u) * sums_stride);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            float v[kPer];
+            unpack(raw[u], v);
+            add_to(sum, v);
+        }
+    }
+    piece.store(large + c * sums_stride, sum);
+}
+
+// A group to `per` rows of the table: their places in the sorted list by bisection,
+// then one pass over these, U entries' loads in flight whichever rows they belong to.
+template <typename TG, typename TO, bool VECTOR>
+__global__ void __launch_bounds__(kThreads)
+k_embedding_rows(const TG* __restrict__ grad, int64_t gs,
+                 const unsigned long long* __restrict__ sorted,
+                 const unsigned long long* __restrict__ count, const float* __restrict__ sums,
+                 const float* __restrict__ large, int64_t sums_stride, float scale, TO* out,
+                 int64_t os, int64_t rows, int per, Spread s) {
+    pdl_prologue();
+    int block;
+    const int64_t v0 = group_of(s, &block) * per, v1 = v0 + per < rows ? v0 + per : rows;
+    const Piece<VECTOR> piece(s, block);
+    if (!piece.any() || v0 >= rows) return;
+    // the first place at or behind v0, and at or behind v1
+    int64_t i = 0, end = 0;
+    {
+        int64_t a = (int64_t)*count, b = a;
+        while (i < a || end < b) {
+            const int64_t m = (i + a) >> 1, n = (end + b) >> 1;
+            const uint32_t x = i < a ? key_of(sorted[m]) : 0u, y = end < b ? key_of(sorted[n]) : 0u;
+            if (i < a) {
+                if (x < v0) i = m + 1;
+                else a = m;
+            }
+            if (end < b) {
+                if (y < v1) end = n + 1;
+                else b = n;
+            }
+        }
+    }
+    const float none[kPer] = {};
+    float sum[kPer] = {};
+    int64_t row = v0;
+    auto leave = [&](int64_t to) {   // store the row, and zeros up to `to`
+        float v[kPer];
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) {
+            v[e] = sum[e] * scale;
+            sum[e] = 0.f;
+        }
+        piece.store(out + row * os, v);
+        for (++row; row < to; ++row) piece.store(out + row * os, none);
+    };
+    constexpr int U = 4;
+    while (i < end) {
+        if (i % kChunk == 0 && i + kChunk <= end) {
+            const uint32_t k = key_of(sorted[i]);
+            if (k == key_of(sorted[i + kChunk - 1])) {
+                if (k != row) leave(k);
+                const bool more = i % kLarge == 0 && i + kLarge <= end &&
+                                  k == key_of(sorted[i + kLarge - 1]);
+                float v[kPer];
+                unpack(piece.load(more ? large + i / kLarge * sums_stride
+                                       : sums + i / kChunk * sums_stride), v);
+                add_to(sum, v);
+                i += more ? kLarge : kChunk;
+                continue;
+            }
+        }
+        unsigned long long e[U];
+        Raw8<TG> raw[U];
+        const int n = (int)(end - i < U - i % U ? end - i : U - i % U);
+#pragma unroll
+        for (int u = 0; u < U; ++u) e[u] = u < n ? sorted[i + u] : 0ull;
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            raw[u] = u < n ? piece.load(grad + (uint32_t)e[u] * gs) : Raw8<TG>{};
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (u >= n) break;
+            if (key_of(e[u]) != row) leave(key_of(e[u]));
+            float v[kPer];
+            unpack(raw[u], v);
+            add_to(sum, v);
+        }
+        i += n;
+    }
+    leave(v1);
+}
+
+// ---- host --------------------------------------------------------------------
+
+constexpr int64_t kMost = (int64_t(1) << 31) - 1024;   // rows, tokens
+constexpr int64_t kMostCols = int64_t(1) << 20;
+
+Spread spread(int64_t cols) {
+    Spread s{0, 1, (int)cols};
+    const int64_t vecs = (cols + kPer - 1) / kPer;
+    while (s.log2_lanes < 5 && (1 << s.log2_lanes) < vecs) ++s.log2_lanes;
+    s.blocks = (int)((vecs + (1 << s.log2_lanes) - 1) >> s.log2_lanes);
+    return s;
+}
+
+// CTAs that hold a group to each of n * blocks parts; 0: more than a launch takes.
+unsigned ctas(int64_t n, const Spread& s) {
+    const int64_t per = kThreads >> s.log2_lanes;
+    const int64_t c = (n * s.blocks + per - 1) / per;
+    return c < (int64_t(1) << 31) ? (unsigned)c : 0u;
+}
+
+struct Work {
+    uint32_t *keys, *places, *cnt, *tot, *dstart, *done;
+    unsigned long long *sorted, *other, *count;
+    float *sums, *large;
+    int64_t stride;   // of a piece's sum
+};
+// Where each part of the workspace lies; returns the bytes.
+int64_t lay_out(int64_t tokens, int64_t rows, int64_t cols, void* base, Work* w) {
+    int64_t at = 0;
+    char* b = static_cast<char*>(base);
+    auto take = [&](int64_t bytes) {
+        char* q = b + at;
+        at += (bytes + 255) / 256 * 256;
+        return q;
+    };
+    *w = Work{};
+    w->stride = (cols + kPer - 1) / kPer * kPer;
+    w->count = reinterpret_cast<unsigned long long*>(take(16));
+    w->done = reinterpret_cast<uint32_t*>(take(4));
+    w->sorted = reinterpret_cast<unsigned long long*>(take(8 * tokens));
+    w->sums = reinterpret_cast<float*>(take(tokens / kChunk * w->stride * 4));
+    w->large = reinterpret_cast<float*>(take(tokens / kLarge * w->stride * 4));
+    if (tokens > kSmall) {
+        const RadixPlan plan = radix_plan((uint64_t)(rows > 0 ? rows : 1), 0);
+        w->other = reinterpret_cast<unsigned long long*>(take(8 * tokens));
+        w->keys = reinterpret_cast<uint32_t*>(take(4 * tokens));
+        w->places = reinterpret_cast<uint32_t*>(take(4 * tokens));
+        w->cnt = reinterpret_cast<uint32_t*>(take(4 * radix_tiles(tokens) << plan.bits[0]));
+        w->tot = reinterpret_cast<uint32_t*>(take(4 << kRadixMaxBits));
+        w->dstart = reinterpret_cast<uint32_t*>(take(4 << kRadixMaxBits));
+    }
+    return at;
+}
+
+cudaError_t sort_tokens(const int64_t* ids, int64_t tokens, int64_t rows, const Work& w,
+                        unsigned long long* status, cudaStream_t st) {
+    if (tokens <= kSmall) {
+        int size = 1;
+        while (size < tokens) size *= 2;
+        return launch_k(k_embedding_sort, dim3(1), dim3(kSortThreads), 0, st, ids, (int)tokens,
+                        size, rows, w.sorted, w.count, status);
+    }
+    cudaError_t e = launch_k(k_embedding_keys, dim3((unsigned)((tokens + kThreads - 1) / kThreads)),
+                             dim3(kThreads), 0, st, ids, tokens, rows, w.keys, w.places, w.done,
+                             status);
+    if (e != cudaSuccess) return e;
+    SortedBuffers sb{};
+    sb.pair_x = w.keys;
+    sb.q_row = w.places;
+    sb.sorted_e = w.sorted;
+    sb.tmp_e = w.other;
+    sb.stats = w.count;
+    sb.cnt = w.cnt;
+    sb.tot = w.tot;
+    sb.dstart = w.dstart;
+    sb.done = w.done;
+    return launch_radix_sort(sb, tokens, 1, 0u, radix_plan((uint64_t)rows, 0), st);
+}
+
+bool sizes_ok(int64_t tokens, int64_t rows, int64_t cols) {
+    return tokens >= 0 && rows >= 0 && cols >= 0 && tokens < kMost && rows < kMost;
+}
+
+pss_status clear_status(int64_t* status, cudaStream_t st) {
+    return status ? status_of(cudaMemsetAsync(status, 0xff, 8, st)) : PSS_OK;
+}
+
+}  // namespace
+
+extern "C" pss_status pss_embedding_forward(const void* weight, pss_dtype weight_type,
+                                            int64_t weight_stride, int64_t rows, int64_t cols,
+                                            const int64_t* ids, int64_t tokens, float scale,
+                                            void* out, pss_dtype out_type, int64_t out_stride,
+                                            int64_t* status, pss_stream stream) {
+    if (!dtype_ok(weight_type) || !dtype_ok(out_type) || !sizes_ok(tokens, rows, cols) ||
+        weight_stride < cols || out_stride < cols || !std::isfinite(scale))
+        return PSS_ERR_INVALID_ARG;
+    if (cols > kMostCols) return PSS_ERR_UNSUPPORTED;
+    if (status && !(device_ptr(status) && aligned_to(status, 8))) return PSS_ERR_INVALID_ARG;
+    const bool some = tokens > 0 && cols > 0;
+    if (some) {
+        if (!device_ptr(ids) || !aligned_to(ids, 8) || !device_ptr(out) ||
+            !aligned_to(out, dtype_size(out_type)))
+            return PSS_ERR_INVALID_ARG;
+        if (rows > 0 && (!device_ptr(weight) || !aligned_to(weight, dtype_size(weight_type))))
+            return PSS_ERR_INVALID_ARG;
+    }
+    const Spread s = spread(cols > 0 ? cols : 1);
+    // one token to a group while these do not fill the GPU
+    const int64_t fill = (int64_t)sm_count() * 4 * (kThreads >> s.log2_lanes);
+    const bool one = tokens * s.blocks <= fill;
+    const unsigned n = ctas(one ? tokens : (tokens + 3) / 4, s);
+    if (some && n == 0) return PSS_ERR_UNSUPPORTED;
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    const pss_status rc = clear_status(status, st);
+    if (rc != PSS_OK || !some) return rc;
+    const bool vector = cols % 8 == 0 && aligned8(out, out_stride, dtype_size(out_type)) &&
+                        aligned8(weight, weight_stride, dtype_size(weight_type));
+    return status_of(with_type(weight_type, [&](auto tw) {
+        return with_type(out_type, [&](auto to) {
+            using TW = decltype(tw);
+            using TO = decltype(to);
+            auto go = [&](auto* k) {
+                return launch_k(k, dim3(n), dim3(kThreads), 0, st, static_cast<const TW*>(weight),
+                                weight_stride, rows, ids, tokens, scale, static_cast<TO*>(out),
+                                out_stride, reinterpret_cast<unsigned long long*>(status), s);
+            };
+            return vector ? one ? go(k_embedding_forward<TW, TO, true, 1>)
+                                : go(k_embedding_forward<TW, TO, true, 4>)
+                   : one  ? go(k_embedding_forward<TW, TO, false, 1>)
+                          : go(k_embedding_forward<TW, TO, false, 4>);
+        });
+    }));
+}
+
+extern "C" int64_t pss_embedding_workspace(int64_t tokens, int64_t rows, int64_t cols) {
+    if (!sizes_ok(tokens, rows, cols) || cols > kMostCols || tokens == 0 || rows == 0 || cols == 0)
+        return 0;
+    Work w;
+    return lay_out(tokens, rows, cols, nullptr, &w);
+}
+
+extern "C" pss_status pss_embedding_backward(const void* grad, pss_dtype grad_type,
+                                             int64_t grad_stride, const int64_t* ids,
+                                             int64_t tokens, float scale, int64_t rows,
+                                             int64_t cols, void* dweight, pss_dtype dweight_type,
+                                             int64_t dweight_stride, void* workspace,
+                                             int64_t workspace_bytes, int64_t* status,
+                                             pss_stream stream) {
+    if (!dtype_ok(grad_type) || !dtype_ok(dweight_type) || !sizes_ok(tokens, rows, cols) ||
+        grad_stride < cols || dweight_stride < cols || !std::isfinite(scale))
+        return PSS_ERR_INVALID_ARG;
+    if (cols > kMostCols) return PSS_ERR_UNSUPPORTED;
+    if (status && !(device_ptr(status) && aligned_to(status, 8))) return PSS_ERR_INVALID_ARG;
+    if (tokens > 0 && (!device_ptr(ids) || !aligned_to(ids, 8))) return PSS_ERR_INVALID_ARG;
+    const bool some = rows > 0 && cols > 0;
+    const Spread s = spread(cols > 0 ? cols : 1);
+    // rows of a group: few enough that all of the GPU has some
+    int per = 16;
+    while (per > 1 && (rows + per - 1) / per * s.blocks <
+                          (int64_t)sm_count() * 8 * (kThreads >> s.log2_lanes))
+        per /= 2;
+    const unsigned n = ctas((rows + per - 1) / per, s), pieces = ctas(tokens / kChunk, s);
+    if (some) {
+        if (!device_ptr(dweight) || !aligned_to(dweight, dtype_size(dweight_type)))
+            return PSS_ERR_INVALID_ARG;
+        if (tokens > 0 &&
+            (!device_ptr(grad) || !aligned_to(grad, dtype_size(grad_type)) ||
+             !device_ptr(workspace) || !aligned_to(workspace, 16) ||
+             workspace_bytes < pss_embedding_workspace(tokens, rows, cols)))
+            return PSS_ERR_INVALID_ARG;
+        if (n == 0 || (tokens >= kChunk && pieces == 0)) return PSS_ERR_UNSUPPORTED;
+    }
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    const pss_status rc = clear_status(status, st);
+    if (rc != PSS_OK || !some) return rc;
+    if (tokens == 0)
+        return status_of(cudaMemset2DAsync(dweight, dweight_stride * dtype_size(dweight_type), 0,
+                                           cols * dtype_size(dweight_type), rows, st));
+    Work w;
+    lay_out(tokens, rows, cols, workspace, &w);
+    cudaError_t e = sort_tokens(ids, tokens, rows, w,
+                                reinterpret_cast<unsigned long long*>(status), st);
+    if (e != cudaSuccess) return status_of(e);
+    const bool vector = cols % 8 == 0 && aligned8(grad, grad_stride, dtype_size(grad_type)) &&
+                        aligned8(dweight, dweight_stride, dtype_size(dweight_type));
+    return status_of(with_type(grad_type, [&](auto tg) {
+        using TG = decltype(tg);
+        const TG* g = static_cast<const TG*>(grad);
+        if (pieces > 0) {
+            auto* k = vector ? k_embedding_pieces<TG, true> : k_embedding_pieces<TG, false>;
+            e = launch_k(k, dim3(pieces), dim3(kThreads), 0, st, g, grad_stride, w.sorted, w.count,
+                         w.sums, w.stride, s);
+            if (e != cudaSuccess) return e;
+        }
+        if (tokens >= kLarge) {
+            auto* k = vector ? k_embedding_large_pieces<true> : k_embedding_large_pieces<false>;
+            e = launch_k(k, dim3(ctas(tokens / kLarge, s)), dim3(kThreads), 0, st, w.sums, w.stride,
+                         w.sorted, w.count, w.large, s);
+            if (e != cudaSuccess) return e;
+        }
+        return with_type(dweight_type, [&](auto to) {
+            using TO = decltype(to);
+            auto* k = vector ? k_embedding_rows<TG, TO, true> : k_embedding_rows<TG, TO, false>;
+            return launch_k(k, dim3(n), dim3(kThreads), 0, st, g, grad_stride, w.sorted, w.count,
+                            w.sums, w.large, w.stride, scale, static_cast<TO*>(dweight),
+                            dweight_stride, rows, per, s);
+        });
+    }));
+}

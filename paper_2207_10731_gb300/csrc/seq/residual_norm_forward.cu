@@ -1,0 +1,182 @@
+// The norms after and before a block, forward.  Bound by memory: a row of the block's
+// output, its gate and the stream is read once, kept in registers through both
+// reductions and written once; the next row's loads are under way meanwhile.
+#include <cmath>
+
+#include "residual_norm.cuh"
+
+using namespace pss;
+using namespace pss::seq;
+
+namespace {
+
+template <typename T, typename R>
+struct Forward {
+    const T* x;
+    const R* residual;
+    const T* gate;
+    R* total;
+    T* y;
+    int64_t xs, rs, gs, ts, ys;   // strides
+    const float *post, *pre;
+    float *post_rstd, *pre_rstd;
+    float scale, eps;
+    int gates;
+    Shape sh;
+};
+
+template <typename T, typename R, int VEC, int KIND, int MODE>
+__global__ void __launch_bounds__(Fit<VEC, KIND>::kMost)
+k_residual_norm_forward(const __grid_constant__ Forward<T, R> a) {
+    pdl_prologue();
+    using F = Fit<VEC, KIND>;
+    constexpr int CH = F::kVectors;
+    __shared__ float2 slots[2][32];
+    const Shape& sh = a.sh;
+    const Place<VEC, MODE> place(sh);
+    const float inv_n = 1.f / (float)sh.cols;
+    bool in[CH];
+#pragma unroll
+    for (int c = 0; c < CH; ++c) in[c] = place.at(sh, c) < sh.cols;
+    const int64_t step = (int64_t)gridDim.x * sh.groups;
+    Part<T, VEC, CH> next_x, next_g;
+    Part<R, VEC, CH> next_r;
+    float next_gate = 0.f;
+    auto fetch = [&](int64_t r) {
+        const bool live = r < sh.rows;
+        auto whole = [&](int64_t stride) { return MODE == ALIGNED || inner(sh, r, stride); };
+        next_x.load(a.x + r * a.xs, live, whole(a.xs), in, place, sh);
+        next_r.load(a.residual + r * a.rs, live, whole(a.rs), in, place, sh);
+        if (a.gates == VALUE_GATE)
+            next_g.load(a.gate + r * a.gs, live, whole(a.gs), in, place, sh);
+        if (a.gates == ROW_GATE) next_gate = live ? load_f32(a.gate[r * a.gs]) : 0.f;
+    };
+    if (F::kAhead) fetch((int64_t)blockIdx.x * sh.groups + place.group);
+    int turn = 0;
+    // the same trip count for every thread of the CTA (shuffles and barriers inside);
+    // rows past the end are computed from zeros and dropped
+    for (int64_t r0 = (int64_t)blockIdx.x * sh.groups; r0 < sh.rows; r0 += step) {
+        const int64_t r = r0 + place.group;
+        const bool live = r < sh.rows;
+        if (!F::kAhead) fetch(r);
+        const Part<T, VEC, CH> part_x = next_x, part_g = next_g;
+        const Part<R, VEC, CH> part_r = next_r;
+        const float row_gate = next_gate;
+        if (F::kAhead && r0 + step < sh.rows) fetch(r + step);
+        float v[CH][VEC];
+#pragma unroll
+        for (int c = 0; c < CH; ++c) part_x.get(c, v[c]);
+        if (a.post) {
+            float s = 0.f;
+#pragma unroll
+            for (int c = 0; c < CH; ++c)
+#pragma unroll
+                for (int i = 0; i < VEC; ++i)
+                    if (inside<MODE>(place.at(sh, c) + i, sh.cols, true)) s += v[c][i] * v[c][i];
+            s = row_sums(make_float2(s, 0.f), sh.lanes, slots, turn).x;
+            const float rstd = 1.f / sqrtf(s * inv_n + a.eps);
+            if (live && place.t == 0) a.post_rstd[r] = rstd;
+#pragma unroll
+            for (int c = 0; c < CH; ++c) {
+                float w[VEC];
+                load_weight<VEC, MODE>(a.post, place.at(sh, c), sh.cols, in[c], w);
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) v[c][i] *= rstd * w[i];
+            }
+        }
+        float s = 0.f;
+        const float row_scale = a.gates == ROW_GATE ? a.scale * sigmoid(row_gate) : a.scale;
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            float t[VEC], g[VEC];
+            part_r.get(c, t);
+            if (a.gates == VALUE_GATE) {
+                part_g.get(c, g);
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) v[c][i] *= sigmoid(g[i]);
+            }
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                v[c][i] = t[i] + row_scale * v[c][i];
+                if (inside<MODE>(place.at(sh, c) + i, sh.cols, true)) s += v[c][i] * v[c][i];
+            }
+            if (live && in[c]) store_part(a.total + r * a.ts, place.at(sh, c), sh.cols, v[c]);
+        }
+        if (a.pre) {
+            // of the unrounded sum: total's rounding is not in y
+            s = row_sums(make_float2(s, 0.f), sh.lanes, slots, turn).x;
+            const float rstd = 1.f / sqrtf(s * inv_n + a.eps);
+            if (live && place.t == 0) a.pre_rstd[r] = rstd;
+#pragma unroll
+            for (int c = 0; c < CH; ++c) {
+                float w[VEC];
+                load_weight<VEC, MODE>(a.pre, place.at(sh, c), sh.cols, in[c], w);
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) v[c][i] *= rstd * w[i];
+                if (live && in[c]) store_part(a.y + r * a.ys, place.at(sh, c), sh.cols, v[c]);
+            }
+        }
+    }
+}
+
+}  // namespace
+
+extern "C" pss_status pss_residual_norm_forward(
+    const void* x, pss_dtype type, int64_t x_stride, const void* residual, pss_dtype stream_type,
+    int64_t residual_stride, const void* gate, int32_t gates, int64_t gate_stride,
+    const float* post_weight, const float* pre_weight, int64_t rows, int64_t cols, float scale,
+    float eps, void* total, int64_t total_stride, void* y, int64_t y_stride, float* post_rstd,
+    float* pre_rstd, pss_stream stream) {
+    if (!dtype_ok(type) || (stream_type != type && stream_type != PSS_F32) || rows < 0 ||
+        cols < 1 || !(eps >= 0.f) || std::isinf(eps) || !std::isfinite(scale) || x_stride < cols ||
+        residual_stride < cols || total_stride < cols || (pre_weight && y_stride < cols) ||
+        gates < 0 || gates > 2 || (gates == 1 && gate_stride < 1) ||
+        (gates == 2 && gate_stride < cols))
+        return PSS_ERR_INVALID_ARG;
+    if (cols > kNormMaxCols) return PSS_ERR_UNSUPPORTED;
+    if (rows == 0) return PSS_OK;
+    const size_t a = dtype_size(type), b = dtype_size(stream_type);
+    auto ok = [](const void* p, size_t size) { return device_ptr(p) && aligned_to(p, size); };
+    if (!ok(x, a) || !ok(residual, b) || !ok(total, b) || (gates && !ok(gate, a)) ||
+        (post_weight && (!ok(post_weight, 4) || !ok(post_rstd, 4))) ||
+        (pre_weight && (!ok(pre_weight, 4) || !ok(pre_rstd, 4) || !ok(y, a))))
+        return PSS_ERR_INVALID_ARG;
+    const bool values = gates == VALUE_GATE;
+    const Lie lie = rows_lie<5>(
+        cols, {x, residual, total, pre_weight ? y : x, values ? gate : x},
+        {x_stride, residual_stride, total_stride, pre_weight ? y_stride : x_stride,
+         values ? gate_stride : x_stride},
+        {type, stream_type, stream_type, type, type});
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    auto go = [&](auto t, auto r) {
+        using T = decltype(t);
+        using R = decltype(r);
+        Forward<T, R> f{static_cast<const T*>(x), static_cast<const R*>(residual),
+                        static_cast<const T*>(gate), static_cast<R*>(total), static_cast<T*>(y),
+                        x_stride, residual_stride, gate_stride, total_stride, y_stride,
+                        post_weight, pre_weight, post_rstd, pre_rstd, scale, eps, gates, Shape{}};
+        const bool ragged = lie.how == SHIFTED && cols <= kNormMaxCols - 8;
+        int kind;
+        const Split s = norm_split((int)cols, ragged ? 7 : 0, &kind);
+        f.sh = Shape{rows, (int)cols, s.lanes, s.log2_lanes, s.groups, lie.shift0, lie.step};
+        auto with = [&](auto vec, auto k, auto mode) {
+            auto* kernel = k_residual_norm_forward<T, R, decltype(vec)::value, decltype(k)::value,
+                                                   decltype(mode)::value>;
+            const int n = ctas_of(rows, s, [&] { return resident(kernel, s.threads, 0, 32); },
+                                  decltype(mode)::value);
+            return launch_k(kernel, dim3(n), dim3(s.threads), 0, st, f);
+        };
+        auto wide = [&](auto vec, auto mode) {
+            return kind == NARROW ? with(vec, Int<NARROW>(), mode)
+                   : kind == WIDE ? with(vec, Int<WIDE>(), mode)
+                                  : with(vec, Int<WIDEST>(), mode);
+        };
+        return lie.how == VECTORS ? wide(Int<8>(), Int<ALIGNED>())
+               : ragged           ? wide(Int<8>(), Int<RAGGED>())
+                                  : wide(Int<1>(), Int<ALIGNED>());
+    };
+    return status_of(stream_type != type  ? type == PSS_BF16 ? go(bf16(), float()) : go(f16(), float())
+                     : type == PSS_F32    ? go(float(), float())
+                     : type == PSS_BF16   ? go(bf16(), bf16())
+                                          : go(f16(), f16()));
+}

@@ -331,3 +331,235 @@ def attention_backward(grad, q, k, v, out, lse, q_offsets, kv_offsets=None, caus
     if rc:
         binding._check(rc, "pss_attention_backward")
     return dq, dk, dv
+
+
+def _ids(ids, device):
+    _tensor(ids, "ids", device)
+    if ids.dtype != torch.int64:
+        raise TypeError(f"ids must be torch.int64, got {ids.dtype}")
+    if not ids.is_contiguous():
+        raise ValueError("ids must be contiguous")
+    return ids.data_ptr()
+
+
+def _type_of(dtype, name):
+    if dtype not in _types:
+        raise TypeError(f"{name} must be float32, bfloat16 or float16, got {dtype}")
+    return _types[dtype]
+
+
+def _table(t, name, device, rows=None, cols=None):
+    """The row stride of a two-dimensional tensor."""
+    _tensor(t, name, device)
+    if t.dim() != 2 or (rows is not None and (t.shape[0] != rows or t.shape[1] != cols)):
+        raise ValueError(f"{name} must have shape {'[rows, cols]' if rows is None else [rows, cols]}"
+                         f", got {list(t.shape)}")
+    return _rows(t, name, device)[2]
+
+
+def embedding_forward(weight, ids, scale: float = 1.0, out=None, out_dtype=None, status=None,
+                      stream=None):
+    """scale * weight[ids], the rows of a dense table (pss_embedding_forward).
+
+    weight: [rows, cols] float32, bfloat16 or float16; ids: int64 of any shape.  The
+    result has shape [*ids.shape, cols] and ``out_dtype`` (default: weight's), or is
+    ``out``.  An id outside the table, say -1 for padding, gives a zero row;
+    ``status`` (int64, one value on the device) receives the smallest position of
+    one, or -1."""
+    if stream is not None:
+        return _under(stream, embedding_forward, weight, ids, scale, out, out_dtype, status)
+    device = _device()
+    ws = _table(weight, "weight", device)
+    rows, cols = weight.shape
+    at = _ids(ids, device)
+    if out is None:
+        out = torch.empty((*ids.shape, cols), dtype=out_dtype or weight.dtype, device=weight.device)
+        os = cols
+    else:
+        if out_dtype is not None and out.dtype != out_dtype:
+            raise TypeError(f"out must be {out_dtype}, got {out.dtype}")
+        _tensor(out, "out", device)
+        if out.shape != (*ids.shape, cols):
+            raise ValueError(f"out must have shape {(*ids.shape, cols)}, got {tuple(out.shape)}")
+        os = _rows(out, "out", device)[2]
+    rc = _lib.pss_embedding_forward(
+        weight.data_ptr(), _types[weight.dtype], ws, rows, cols, at, ids.numel(), scale,
+        out.data_ptr(), _type_of(out.dtype, "out_dtype"), os, _status(status, device),
+        torch._C._cuda_getCurrentRawStream(device))
+    if rc:
+        binding._check(rc, "pss_embedding_forward")
+    return out
+
+
+def embedding_backward(grad, ids, rows: int, scale: float = 1.0, out=None, out_dtype=None,
+                       status=None, stream=None):
+    """The gradient of ``embedding_forward``'s weight for the upstream gradient ``grad``
+    [*ids.shape, cols] (pss_embedding_backward): [rows, cols], zeros where no id
+    names the row, in ``out_dtype`` (default: float32) or in ``out``.  Equal inputs
+    give equal bits."""
+    if stream is not None:
+        return _under(stream, embedding_backward, grad, ids, rows, scale, out, out_dtype, status)
+    device = _device()
+    at = _ids(ids, device)
+    _, cols, gs = _rows(grad, "grad", device)
+    if grad.shape[:-1] != ids.shape:
+        raise ValueError(f"grad must have shape {(*ids.shape, cols)}, got {tuple(grad.shape)}")
+    if out is None:
+        out = torch.empty((rows, cols), dtype=out_dtype or torch.float32, device=grad.device)
+        os = cols
+    else:
+        if out_dtype is not None and out.dtype != out_dtype:
+            raise TypeError(f"out must be {out_dtype}, got {out.dtype}")
+        os = _table(out, "out", device, rows, cols)
+    tokens = ids.numel()
+    size = _lib.pss_embedding_workspace(tokens, rows, cols)
+    work = torch.empty(size, dtype=torch.uint8, device=grad.device)
+    rc = _lib.pss_embedding_backward(
+        grad.data_ptr(), _types[grad.dtype], gs, at, tokens, scale, rows, cols, out.data_ptr(),
+        _type_of(out.dtype, "out_dtype"), os, work.data_ptr(), size, _status(status, device),
+        torch._C._cuda_getCurrentRawStream(device))
+    if rc:
+        binding._check(rc, "pss_embedding_backward")
+    return out
+
+
+def _gate(gate, x, name, device):
+    """(data, kind, stride) of a gate: one value to each of x's, or one to a row."""
+    if gate is None:
+        return None, 0, 0
+    if gate.shape == x.shape and x.shape[-1] != 1:
+        return gate.data_ptr(), 2, _rows(gate, name, device, dtype=x.dtype)[2]
+    _tensor(gate, name, device)
+    if gate.shape != (*x.shape[:-1], 1):
+        raise ValueError(f"{name} must have shape {tuple(x.shape)} or {(*x.shape[:-1], 1)}, "
+                         f"got {tuple(gate.shape)}")
+    return gate.data_ptr(), 1, _rows(gate, name, device, dtype=x.dtype)[2]
+
+
+def _stream_rows(t, x, name, device):
+    """The stride of the residual stream's rows: x's shape; x's type or float32."""
+    stride = _rows(t, name, device, like=x)[2]
+    if t.dtype != x.dtype and t.dtype != torch.float32:
+        raise TypeError(f"{name} must be {x.dtype} or torch.float32, got {t.dtype}")
+    return stride
+
+
+def residual_norm_forward(x, residual, post_weight=None, pre_weight=None, gate=None,
+                          scale: float = 1.0, eps: float = 1e-5, total=None, y=None, stream=None):
+    """(total, y, post_rstd, pre_rstd): what lies between two blocks
+    (pss_residual_norm_forward).  With rms(v, w) = v / sqrt(mean(v^2) + eps) * w over
+    the last dimension,
+
+        total = residual + scale * sigmoid(gate) * rms(x, post_weight)
+        y = rms(total, pre_weight)
+
+    x: the block's output, float32, bfloat16 or float16; residual: the stream, x's
+    type or float32; weights: float32, either may be None (no such norm; y and its
+    rstd are None then); gate: None, or logits of x's type, one to a value or one to a
+    row ([..., 1]).  total (residual's type) and y (x's) go to the tensors of that name
+    if given: total may be residual, y may be x.  The rstd are float32, for the
+    backward call."""
+    if stream is not None:
+        return _under(stream, residual_norm_forward, x, residual, post_weight, pre_weight, gate,
+                      scale, eps, total, y)
+    device = _device()
+    rows, cols, xs = _rows(x, "x", device)
+    rs = _stream_rows(residual, x, "residual", device)
+    pg, gates, gs = _gate(gate, x, "gate", device)
+    if total is None:
+        total, ts = torch.empty_like(residual, memory_format=torch.contiguous_format), cols
+    else:
+        ts = _rows(total, "total", device, like=x, dtype=residual.dtype)[2]
+    ys = cols
+    if pre_weight is None:
+        if y is not None:
+            raise ValueError("y needs pre_weight")
+    elif y is None:
+        y = torch.empty_like(x, memory_format=torch.contiguous_format)
+    else:
+        ys = _rows(y, "y", device, like=x, dtype=x.dtype)[2]
+    post = pre = post_rstd = pre_rstd = None
+    if post_weight is not None:
+        post = _vector(post_weight, cols, "post_weight", device)
+        post_rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
+    if pre_weight is not None:
+        pre = _vector(pre_weight, cols, "pre_weight", device)
+        pre_rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
+    rc = _lib.pss_residual_norm_forward(
+        x.data_ptr(), _types[x.dtype], xs, residual.data_ptr(), _types[residual.dtype], rs, pg,
+        gates, gs, post, pre, rows, cols, scale, eps, total.data_ptr(), ts,
+        None if y is None else y.data_ptr(), ys,
+        None if post is None else post_rstd.data_ptr(),
+        None if pre is None else pre_rstd.data_ptr(),
+        torch._C._cuda_getCurrentRawStream(device))
+    if rc:
+        binding._check(rc, "pss_residual_norm_forward")
+    return total, y, post_rstd, pre_rstd
+
+
+def residual_norm_backward(grad_total, grad_y, x, total, post_rstd, pre_rstd, post_weight=None,
+                           pre_weight=None, gate=None, scale: float = 1.0, dx=None,
+                           dresidual=None, dgate=None, stream=None):
+    """(dx, dresidual, dgate, dpost_weight, dpre_weight) of ``residual_norm_forward``
+    (pss_residual_norm_backward); None for what was not there.  grad_total: the
+    gradient of total (residual's type; None: zero); grad_y: that of y (x's type; None
+    without pre_weight); x, total and the rstd as the forward call took and gave
+    them.  The first three go to the tensors of that name if given: dx may be x or
+    grad_y, dresidual may be grad_total, dgate may be gate.  The weights' gradients
+    are float32."""
+    if stream is not None:
+        return _under(stream, residual_norm_backward, grad_total, grad_y, x, total, post_rstd,
+                      pre_rstd, post_weight, pre_weight, gate, scale, dx, dresidual, dgate)
+    device = _device()
+    rows, cols, xs = _rows(x, "x", device)
+    ts = _stream_rows(total, x, "total", device)
+    pg, gates, gs = _gate(gate, x, "gate", device)
+    pt = py = None
+    gts = gys = cols
+    if grad_total is not None:
+        gts = _rows(grad_total, "grad_total", device, like=x, dtype=total.dtype)[2]
+        pt = grad_total.data_ptr()
+    if (grad_y is None) != (pre_weight is None):
+        raise ValueError("grad_y and pre_weight go together")
+    if grad_y is not None:
+        gys = _rows(grad_y, "grad_y", device, like=x, dtype=x.dtype)[2]
+        py = grad_y.data_ptr()
+    dxs = drs = cols
+    if dx is None:
+        dx = torch.empty_like(x, memory_format=torch.contiguous_format)
+    else:
+        dxs = _rows(dx, "dx", device, like=x, dtype=x.dtype)[2]
+    if dresidual is None:
+        dresidual = torch.empty_like(total, memory_format=torch.contiguous_format)
+    else:
+        drs = _rows(dresidual, "dresidual", device, like=x, dtype=total.dtype)[2]
+    if gate is None:
+        if dgate is not None:
+            raise ValueError("dgate needs gate")
+        pdg, dgs = None, 0
+    else:
+        if dgate is None:
+            dgate = torch.empty_like(gate, memory_format=torch.contiguous_format)
+        dgs = _rows(dgate, "dgate", device, like=gate, dtype=x.dtype)[2]
+        pdg = dgate.data_ptr()
+    post = pre = ppost = ppre = dpost = dpre = None
+    size = 0
+    if post_weight is not None or pre_weight is not None:
+        both = torch.empty((2, cols), dtype=torch.float32, device=x.device)
+        size = _lib.pss_residual_norm_workspace(rows, cols)
+    work = torch.empty(size, dtype=torch.uint8, device=x.device)
+    if post_weight is not None:
+        post = _vector(post_weight, cols, "post_weight", device)
+        ppost, dpost = _vector(post_rstd, rows, "post_rstd", device), both[0]
+    if pre_weight is not None:
+        pre = _vector(pre_weight, cols, "pre_weight", device)
+        ppre, dpre = _vector(pre_rstd, rows, "pre_rstd", device), both[1]
+    rc = _lib.pss_residual_norm_backward(
+        pt, gts, py, gys, x.data_ptr(), _types[x.dtype], xs, total.data_ptr(), _types[total.dtype],
+        ts, pg, gates, gs, post, pre, ppost, ppre, rows, cols, scale, dx.data_ptr(), dxs,
+        dresidual.data_ptr(), drs, pdg, dgs, None if dpost is None else dpost.data_ptr(),
+        None if dpre is None else dpre.data_ptr(), work.data_ptr(), size,
+        torch._C._cuda_getCurrentRawStream(device))
+    if rc:
+        binding._check(rc, "pss_residual_norm_backward")
+    return dx, dresidual, dgate, dpost, dpre
