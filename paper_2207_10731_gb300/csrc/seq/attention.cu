@@ -191,9 +191,6 @@ extern "C" pss_status pss_attention_backward(const pss_attention_shape* shape, c
 namespace pss {
 namespace seq {
 
-namespace {
-
-// A driver function, looked up once.
 void* driver_call(const char* name, std::atomic<void*>* found) {
     void* fn = found->load(std::memory_order_acquire);
     if (fn) return fn;
@@ -208,7 +205,15 @@ void* driver_call(const char* name, std::atomic<void*>* found) {
     return fn;
 }
 
-}  // namespace
+cudaError_t bind_context() {
+    static thread_local int bound = -1;
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess || dev == bound) return e;
+    e = cudaSetDevice(dev);
+    if (e == cudaSuccess) bound = dev;
+    return e;
+}
 
 bool device_ptr(const void* p) {
     static std::atomic<void*> found{nullptr};
@@ -225,6 +230,8 @@ cudaError_t tile_map(CUtensorMap* map, const Rows& r, int tokens, int heads, int
     static std::atomic<void*> found{nullptr};
     void* fn = driver_call("cuTensorMapEncodeTiled", &found);
     if (!fn) return cudaErrorNotSupported;
+    const cudaError_t bound = bind_context();
+    if (bound != cudaSuccess) return bound;
     const bool empty = tokens == 0;   // nothing is loaded; the map only has to be valid
     // a stride over a size of one is free, but the encoder checks it
     const int64_t row = heads == 1 ? dim : r.head, token = tokens <= 1 ? dim : r.token;

@@ -9,6 +9,13 @@
 namespace pss {
 namespace seq {
 
+// A driver function, looked up once; null where there is none.
+void* driver_call(const char* name, std::atomic<void*>* found);
+
+// The driver's encoder of tensor maps wants the device's context bound to the calling
+// thread, which no runtime call may have done yet in a new one.
+cudaError_t bind_context();
+
 // A map of rows [tokens][heads][dim] whose boxes are 64 values of `heads_box`
 // heads of `tokens_box` tokens, in the 128-byte swizzle; what lies outside the
 // tensor reads as zero.  spare: any device memory, the address of an empty tensor.
