@@ -614,6 +614,76 @@ pss_status pss_residual_norm_backward(
     float* dpost_weight, float* dpre_weight, void* workspace, int64_t workspace_bytes,
     pss_stream stream);
 
+/*
+ * A product with its bias, activation and residual in one pass over the result:
+ *   z = x weight + bias,   y = act(z) + residual,
+ * x[tokens][in], weight[in][out], the sums in fp32, z and y rounded once each.
+ *   act: PSS_ACT_NONE, RELU, GELU (z Phi(z), the exact form), SILU (z sigmoid(z)).
+ */
+typedef enum { PSS_ACT_NONE = 0, PSS_ACT_RELU = 1, PSS_ACT_GELU = 2, PSS_ACT_SILU = 3 } pss_activation;
+typedef struct {
+    int64_t tokens, in, out;             /* tokens >= 0, in, out >= 1; below 2^31 - 1024 */
+    const void* x;                       /* `type`; rows x_stride apart */
+    int64_t x_stride;
+    const void* weight;                  /* `type`; one of the two strides is 1 */
+    int64_t weight_in_stride, weight_out_stride;
+    const float* bias;                   /* fp32[out], or NULL */
+    const void* residual;                /* y_type, or NULL */
+    int64_t residual_stride;
+    void* y;                             /* y_type */
+    int64_t y_stride;
+    void* z;                             /* `type`, or NULL: not wanted */
+    int64_t z_stride;
+    int32_t type;                        /* PSS_BF16 or PSS_F16 */
+    int32_t y_type;                      /* `type` or PSS_F32 */
+    int32_t activation;                  /* pss_activation */
+    int32_t reserved;
+} pss_linear_forward_args;
+
+/*
+ *   workspace: device, 16-byte aligned, at least pss_linear_forward_workspace(args) bytes (partial
+ *   sums where the contraction is split, and copies of an x or weight whose rows do not start at
+ *   multiples of 16 bytes); means nothing between calls.
+ *   status: NULL or device int64[1], set to -1, or to -2 when a wait inside a kernel gave up after
+ *   2 s (y and z are undefined then).
+ * y may be residual where the strides are equal; other overlaps with inputs are undefined.
+ * Equal inputs give equal bits.
+ * Errors: PSS_ERR_INVALID_ARG, PSS_ERR_UNSUPPORTED (2^31 tiles of 128 x 256 and more),
+ * PSS_ERR_CUDA.
+ */
+int64_t pss_linear_forward_workspace(const pss_linear_forward_args* args);
+pss_status pss_linear_forward(const pss_linear_forward_args* args, void* workspace,
+                              int64_t workspace_bytes, int64_t* status, pss_stream stream);
+
+/*
+ * Its gradients, for the upstream gradient of y (the residual's gradient is that one itself):
+ *   dz = grad act'(z),  dx = dz weight^T,  dweight = x^T dz,  dbias = sum over tokens of dz.
+ * dz enters the two products rounded to `type`; dbias is the sum of the unrounded values.  All
+ * sums are fp32, in a fixed order.  Results that are NULL are not computed.
+ */
+typedef struct {
+    int64_t tokens, in, out;
+    const void* grad;                    /* grad_type */
+    int64_t grad_stride;
+    const void* x;                       /* `type`; read for dweight */
+    int64_t x_stride;
+    const void* weight;                  /* `type`; read for dx */
+    int64_t weight_in_stride, weight_out_stride;
+    const void* z;                       /* `type`: the forward call's; read with an activation */
+    int64_t z_stride;
+    void* dx;                            /* `type`, or NULL */
+    int64_t dx_stride;
+    void* dweight;                       /* dweight_type, or NULL; one of the two strides is 1 */
+    int64_t dweight_in_stride, dweight_out_stride;
+    float* dbias;                        /* fp32[out], or NULL */
+    int32_t type;                        /* PSS_BF16 or PSS_F16 */
+    int32_t grad_type, dweight_type;     /* `type` or PSS_F32 */
+    int32_t activation;
+} pss_linear_backward_args;
+int64_t pss_linear_backward_workspace(const pss_linear_backward_args* args);
+pss_status pss_linear_backward(const pss_linear_backward_args* args, void* workspace,
+                               int64_t workspace_bytes, int64_t* status, pss_stream stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -45,7 +45,8 @@ EXPORTS = [
     "pss_layer_norm_backward", "pss_dropout", "pss_attention_workspace", "pss_attention_forward",
     "pss_attention_backward", "pss_embedding_forward", "pss_embedding_workspace",
     "pss_embedding_backward", "pss_residual_norm_forward", "pss_residual_norm_workspace",
-    "pss_residual_norm_backward",
+    "pss_residual_norm_backward", "pss_linear_forward_workspace", "pss_linear_forward",
+    "pss_linear_backward_workspace", "pss_linear_backward",
 ]
 
 
@@ -120,6 +121,8 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
             "pss_residual_norm_backward": [vp, i64, vp, i64, vp, i32, i64, vp, i32, i64, vp, i32,
                                            i64, vp, vp, vp, vp, i64, i64, f32, vp, i64, vp, i64,
                                            vp, i64, vp, vp, vp, i64, vp],
+            "pss_linear_forward": [vp, vp, i64, vp, vp],
+            "pss_linear_backward": [vp, vp, i64, vp, vp],
         }
         for name, args in sigs.items():
             fn = getattr(lib, name)
@@ -127,6 +130,9 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
             fn.restype = ctypes.c_int
         lib.pss_layer_norm_workspace.argtypes = [i64, i64]
         lib.pss_layer_norm_workspace.restype = i64
+        for fn in (lib.pss_linear_forward_workspace, lib.pss_linear_backward_workspace):
+            fn.argtypes = [vp]
+            fn.restype = i64
         lib.pss_embedding_workspace.argtypes = [i64, i64, i64]
         lib.pss_embedding_workspace.restype = i64
         lib.pss_residual_norm_workspace.argtypes = [i64, i64]

@@ -23,7 +23,8 @@ LIB_PATH = os.path.join(OUT_DIR, "libpss.so")
 SOURCES = ["pss_api.cu", "pss_kernels.cu", "pss_tiled.cu", "pss_sorted.cu", "pss_noalloc.cu",
            "pss_probe.cu", "seq/layer_norm.cu", "seq/dropout.cu", "seq/attention.cu",
            "seq/attention_plan.cu", "seq/attention_forward.cu", "seq/attention_backward.cu",
-           "seq/embedding.cu", "seq/residual_norm_forward.cu", "seq/residual_norm_backward.cu"]
+           "seq/embedding.cu", "seq/residual_norm_forward.cu", "seq/residual_norm_backward.cu",
+           "seq/linear.cu", "seq/linear_product.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 

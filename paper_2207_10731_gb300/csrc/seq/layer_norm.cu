@@ -298,7 +298,7 @@ cudaError_t launch_backward(const TG* g, int64_t gs, const TX* x, int64_t xs, co
                              dx, ds, partial, sh);
     if (e != cudaSuccess) return e;
     return launch_k(k_row_columns, dim3((2 * cols + 31) / 32), dim3(1024), 0, st,
-                    static_cast<const float*>(partial), ctas, cols, 0, 2 * cols, dw, db);
+                    static_cast<const float*>(partial), ctas, 2 * cols, cols, 0, 2 * cols, dw, db);
 }
 
 }  // namespace

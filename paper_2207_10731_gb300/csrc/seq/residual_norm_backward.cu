@@ -324,7 +324,7 @@ extern "C" pss_status pss_residual_norm_backward(
             // a norm that is not there has no sums: its columns are left out
             const int first = post_weight ? 0 : (int)cols, last = pre_weight ? 2 * (int)cols : (int)cols;
             return launch_k(k_row_columns, dim3((unsigned)((last - first + 31) / 32)), dim3(1024), 0,
-                            st, static_cast<const float*>(workspace), n, (int)cols, first, last,
+                            st, static_cast<const float*>(workspace), n, 2 * (int)cols, (int)cols, first, last,
                             dpost_weight, dpre_weight);
         };
         auto wide = [&](auto vec, auto mode) {

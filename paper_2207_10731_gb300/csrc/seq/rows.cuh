@@ -92,19 +92,19 @@ struct Part<T, 1, CH> {
     __device__ __forceinline__ void get(int c, float (&to)[1]) const { to[0] = v[c]; }
 };
 
-// Column sums of the partial rows [parts][2 * cols]: columns first .. last, the first
-// `cols` to `one`, the others to `two`.  A CTA takes 32 columns, its 32 warps every
+// Column sums of the partial rows [parts][width]: columns first .. last, the first `cols`
+// to `one`, the others to `two`.  A CTA takes 32 columns, its 32 warps every
 // 32nd partial row.
 static __global__ void __launch_bounds__(1024)
-k_row_columns(const float* __restrict__ partial, int parts, int cols, int first, int last,
-              float* __restrict__ one, float* __restrict__ two) {
+k_row_columns(const float* __restrict__ partial, int parts, int width, int cols, int first,
+              int last, float* __restrict__ one, float* __restrict__ two) {
     pdl_prologue();
     __shared__ float part[32][33];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int k = first + blockIdx.x * 32 + lane;
     float s = 0.f;
     if (k < last)
-        for (int p = warp; p < parts; p += 32) s += partial[(int64_t)p * 2 * cols + k];
+        for (int p = warp; p < parts; p += 32) s += partial[(int64_t)p * width + k];
     part[warp][lane] = s;
     __syncthreads();
     s = part[lane][warp];

@@ -563,3 +563,177 @@ def residual_norm_backward(grad_total, grad_y, x, total, post_rstd, pre_rstd, po
     if rc:
         binding._check(rc, "pss_residual_norm_backward")
     return dx, dresidual, dgate, dpost, dpre
+
+
+# pss_linear_forward_args, pss_linear_backward_args; the activations of pss_activation
+_FORWARD = struct.Struct("3qPqP2qPPqPqPq4i")
+_BACKWARD = struct.Struct("3qPqPqP2qPqPqP2qP4i")
+_ACTIVATIONS = {None: 0, "relu": 1, "gelu": 2, "silu": 3}
+
+
+def _packed(form, *values):
+    """Address of a call's structure, in a buffer of this thread that the library reads
+    before it returns."""
+    try:
+        buffer, start = _local.linear
+    except AttributeError:
+        buffer = bytearray(max(_FORWARD.size, _BACKWARD.size))
+        start = binding.ctypes.addressof(binding.ctypes.c_char.from_buffer(buffer))
+        _local.linear = buffer, start
+    form.pack_into(buffer, 0, *values)
+    return start
+
+
+def _activation(name):
+    try:
+        return _ACTIVATIONS[name]
+    except (KeyError, TypeError):
+        raise ValueError(f"activation must be None, 'relu', 'gelu' or 'silu', got {name!r}") from None
+
+
+def _half(t, name):
+    if t.dtype != torch.bfloat16 and t.dtype != torch.float16:
+        raise TypeError(f"{name} must be bfloat16 or float16, got {t.dtype}")
+
+
+def _weight(t, name, device, dtype, shape=None):
+    """(data, stride of in, stride of out) of a matrix [in, out] with one dense dimension."""
+    _tensor(t, name, device)
+    if t.dtype not in dtype:
+        raise TypeError(f"{name} must be {' or '.join(map(str, dtype))}, got {t.dtype}")
+    if t.dim() != 2 or (shape is not None and t.shape != shape):
+        raise ValueError(f"{name} must have shape {'[in, out]' if shape is None else list(shape)}, "
+                         f"got {list(t.shape)}")
+    return t.data_ptr(), *t.stride()
+
+
+def _result(out, like, cols, dtype, name, device):
+    """A tensor [..., cols] over the rows of ``like``, made here or given, and its row stride."""
+    shape = (*like.shape[:-1], cols)
+    if out is None:
+        return torch.empty(shape, dtype=dtype, device=like.device), cols
+    _tensor(out, name, device)
+    if out.shape != shape:
+        raise ValueError(f"{name} must have shape {shape}, got {tuple(out.shape)}")
+    return out, _rows(out, name, device, dtype=dtype)[2]
+
+
+def linear_forward(x, weight, bias=None, activation=None, residual=None, keep: bool = False,
+                   out=None, out_dtype=None, status=None, stream=None):
+    """act(x @ weight + bias) + residual (pss_linear_forward); (that, z) with ``keep``,
+    where z = x @ weight + bias in x's type is what the backward call needs of an
+    activation.
+
+    x: bfloat16 or float16 [..., in], rows evenly spaced; weight: x's type, [in, out]
+    with either dimension dense (the transpose of an [out, in] tensor will do); bias:
+    float32 [out]; activation: None, "relu", "gelu" (the exact form) or "silu";
+    residual: [..., out] of the result's type.  The result has ``out_dtype`` (x's type,
+    the default, or float32) or is ``out``, which may be residual.  Sums are fp32;
+    each result is rounded once.  ``status`` (int64, one value on the device)
+    receives -1, or -2 if a device wait gave up (the results are undefined then)."""
+    if stream is not None:
+        return _under(stream, linear_forward, x, weight, bias, activation, residual, keep, out,
+                      out_dtype, status)
+    device = _device()
+    act = _activation(activation)
+    if keep and not act:
+        raise ValueError("keep needs an activation")
+    tokens, n, xs = _rows(x, "x", device)
+    _half(x, "x")
+    pw, wi, wo = _weight(weight, "weight", device, (x.dtype,))
+    m = weight.shape[1]
+    if weight.shape[0] != n:
+        raise ValueError(f"weight must have {n} rows, got {weight.shape[0]}")
+    kind = out.dtype if out is not None and out_dtype is None else out_dtype or x.dtype
+    if kind != x.dtype and kind != torch.float32:
+        raise TypeError(f"out_dtype must be {x.dtype} or torch.float32, got {kind}")
+    out, ys = _result(out, x, m, kind, "out", device)
+    pr = pz = None
+    rs = zs = m
+    if residual is not None:
+        rs = _rows(residual, "residual", device, like=out, dtype=kind)[2]
+        pr = residual.data_ptr()
+    if keep:
+        z = torch.empty(out.shape, dtype=x.dtype, device=x.device)
+        pz = z.data_ptr()
+    pb = None if bias is None else _vector(bias, m, "bias", device)
+    at = _packed(_FORWARD, tokens, n, m, x.data_ptr(), xs, pw, wi, wo, pb or 0, pr or 0, rs,
+                 out.data_ptr(), ys, pz or 0, zs, _types[x.dtype], _types[kind], act, 0)
+    size = _lib.pss_linear_forward_workspace(at)
+    work = torch.empty(size, dtype=torch.uint8, device=x.device) if size else None
+    rc = _lib.pss_linear_forward(at, work.data_ptr() if size else None, size,
+                                 _status(status, device),
+                                 torch._C._cuda_getCurrentRawStream(device))
+    if rc:
+        binding._check(rc, "pss_linear_forward")
+    return (out, z) if keep else out
+
+
+def linear_backward(grad, x, weight, z=None, activation=None, dx=True, dweight=True, dbias=True,
+                    dweight_dtype=None, status=None, stream=None):
+    """(dx, dweight, dbias) of ``linear_forward`` for the upstream gradient ``grad``
+    [..., out] (pss_linear_backward), which itself is the residual's gradient.
+
+    grad: x's type or float32; z: the forward call's, with an activation.  Each of
+    dx, dweight and dbias is True, False (not wanted: None is returned) or the
+    tensor to fill.  dx has x's type and shape; dweight lies in memory as weight does,
+    in ``dweight_dtype`` (weight's type, the default, or float32); dbias is float32.
+    grad * act'(z) enters the products rounded to x's type, and dbias unrounded."""
+    if stream is not None:
+        return _under(stream, linear_backward, grad, x, weight, z, activation, dx, dweight, dbias,
+                      dweight_dtype, status)
+    device = _device()
+    act = _activation(activation)
+    tokens, n, xs = _rows(x, "x", device)
+    _half(x, "x")
+    pw, wi, wo = _weight(weight, "weight", device, (x.dtype,))
+    m = weight.shape[1]
+    if weight.shape[0] != n:
+        raise ValueError(f"weight must have {n} rows, got {weight.shape[0]}")
+    _, gm, gs = _rows(grad, "grad", device)
+    if grad.shape[:-1] != x.shape[:-1] or gm != m:
+        raise ValueError(f"grad must have shape {(*x.shape[:-1], m)}, got {tuple(grad.shape)}")
+    if grad.dtype != x.dtype and grad.dtype != torch.float32:
+        raise TypeError(f"grad must be {x.dtype} or torch.float32, got {grad.dtype}")
+    pz, zs = 0, m
+    if act:
+        if z is None:
+            raise ValueError("z is needed with an activation")
+        pz, zs = z.data_ptr(), _rows(z, "z", device, like=grad, dtype=x.dtype)[2]
+    px = pdw = pb = 0
+    dxs, dwi, dwo = n, 0, 0
+    kind = weight.dtype
+    if dx is False or dx is None:
+        dx = None
+    else:
+        dx, dxs = _result(None if dx is True else dx, x, n, x.dtype, "dx", device)
+        px = dx.data_ptr()
+    if dweight is False or dweight is None:
+        dweight = None
+    else:
+        if dweight is True:
+            kind = dweight_dtype or weight.dtype
+            if wo == 1 or m == 1:
+                dweight = torch.empty((n, m), dtype=kind, device=x.device)
+            else:
+                dweight = torch.empty((m, n), dtype=kind, device=x.device).t()
+        elif dweight_dtype is not None and dweight.dtype != dweight_dtype:
+            raise TypeError(f"dweight must be {dweight_dtype}, got {dweight.dtype}")
+        pdw, dwi, dwo = _weight(dweight, "dweight", device, (x.dtype, torch.float32), weight.shape)
+        kind = dweight.dtype
+    if dbias is False or dbias is None:
+        dbias = None
+    else:
+        if dbias is True:
+            dbias = torch.empty(m, dtype=torch.float32, device=x.device)
+        pb = _vector(dbias, m, "dbias", device)
+    at = _packed(_BACKWARD, tokens, n, m, grad.data_ptr(), gs, x.data_ptr(), xs, pw, wi, wo, pz, zs,
+                 px, dxs, pdw, dwi, dwo, pb, _types[x.dtype], _types[grad.dtype], _types[kind], act)
+    size = _lib.pss_linear_backward_workspace(at)
+    work = torch.empty(size, dtype=torch.uint8, device=x.device) if size else None
+    rc = _lib.pss_linear_backward(at, work.data_ptr() if size else None, size,
+                                  _status(status, device),
+                                  torch._C._cuda_getCurrentRawStream(device))
+    if rc:
+        binding._check(rc, "pss_linear_backward")
+    return dx, dweight, dbias
