@@ -6,13 +6,34 @@
 namespace pss {
 namespace seq {
 
-constexpr float kRootHalf = 0.70710678118654752f;
 constexpr float kInvRoot2Pi = 0.39894228040143268f;
+
+// Phi(-a) = exp(-a^2 / 2) P(t) for a >= 0, t = 1 / (1 + 0.23 a): P is the polynomial of degree 8
+// nearest to erfcx(a / sqrt 2) / 2 in relative error on 0 <= a <= 15 (a least-squares fit
+// with weights raised where it is worst; 4.8e-8, and 4.3e-7 evaluated in fp32).  gelu and its slope
+// share the exponential, and both ends keep their relative accuracy.  CUDA's erfcf, which is
+// exact to a few units, made the pass over the gradient of 16384 x 4096 144 us instead of SLOPE.
+__device__ __forceinline__ float normal_below(float a, float e) {
+    const float t = __fdividef(1.f, fmaf(0.23f, a, 1.f));
+    float p = -0.07848794013261795f;
+    p = fmaf(p, t, 0.2905181646347046f);
+    p = fmaf(p, t, -0.2783527970314026f);
+    p = fmaf(p, t, 0.30174607038497925f);
+    p = fmaf(p, t, -0.033121444284915924f);
+    p = fmaf(p, t, 0.11960627138614655f);
+    p = fmaf(p, t, 0.08573728799819946f);
+    p = fmaf(p, t, 0.09238240122795105f);
+    p = fmaf(p, t, -2.8019605451845564e-05f);
+    return e * p;
+}
 
 template <int ACT>
 __device__ __forceinline__ float activate(float z) {
     if (ACT == ACT_RELU) return z < 0.f ? 0.f : z;   // NaN stays
-    if (ACT == ACT_GELU) return 0.5f * z * erfcf(-kRootHalf * z);
+    if (ACT == ACT_GELU) {
+        const float q = normal_below(fabsf(z), __expf(-0.5f * z * z));
+        return z < 0.f ? z * q : z - z * q;
+    }
     if (ACT == ACT_SILU) {
         const float e = __expf(-fabsf(z)), inv = __fdividef(z, 1.f + e);
         return z < 0.f ? e * inv : inv;
@@ -23,8 +44,10 @@ __device__ __forceinline__ float activate(float z) {
 template <int ACT>
 __device__ __forceinline__ float slope_of(float z) {
     if (ACT == ACT_RELU) return z > 0.f ? 1.f : z <= 0.f ? 0.f : z;
-    if (ACT == ACT_GELU)
-        return 0.5f * erfcf(-kRootHalf * z) + z * kInvRoot2Pi * __expf(-0.5f * z * z);
+    if (ACT == ACT_GELU) {
+        const float e = __expf(-0.5f * z * z), q = normal_below(fabsf(z), e);
+        return (z < 0.f ? q : 1.f - q) + z * kInvRoot2Pi * e;
+    }
     if (ACT == ACT_SILU) {
         const float e = __expf(-fabsf(z)), inv = __fdividef(1.f, 1.f + e);
         const float s = z < 0.f ? e * inv : inv;

@@ -21,8 +21,10 @@ using namespace pss::seq;
 namespace {
 
 constexpr int kPer = 8;          // values of a row that a thread holds
-constexpr int kChunk = 64;       // sorted places of a piece, and pieces of a large piece
-constexpr int kLarge = kChunk * kChunk;
+constexpr int kChunk = 32;       // sorted places of a piece
+constexpr int kPieces = 64;      // pieces of a large piece
+constexpr int kLarge = kChunk * kPieces;
+constexpr int kRows = 8;         // rows of the table that a group sums
 constexpr int kSmall = 4096;     // tokens that one CTA sorts
 constexpr int kSortThreads = 1024;
 constexpr uint32_t kNone = 0xffffffffu;
@@ -70,8 +72,8 @@ struct Piece {
 };
 
 // A group's number and the block of its row's values.
-__device__ __forceinline__ int64_t group_of(const Spread& s, int* block) {
-    const int64_t g = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) >> s.log2_lanes;
+__device__ __forceinline__ int64_t group_of(const Spread& s, unsigned cta, int* block) {
+    const int64_t g = ((int64_t)cta * blockDim.x + threadIdx.x) >> s.log2_lanes;
     if (s.blocks == 1) {
         *block = 0;
         return g;
@@ -93,7 +95,7 @@ k_embedding_forward(const TW* __restrict__ weight, int64_t ws, int64_t rows,
                     int64_t os, unsigned long long* status, Spread s) {
     pdl_prologue();
     int block;
-    const int64_t t0 = group_of(s, &block) * U;
+    const int64_t t0 = group_of(s, blockIdx.x, &block) * U;
     const Piece<VECTOR> piece(s, block);
     if (!piece.any() || t0 >= tokens) return;
     int64_t id[U];
@@ -134,47 +136,76 @@ k_embedding_keys(const int64_t* __restrict__ ids, int64_t tokens, int64_t rows, 
     places[t] = (uint32_t)t;
 }
 
-// Up to kSmall tokens in one CTA's shared memory: id << 32 | place, all different, so
-// that any sort of them is stable.
+// Up to kSmall tokens in one CTA: id << 32 | place, all different, so that any sort of them
+// is stable.  A bitonic sort of 1024 E entries, entry x * 1024 + t in thread t's register x:
+// exchanges below 32 go through shuffles, between registers through none, the others through
+// shared memory.
+template <int E>
 __global__ void __launch_bounds__(kSortThreads)
-k_embedding_sort(const int64_t* __restrict__ ids, int tokens, int size, int64_t rows,
+k_embedding_sort(const int64_t* __restrict__ ids, int tokens, int64_t rows,
                  unsigned long long* __restrict__ sorted, unsigned long long* __restrict__ count,
                  unsigned long long* status) {
     pdl_prologue();
-    __shared__ unsigned long long e[kSmall];
+    __shared__ unsigned long long shared[E * kSortThreads];
     __shared__ int valid;
-    if (threadIdx.x == 0) valid = 0;
+    const int t = threadIdx.x;
+    if (t == 0) valid = 0;
     __syncthreads();
+    unsigned long long v[E];
     int mine = 0;
-    for (int t = threadIdx.x; t < size; t += kSortThreads) {
-        unsigned long long v = ~0ull;
-        if (t < tokens) {
-            const int64_t id = ids[t];
-            if ((uint64_t)id < (uint64_t)rows) {
-                v = ((unsigned long long)id << 32) | (unsigned)t;
-                ++mine;
-            } else {
-                note_outside(status, t);
-            }
-        }
-        e[t] = v;
+#pragma unroll
+    for (int x = 0; x < E; ++x) {
+        const int i = x * kSortThreads + t;
+        const int64_t id = i < tokens ? ids[i] : -1;
+        const bool in = (uint64_t)id < (uint64_t)rows;
+        if (!in && i < tokens) note_outside(status, i);
+        v[x] = in ? ((unsigned long long)id << 32) | (unsigned)i : ~0ull;
+        mine += in;
     }
     if (mine) atomicAdd(&valid, mine);
-    __syncthreads();
+    int size = 1;
+    while (size < tokens) size *= 2;
     for (int k = 2; k <= size; k *= 2)
         for (int j = k / 2; j > 0; j /= 2) {
-            for (int i = threadIdx.x; i < size / 2; i += kSortThreads) {
-                const int a = 2 * i - (i & (j - 1)), b = a + j;
-                const unsigned long long x = e[a], y = e[b];
-                if ((x > y) == ((a & k) == 0)) {
-                    e[a] = y;
-                    e[b] = x;
-                }
+            if (j >= kSortThreads) {
+                const int d = j / kSortThreads;
+#pragma unroll
+                for (int x = 0; x < E; ++x)
+#pragma unroll
+                    for (int y = x + 1; y < E; ++y) {
+                        if ((x ^ y) != d) continue;
+                        const bool up = ((x * kSortThreads + t) & k) == 0;
+                        if ((v[x] > v[y]) == up) {
+                            const unsigned long long w = v[x];
+                            v[x] = v[y];
+                            v[y] = w;
+                        }
+                    }
+                continue;
             }
-            __syncthreads();
+            unsigned long long other[E];
+            if (j >= 32) {
+                __syncthreads();
+#pragma unroll
+                for (int x = 0; x < E; ++x) shared[x * kSortThreads + t] = v[x];
+                __syncthreads();
+#pragma unroll
+                for (int x = 0; x < E; ++x) other[x] = shared[x * kSortThreads + (t ^ j)];
+            } else {
+#pragma unroll
+                for (int x = 0; x < E; ++x) other[x] = __shfl_xor_sync(0xffffffffu, v[x], j);
+            }
+#pragma unroll
+            for (int x = 0; x < E; ++x) {
+                const bool up = ((x * kSortThreads + t) & k) == 0, low = (t & j) == 0;
+                if ((v[x] > other[x]) == (up == low)) v[x] = other[x];
+            }
         }
-    for (int t = threadIdx.x; t < valid; t += kSortThreads) sorted[t] = e[t];
-    if (threadIdx.x == 0) *count = (unsigned long long)valid;
+    __syncthreads();
+#pragma unroll
+    for (int x = 0; x < E; ++x)
+        if (x * kSortThreads + t < valid) sorted[x * kSortThreads + t] = v[x];
+    if (t == 0) *count = (unsigned long long)valid;
 }
 
 // ---- sums --------------------------------------------------------------------
@@ -196,7 +227,7 @@ k_embedding_pieces(const TG* __restrict__ grad, int64_t gs,
                    int64_t sums_stride, Spread s) {
     pdl_prologue();
     int block;
-    const int64_t c = group_of(s, &block), i0 = c * kChunk;
+    const int64_t c = group_of(s, blockIdx.x, &block), i0 = c * kChunk;
     const Piece<VECTOR> piece(s, block);
     if (!piece.any() || i0 + kChunk > (int64_t)*count ||
         key_of(sorted[i0]) != key_of(sorted[i0 + kChunk - 1]))
@@ -217,7 +248,7 @@ k_embedding_pieces(const TG* __restrict__ grad, int64_t gs,
     piece.store(sums + c * sums_stride, sum);
 }
 
-// kChunk pieces of one id again.
+// kPieces pieces of one id again.
 template <bool VECTOR>
 __global__ void __launch_bounds__(kThreads)
 k_embedding_large_pieces(const float* __restrict__ sums, int64_t sums_stride,
@@ -226,17 +257,17 @@ k_embedding_large_pieces(const float* __restrict__ sums, int64_t sums_stride,
                          Spread s) {
     pdl_prologue();
     int block;
-    const int64_t c = group_of(s, &block), i0 = c * kLarge;
+    const int64_t c = group_of(s, blockIdx.x, &block), i0 = c * kLarge;
     const Piece<VECTOR> piece(s, block);
     if (!piece.any() || i0 + kLarge > (int64_t)*count ||
         key_of(sorted[i0]) != key_of(sorted[i0 + kLarge - 1]))
         return;
     constexpr int U = 8;
     float sum[kPer] = {};
-    for (int i = 0; i < kChunk; i += U) {
+    for (int i = 0; i < kPieces; i += U) {
         Raw8<float> raw[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) raw[u] = piece.load(sums + (c * kChunk + i + u) * sums_stride);
+        for (int u = 0; u < U; ++u) raw[u] = piece.load(sums + (c * kPieces + i + u) * sums_stride);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             float v[kPer];
@@ -247,85 +278,134 @@ k_embedding_large_pieces(const float* __restrict__ sums, int64_t sums_stride,
     piece.store(large + c * sums_stride, sum);
 }
 
-// A group to `per` rows of the table: their places in the sorted list by bisection,
-// then one pass over these, U entries' loads in flight whichever rows they belong to.
+// The first place of lo .. hi whose key is at or behind v, or hi.
+__device__ __forceinline__ int first_place(const unsigned long long* __restrict__ sorted, int lo,
+                                           int hi, int64_t v) {
+    while (lo < hi) {
+        const int m = (int)(((unsigned)lo + (unsigned)hi) >> 1);
+        if (key_of(sorted[m]) < v)
+            lo = m + 1;
+        else
+            hi = m;
+    }
+    return lo;
+}
+
+// Whether the run from .. to holds a whole piece.
+__device__ __forceinline__ bool is_long(int from, int to) {
+    return (from + kChunk - 1) / kChunk * kChunk + kChunk <= to;
+}
+
+// The sums of the table's rows.  CTAs up to long_ctas: a group to a piece, which answers for
+// its row where it is the first whole piece of the run: head, pieces (kPieces of them at
+// once where these were summed) and tail.  The others: a group to kRows rows, whose places its
+// lanes find by bisection; then one pass over the short runs, U entries' loads in flight
+// whichever rows these belong to.  (All runs in that pass: 943 us for the popular ids of a
+// batch of 1.7 M x 128, the chains of a few groups.)
 template <typename TG, typename TO, bool VECTOR>
 __global__ void __launch_bounds__(kThreads)
 k_embedding_rows(const TG* __restrict__ grad, int64_t gs,
                  const unsigned long long* __restrict__ sorted,
                  const unsigned long long* __restrict__ count, const float* __restrict__ sums,
                  const float* __restrict__ large, int64_t sums_stride, float scale, TO* out,
-                 int64_t os, int64_t rows, int per, Spread s) {
+                 int64_t os, int64_t rows, unsigned long_ctas, Spread s) {
     pdl_prologue();
-    int block;
-    const int64_t v0 = group_of(s, &block) * per, v1 = v0 + per < rows ? v0 + per : rows;
-    const Piece<VECTOR> piece(s, block);
-    if (!piece.any() || v0 >= rows) return;
-    // the first place at or behind v0, and at or behind v1
-    int64_t i = 0, end = 0;
-    {
-        int64_t a = (int64_t)*count, b = a;
-        while (i < a || end < b) {
-            const int64_t m = (i + a) >> 1, n = (end + b) >> 1;
-            const uint32_t x = i < a ? key_of(sorted[m]) : 0u, y = end < b ? key_of(sorted[n]) : 0u;
-            if (i < a) {
-                if (x < v0) i = m + 1;
-                else a = m;
-            }
-            if (end < b) {
-                if (y < v1) end = n + 1;
-                else b = n;
-            }
-        }
-    }
-    const float none[kPer] = {};
+    constexpr int U = 8;
+    __shared__ int places[kThreads][kRows + 1];
+    const int n = (int)*count;
     float sum[kPer] = {};
-    int64_t row = v0;
-    auto leave = [&](int64_t to) {   // store the row, and zeros up to `to`
-        float v[kPer];
+    int block;
+    if (blockIdx.x < long_ctas) {
+        const int64_t c64 = group_of(s, blockIdx.x, &block);
+        const Piece<VECTOR> piece(s, block);
+        if (!piece.any() || (c64 + 1) * kChunk > n) return;
+        const int c = (int)c64, at = c * kChunk;
+        const uint32_t k = key_of(sorted[at]);
+        if (k != key_of(sorted[at + kChunk - 1]) ||
+            (at > 0 && key_of(sorted[at - kChunk]) == k))
+            return;
+        const int begin = first_place(sorted, at > 0 ? at - kChunk + 1 : 0, at, k);
+        const int end = first_place(sorted, at + kChunk, n, (int64_t)k + 1), last = end / kChunk;
+        auto add = [&](int from, int to, auto load) {
+            for (int i = from; i < to; i += U) {
+                decltype(load(i)) raw[U];
 #pragma unroll
-        for (int e = 0; e < kPer; ++e) {
-            v[e] = sum[e] * scale;
-            sum[e] = 0.f;
-        }
-        piece.store(out + row * os, v);
-        for (++row; row < to; ++row) piece.store(out + row * os, none);
-    };
-    constexpr int U = 4;
-    while (i < end) {
-        if (i % kChunk == 0 && i + kChunk <= end) {
-            const uint32_t k = key_of(sorted[i]);
-            if (k == key_of(sorted[i + kChunk - 1])) {
-                if (k != row) leave(k);
-                const bool more = i % kLarge == 0 && i + kLarge <= end &&
-                                  k == key_of(sorted[i + kLarge - 1]);
-                float v[kPer];
-                unpack(piece.load(more ? large + i / kLarge * sums_stride
-                                       : sums + i / kChunk * sums_stride), v);
-                add_to(sum, v);
-                i += more ? kLarge : kChunk;
-                continue;
+                for (int u = 0; u < U; ++u)
+                    if (i + u < to) raw[u] = load(i + u);
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    if (i + u >= to) break;
+                    float v[kPer];
+                    unpack(raw[u], v);
+                    add_to(sum, v);
+                }
             }
+        };
+        auto entry = [&](int i) { return piece.load(grad + (uint32_t)sorted[i] * gs); };
+        auto of_piece = [&](int i) { return piece.load(sums + i * sums_stride); };
+        auto of_large = [&](int i) { return piece.load(large + i * sums_stride); };
+        const int l0 = (c + kPieces - 1) / kPieces, l1 = last / kPieces;
+        add(begin, at, entry);
+        if (l1 > l0) {
+            add(c, l0 * kPieces, of_piece);
+            add(l0, l1, of_large);
+            add(l1 * kPieces, last, of_piece);
+        } else {
+            add(c, last, of_piece);
         }
-        unsigned long long e[U];
-        Raw8<TG> raw[U];
-        const int n = (int)(end - i < U - i % U ? end - i : U - i % U);
+        add(last * kChunk, end, entry);
 #pragma unroll
-        for (int u = 0; u < U; ++u) e[u] = u < n ? sorted[i + u] : 0ull;
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            raw[u] = u < n ? piece.load(grad + (uint32_t)e[u] * gs) : Raw8<TG>{};
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (u >= n) break;
-            if (key_of(e[u]) != row) leave(key_of(e[u]));
-            float v[kPer];
-            unpack(raw[u], v);
-            add_to(sum, v);
-        }
-        i += n;
+        for (int e = 0; e < kPer; ++e) sum[e] *= scale;
+        piece.store(out + (int64_t)k * os, sum);
+        return;
     }
-    leave(v1);
+    const int64_t v0 = group_of(s, blockIdx.x - long_ctas, &block) * kRows;
+    const Piece<VECTOR> piece(s, block);
+    const int lanes = 1 << s.log2_lanes, lane = threadIdx.x & (lanes - 1);
+    const int some = rows - v0 < kRows ? (int)(rows - v0) : kRows;   // may be below 1
+    int* place = places[threadIdx.x >> s.log2_lanes];
+    for (int j = lane; j <= some; j += lanes) place[j] = first_place(sorted, 0, n, v0 + j);
+    __syncwarp();
+    if (!piece.any() || some < 1) return;
+    const float none[kPer] = {};
+    for (int r = 0; r < some; ++r) {
+        if (is_long(place[r], place[r + 1])) continue;
+        int to = r;   // rows r .. to are short
+        while (to + 1 < some && !is_long(place[to + 1], place[to + 2])) ++to;
+        int i = place[r];
+        const int end = place[to + 1];
+        int64_t row = v0 + r;
+        auto leave = [&](int64_t next) {   // store the row, and zeros up to the next
+            float v[kPer];
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) {
+                v[e] = sum[e] * scale;
+                sum[e] = 0.f;
+            }
+            piece.store(out + row * os, v);
+            for (++row; row < next; ++row) piece.store(out + row * os, none);
+        };
+        while (i < end) {
+            unsigned long long e[U];
+            Raw8<TG> raw[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) e[u] = i + u < end ? sorted[i + u] : 0ull;
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (i + u < end) raw[u] = piece.load(grad + (uint32_t)e[u] * gs);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (i + u >= end) break;
+                if (key_of(e[u]) != row) leave(key_of(e[u]));
+                float v[kPer];
+                unpack(raw[u], v);
+                add_to(sum, v);
+            }
+            i += U;
+        }
+        leave(v0 + to + 1);
+        r = to;
+    }
 }
 
 // ---- host --------------------------------------------------------------------
@@ -385,10 +465,11 @@ int64_t lay_out(int64_t tokens, int64_t rows, int64_t cols, void* base, Work* w)
 cudaError_t sort_tokens(const int64_t* ids, int64_t tokens, int64_t rows, const Work& w,
                         unsigned long long* status, cudaStream_t st) {
     if (tokens <= kSmall) {
-        int size = 1;
-        while (size < tokens) size *= 2;
-        return launch_k(k_embedding_sort, dim3(1), dim3(kSortThreads), 0, st, ids, (int)tokens,
-                        size, rows, w.sorted, w.count, status);
+        auto* k = tokens <= kSortThreads       ? k_embedding_sort<1>
+                  : tokens <= 2 * kSortThreads ? k_embedding_sort<2>
+                                               : k_embedding_sort<4>;
+        return launch_k(k, dim3(1), dim3(kSortThreads), 0, st, ids, (int)tokens, rows, w.sorted,
+                        w.count, status);
     }
     cudaError_t e = launch_k(k_embedding_keys, dim3((unsigned)((tokens + kThreads - 1) / kThreads)),
                              dim3(kThreads), 0, st, ids, tokens, rows, w.keys, w.places, w.done,
@@ -485,12 +566,7 @@ extern "C" pss_status pss_embedding_backward(const void* grad, pss_dtype grad_ty
     if (tokens > 0 && (!device_ptr(ids) || !aligned_to(ids, 8))) return PSS_ERR_INVALID_ARG;
     const bool some = rows > 0 && cols > 0;
     const Spread s = spread(cols > 0 ? cols : 1);
-    // rows of a group: few enough that all of the GPU has some
-    int per = 16;
-    while (per > 1 && (rows + per - 1) / per * s.blocks <
-                          (int64_t)sm_count() * 8 * (kThreads >> s.log2_lanes))
-        per /= 2;
-    const unsigned n = ctas((rows + per - 1) / per, s), pieces = ctas(tokens / kChunk, s);
+    const unsigned n = ctas((rows + kRows - 1) / kRows, s), pieces = ctas(tokens / kChunk, s);
     if (some) {
         if (!device_ptr(dweight) || !aligned_to(dweight, dtype_size(dweight_type)))
             return PSS_ERR_INVALID_ARG;
@@ -499,7 +575,8 @@ extern "C" pss_status pss_embedding_backward(const void* grad, pss_dtype grad_ty
              !device_ptr(workspace) || !aligned_to(workspace, 16) ||
              workspace_bytes < pss_embedding_workspace(tokens, rows, cols)))
             return PSS_ERR_INVALID_ARG;
-        if (n == 0 || (tokens >= kChunk && pieces == 0)) return PSS_ERR_UNSUPPORTED;
+        if (n == 0 || (tokens >= kChunk && pieces == 0) || (int64_t)n + pieces >= (int64_t(1) << 31))
+            return PSS_ERR_UNSUPPORTED;
     }
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     const pss_status rc = clear_status(status, st);
@@ -532,9 +609,9 @@ extern "C" pss_status pss_embedding_backward(const void* grad, pss_dtype grad_ty
         return with_type(dweight_type, [&](auto to) {
             using TO = decltype(to);
             auto* k = vector ? k_embedding_rows<TG, TO, true> : k_embedding_rows<TG, TO, false>;
-            return launch_k(k, dim3(n), dim3(kThreads), 0, st, g, grad_stride, w.sorted, w.count,
-                            w.sums, w.large, w.stride, scale, static_cast<TO*>(dweight),
-                            dweight_stride, rows, per, s);
+            return launch_k(k, dim3(n + pieces), dim3(kThreads), 0, st, g, grad_stride, w.sorted,
+                            w.count, w.sums, w.large, w.stride, scale, static_cast<TO*>(dweight),
+                            dweight_stride, rows, pieces, s);
         });
     }));
 }

@@ -456,28 +456,39 @@ cudaError_t copy_matrix(Matrix* x, void* to, cudaStream_t st) {
     return e;
 }
 
+// The width of the tiles and the parts of the contraction: the pair that leaves the fullest SM
+// the least time, by what was measured of a block (64 along the contraction) of each width, of a
+// unit's start and end, and of the parts' way through memory; in SM cycles.
 void plan_product(Product* p) {
     p->m = (int)p->a.rows();
     p->n = (int)p->b.rows();
     p->blocks = (int)((p->a.k() + kBlock - 1) / kBlock);
     p->m_tiles = (p->m + 127) / 128;
-    const int sms = sm_count() > 0 ? sm_count() : 1;
-    auto tiles = [&](int bn) { return (int64_t)p->m_tiles * ((p->n + bn - 1) / bn); };
-    p->bn = p->n <= 32 && !p->b.across ? 32 : p->n <= 64 ? 64 : p->n <= 128 ? 128 : 256;
-    while (p->bn > 64 && tiles(p->bn) < sms && tiles(p->bn / 2) <= 2 * sms) p->bn /= 2;
-    p->n_tiles = (p->n + p->bn - 1) / p->bn;
-    // Parts of the contraction: as many as give the least time of the fullest SM, a unit
-    // costing its blocks and about four more for its start and end, and each further part its
-    // values' way through memory.
-    const int64_t all = tiles(p->bn);
-    p->splits = 1;
-    int64_t best = 0;
-    for (int s = 1; s <= 32 && s <= p->blocks; ++s) {
-        const int64_t rounds = (all * s + sms - 1) / sms;
-        const int64_t cost = rounds * ((p->blocks + s - 1) / s + 4) + (s > 1 ? 8 + all * s / sms * 2 : 0);
-        if (s == 1 || cost < best) best = cost, p->splits = s;
-    }
     p->ld = ((p->f.swapped ? p->m : p->n) + 7) / 8 * 8;
+    const int sms = sm_count() > 0 ? sm_count() : 1;
+    const int widths[] = {256, 128, 64, 32}, cycles[] = {560, 330, 250, 220};
+    double best = 0;
+    p->bn = 0;
+    for (int i = 0; i < 4; ++i) {
+        const int bn = widths[i];
+        if (bn == 32 && (p->b.across || p->n > 32)) continue;   // a box across is 64 wide
+        if (bn > 64 && p->n <= bn / 2) continue;
+        const int n_tiles = (p->n + bn - 1) / bn;
+        const int64_t tiles = (int64_t)p->m_tiles * n_tiles;
+        for (int s = 1; s <= 64 && s <= p->blocks; ++s) {
+            const int64_t rounds = (tiles * s + sms - 1) / sms;
+            double cost = 2000. + (double)rounds * ((p->blocks + s - 1) / s * cycles[i] + 300.);
+            // written and read at some 1800 bytes a cycle each, and a launch
+            if (s > 1) cost += 4000. + (double)p->m * p->n * s * 8 / 1800;
+            if (p->bn == 0 || cost < best) {
+                best = cost;
+                p->bn = bn;
+                p->n_tiles = n_tiles;
+                p->splits = s;
+            }
+            if (tiles * s >= 16 * sms) break;
+        }
+    }
 }
 
 int64_t partial_values(const Product& p) {

@@ -17,7 +17,13 @@ namespace pss {
 namespace seq {
 
 constexpr int kNormMaxCols = 16384;
-constexpr int kNormPerSm = 4;   // CTAs an SM, at most, that the backward's partial sums have room for
+
+// CTAs an SM, at most, that the backward's partial sums have room for: 1024 threads' worth
+// (40001 x 333 with four of 64 threads: 182 us).
+inline int norm_per_sm(int64_t cols) {
+    const int64_t threads = cols <= 256 ? 256 : cols <= 4096 ? (cols + 255) / 256 * 32 : 512;
+    return (int)(1024 / threads);
+}
 
 // Rows up to 32 lanes' vectors: several to a CTA of 256 threads, within shuffles.  Up to
 // 512 threads': a CTA to a row, the next row's loads ahead.  Above: two vectors to a

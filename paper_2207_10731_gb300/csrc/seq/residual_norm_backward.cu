@@ -239,7 +239,7 @@ k_residual_norm_backward(const __grid_constant__ Backward<T, R> a) {
 
 extern "C" int64_t pss_residual_norm_workspace(int64_t rows, int64_t cols) {
     if (rows < 1 || cols < 1 || cols > kNormMaxCols) return 0;
-    const int64_t most = (int64_t)kNormPerSm * sm_count();
+    const int64_t most = (int64_t)norm_per_sm(cols) * sm_count();
     return (rows < most ? rows : most) * 8 * cols;
 }
 
@@ -317,7 +317,7 @@ extern "C" pss_status pss_residual_norm_backward(
                                          (int)smem);
             if (e != cudaSuccess) return e;
             const int n = ctas_of(
-                rows, s, [&] { return resident(kernel, s.threads, smem, kNormPerSm); },
+                rows, s, [&] { return resident(kernel, s.threads, smem, norm_per_sm(cols)); },
                 decltype(mode)::value);
             e = launch_k(kernel, dim3(n), dim3(s.threads), smem, st, f);
             if (e != cudaSuccess || !sums) return e;
