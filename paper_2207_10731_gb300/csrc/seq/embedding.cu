@@ -4,8 +4,8 @@
 // Backward: dweight[v] = scale * sum over t with ids[t] = v of grad[t].
 //
 // Both are bound by memory.  Backward, the token positions are sorted by id, stable
-// (one CTA's bitonic sort up to kSmall tokens, else the radix sort of the shared
-// array's backward), so that each row of the table is summed by one group of threads
+// (by counting up to kSmall tokens, else by the radix sort of the shared array's
+// backward), so that each row of the table is summed by one group of threads
 // in the order of the tokens and stored once, rows without a token as zeros: no
 // atomics, and equal inputs give equal bits.  A popular id's run would be one group's
 // long chain: runs are cut at multiples of kChunk sorted places, the pieces that lie
@@ -25,8 +25,7 @@ constexpr int kChunk = 32;       // sorted places of a piece
 constexpr int kPieces = 64;      // pieces of a large piece
 constexpr int kLarge = kChunk * kPieces;
 constexpr int kRows = 8;         // rows of the table that a group sums
-constexpr int kSmall = 4096;     // tokens that one CTA sorts
-constexpr int kSortThreads = 1024;
+constexpr int kSmall = 8192;     // tokens that are ranked instead of sorted
 constexpr uint32_t kNone = 0xffffffffu;
 
 // How a row is spread: `lanes` threads (a power of two up to 32) to a block of 8 * lanes
@@ -136,76 +135,52 @@ k_embedding_keys(const int64_t* __restrict__ ids, int64_t tokens, int64_t rows, 
     places[t] = (uint32_t)t;
 }
 
-// Up to kSmall tokens in one CTA: id << 32 | place, all different, so that any sort of them
-// is stable.  A bitonic sort of 1024 E entries, entry x * 1024 + t in thread t's register x:
-// exchanges below 32 go through shuffles, between registers through none, the others through
-// shared memory.
-template <int E>
-__global__ void __launch_bounds__(kSortThreads)
-k_embedding_sort(const int64_t* __restrict__ ids, int tokens, int64_t rows,
+// Up to kSmall tokens: a token's place is the number of smaller ids and of equal ones in front
+// of it, counted by a warp for kRanked tokens at a time against all ids in shared memory.
+// (One CTA's bitonic sort of 2011: 15 us, its steps in turn, against 6.5; here CTAs know
+// nothing of each other.)
+constexpr int kRanked = 4;
+__global__ void __launch_bounds__(kThreads)
+k_embedding_rank(const int64_t* __restrict__ ids, int tokens, int64_t rows,
                  unsigned long long* __restrict__ sorted, unsigned long long* __restrict__ count,
                  unsigned long long* status) {
     pdl_prologue();
-    __shared__ unsigned long long shared[E * kSortThreads];
-    __shared__ int valid;
-    const int t = threadIdx.x;
-    if (t == 0) valid = 0;
-    __syncthreads();
-    unsigned long long v[E];
-    int mine = 0;
-#pragma unroll
-    for (int x = 0; x < E; ++x) {
-        const int i = x * kSortThreads + t;
-        const int64_t id = i < tokens ? ids[i] : -1;
+    extern __shared__ __align__(16) uint32_t keys[];   // kNone: outside the table, and past the end
+    const int lane = threadIdx.x & 31, all = (tokens + 127) / 128 * 128;
+    int valid = 0;
+    for (int t0 = 0; t0 < all; t0 += kThreads) {
+        const int t = t0 + threadIdx.x;
+        const int64_t id = t < tokens ? ids[t] : -1;
         const bool in = (uint64_t)id < (uint64_t)rows;
-        if (!in && i < tokens) note_outside(status, i);
-        v[x] = in ? ((unsigned long long)id << 32) | (unsigned)i : ~0ull;
-        mine += in;
-    }
-    if (mine) atomicAdd(&valid, mine);
-    int size = 1;
-    while (size < tokens) size *= 2;
-    for (int k = 2; k <= size; k *= 2)
-        for (int j = k / 2; j > 0; j /= 2) {
-            if (j >= kSortThreads) {
-                const int d = j / kSortThreads;
-#pragma unroll
-                for (int x = 0; x < E; ++x)
-#pragma unroll
-                    for (int y = x + 1; y < E; ++y) {
-                        if ((x ^ y) != d) continue;
-                        const bool up = ((x * kSortThreads + t) & k) == 0;
-                        if ((v[x] > v[y]) == up) {
-                            const unsigned long long w = v[x];
-                            v[x] = v[y];
-                            v[y] = w;
-                        }
-                    }
-                continue;
-            }
-            unsigned long long other[E];
-            if (j >= 32) {
-                __syncthreads();
-#pragma unroll
-                for (int x = 0; x < E; ++x) shared[x * kSortThreads + t] = v[x];
-                __syncthreads();
-#pragma unroll
-                for (int x = 0; x < E; ++x) other[x] = shared[x * kSortThreads + (t ^ j)];
-            } else {
-#pragma unroll
-                for (int x = 0; x < E; ++x) other[x] = __shfl_xor_sync(0xffffffffu, v[x], j);
-            }
-#pragma unroll
-            for (int x = 0; x < E; ++x) {
-                const bool up = ((x * kSortThreads + t) & k) == 0, low = (t & j) == 0;
-                if ((v[x] > other[x]) == (up == low)) v[x] = other[x];
-            }
+        if (t < all) keys[t] = in ? (uint32_t)id : kNone;
+        if (blockIdx.x == 0) {
+            if (!in && t < tokens) note_outside(status, t);
+            valid += __syncthreads_count(in);
         }
+    }
+    if (blockIdx.x == 0 && threadIdx.x == 0) *count = (unsigned long long)valid;
     __syncthreads();
+    const int t0 = (blockIdx.x * kWarps + (threadIdx.x >> 5)) * kRanked;
+    if (t0 >= tokens) return;
+    uint32_t k[kRanked];
+    int rank[kRanked] = {};
 #pragma unroll
-    for (int x = 0; x < E; ++x)
-        if (x * kSortThreads + t < valid) sorted[x * kSortThreads + t] = v[x];
-    if (t == 0) *count = (unsigned long long)valid;
+    for (int x = 0; x < kRanked; ++x) k[x] = keys[t0 + x];
+    for (int j = 4 * lane; j < all; j += 128) {
+        const uint4 w = *reinterpret_cast<const uint4*>(keys + j);
+        const uint32_t v[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+            for (int x = 0; x < kRanked; ++x)
+                rank[x] += v[e] < k[x] || (v[e] == k[x] && j + e < t0 + x);
+    }
+#pragma unroll
+    for (int x = 0; x < kRanked; ++x) {
+        rank[x] = __reduce_add_sync(0xffffffffu, rank[x]);
+        if (lane == x && k[x] != kNone)
+            sorted[rank[x]] = ((unsigned long long)k[x] << 32) | (unsigned)(t0 + x);
+    }
 }
 
 // ---- sums --------------------------------------------------------------------
@@ -220,7 +195,7 @@ __device__ __forceinline__ void add_to(float (&sum)[kPer], const float (&v)[kPer
 // A group to a piece of kChunk sorted places that belong to one id: its sum in fp32.
 // Other pieces are left alone (and never read).
 template <typename TG, bool VECTOR>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, 2)
 k_embedding_pieces(const TG* __restrict__ grad, int64_t gs,
                    const unsigned long long* __restrict__ sorted,
                    const unsigned long long* __restrict__ count, float* __restrict__ sums,
@@ -232,12 +207,16 @@ k_embedding_pieces(const TG* __restrict__ grad, int64_t gs,
     if (!piece.any() || i0 + kChunk > (int64_t)*count ||
         key_of(sorted[i0]) != key_of(sorted[i0 + kChunk - 1]))
         return;
-    constexpr int U = 8;
+    constexpr int U = 32 / sizeof(TG);
     float sum[kPer] = {};
+#pragma unroll 1
     for (int i = 0; i < kChunk; i += U) {
+        uint32_t t[U];
         Raw8<TG> raw[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) raw[u] = piece.load(grad + (uint32_t)sorted[i0 + i + u] * gs);
+        for (int u = 0; u < U; ++u) t[u] = (uint32_t)sorted[i0 + i + u];
+#pragma unroll
+        for (int u = 0; u < U; ++u) raw[u] = piece.load(grad + t[u] * gs);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             float v[kPer];
@@ -291,6 +270,23 @@ __device__ __forceinline__ int first_place(const unsigned long long* __restrict_
     return lo;
 }
 
+// The same in all of the list, by a warp: 32 places a step.
+__device__ __forceinline__ int first_place_warp(const unsigned long long* __restrict__ sorted,
+                                                int n, int64_t v) {
+    const int lane = threadIdx.x & 31;
+    int lo = 0, hi = n;
+    while (lo < hi) {
+        // places lo + step, lo + 2 step ..: the answer lies behind the last smaller key
+        const int step = (hi - lo + 32) / 33, at = lo + (lane + 1) * step - 1;
+        const unsigned less = __ballot_sync(0xffffffffu, at < hi && key_of(sorted[at]) < v);
+        const int k = __popc(less);   // keys do not fall: the first k lanes say yes
+        const int from = lo + k * step;
+        if (k < 32) hi = min(hi, from + step - 1);
+        lo = min(from, hi);
+    }
+    return lo;
+}
+
 // Whether the run from .. to holds a whole piece.
 __device__ __forceinline__ bool is_long(int from, int to) {
     return (from + kChunk - 1) / kChunk * kChunk + kChunk <= to;
@@ -303,15 +299,15 @@ __device__ __forceinline__ bool is_long(int from, int to) {
 // whichever rows these belong to.  (All runs in that pass: 943 us for the popular ids of a
 // batch of 1.7 M x 128, the chains of a few groups.)
 template <typename TG, typename TO, bool VECTOR>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, 3)
 k_embedding_rows(const TG* __restrict__ grad, int64_t gs,
                  const unsigned long long* __restrict__ sorted,
                  const unsigned long long* __restrict__ count, const float* __restrict__ sums,
                  const float* __restrict__ large, int64_t sums_stride, float scale, TO* out,
                  int64_t os, int64_t rows, unsigned long_ctas, Spread s) {
     pdl_prologue();
-    constexpr int U = 8;
-    __shared__ int places[kThreads][kRows + 1];
+    constexpr int U = 16 / sizeof(TG);
+    __shared__ int places[kThreads][kRows + 1], ends[2];
     const int n = (int)*count;
     float sum[kPer] = {};
     int block;
@@ -364,7 +360,21 @@ k_embedding_rows(const TG* __restrict__ grad, int64_t gs,
     const int lanes = 1 << s.log2_lanes, lane = threadIdx.x & (lanes - 1);
     const int some = rows - v0 < kRows ? (int)(rows - v0) : kRows;   // may be below 1
     int* place = places[threadIdx.x >> s.log2_lanes];
-    for (int j = lane; j <= some; j += lanes) place[j] = first_place(sorted, 0, n, v0 + j);
+    // the CTA's rows lie side by side: two warps find their ends in the list, and each row is
+    // looked for between these (all in the whole list: 20 steps a row, 317 instead of 240 us for a
+    // million rows; the runs' ends noted in a table beforehand: 233, and two launches more)
+    {
+        const int64_t cta = blockIdx.x - long_ctas, per = kThreads >> s.log2_lanes;
+        const int64_t first = cta * per / s.blocks * kRows;
+        const int64_t last = (((cta + 1) * per - 1) / s.blocks + 1) * kRows;
+        const int warp = threadIdx.x >> 5;
+        if (warp < 2) {
+            const int at = first_place_warp(sorted, n, warp == 0 ? first : last);
+            if ((threadIdx.x & 31) == 0) ends[warp] = at;
+        }
+    }
+    __syncthreads();
+    for (int j = lane; j <= some; j += lanes) place[j] = first_place(sorted, ends[0], ends[1], v0 + j);
     __syncwarp();
     if (!piece.any() || some < 1) return;
     const float none[kPer] = {};
@@ -465,11 +475,9 @@ int64_t lay_out(int64_t tokens, int64_t rows, int64_t cols, void* base, Work* w)
 cudaError_t sort_tokens(const int64_t* ids, int64_t tokens, int64_t rows, const Work& w,
                         unsigned long long* status, cudaStream_t st) {
     if (tokens <= kSmall) {
-        auto* k = tokens <= kSortThreads       ? k_embedding_sort<1>
-                  : tokens <= 2 * kSortThreads ? k_embedding_sort<2>
-                                               : k_embedding_sort<4>;
-        return launch_k(k, dim3(1), dim3(kSortThreads), 0, st, ids, (int)tokens, rows, w.sorted,
-                        w.count, status);
+        const int all = (int)(tokens + 127) / 128 * 128, per = kWarps * kRanked;
+        return launch_k(k_embedding_rank, dim3((unsigned)((tokens + per - 1) / per)), dim3(kThreads),
+                        (size_t)all * 4, st, ids, (int)tokens, rows, w.sorted, w.count, status);
     }
     cudaError_t e = launch_k(k_embedding_keys, dim3((unsigned)((tokens + kThreads - 1) / kThreads)),
                              dim3(kThreads), 0, st, ids, tokens, rows, w.keys, w.places, w.done,

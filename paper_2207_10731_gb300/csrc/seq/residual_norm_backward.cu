@@ -4,6 +4,7 @@
 // so their sums are its own, in registers (rows of a warp) or in shared memory (rows of
 // a CTA, where two sums a value would take the registers of the next row's loads); a
 // CTA leaves one partial row, and a second kernel adds these in a fixed order.
+#include <algorithm>
 #include <cmath>
 
 #include "residual_norm.cuh"
@@ -32,10 +33,14 @@ struct Backward {
     Shape sh;
 };
 
-template <typename T, typename R, int VEC, int KIND, int MODE>
-__global__ void __launch_bounds__(Fit<VEC, KIND>::kMost)
+template <typename T, typename R, int VEC, int KIND, int MODE, int FULL>
+__global__ void __launch_bounds__(Fit<VEC, KIND>::kMost, Fit<VEC, KIND>::kLeast)
 k_residual_norm_backward(const __grid_constant__ Backward<T, R> a) {
     pdl_prologue();
+    // constants where FULL
+    const int gates = FULL == ANY ? a.gates : FULL;
+    const bool post = FULL != ANY || a.post, pre = FULL != ANY || a.pre;
+    const bool grad_total = FULL != ANY || a.grad_total, reads_x = FULL != ANY || a.reads_x;
     using F = Fit<VEC, KIND>;
     constexpr int CH = F::kVectors;
     constexpr bool kShared = KIND != NARROW;
@@ -79,130 +84,155 @@ k_residual_norm_backward(const __grid_constant__ Backward<T, R> a) {
                 for (int i = 0; i < VEC; ++i) *slot(k, c, i) = 0.f;
 
     const int64_t step = (int64_t)gridDim.x * sh.groups;
-    Part<R, VEC, CH> next_gt, next_t;
-    Part<T, VEC, CH> next_gy, next_x, next_g;
+    Held<R, VEC, CH, F::kAhead> held_gt, held_t;
+    Held<T, VEC, CH, F::kAhead> held_gy, held_x, held_g;
+    {
+        uint32_t at = smem_addr(sums) + (kShared ? 8 * CH * VEC * blockDim.x : 0);
+        if (grad_total) at = held_gt.place_at(at);
+        if (pre) at = held_gy.place_at(held_t.place_at(at));
+        if (reads_x) at = held_x.place_at(at);
+        if (gates == VALUE_GATE) at = held_g.place_at(at);
+    }
     float next_gate = 0.f, next_post = 0.f, next_pre = 0.f;
-    auto fetch = [&](int64_t r) {
-        const bool live = r < sh.rows;
+    auto fetch = [&](int stage, int64_t r) {
+        const bool live = KIND != NARROW || r < sh.rows;
         auto whole = [&](int64_t stride) { return MODE == ALIGNED || inner(sh, r, stride); };
-        if (a.pre) {
-            next_t.load(a.total + r * a.ts, live, whole(a.ts), in, place, sh);
-            next_gy.load(a.grad_y + r * a.gys, live, whole(a.gys), in, place, sh);
+        if (pre) {
+            held_t.fetch(stage, a.total + r * a.ts, live, whole(a.ts), in, place, sh);
+            held_gy.fetch(stage, a.grad_y + r * a.gys, live, whole(a.gys), in, place, sh);
             next_pre = live ? a.pre_rstd[r] : 0.f;
         }
-        next_gt.load(a.grad_total + r * a.gts, live && a.grad_total, whole(a.gts), in, place, sh);
-        if (a.reads_x) next_x.load(a.x + r * a.xs, live, whole(a.xs), in, place, sh);
-        if (a.post) next_post = live ? a.post_rstd[r] : 0.f;
-        if (a.gates == VALUE_GATE)
-            next_g.load(a.gate + r * a.gs, live, whole(a.gs), in, place, sh);
-        if (a.gates == ROW_GATE) next_gate = live ? load_f32(a.gate[r * a.gs]) : 0.f;
+        if (grad_total)
+            held_gt.fetch(stage, a.grad_total + r * a.gts, live, whole(a.gts), in, place, sh);
+        if (reads_x) held_x.fetch(stage, a.x + r * a.xs, live, whole(a.xs), in, place, sh);
+        if (post) next_post = live ? a.post_rstd[r] : 0.f;
+        if (gates == VALUE_GATE)
+            held_g.fetch(stage, a.gate + r * a.gs, live, whole(a.gs), in, place, sh);
+        if (gates == ROW_GATE) next_gate = live ? load_f32(a.gate[r * a.gs]) : 0.f;
     };
-    if (F::kAhead) fetch((int64_t)blockIdx.x * sh.groups + place.group);
-    int turn = 0;
-    for (int64_t r0 = (int64_t)blockIdx.x * sh.groups; r0 < sh.rows; r0 += step) {
+    if (F::kAhead) fetch(0, (int64_t)blockIdx.x * sh.groups + place.group);
+    copies_issued();
+    int turn = 0, stage = 0;
+    for (int64_t r0 = (int64_t)blockIdx.x * sh.groups; r0 < sh.rows; r0 += step, stage ^= 1) {
         const int64_t r = r0 + place.group;
-        const bool live = r < sh.rows;
-        if (!F::kAhead) fetch(r);
-        const Part<R, VEC, CH> part_gt = next_gt, part_t = next_t;
-        const Part<T, VEC, CH> part_gy = next_gy, part_x = next_x, part_g = next_g;
+        const bool live = KIND != NARROW || r < sh.rows;
+        if (!F::kAhead) fetch(0, r);
         const float row_gate = next_gate, post_rstd = next_post, pre_rstd = next_pre;
-        if (F::kAhead && r0 + step < sh.rows) fetch(r + step);
+        if (F::kAhead) {
+            if (r0 + step < sh.rows) fetch(stage ^ 1, r + step);
+            copies_issued();
+            copies_arrived();
+        }
 
-        // the second norm: d
+        // the second norm: d = dt + r g - that (r / n sum g that)
         float d[CH][VEC];
 #pragma unroll
-        for (int c = 0; c < CH; ++c) part_gt.get(c, d[c]);
-        if (a.pre) {
-            float g[CH][VEC], s = 0.f;
+        for (int c = 0; c < CH; ++c) {
+            if (grad_total) {
+                held_gt.get(stage, c, d[c]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) d[c][i] = 0.f;
+            }
+        }
+        if (pre) {
+            float sum = 0.f;
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
-                float t[VEC], w[VEC], p[VEC];
-                part_gy.get(c, g[c]);
-                part_t.get(c, t);
+                float g[VEC], t[VEC], w[VEC];
+                held_gy.get(stage, c, g);
+                held_t.get(stage, c, t);
+                own_only<VEC, MODE>(g, place.at(sh, c), sh.cols);
+                own_only<VEC, MODE>(t, place.at(sh, c), sh.cols);
                 load_weight<VEC, MODE>(a.pre, place.at(sh, c), sh.cols, in[c], w);
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) {
-                    const bool use = live && inside<MODE>(place.at(sh, c) + i, sh.cols, in[c]);
-                    t[i] *= pre_rstd;
-                    p[i] = use ? g[c][i] * t[i] : 0.f;
-                    g[c][i] *= w[i];
-                    s += use ? g[c][i] * t[i] : 0.f;
-                }
-                add(1, c, p);
+                mul(t, t, pre_rstd);
+                mul(t, t, g);   // g that, before the weight
+                add(1, c, t);
+                sum += dot(t, w);
+                mul(g, g, w);
+                fma(d[c], g, pre_rstd);
             }
-            s = row_sums(make_float2(s, 0.f), sh.lanes, slots, turn).x * inv_n;
+            const float s = row_sums<KIND>(sum, sh.lanes, slots, turn) * inv_n;
+            const float k = -s * pre_rstd * pre_rstd;
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
                 float t[VEC];
-                part_t.get(c, t);
-#pragma unroll
-                for (int i = 0; i < VEC; ++i)
-                    d[c][i] += (g[c][i] - t[i] * pre_rstd * s) * pre_rstd;
+                held_t.get(stage, c, t);
+                fma(d[c], t, k);
             }
         }
-        if (live)
 #pragma unroll
-            for (int c = 0; c < CH; ++c)
-                if (in[c]) store_part(a.dresidual + r * a.drs, place.at(sh, c), sh.cols, d[c]);
+        for (int c = 0; c < CH; ++c) {
+            if (live && in[c]) store_part(a.dresidual + r * a.drs, place.at(sh, c), sh.cols, d[c]);
+            own_only<VEC, MODE>(d[c], place.at(sh, c), sh.cols);
+        }
 
         // the gate and the first norm
         float row_slope = 0.f;
-        const float row_open = a.gates == ROW_GATE ? sigmoid(row_gate, &row_slope) : 1.f;
-        float2 s = make_float2(0.f, 0.f);   // of h xhat; of the row's gate gradient
+        const float row_open = gates == ROW_GATE ? sigmoid(row_gate, &row_slope) : 1.f;
+        float2 sum = make_float2(0.f, 0.f);   // of h xhat; of the row's gate gradient
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
-            float x[VEC], w[VEC], p[VEC], g[VEC];
-            if (a.reads_x) {
-                part_x.get(c, x);
+            float hat[VEC], u[VEC], w[VEC];
+            if (reads_x) {
+                held_x.get(stage, c, hat);
+                own_only<VEC, MODE>(hat, place.at(sh, c), sh.cols);
             } else {
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) x[i] = 0.f;
+                for (int i = 0; i < VEC; ++i) hat[i] = 0.f;
             }
-            if (a.post) load_weight<VEC, MODE>(a.post, place.at(sh, c), sh.cols, in[c], w);
-            if (a.gates == VALUE_GATE) part_g.get(c, g);
+            mul(d[c], d[c], a.scale);
+            if (post) {
+                load_weight<VEC, MODE>(a.post, place.at(sh, c), sh.cols, in[c], w);
+                mul(hat, hat, post_rstd);
+                mul(u, hat, w);
+            } else {
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) {
-                const bool use = live && inside<MODE>(place.at(sh, c) + i, sh.cols, in[c]);
-                const float hat = a.post ? x[i] * post_rstd : x[i];
-                const float u = a.post ? hat * w[i] : hat;
-                float open = row_open, slope = 0.f;
-                if (a.gates == VALUE_GATE) open = sigmoid(g[i], &slope);
-                const float e = d[c][i] * a.scale;
-                const float through = e * u;
-                d[c][i] = e * open;
-                if (a.gates == VALUE_GATE) g[i] = through * slope;
-                s.y += use ? through : 0.f;
-                p[i] = use ? d[c][i] * hat : 0.f;
-                if (a.post) {
-                    d[c][i] *= w[i];
-                    s.x += use ? d[c][i] * hat : 0.f;
-                }
+                for (int i = 0; i < VEC; ++i) u[i] = hat[i];
             }
-            if (a.post) add(0, c, p);
-            if (a.gates == VALUE_GATE && live && in[c])
-                store_part(a.dgate + r * a.dgs, place.at(sh, c), sh.cols, g);
+            if (gates == VALUE_GATE) {
+                float g[VEC], slope[VEC];
+                held_g.get(stage, c, g);
+                own_only<VEC, MODE>(g, place.at(sh, c), sh.cols);
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) g[i] = sigmoid(g[i], &slope[i]);
+                mul(slope, slope, u);
+                mul(slope, slope, d[c]);
+                if (live && in[c])
+                    store_part(a.dgate + r * a.dgs, place.at(sh, c), sh.cols, slope);
+                mul(d[c], d[c], g);
+            } else if (gates == ROW_GATE) {
+                sum.y += dot(d[c], u);
+                mul(d[c], d[c], row_open);
+            }
+            if (post) {
+                mul(hat, hat, d[c]);   // e xhat
+                add(0, c, hat);
+                sum.x += dot(hat, w);
+                mul(d[c], d[c], w);
+            }
         }
-        if (a.post || a.gates == ROW_GATE) {
-            s = row_sums(s, sh.lanes, slots, turn);
-            s.x *= inv_n;
-            if (a.gates == ROW_GATE && live && place.t == 0)
+        if (post || gates == ROW_GATE) {
+            const float2 s = gates == ROW_GATE
+                                 ? row_sums<KIND>(sum, sh.lanes, slots, turn)
+                                 : make_float2(row_sums<KIND>(sum.x, sh.lanes, slots, turn), 0.f);
+            if (gates == ROW_GATE && live && place.t == 0)
                 a.dgate[r * a.dgs] = round_to<T>(s.y * row_slope);
+            sum.x = s.x * inv_n;
         }
-        if (live)
+        const float k = -sum.x * post_rstd * post_rstd;
 #pragma unroll
-            for (int c = 0; c < CH; ++c) {
-                if (!in[c]) continue;
-                if (a.post) {
-                    float x[VEC];
-                    part_x.get(c, x);
-#pragma unroll
-                    for (int i = 0; i < VEC; ++i)
-                        d[c][i] = (d[c][i] - x[i] * post_rstd * s.x) * post_rstd;
-                }
-                store_part(a.dx + r * a.dxs, place.at(sh, c), sh.cols, d[c]);
+        for (int c = 0; c < CH; ++c) {
+            if (post) {
+                float x[VEC];
+                held_x.get(stage, c, x);
+                mul(d[c], d[c], post_rstd);
+                fma(d[c], x, k);
             }
+            if (live && in[c]) store_part(a.dx + r * a.dxs, place.at(sh, c), sh.cols, d[c]);
+        }
     }
-    if (!a.post && !a.pre) return;   // no weights, and no workspace
+    if (!post && !pre) return;   // no weights, and no workspace
     // the CTA's partial row: [post, pre][cols] at blockIdx.x
     float* out = a.partial + (int64_t)blockIdx.x * 2 * sh.cols;
     if constexpr (kShared) {
@@ -215,7 +245,8 @@ k_residual_norm_backward(const __grid_constant__ Backward<T, R> a) {
                     if (inside<MODE>(at, sh.cols, in[c])) out[k * sh.cols + at] = *slot(k, c, i);
                 }
     } else {
-        // add the groups of the CTA: shared memory holds [groups][2][cols]
+        // add the groups of the CTA: shared memory holds [groups][2][cols], over the rows
+        __syncthreads();
 #pragma unroll
         for (int k = 0; k < 2; ++k)
 #pragma unroll
@@ -304,15 +335,21 @@ extern "C" pss_status pss_residual_norm_backward(
         const Split s = norm_split((int)cols, ragged ? 7 : 0, &kind);
         f.sh = Shape{rows, (int)cols, s.lanes, s.log2_lanes, s.groups, lie.shift0, lie.step};
         f.partial = static_cast<float*>(workspace);
-        auto with = [&](auto vec, auto k, auto mode) -> cudaError_t {
+        auto launch = [&](auto vec, auto k, auto mode, auto full) -> cudaError_t {
             auto* kernel = k_residual_norm_backward<T, R, decltype(vec)::value, decltype(k)::value,
-                                                    decltype(mode)::value>;
+                                                    decltype(mode)::value, decltype(full)::value>;
             using F = Fit<decltype(vec)::value, decltype(k)::value>;
-            const size_t smem = s.lanes <= 32
-                                    ? (size_t)s.groups * 8 * cols
-                                    : (size_t)8 * F::kVectors * decltype(vec)::value * s.threads;
+            constexpr int kT = held_bytes<T, F::kVectors>(), kR = held_bytes<R, F::kVectors>();
+            const size_t ahead =
+                F::kAhead ? s.threads * (size_t)((grad_total ? kR : 0) + (pre_weight ? kR + kT : 0) +
+                                                 (reads_x ? kT : 0) + (values ? kT : 0))
+                          : 0;
+            // rows of a warp: at the end, the groups' sums instead
+            const size_t smem =
+                kind == NARROW ? std::max(ahead, (size_t)s.groups * 8 * cols)
+                              : ahead + (size_t)8 * F::kVectors * decltype(vec)::value * s.threads;
             cudaError_t e = cudaSuccess;
-            if (smem > 48 * 1024)
+            if (smem + 1024 > 48 * 1024)   // 48 KB with the kernel's own
                 e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                          (int)smem);
             if (e != cudaSuccess) return e;
@@ -327,10 +364,21 @@ extern "C" pss_status pss_residual_norm_backward(
                             st, static_cast<const float*>(workspace), n, 2 * (int)cols, (int)cols, first, last,
                             dpost_weight, dpre_weight);
         };
+        auto with = [&](auto vec, auto k, auto mode) -> cudaError_t {
+            if constexpr (decltype(vec)::value == 8 && decltype(mode)::value == ALIGNED &&
+                          decltype(k)::value <= WIDE) {
+                if (post_weight && pre_weight && grad_total)
+                    return gates == NO_GATE    ? launch(vec, k, mode, Int<NO_GATE>())
+                           : gates == ROW_GATE ? launch(vec, k, mode, Int<ROW_GATE>())
+                                               : launch(vec, k, mode, Int<VALUE_GATE>());
+            }
+            return launch(vec, k, mode, Int<ANY>());
+        };
         auto wide = [&](auto vec, auto mode) {
-            return kind == NARROW ? with(vec, Int<NARROW>(), mode)
-                   : kind == WIDE ? with(vec, Int<WIDE>(), mode)
-                                  : with(vec, Int<WIDEST>(), mode);
+            return kind == NARROW   ? with(vec, Int<NARROW>(), mode)
+                   : kind == MIDDLE ? with(vec, Int<MIDDLE>(), mode)
+                   : kind == WIDE   ? with(vec, Int<WIDE>(), mode)
+                                    : with(vec, Int<WIDEST>(), mode);
         };
         return lie.how == VECTORS ? wide(Int<8>(), Int<ALIGNED>())
                : ragged           ? wide(Int<8>(), Int<RAGGED>())
