@@ -189,6 +189,7 @@ struct Held {
         part.load(row, live, whole, in, place, sh);
     }
     __device__ __forceinline__ void get(int, int c, float (&to)[VEC]) const { part.get(c, to); }
+    __device__ __forceinline__ void own(int, int) const {}
 };
 template <typename T, int CH>
 constexpr int held_bytes() {   // a thread's
@@ -207,6 +208,9 @@ struct Held<T, 8, CH, true> {
     __device__ __forceinline__ uint32_t slot(int stage, int c, int h) const {
         return base + ((stage * CH + c) * kPieces + h) * step;
     }
+    // A vector that begins before its row is copied as it lies in memory (with what is in front
+    // of the row, if `whole` says that there is memory) and cleaned by own() when it has arrived;
+    // what lies behind the row's end arrives as zeros.
     template <int MODE>
     __device__ __forceinline__ void fetch(int stage, const T* row, bool live, bool whole,
                                           const bool (&in)[CH], const Place<8, MODE>& place,
@@ -214,12 +218,20 @@ struct Held<T, 8, CH, true> {
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
             const int at = place.at(sh, c);
-            if (live && in[c] && (whole || (at >= 0 && at + 8 <= sh.cols))) {
+            if (live && in[c] && (MODE == ALIGNED || whole || at >= 0)) {
 #pragma unroll
-                for (int h = 0; h < kPieces; ++h)
-                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;"
-                                 :: "r"(slot(stage, c, h)), "l"(row + at + h * (8 / kPieces))
-                                 : "memory");
+                for (int h = 0; h < kPieces; ++h) {
+                    const T* from = row + at + h * (8 / kPieces);
+                    if (MODE == ALIGNED) {
+                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;"
+                                     :: "r"(slot(stage, c, h)), "l"(from) : "memory");
+                    } else {
+                        const int left = (sh.cols - at) * (int)sizeof(T) - 16 * h;
+                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;"
+                                     :: "r"(slot(stage, c, h)), "l"(left > 0 ? from : row),
+                                        "r"(min(max(left, 0), 16)) : "memory");
+                    }
+                }
             } else {
                 const Raw8<T> r = live && in[c] ? load_raw_part(row, at, sh.cols, false) : Raw8<T>{};
 #pragma unroll
@@ -228,6 +240,17 @@ struct Held<T, 8, CH, true> {
                                  :: "r"(slot(stage, c, h)), "r"(r.w[4 * h]), "r"(r.w[4 * h + 1]),
                                     "r"(r.w[4 * h + 2]), "r"(r.w[4 * h + 3]) : "memory");
             }
+        }
+    }
+    // Zeros for the values in front of the row: the first thread's, once a row has arrived.
+    __device__ __forceinline__ void own(int stage, int before) const {
+        for (int i = 0; i < before; ++i) {
+            if (sizeof(T) == 4)
+                asm volatile("st.shared.u32 [%0], %1;" :: "r"(slot(stage, 0, i / 4) + 4 * (i & 3)), "r"(0)
+                             : "memory");
+            else
+                asm volatile("st.shared.u16 [%0], %1;" :: "r"(slot(stage, 0, 0) + 2 * i), "h"((short)0)
+                             : "memory");
         }
     }
     __device__ __forceinline__ void get(int stage, int c, float (&to)[8]) const {

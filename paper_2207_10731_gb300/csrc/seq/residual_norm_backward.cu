@@ -44,6 +44,7 @@ k_residual_norm_backward(const __grid_constant__ Backward<T, R> a) {
     using F = Fit<VEC, KIND>;
     constexpr int CH = F::kVectors;
     constexpr bool kShared = KIND != NARROW;
+    constexpr int kDirty = F::kAhead ? ALIGNED : MODE;   // whether a vector may hold a neighbour's values
     extern __shared__ __align__(16) float sums[];
     __shared__ float2 slots[2][32];
     const Shape& sh = a.sh;
@@ -86,13 +87,39 @@ k_residual_norm_backward(const __grid_constant__ Backward<T, R> a) {
     const int64_t step = (int64_t)gridDim.x * sh.groups;
     Held<R, VEC, CH, F::kAhead> held_gt, held_t;
     Held<T, VEC, CH, F::kAhead> held_gy, held_x, held_g;
-    {
-        uint32_t at = smem_addr(sums) + (kShared ? 8 * CH * VEC * blockDim.x : 0);
-        if (grad_total) at = held_gt.place_at(at);
-        if (pre) at = held_gy.place_at(held_t.place_at(at));
-        if (reads_x) at = held_x.place_at(at);
-        if (gates == VALUE_GATE) at = held_g.place_at(at);
+    uint32_t at = smem_addr(sums) + (kShared ? 8 * CH * VEC * blockDim.x : 0);
+    if (grad_total) at = held_gt.place_at(at);
+    if (pre) at = held_gy.place_at(held_t.place_at(at));
+    if (reads_x) at = held_x.place_at(at);
+    if (gates == VALUE_GATE) at = held_g.place_at(at);
+    // A ragged row's weights are no vectors: they are laid out once, since a thread's columns are
+    // the same in all of its rows.
+    constexpr bool kLaid = MODE == RAGGED && F::kAhead;
+    uint32_t laid = 0;
+    if constexpr (kLaid) {
+        laid = at + threadIdx.x * 16;
+        for (int k = 0; k < 2; ++k) {
+            float w[8] = {};
+            const float* from = k == 0 ? a.post : a.pre;
+            if (from) load_weight<VEC, MODE>(from, place.at(sh, 0), sh.cols, in[0], w);
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                asm volatile("st.shared.v4.f32 [%0], {%1,%2,%3,%4};"
+                             :: "r"(laid + (2 * k + h) * blockDim.x * 16), "f"(w[4 * h]),
+                                "f"(w[4 * h + 1]), "f"(w[4 * h + 2]), "f"(w[4 * h + 3]) : "memory");
+        }
     }
+    auto weights = [&](int k, int c, float (&w)[VEC]) {
+        if constexpr (kLaid) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];"
+                             : "=f"(w[4 * h]), "=f"(w[4 * h + 1]), "=f"(w[4 * h + 2]), "=f"(w[4 * h + 3])
+                             : "r"(laid + (2 * k + h) * blockDim.x * 16) : "memory");
+        } else {
+            load_weight<VEC, MODE>(k == 0 ? a.post : a.pre, place.at(sh, c), sh.cols, in[c], w);
+        }
+    };
     float next_gate = 0.f, next_post = 0.f, next_pre = 0.f;
     auto fetch = [&](int stage, int64_t r) {
         const bool live = KIND != NARROW || r < sh.rows;
@@ -122,6 +149,12 @@ k_residual_norm_backward(const __grid_constant__ Backward<T, R> a) {
             if (r0 + step < sh.rows) fetch(stage ^ 1, r + step);
             copies_issued();
             copies_arrived();
+            if (MODE == RAGGED && place.t == 0 && place.shift > 0) {
+                if (pre) held_t.own(stage, place.shift), held_gy.own(stage, place.shift);
+                if (grad_total) held_gt.own(stage, place.shift);
+                if (reads_x) held_x.own(stage, place.shift);
+                if (gates == VALUE_GATE) held_g.own(stage, place.shift);
+            }
         }
 
         // the second norm: d = dt + r g - that (r / n sum g that)
@@ -142,9 +175,9 @@ k_residual_norm_backward(const __grid_constant__ Backward<T, R> a) {
                 float g[VEC], t[VEC], w[VEC];
                 held_gy.get(stage, c, g);
                 held_t.get(stage, c, t);
-                own_only<VEC, MODE>(g, place.at(sh, c), sh.cols);
-                own_only<VEC, MODE>(t, place.at(sh, c), sh.cols);
-                load_weight<VEC, MODE>(a.pre, place.at(sh, c), sh.cols, in[c], w);
+                own_only<VEC, kDirty>(g, place.at(sh, c), sh.cols);
+                own_only<VEC, kDirty>(t, place.at(sh, c), sh.cols);
+                weights(1, c, w);
                 mul(t, t, pre_rstd);
                 mul(t, t, g);   // g that, before the weight
                 add(1, c, t);
@@ -164,7 +197,7 @@ k_residual_norm_backward(const __grid_constant__ Backward<T, R> a) {
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
             if (live && in[c]) store_part(a.dresidual + r * a.drs, place.at(sh, c), sh.cols, d[c]);
-            own_only<VEC, MODE>(d[c], place.at(sh, c), sh.cols);
+            own_only<VEC, kDirty>(d[c], place.at(sh, c), sh.cols);
         }
 
         // the gate and the first norm
@@ -176,14 +209,14 @@ k_residual_norm_backward(const __grid_constant__ Backward<T, R> a) {
             float hat[VEC], u[VEC], w[VEC];
             if (reads_x) {
                 held_x.get(stage, c, hat);
-                own_only<VEC, MODE>(hat, place.at(sh, c), sh.cols);
+                own_only<VEC, kDirty>(hat, place.at(sh, c), sh.cols);
             } else {
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) hat[i] = 0.f;
             }
             mul(d[c], d[c], a.scale);
             if (post) {
-                load_weight<VEC, MODE>(a.post, place.at(sh, c), sh.cols, in[c], w);
+                weights(0, c, w);
                 mul(hat, hat, post_rstd);
                 mul(u, hat, w);
             } else {
@@ -193,7 +226,7 @@ k_residual_norm_backward(const __grid_constant__ Backward<T, R> a) {
             if (gates == VALUE_GATE) {
                 float g[VEC], slope[VEC];
                 held_g.get(stage, c, g);
-                own_only<VEC, MODE>(g, place.at(sh, c), sh.cols);
+                own_only<VEC, kDirty>(g, place.at(sh, c), sh.cols);
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) g[i] = sigmoid(g[i], &slope[i]);
                 mul(slope, slope, u);
@@ -341,7 +374,8 @@ extern "C" pss_status pss_residual_norm_backward(
             using F = Fit<decltype(vec)::value, decltype(k)::value>;
             constexpr int kT = held_bytes<T, F::kVectors>(), kR = held_bytes<R, F::kVectors>();
             const size_t ahead =
-                F::kAhead ? s.threads * (size_t)((grad_total ? kR : 0) + (pre_weight ? kR + kT : 0) +
+                F::kAhead ? s.threads * (size_t)((decltype(mode)::value == RAGGED ? 64 : 0) +
+                                                 (grad_total ? kR : 0) + (pre_weight ? kR + kT : 0) +
                                                  (reads_x ? kT : 0) + (values ? kT : 0))
                           : 0;
             // rows of a warp: at the end, the groups' sums instead
@@ -365,8 +399,8 @@ extern "C" pss_status pss_residual_norm_backward(
                             dpost_weight, dpre_weight);
         };
         auto with = [&](auto vec, auto k, auto mode) -> cudaError_t {
-            if constexpr (decltype(vec)::value == 8 && decltype(mode)::value == ALIGNED &&
-                          decltype(k)::value <= WIDE) {
+            if constexpr (decltype(vec)::value == 8 &&
+                          decltype(k)::value <= (decltype(mode)::value == ALIGNED ? WIDE : MIDDLE)) {
                 if (post_weight && pre_weight && grad_total)
                     return gates == NO_GATE    ? launch(vec, k, mode, Int<NO_GATE>())
                            : gates == ROW_GATE ? launch(vec, k, mode, Int<ROW_GATE>())
