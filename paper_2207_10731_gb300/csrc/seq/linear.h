@@ -37,12 +37,13 @@ struct Finish {
     bool vectors;           // rows of all tensors start at multiples of 32 bytes
 };
 
-// One product m x n x k: tiles of 128 x bn, each contraction in `splits` parts whose sums go to
+// One product m x n x k: tiles of 128 x bn (of 256 x bn by a pair of CTAs), each contraction in `splits` parts whose sums go to
 // partial[split][t][c] (fp32, rows of `ld`) and are joined by a second kernel.
 struct Product {
     Operand a, b;
     Finish f;
     int m, n, bn, blocks;   // blocks: of 64 along the contraction
+    bool pair;
     int m_tiles, n_tiles, splits;
     float* partial;
     int64_t ld;             // of a partial row

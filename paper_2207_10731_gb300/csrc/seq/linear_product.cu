@@ -29,10 +29,15 @@ constexpr int kFinishers = 8;                // warps
 constexpr int kProductThreads = 128 + 32 * kFinishers;
 constexpr int kPad = 33;                     // a staged row of 32 values
 
-template <int BN>
+// PAIR: two CTAs of a cluster, on neighbouring SMs, make a tile of 256 x BN: each loads its 128
+// rows of A and half of B's, one thread of the first issues products that read both, and
+// each CTA's tensor memory holds its rows of the result.  B so passes through each SM's shared
+// memory half as often.
+template <int BN, bool PAIR>
 struct Ring {
-    static constexpr int kA = 128 * kBlock * 2, kB = BN * kBlock * 2, kStage = kA + kB;
-    static constexpr int kStages = BN == 256 ? 4 : BN == 128 ? 6 : 8;
+    static constexpr int kA = 128 * kBlock * 2, kRows = PAIR ? BN / 2 : BN, kB = kRows * kBlock * 2;
+    static constexpr int kStage = kA + kB;
+    static constexpr int kStages = PAIR || BN == 128 ? 6 : BN == 256 ? 4 : 8;
     static constexpr int kStaging = kFinishers * 32 * kPad * 4;
     static constexpr int kSmem = kStages * kStage + kStaging;
     static constexpr int kCols = 2 * BN;     // tensor-memory columns: two accumulators
@@ -46,11 +51,81 @@ __device__ __forceinline__ void tma_load2(void* dst, const CUtensorMap* map, int
         :: "r"(smem_addr(dst)), "l"(map), "r"(c0), "r"(c1), "r"(smem_addr(bar)) : "memory");
 }
 
-// 128 x N, fp32 sums of f16 or bf16; which operands lie across the contraction.
-__device__ __forceinline__ uint32_t product_desc(int n, bool half, bool a_across, bool b_across) {
+// ---- pairs of CTAs -------------------------------------------------------------
+
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// The address, in the cluster's shared memory, of p in its first CTA.
+__device__ __forceinline__ uint32_t first_cta(const void* p) {
+    uint32_t r;
+    asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(smem_addr(p)));
+    return r;
+}
+// A load into this CTA that reports to a barrier of the first one.
+__device__ __forceinline__ void tma_load2_pair(void* dst, const CUtensorMap* map, int c0, int c1,
+                                               uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+        " [%0], [%1, {%2, %3}], [%4];"
+        :: "r"(smem_addr(dst)), "l"(map), "r"(c0), "r"(c1), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void tmem_alloc_pair(uint32_t* at, uint32_t cols) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;"
+                 :: "r"(smem_addr(at)), "r"(cols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void tmem_free_pair(uint32_t addr, uint32_t cols) {
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" :: "r"(addr), "r"(cols)
+                 : "memory");
+}
+__device__ __forceinline__ void mma_pair(uint32_t d, uint64_t a, uint64_t b, uint32_t desc,
+                                         bool add) {
+    asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n"
+                 " tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}"
+                 :: "r"(d), "l"(a), "l"(b), "r"(desc), "r"((uint32_t)add) : "memory");
+}
+// The barrier of both CTAs receives one arrival when this thread's products have completed.
+__device__ __forceinline__ void tc_commit_pair(uint64_t* bar) {
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster"
+                 ".multicast::cluster.b64 [%0], %1;"
+                 :: "r"(smem_addr(bar)), "h"((uint16_t)3) : "memory");
+}
+__device__ __forceinline__ void bar_arrive_first(uint64_t* bar) {
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" :: "r"(first_cta(bar))
+                 : "memory");
+}
+// As bar_wait, for what a thread of the other CTA did before it arrived.
+__device__ __forceinline__ bool bar_wait_cluster(uint64_t* b, uint32_t parity, volatile int* stop) {
+    const uint64_t start = now_ns();
+    for (;;) {
+        uint32_t ok;
+        asm volatile("{\n .reg .pred p;\n"
+                     " mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n"
+                     " selp.u32 %0, 1, 0, p;\n}"
+                     : "=r"(ok) : "r"(smem_addr(b)), "r"(parity) : "memory");
+        if (ok) return true;
+        if (*stop) return false;
+        if (now_ns() - start > kWaitNs) {
+            *stop = 1;
+            return false;
+        }
+    }
+}
+
+// 128 (or, of a pair, 256) x N, fp32 sums of f16 or bf16; which operands lie across the
+// contraction.
+__device__ __forceinline__ uint32_t product_desc(int m, int n, bool half, bool a_across,
+                                                 bool b_across) {
     const uint32_t format = half ? 0u : 1u;
     return (1u << 4) | (format << 7) | (format << 10) | ((a_across ? 1u : 0u) << 15) |
-           ((b_across ? 1u : 0u) << 16) | ((uint32_t)(n / 8) << 17) | (8u << 24);
+           ((b_across ? 1u : 0u) << 16) | ((uint32_t)(n / 8) << 17) | ((uint32_t)(m / 16) << 24);
 }
 
 struct Args {
@@ -135,21 +210,26 @@ __device__ __forceinline__ void add32(const float* p, float (&v)[32]) {
     }
 }
 
-// One value of the result.
+template <typename T>
+__device__ __forceinline__ float residual_at(const Finish& f, int64_t t, int64_t c) {
+    const int64_t at = t * f.residual_stride + c;
+    return f.y_f32 ? static_cast<const float*>(f.residual)[at]
+                   : load_f32(static_cast<const T*>(f.residual)[at]);
+}
+
+// One value of the result; `more`: its residual.
 template <typename T>
 __device__ __forceinline__ void finish_one(const Finish& f, float v, int64_t t, int64_t c,
-                                           float bias) {
+                                           float bias, float more) {
     v += bias;
     if (f.z) static_cast<T*>(f.z)[t * f.z_stride + c] = round_to<T>(v);
     with_activation(f.activation, [&](auto act) { v = activate<decltype(act)::value>(v); });
-    const int64_t at = t * f.y_stride + c, from = t * f.residual_stride + c;
-    if (f.y_f32) {
-        if (f.residual) v += static_cast<const float*>(f.residual)[from];
+    const int64_t at = t * f.y_stride + c;
+    if (f.residual) v += more;
+    if (f.y_f32)
         static_cast<float*>(f.y)[at] = v;
-    } else {
-        if (f.residual) v += load_f32(static_cast<const T*>(f.residual)[from]);
+    else
         static_cast<T*>(f.y)[at] = round_to<T>(v);
-    }
 }
 
 // 32 values of row t from column c on, all inside.
@@ -174,17 +254,20 @@ __device__ __forceinline__ void finish_32(const Finish& f, float (&v)[32], int64
     }
 }
 
-template <int BN, typename T>
+template <int BN, bool PAIR, typename T>
 __global__ void __launch_bounds__(kProductThreads, 1)
 k_linear_product(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUtensorMap mb,
                  const __grid_constant__ Args a) {
     pdl_prologue();
-    using R = Ring<BN>;
+    using R = Ring<BN, PAIR>;
     extern __shared__ __align__(1024) uint8_t smem[];
     __shared__ uint64_t full[R::kStages], empty[R::kStages], done[2], free_[2], drained;
     __shared__ uint32_t tmem_at;
     __shared__ volatile int stop;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    constexpr int kCtas = PAIR ? 2 : 1;
+    const int rank = PAIR ? (int)cluster_rank() : 0;
+    const int first_unit = blockIdx.x / kCtas, step = gridDim.x / kCtas;
     if (threadIdx.x == 0) {
         prefetch_map(&ma);
         prefetch_map(&mb);
@@ -195,14 +278,20 @@ k_linear_product(const __grid_constant__ CUtensorMap ma, const __grid_constant__
         }
         for (int i = 0; i < 2; ++i) {
             bar_init(&done[i], 1);
-            bar_init(&free_[i], kFinishers);
+            bar_init(&free_[i], kCtas * kFinishers);
         }
         bar_init(&drained, 1);
         bar_init_done();
     }
-    if (warp == 1) tmem_alloc(&tmem_at, R::kCols);
+    if (warp == 1) {
+        if (PAIR)
+            tmem_alloc_pair(&tmem_at, R::kCols);
+        else
+            tmem_alloc(&tmem_at, R::kCols);
+    }
     tc_before_sync();
     __syncthreads();
+    if (PAIR) cluster_sync();
     tc_after_sync();
     const uint32_t tmem = tmem_at;
 
@@ -211,8 +300,9 @@ k_linear_product(const __grid_constant__ CUtensorMap ma, const __grid_constant__
         if (lane == 0) {
             int s = 0;
             bool ok = true;
-            for (int u = blockIdx.x; ok && u < a.units; u += gridDim.x) {
+            for (int u = first_unit; ok && u < a.units; u += step) {
                 const Unit w = unit_of(a, u);
+                const int row = (w.m * kCtas + rank) * 128, col = w.n * BN + rank * R::kRows;
                 for (int k = w.k0; k < w.k1; ++k, ++s) {
                     const int slot = s % R::kStages, turn = s / R::kStages;
                     if (turn > 0 && !bar_wait(&empty[slot], (turn - 1) & 1, &stop)) {
@@ -220,41 +310,61 @@ k_linear_product(const __grid_constant__ CUtensorMap ma, const __grid_constant__
                         break;
                     }
                     uint8_t* at = smem + slot * R::kStage;
-                    bar_expect(&full[slot], R::kStage);
+                    if (rank == 0) bar_expect(&full[slot], kCtas * R::kStage);
+                    const uint32_t bar = PAIR ? first_cta(&full[slot]) : 0;
+                    auto load = [&](uint8_t* to, const CUtensorMap* map, int c0, int c1) {
+                        if (PAIR)
+                            tma_load2_pair(to, map, c0, c1, bar);
+                        else
+                            tma_load2(to, map, c0, c1, &full[slot]);
+                    };
                     if (a.a_across) {
                         for (int i = 0; i < 2; ++i)
-                            tma_load2(at + i * 8192, &ma, w.m * 128 + i * 64, k * kBlock, &full[slot]);
+                            load(at + i * 8192, &ma, row + i * 64, k * kBlock);
                     } else {
-                        tma_load2(at, &ma, k * kBlock, w.m * 128, &full[slot]);
+                        load(at, &ma, k * kBlock, row);
                     }
                     at += R::kA;
                     if (a.b_across) {
-                        for (int i = 0; i < BN / 64; ++i)
-                            tma_load2(at + i * 8192, &mb, w.n * BN + i * 64, k * kBlock, &full[slot]);
+                        for (int i = 0; i < R::kRows / 64; ++i)
+                            load(at + i * 8192, &mb, col + i * 64, k * kBlock);
                     } else {
-                        tma_load2(at, &mb, k * kBlock, w.n * BN, &full[slot]);
+                        load(at, &mb, k * kBlock, col);
                     }
                 }
             }
-            // the loads must land before the CTA ends, also where nobody waits for them
+            // The loads must land before the CTA ends, also where nobody waits for them.  A pair's
+            // second CTA cannot see them land: the first one's wait ends after them, and both
+            // CTAs end together.
             int never = 0;
-            for (int w = max(0, s - R::kStages); w < s; ++w)
-                bar_wait(&full[w % R::kStages], (w / R::kStages) & 1, &never);
+            if (rank == 0)
+                for (int w = max(0, s - R::kStages); w < s; ++w)
+                    bar_wait(&full[w % R::kStages], (w / R::kStages) & 1, &never);
+            else if (!ok)
+                for (const uint64_t t = now_ns(); now_ns() - t < 10000000ull;) __nanosleep(1000);
         }
     } else if (warp == 1) {
         // ---- products ----
-        if (lane == 0) {
+        if (lane == 0 && rank == 0) {
             const uint32_t desc =
-                product_desc(BN, std::is_same<T, f16>::value, a.a_across, a.b_across);
+                product_desc(128 * kCtas, BN, std::is_same<T, f16>::value, a.a_across, a.b_across);
             const uint32_t base = smem_addr(smem);
             const uint32_t a_lead = a.a_across ? 8192 : 16, b_lead = a.b_across ? 8192 : 16;
             const uint32_t a_step = a.a_across ? 2048 : 32, b_step = a.b_across ? 2048 : 32;
+            auto commit = [&](uint64_t* bar) {
+                if (PAIR)
+                    tc_commit_pair(bar);
+                else
+                    tc_commit(bar);
+            };
             int s = 0, i = 0;
             bool ok = true;
-            for (int u = blockIdx.x; ok && u < a.units; u += gridDim.x, ++i) {
+            for (int u = first_unit; ok && u < a.units; u += step, ++i) {
                 const Unit w = unit_of(a, u);
                 const uint32_t d = tmem + (i & 1) * BN;
-                if (i > 1) ok = bar_wait(&free_[i & 1], ((i >> 1) - 1) & 1, &stop);
+                if (i > 1)
+                    ok = PAIR ? bar_wait_cluster(&free_[i & 1], ((i >> 1) - 1) & 1, &stop)
+                              : bar_wait(&free_[i & 1], ((i >> 1) - 1) & 1, &stop);
                 for (int k = w.k0; ok && k < w.k1; ++k, ++s) {
                     const int slot = s % R::kStages;
                     ok = bar_wait(&full[slot], (s / R::kStages) & 1, &stop);
@@ -262,16 +372,21 @@ k_linear_product(const __grid_constant__ CUtensorMap ma, const __grid_constant__
                     tc_after_sync();
                     const uint32_t a_at = base + slot * R::kStage, b_at = a_at + R::kA;
 #pragma unroll
-                    for (int j = 0; j < kBlock / 16; ++j)
-                        mma_ss(d, smem_desc(a_at + j * a_step, a_lead),
-                               smem_desc(b_at + j * b_step, b_lead), desc, k > w.k0 || j > 0);
-                    tc_commit(&empty[slot]);
+                    for (int j = 0; j < kBlock / 16; ++j) {
+                        const uint64_t x = smem_desc(a_at + j * a_step, a_lead);
+                        const uint64_t y = smem_desc(b_at + j * b_step, b_lead);
+                        if (PAIR)
+                            mma_pair(d, x, y, desc, k > w.k0 || j > 0);
+                        else
+                            mma_ss(d, x, y, desc, k > w.k0 || j > 0);
+                    }
+                    commit(&empty[slot]);
                 }
-                if (ok) tc_commit(&done[i & 1]);
+                if (ok) commit(&done[i & 1]);
             }
             // the products must end before their memory is freed, also after a wait gave up
             int never = 0;
-            tc_commit(&drained);
+            commit(&drained);
             bar_wait(&drained, 0, &never);
         }
     } else if (warp >= 4) {
@@ -280,12 +395,12 @@ k_linear_product(const __grid_constant__ CUtensorMap ma, const __grid_constant__
         float* staged = reinterpret_cast<float*>(smem + R::kStages * R::kStage) +
                         (warp - 4) * 32 * kPad;
         int i = 0;
-        for (int u = blockIdx.x; u < a.units; u += gridDim.x, ++i) {
+        for (int u = first_unit; u < a.units; u += step, ++i) {
             const Unit w = unit_of(a, u);
             if (!__all_sync(0xffffffffu, bar_wait(&done[i & 1], (i >> 1) & 1, &stop))) break;
             tc_after_sync();
             const uint32_t d = tmem + (i & 1) * BN + ((uint32_t)quarter << 21);
-            const int row0 = w.m * 128 + quarter * 32, row = row0 + lane;
+            const int row0 = (w.m * kCtas + rank) * 128 + quarter * 32, row = row0 + lane;
             const Finish& f = a.f;
             float* partial = a.partial ? a.partial + (int64_t)w.split * (f.swapped ? a.n : a.m) * a.ld
                                        : nullptr;
@@ -306,7 +421,8 @@ k_linear_product(const __grid_constant__ CUtensorMap ma, const __grid_constant__
                             if (partial)
                                 partial[(int64_t)(col + j) * a.ld + row] = v[j];
                             else
-                                finish_one<T>(f, v[j], col + j, row, bias);
+                                finish_one<T>(f, v[j], col + j, row, bias,
+                                              f.residual ? residual_at<T>(f, col + j, row) : 0.f);
                         }
                     }
                 } else if (partial) {
@@ -329,20 +445,43 @@ k_linear_product(const __grid_constant__ CUtensorMap ma, const __grid_constant__
                     __syncwarp();
                     if (col + lane < a.n) {
                         const float bias = f.bias ? f.bias[col + lane] : 0.f;
-                        for (int j = 0; j < 32 && row0 + j < a.m; ++j)
-                            finish_one<T>(f, staged[j * kPad + lane], row0 + j, col + lane, bias);
+                        const int last = min(32, a.m - row0);
+                        // eight rows' residuals are asked for before the first is waited for
+                        for (int j = 0; j < last; j += 8) {
+                            float more[8];
+#pragma unroll
+                            for (int e = 0; e < 8; ++e)
+                                more[e] = f.residual && j + e < last
+                                              ? residual_at<T>(f, row0 + j + e, col + lane) : 0.f;
+#pragma unroll
+                            for (int e = 0; e < 8; ++e)
+                                if (j + e < last)
+                                    finish_one<T>(f, staged[(j + e) * kPad + lane], row0 + j + e,
+                                                  col + lane, bias, more[e]);
+                        }
                     }
                 }
             }
             tc_before_sync();
             __syncwarp();
-            if (lane == 0) bar_arrive(&free_[i & 1]);
+            if (lane == 0) {
+                if (PAIR)
+                    bar_arrive_first(&free_[i & 1]);
+                else
+                    bar_arrive(&free_[i & 1]);
+            }
         }
     }
     tc_before_sync();
     __syncthreads();
+    if (PAIR) cluster_sync();   // neither CTA ends while the other may reach into it
     tc_after_sync();
-    if (warp == 1) tmem_free(tmem, R::kCols);
+    if (warp == 1) {
+        if (PAIR)
+            tmem_free_pair(tmem, R::kCols);
+        else
+            tmem_free(tmem, R::kCols);
+    }
     if (threadIdx.x == 0 && stop) report_stop(a.status);
 }
 
@@ -374,7 +513,9 @@ k_linear_join(const float* __restrict__ partial, int splits, int64_t rows, int c
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e)
-        if (c + e < cols) finish_one<T>(f, sum[e], t, c + e, f.bias ? f.bias[c + e] : 0.f);
+        if (c + e < cols)
+            finish_one<T>(f, sum[e], t, c + e, f.bias ? f.bias[c + e] : 0.f,
+                          f.residual ? residual_at<T>(f, t, c + e) : 0.f);
 }
 
 // Boxes of 64 along the dense dimension and `box` (at most 256) along the other.
@@ -399,22 +540,34 @@ cudaError_t operand_map(CUtensorMap* map, const Operand& o, int box, int type) {
     return rc == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
 
-template <int BN, typename T>
+template <int BN, bool PAIR, typename T>
 cudaError_t launch(const Product& p, int type, unsigned long long* status, cudaStream_t st) {
-    using R = Ring<BN>;
+    using R = Ring<BN, PAIR>;
     CUtensorMap ma, mb;
     cudaError_t e = operand_map(&ma, p.a, 128, type);
-    if (e == cudaSuccess) e = operand_map(&mb, p.b, BN, type);
+    if (e == cudaSuccess) e = operand_map(&mb, p.b, R::kRows, type);
     if (e != cudaSuccess) return e;
-    auto* k = k_linear_product<BN, T>;
+    auto* k = k_linear_product<BN, PAIR, T>;
     static std::atomic<uint64_t> ready{0};
     e = allow_smem(k, R::kSmem, &ready);
     if (e != cudaSuccess) return e;
-    const int units = p.m_tiles * p.n_tiles * p.splits;
+    const int units = p.m_tiles * p.n_tiles * p.splits, fit = sm_count() / (PAIR ? 2 : 1);
     const Args a{p.f, p.splits > 1 ? p.partial : nullptr, p.ld, p.m, p.n, p.blocks, p.m_tiles,
                  p.n_tiles, p.splits, units, p.a.across, p.b.across, status};
-    e = launch_k(k, dim3(units < sm_count() ? units : sm_count()), dim3(kProductThreads), R::kSmem,
-                 st, ma, mb, a);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)((units < fit ? units : fit) * (PAIR ? 2 : 1)));
+    cfg.blockDim = dim3(kProductThreads);
+    cfg.dynamicSmemBytes = R::kSmem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = 2;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = PAIR ? 2 : 1;
+    e = cudaLaunchKernelEx(&cfg, k, ma, mb, a);
     if (e != cudaSuccess || p.splits == 1) return e;
     const int64_t rows = p.f.swapped ? p.n : p.m, threads = rows * (p.ld / 8);
     return launch_k(k_linear_join<T>, dim3((unsigned)((threads + kThreads - 1) / kThreads)),
@@ -463,30 +616,37 @@ void plan_product(Product* p) {
     p->m = (int)p->a.rows();
     p->n = (int)p->b.rows();
     p->blocks = (int)((p->a.k() + kBlock - 1) / kBlock);
-    p->m_tiles = (p->m + 127) / 128;
     p->ld = ((p->f.swapped ? p->m : p->n) + 7) / 8 * 8;
-    const int sms = sm_count() > 0 ? sm_count() : 1;
-    const int widths[] = {256, 128, 64, 32}, cycles[] = {560, 330, 250, 220};
+    const int sms = sm_count() > 1 ? sm_count() : 2;
+    struct Kind {
+        int bn, cycles;
+        bool pair;
+    };
+    const Kind kinds[] = {{256, 530, true}, {256, 560, false}, {128, 330, false}, {64, 250, false},
+                          {32, 220, false}};
     double best = 0;
     p->bn = 0;
-    for (int i = 0; i < 4; ++i) {
-        const int bn = widths[i];
+    for (const Kind& kind : kinds) {
+        const int bn = kind.bn, rows = kind.pair ? 256 : 128, fit = kind.pair ? sms / 2 : sms;
         if (bn == 32 && (p->b.across || p->n > 32)) continue;   // a box across is 64 wide
         if (bn > 64 && p->n <= bn / 2) continue;
-        const int n_tiles = (p->n + bn - 1) / bn;
-        const int64_t tiles = (int64_t)p->m_tiles * n_tiles;
+        if (kind.pair && p->m <= 128) continue;
+        const int m_tiles = (p->m + rows - 1) / rows, n_tiles = (p->n + bn - 1) / bn;
+        const int64_t tiles = (int64_t)m_tiles * n_tiles;
         for (int s = 1; s <= 64 && s <= p->blocks; ++s) {
-            const int64_t rounds = (tiles * s + sms - 1) / sms;
-            double cost = 2000. + (double)rounds * ((p->blocks + s - 1) / s * cycles[i] + 300.);
+            const int64_t rounds = (tiles * s + fit - 1) / fit;
+            double cost = 2000. + (double)rounds * ((p->blocks + s - 1) / s * kind.cycles + 300.);
             // written and read at some 1800 bytes a cycle each, and a launch
             if (s > 1) cost += 4000. + (double)p->m * p->n * s * 8 / 1800;
             if (p->bn == 0 || cost < best) {
                 best = cost;
                 p->bn = bn;
+                p->pair = kind.pair;
+                p->m_tiles = m_tiles;
                 p->n_tiles = n_tiles;
                 p->splits = s;
             }
-            if (tiles * s >= 16 * sms) break;
+            if (tiles * s >= 16 * fit) break;
         }
     }
 }
@@ -500,10 +660,12 @@ cudaError_t launch_product(const Product& p, int type, unsigned long long* statu
     auto go = [&](auto t) {
         using T = decltype(t);
         switch (p.bn) {
-            case 256: return launch<256, T>(p, type, status, st);
-            case 128: return launch<128, T>(p, type, status, st);
-            case 64: return launch<64, T>(p, type, status, st);
-            default: return launch<32, T>(p, type, status, st);
+            case 256:
+                return p.pair ? launch<256, true, T>(p, type, status, st)
+                              : launch<256, false, T>(p, type, status, st);
+            case 128: return launch<128, false, T>(p, type, status, st);
+            case 64: return launch<64, false, T>(p, type, status, st);
+            default: return launch<32, false, T>(p, type, status, st);
         }
     };
     return type == PSS_BF16 ? go(bf16()) : go(f16());
