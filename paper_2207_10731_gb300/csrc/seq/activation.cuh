@@ -8,13 +8,20 @@ namespace seq {
 
 constexpr float kInvRoot2Pi = 0.39894228040143268f;
 
+// 1 / x of a normal number with a normal reciprocal, to a unit in the last place.
+__device__ __forceinline__ float reciprocal(float x) {
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
 // Phi(-a) = exp(-a^2 / 2) P(t) for a >= 0, t = 1 / (1 + 0.23 a): P is the polynomial of degree 8
 // nearest to erfcx(a / sqrt 2) / 2 in relative error on 0 <= a <= 15 (a least-squares fit
 // with weights raised where it is worst; 4.8e-8, and 4.3e-7 evaluated in fp32).  gelu and its slope
 // share the exponential, and both ends keep their relative accuracy.  CUDA's erfcf, which is
 // exact to a few units, made the pass over the gradient of 16384 x 4096 144 us instead of SLOPE.
 __device__ __forceinline__ float normal_below(float a, float e) {
-    const float t = __fdividef(1.f, fmaf(0.23f, a, 1.f));
+    const float t = reciprocal(fmaf(0.23f, a, 1.f));
     float p = -0.07848794013261795f;
     p = fmaf(p, t, 0.2905181646347046f);
     p = fmaf(p, t, -0.2783527970314026f);
@@ -35,7 +42,7 @@ __device__ __forceinline__ float activate(float z) {
         return z < 0.f ? z * q : z - z * q;
     }
     if (ACT == ACT_SILU) {
-        const float e = __expf(-fabsf(z)), inv = __fdividef(z, 1.f + e);
+        const float e = __expf(-fabsf(z)), inv = z * reciprocal(1.f + e);
         return z < 0.f ? e * inv : inv;
     }
     return z;
@@ -49,7 +56,7 @@ __device__ __forceinline__ float slope_of(float z) {
         return (z < 0.f ? q : 1.f - q) + z * kInvRoot2Pi * e;
     }
     if (ACT == ACT_SILU) {
-        const float e = __expf(-fabsf(z)), inv = __fdividef(1.f, 1.f + e);
+        const float e = __expf(-fabsf(z)), inv = reciprocal(1.f + e);
         const float s = z < 0.f ? e * inv : inv;
         return s + z * e * inv * inv;
     }

@@ -155,8 +155,8 @@ bool weight_matrix(const void* data, int64_t in, int64_t out, int64_t in_stride,
     return false;
 }
 
-bool rows32(const void* p, int64_t stride, int size) {
-    return !p || (aligned_to(p, 32) && stride * size % 32 == 0);
+bool rows16(const void* p, int64_t stride, int size) {
+    return !p || (aligned_to(p, 16) && stride * size % 16 == 0);
 }
 
 // Tiles and parts fit a launch.
@@ -193,10 +193,10 @@ int64_t lay_out(const pss_linear_forward_args* a, void* base, ForwardCall* c) {
     if (!on_grid(c->x)) c->x_copy = take(copy_bytes(c->x));
     if (!on_grid(c->w)) c->w_copy = take(copy_bytes(c->w));
     c->p.f = Finish{a->bias, a->residual, a->z, a->y, a->residual_stride, a->z_stride, a->y_stride,
-                    a->activation, a->y_type == PSS_F32, false, false};
+                    a->activation, a->y_type == PSS_F32, false, false, aligned_to(a->bias, 16)};
     const int size = a->y_type == PSS_F32 ? 4 : 2;
-    c->p.f.vectors = rows32(a->y, a->y_stride, size) && rows32(a->z, a->z_stride, 2) &&
-                     rows32(a->residual, a->residual_stride, size);
+    c->p.f.tiles = rows16(a->y, a->y_stride, size) && rows16(a->z, a->z_stride, 2) &&
+                     rows16(a->residual, a->residual_stride, size);
     orient(&c->p, Operand{c->x, false}, Operand{c->w, c->w_along_out});
     c->p.partial = static_cast<float*>(take(partial_values(c->p) * 4));
     return take.at;
@@ -239,7 +239,7 @@ int64_t lay_out(const pss_linear_backward_args* a, void* base, BackwardCall* c) 
     if (a->dx) {
         if (!on_grid(c->w)) c->w_copy = take(copy_bytes(c->w));
         c->dx.f = Finish{nullptr, nullptr, nullptr, a->dx, 0, 0, a->dx_stride, ACT_NONE, false, false,
-                         rows32(a->dx, a->dx_stride, 2)};
+                         rows16(a->dx, a->dx_stride, 2)};
         orient(&c->dx, Operand{c->dz, false}, Operand{c->w, !c->w_along_out});
         shared = partial_values(c->dx);
     }
@@ -247,7 +247,7 @@ int64_t lay_out(const pss_linear_backward_args* a, void* base, BackwardCall* c) 
         if (!on_grid(c->x)) c->x_copy = take(copy_bytes(c->x));
         const bool wide = a->dweight_type == PSS_F32;
         c->dw.f = Finish{nullptr, nullptr, nullptr, a->dweight, 0, 0, dw.stride, ACT_NONE, wide, false,
-                         rows32(a->dweight, dw.stride, wide ? 4 : 2)};
+                         rows16(a->dweight, dw.stride, wide ? 4 : 2)};
         const Operand x{c->x, true}, dz{c->dz, true};
         c->dw.a = c->dw_along_out ? x : dz;
         c->dw.b = c->dw_along_out ? dz : x;

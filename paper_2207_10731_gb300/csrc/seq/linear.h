@@ -34,7 +34,8 @@ struct Finish {
     int64_t residual_stride, z_stride, y_stride;
     int activation;
     bool y_f32, swapped;
-    bool vectors;           // rows of all tensors start at multiples of 32 bytes
+    bool tiles;             // rows of all tensors start at multiples of 16 bytes
+    bool bias_vectors;      // and so does the bias
 };
 
 // One product m x n x k: tiles of 128 x bn (of 256 x bn by a pair of CTAs), each contraction in `splits` parts whose sums go to

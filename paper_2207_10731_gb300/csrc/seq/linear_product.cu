@@ -27,7 +27,8 @@ namespace {
 constexpr int kBlock = 64;                   // of the contraction: 128 bytes
 constexpr int kFinishers = 8;                // warps
 constexpr int kProductThreads = 128 + 32 * kFinishers;
-constexpr int kPad = 33;                     // a staged row of 32 values
+constexpr int kStaged = 8192;                // a finishing warp's: two tiles of 32 rows x 128 bytes
+constexpr int kPad = 33;                     // or 32 rows of 32 fp32 values
 
 // PAIR: two CTAs of a cluster, on neighbouring SMs, make a tile of 256 x BN: each loads its 128
 // rows of A and half of B's, one thread of the first issues products that read both, and
@@ -37,9 +38,8 @@ template <int BN, bool PAIR>
 struct Ring {
     static constexpr int kA = 128 * kBlock * 2, kRows = PAIR ? BN / 2 : BN, kB = kRows * kBlock * 2;
     static constexpr int kStage = kA + kB;
-    static constexpr int kStages = PAIR || BN == 128 ? 6 : BN == 256 ? 4 : 8;
-    static constexpr int kStaging = kFinishers * 32 * kPad * 4;
-    static constexpr int kSmem = kStages * kStage + kStaging;
+    static constexpr int kStages = PAIR || BN == 128 ? 5 : BN == 64 ? 6 : 8;
+    static constexpr int kSmem = kStages * kStage + kFinishers * kStaged;
     static constexpr int kCols = 2 * BN;     // tensor-memory columns: two accumulators
 };
 
@@ -142,6 +142,10 @@ struct Args {
 struct Unit {
     int m, n, k0, k1, split;
 };
+// blocks < 2^25, splits <= 64
+__device__ __forceinline__ int part_start(const Args& a, int split) {
+    return a.splits == 1 ? split * a.blocks : (int)((unsigned)(a.blocks * split) / (unsigned)a.splits);
+}
 __device__ __forceinline__ Unit unit_of(const Args& a, int u) {
     constexpr int kBand = 16;
     Unit w;
@@ -150,64 +154,94 @@ __device__ __forceinline__ Unit unit_of(const Args& a, int u) {
     const int high = min(kBand, a.m_tiles - band * kBand);
     w.n = in / high;
     w.m = band * kBand + in - w.n * high;
-    w.k0 = (int)((int64_t)a.blocks * w.split / a.splits);
-    w.k1 = (int)((int64_t)a.blocks * (w.split + 1) / a.splits);
+    w.k0 = part_start(a, w.split);
+    w.k1 = part_start(a, w.split + 1);
     return w;
 }
+// The blocks of unit u.
+__device__ __forceinline__ int blocks_of(const Args& a, int u) {
+    if (a.splits == 1) return a.blocks;
+    const int split = u % a.splits;
+    return part_start(a, split + 1) - part_start(a, split);
+}
 
-// 16 values of 16 bits, or 8 of 32: 32 bytes in one instruction.
-__device__ __forceinline__ void load32b(const void* p, uint32_t (&r)[8]) {
-    asm volatile("ld.global.L1::no_allocate.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]),
-                   "=r"(r[6]), "=r"(r[7]) : "l"(p) : "memory");
+// ---- finishing through shared memory -------------------------------------------
+// A warp's tile: 32 rows of 128 bytes, the 16-byte piece p of row r in the 128-byte swizzle, as
+// TMA stores it.  (32-byte stores of a row a lane, 32 lines an instruction: 7400 cycles a tile
+// of 128 x 256 instead of PLAIN.)
+
+__device__ __forceinline__ uint32_t piece_at(uint32_t tile, int row, int p) {
+    return tile + row * 128 + ((p ^ (row & 7)) << 4);
 }
-__device__ __forceinline__ void store32b(void* p, const uint32_t (&r)[8]) {
-    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
-                 :: "l"(p), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]),
-                    "r"(r[6]), "r"(r[7]) : "memory");
+__device__ __forceinline__ void put_piece(uint32_t at, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" :: "r"(at), "r"(a), "r"(b), "r"(c), "r"(d)
+                 : "memory");
 }
-// 32 values of T or fp32 at p.
+__device__ __forceinline__ uint4 get_piece(uint32_t at) {
+    uint4 w;
+    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(w.x), "=r"(w.y), "=r"(w.z), "=r"(w.w) : "r"(at) : "memory");
+    return w;
+}
+// 32 values of row `row`, from its piece p on.
 template <typename T>
-__device__ __forceinline__ void put32(T* p, const float (&v)[32]) {
+__device__ __forceinline__ void put32(uint32_t tile, int row, int p, const float (&v)[32], T) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        uint32_t w[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) w[i] = pack2(v[16 * h + 2 * i], v[16 * h + 2 * i + 1], T());
-        store32b(p + 16 * h, w);
-    }
+    for (int i = 0; i < 4; ++i)
+        put_piece(piece_at(tile, row, p + i), pack2(v[8 * i], v[8 * i + 1], T()),
+                  pack2(v[8 * i + 2], v[8 * i + 3], T()), pack2(v[8 * i + 4], v[8 * i + 5], T()),
+                  pack2(v[8 * i + 6], v[8 * i + 7], T()));
 }
-__device__ __forceinline__ void put32(float* p, const float (&v)[32]) {
+__device__ __forceinline__ void put32(uint32_t tile, int row, int p, const float (&v)[32], float) {
 #pragma unroll
-    for (int h = 0; h < 4; ++h) {
-        uint32_t w[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) w[i] = __float_as_uint(v[8 * h + i]);
-        store32b(p + 8 * h, w);
-    }
+    for (int i = 0; i < 8; ++i)
+        put_piece(piece_at(tile, row, p + i), __float_as_uint(v[4 * i]), __float_as_uint(v[4 * i + 1]),
+                  __float_as_uint(v[4 * i + 2]), __float_as_uint(v[4 * i + 3]));
 }
 template <typename T>
-__device__ __forceinline__ void add32(const T* p, float (&v)[32]) {
+__device__ __forceinline__ void add32(uint32_t tile, int row, int p, float (&v)[32], T) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        uint32_t w[8];
-        load32b(p + 16 * h, w);
+    for (int i = 0; i < 4; ++i) {
+        const uint4 w = get_piece(piece_at(tile, row, p + i));
+        const uint32_t x[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float2 x = unpack2(w[i], T());
-            v[16 * h + 2 * i] += x.x;
-            v[16 * h + 2 * i + 1] += x.y;
+        for (int e = 0; e < 4; ++e) {
+            const float2 y = unpack2(x[e], T());
+            v[8 * i + 2 * e] += y.x;
+            v[8 * i + 2 * e + 1] += y.y;
         }
     }
 }
-__device__ __forceinline__ void add32(const float* p, float (&v)[32]) {
+__device__ __forceinline__ void add32(uint32_t tile, int row, int p, float (&v)[32], float) {
 #pragma unroll
-    for (int h = 0; h < 4; ++h) {
-        uint32_t w[8];
-        load32b(p + 8 * h, w);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[8 * h + i] += __uint_as_float(w[i]);
+    for (int i = 0; i < 8; ++i) {
+        const uint4 w = get_piece(piece_at(tile, row, p + i));
+        v[4 * i] += __uint_as_float(w.x);
+        v[4 * i + 1] += __uint_as_float(w.y);
+        v[4 * i + 2] += __uint_as_float(w.z);
+        v[4 * i + 3] += __uint_as_float(w.w);
     }
+}
+// Copies a tile's rows of the residual in, 8 lanes to a row; zeros outside the tensor.
+template <typename TY>
+__device__ __forceinline__ void fetch_tile(uint32_t tile, const TY* from, int64_t stride, int rows,
+                                           int cols) {
+    constexpr int kValues = 16 / sizeof(TY);
+    const int lane = threadIdx.x & 31, p = lane & 7;
+    const int left = min(16, max(0, (cols - p * kValues) * (int)sizeof(TY)));
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int r = 4 * i + (lane >> 3), size = r < rows ? left : 0;
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;"
+                     :: "r"(piece_at(tile, r, p)),
+                        "l"(size > 0 ? from + r * stride + p * kValues : from), "r"(size) : "memory");
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+}
+__device__ __forceinline__ void tma_store(const CUtensorMap* map, uint32_t tile, int c0, int c1,
+                                          int c2) {
+    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%1, %2, %3}], [%4];"
+                 :: "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(tile) : "memory");
 }
 
 template <typename T>
@@ -232,31 +266,99 @@ __device__ __forceinline__ void finish_one(const Finish& f, float v, int64_t t, 
         static_cast<T*>(f.y)[at] = round_to<T>(v);
 }
 
-// 32 values of row t from column c on, all inside.
 template <typename T>
-__device__ __forceinline__ void finish_32(const Finish& f, float (&v)[32], int64_t t, int64_t c) {
-    if (f.bias) {
+__device__ __forceinline__ void add_bias(const Finish& f, float (&v)[32], int c, int n) {
+    if (f.bias_vectors && c + 32 <= n) {
 #pragma unroll
-        for (int i = 0; i < 32; ++i) v[i] += __ldg(f.bias + c + i);
-    }
-    if (f.z) put32(static_cast<T*>(f.z) + t * f.z_stride + c, v);
-    with_activation(f.activation, [&](auto act) {
-#pragma unroll
-        for (int i = 0; i < 32; ++i) v[i] = activate<decltype(act)::value>(v[i]);
-    });
-    const int64_t at = t * f.y_stride + c, from = t * f.residual_stride + c;
-    if (f.y_f32) {
-        if (f.residual) add32(static_cast<const float*>(f.residual) + from, v);
-        put32(static_cast<float*>(f.y) + at, v);
+        for (int i = 0; i < 8; ++i) {
+            const float4 b = __ldg(reinterpret_cast<const float4*>(f.bias + c) + i);
+            v[4 * i] += b.x;
+            v[4 * i + 1] += b.y;
+            v[4 * i + 2] += b.z;
+            v[4 * i + 3] += b.w;
+        }
     } else {
-        if (f.residual) add32(static_cast<const T*>(f.residual) + from, v);
-        put32(static_cast<T*>(f.y) + at, v);
+#pragma unroll
+        for (int i = 0; i < 32; ++i) v[i] += c + i < n ? __ldg(f.bias + c + i) : 0.f;
     }
+}
+
+// A finishing warp's part of a tile, rows row0 .. +32 and columns col .. of the accumulator at d:
+// tiles of 128 bytes' width (64 columns of 16 bits, 32 of fp32) are made in shared memory,
+// over the residual's where there is one, and stored by TMA, which leaves out what lies outside.
+// wait(): until the accumulator is there; asked for after the first residual.
+template <int BN, typename T, typename TY, typename W>
+__device__ __forceinline__ bool finish_tiles(const Args& a, const CUtensorMap* my,
+                                             const CUtensorMap* mz, uint32_t staged, uint32_t d,
+                                             int row0, int col0, int half, int split, W wait) {
+    const Finish& f = a.f;
+    constexpr int kWide = 128 / sizeof(TY) < BN ? 128 / sizeof(TY) : BN;   // columns of a tile
+    const int lane = threadIdx.x & 31;
+    const bool partial = a.partial != nullptr;
+    const uint32_t y_tile = staged, z_tile = staged + 4096;
+    bool waited = false;
+    for (int c = half * kWide; c < BN; c += 2 * kWide) {
+        const int col = col0 + c;
+        if (col >= a.n || row0 >= a.m) break;
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+        __syncwarp();
+        const bool more = f.residual && !partial;
+        if (more)
+            fetch_tile(y_tile, static_cast<const TY*>(f.residual) + (int64_t)row0 * f.residual_stride + col,
+                       f.residual_stride, a.m - row0, a.n - col);
+        if (!waited) {
+            if (!wait()) return false;
+            waited = true;
+        }
+        if (more) {
+            asm volatile("cp.async.wait_all;" ::: "memory");
+            __syncwarp();
+        }
+#pragma unroll
+        for (int h = 0; h < kWide; h += 32) {
+            float v[32];
+            tmem_load32(d + c + h, v);
+            tmem_wait_load();
+            tmem_loaded(v);
+            if (!partial) {
+                if (f.bias) add_bias<T>(f, v, col + h, a.n);
+                if (f.z) {
+                    if (sizeof(TY) == 2) {
+                        put32(z_tile, lane, h / 8, v, T());
+                    } else if (row0 + lane < a.m) {   // half a tile's width: as it is
+#pragma unroll
+                        for (int i = 0; i < 32; i += 8) {
+                            float x[8];
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) x[e] = v[i + e];
+                            T* to = static_cast<T*>(f.z) + (int64_t)(row0 + lane) * f.z_stride;
+                            store_part(to, col + i, a.n, x);
+                        }
+                    }
+                }
+                with_activation(f.activation, [&](auto act) {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) v[i] = activate<decltype(act)::value>(v[i]);
+                });
+                if (more) add32(y_tile, lane, h / (16 / (int)sizeof(TY)), v, TY());
+            }
+            put32(y_tile, lane, h / (16 / (int)sizeof(TY)), v, TY());
+        }
+        fence_async();
+        __syncwarp();
+        if (lane == 0) {
+            if (f.z && !partial && sizeof(TY) == 2) tma_store(mz, z_tile, col, row0, 0);
+            tma_store(my, y_tile, col, row0, partial ? split : 0);
+            asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+        }
+    }
+    return waited || wait();
 }
 
 template <int BN, bool PAIR, typename T>
 __global__ void __launch_bounds__(kProductThreads, 1)
 k_linear_product(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUtensorMap mb,
+                 const __grid_constant__ CUtensorMap my, const __grid_constant__ CUtensorMap mz,
                  const __grid_constant__ Args a) {
     pdl_prologue();
     using R = Ring<BN, PAIR>;
@@ -359,13 +461,15 @@ k_linear_product(const __grid_constant__ CUtensorMap ma, const __grid_constant__
             };
             int s = 0, i = 0;
             bool ok = true;
-            for (int u = first_unit; ok && u < a.units; u += step, ++i) {
-                const Unit w = unit_of(a, u);
+            // a unit's blocks are counted while the one before is worked on: divisions between
+            // two units' products leave the tensor core idle
+            int blocks = first_unit < a.units ? blocks_of(a, first_unit) : 0, next = 0;
+            for (int u = first_unit; ok && u < a.units; u += step, ++i, blocks = next) {
                 const uint32_t d = tmem + (i & 1) * BN;
                 if (i > 1)
                     ok = PAIR ? bar_wait_cluster(&free_[i & 1], ((i >> 1) - 1) & 1, &stop)
                               : bar_wait(&free_[i & 1], ((i >> 1) - 1) & 1, &stop);
-                for (int k = w.k0; ok && k < w.k1; ++k, ++s) {
+                for (int k = 0; ok && k < blocks; ++k, ++s) {
                     const int slot = s % R::kStages;
                     ok = bar_wait(&full[slot], (s / R::kStages) & 1, &stop);
                     if (!ok) break;
@@ -376,11 +480,12 @@ k_linear_product(const __grid_constant__ CUtensorMap ma, const __grid_constant__
                         const uint64_t x = smem_desc(a_at + j * a_step, a_lead);
                         const uint64_t y = smem_desc(b_at + j * b_step, b_lead);
                         if (PAIR)
-                            mma_pair(d, x, y, desc, k > w.k0 || j > 0);
+                            mma_pair(d, x, y, desc, k > 0 || j > 0);
                         else
-                            mma_ss(d, x, y, desc, k > w.k0 || j > 0);
+                            mma_ss(d, x, y, desc, k > 0 || j > 0);
                     }
                     commit(&empty[slot]);
+                    if (k == 0) next = blocks_of(a, u + step);
                 }
                 if (ok) commit(&done[i & 1]);
             }
@@ -390,74 +495,75 @@ k_linear_product(const __grid_constant__ CUtensorMap ma, const __grid_constant__
             bar_wait(&drained, 0, &never);
         }
     } else if (warp >= 4) {
-        // ---- finishing: a thread to a row of the tile, every second 32 columns ----
+        // ---- finishing: a thread to a row of the tile, two warps to 32 rows ----
         const int quarter = warp & 3, half = (warp - 4) >> 2;
-        float* staged = reinterpret_cast<float*>(smem + R::kStages * R::kStage) +
-                        (warp - 4) * 32 * kPad;
+        uint8_t* staged = smem + R::kStages * R::kStage + (warp - 4) * kStaged;
+        const Finish& f = a.f;
         int i = 0;
         for (int u = first_unit; u < a.units; u += step, ++i) {
             const Unit w = unit_of(a, u);
-            if (!__all_sync(0xffffffffu, bar_wait(&done[i & 1], (i >> 1) & 1, &stop))) break;
-            tc_after_sync();
             const uint32_t d = tmem + (i & 1) * BN + ((uint32_t)quarter << 21);
             const int row0 = (w.m * kCtas + rank) * 128 + quarter * 32, row = row0 + lane;
-            const Finish& f = a.f;
-            float* partial = a.partial ? a.partial + (int64_t)w.split * (f.swapped ? a.n : a.m) * a.ld
-                                       : nullptr;
-            for (int c = half; c < BN / 32; c += 2) {
-                const int col = w.n * BN + c * 32;
-                if (col >= a.n) break;
-                float v[32];
-                tmem_load32(d + c * 32, v);
-                tmem_wait_load();
-                tmem_loaded(v);
-                if (f.swapped) {
-                    // lanes are neighbours in memory already
-                    if (row < a.m) {
-                        const float bias = !partial && f.bias ? f.bias[row] : 0.f;
+            auto wait = [&] {
+                const bool ok = __all_sync(0xffffffffu, bar_wait(&done[i & 1], (i >> 1) & 1, &stop));
+                tc_after_sync();
+                return ok;
+            };
+            if (f.tiles) {
+                const bool ok =
+                    a.partial || f.y_f32
+                        ? finish_tiles<BN, T, float>(a, &my, &mz, smem_addr(staged), d, row0, w.n * BN,
+                                                     half, w.split, wait)
+                        : finish_tiles<BN, T, T>(a, &my, &mz, smem_addr(staged), d, row0, w.n * BN,
+                                                 half, w.split, wait);
+                if (!ok) break;
+            } else {
+                if (!wait()) break;
+                float* partial = a.partial ? a.partial + (int64_t)w.split * a.n * a.ld : nullptr;
+                for (int c = half; c < BN / 32; c += 2) {
+                    const int col = w.n * BN + c * 32;
+                    if (col >= a.n) break;
+                    float v[32];
+                    tmem_load32(d + c * 32, v);
+                    tmem_wait_load();
+                    tmem_loaded(v);
+                    if (f.swapped) {
+                        // lanes are neighbours in memory already
+                        if (row < a.m) {
+                            const float bias = !partial && f.bias ? f.bias[row] : 0.f;
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) {
-                            if (col + j >= a.n) break;
-                            if (partial)
-                                partial[(int64_t)(col + j) * a.ld + row] = v[j];
-                            else
-                                finish_one<T>(f, v[j], col + j, row, bias,
-                                              f.residual ? residual_at<T>(f, col + j, row) : 0.f);
+                            for (int j = 0; j < 32; ++j) {
+                                if (col + j >= a.n) break;
+                                if (partial)
+                                    partial[(int64_t)(col + j) * a.ld + row] = v[j];
+                                else
+                                    finish_one<T>(f, v[j], col + j, row, bias,
+                                                  f.residual ? residual_at<T>(f, col + j, row) : 0.f);
+                            }
                         }
-                    }
-                } else if (partial) {
-                    if (row < a.m) {
+                    } else {
+                        // through shared memory: a row at a time, a lane to a column
+                        float* values = reinterpret_cast<float*>(staged);
+                        __syncwarp();
 #pragma unroll
-                        for (int j = 0; j < 32; j += 8) {
-                            float x[8];
+                        for (int j = 0; j < 32; ++j) values[lane * kPad + j] = v[j];
+                        __syncwarp();
+                        if (col + lane < a.n) {
+                            const float bias = f.bias ? f.bias[col + lane] : 0.f;
+                            const int last = min(32, a.m - row0);
+                            // eight rows' residuals are asked for before the first is waited for
+                            for (int j = 0; j < last; j += 8) {
+                                float more[8];
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) x[e] = v[j + e];
-                            if (col + j < a.n) store8(partial + (int64_t)row * a.ld + col + j, x);
-                        }
-                    }
-                } else if (f.vectors && col + 32 <= a.n) {
-                    if (row < a.m) finish_32<T>(f, v, row, col);
-                } else {
-                    // through shared memory: a row at a time, a lane to a column
-                    __syncwarp();
+                                for (int e = 0; e < 8; ++e)
+                                    more[e] = f.residual && j + e < last
+                                                  ? residual_at<T>(f, row0 + j + e, col + lane) : 0.f;
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) staged[lane * kPad + j] = v[j];
-                    __syncwarp();
-                    if (col + lane < a.n) {
-                        const float bias = f.bias ? f.bias[col + lane] : 0.f;
-                        const int last = min(32, a.m - row0);
-                        // eight rows' residuals are asked for before the first is waited for
-                        for (int j = 0; j < last; j += 8) {
-                            float more[8];
-#pragma unroll
-                            for (int e = 0; e < 8; ++e)
-                                more[e] = f.residual && j + e < last
-                                              ? residual_at<T>(f, row0 + j + e, col + lane) : 0.f;
-#pragma unroll
-                            for (int e = 0; e < 8; ++e)
-                                if (j + e < last)
-                                    finish_one<T>(f, staged[(j + e) * kPad + lane], row0 + j + e,
-                                                  col + lane, bias, more[e]);
+                                for (int e = 0; e < 8; ++e)
+                                    if (j + e < last)
+                                        finish_one<T>(f, values[(j + e) * kPad + lane], row0 + j + e,
+                                                      col + lane, bias, more[e]);
+                            }
                         }
                     }
                 }
@@ -471,6 +577,8 @@ k_linear_product(const __grid_constant__ CUtensorMap ma, const __grid_constant__
                     bar_arrive(&free_[i & 1]);
             }
         }
+        // the stores have read their tiles before the CTA's memory is another's
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
     }
     tc_before_sync();
     __syncthreads();
@@ -540,19 +648,54 @@ cudaError_t operand_map(CUtensorMap* map, const Operand& o, int box, int type) {
     return rc == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
 
+// Results [parts][rows][cols], stored in boxes of `width` columns (at most 128 bytes) x 32 rows.
+cudaError_t result_map(CUtensorMap* map, void* data, int64_t cols, int64_t rows, int64_t parts,
+                       int64_t stride, int64_t part_stride, int width, int type) {
+    static std::atomic<void*> found{nullptr};
+    void* fn = driver_call("cuTensorMapEncodeTiled", &found);
+    if (!fn) return cudaErrorNotSupported;
+    const int64_t size = type == PSS_F32 ? 4 : 2, grid = 16 / size;
+    if (rows <= 1) stride = (cols + grid - 1) / grid * grid;       // free, but checked
+    if (parts <= 1) part_stride = stride;
+    const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)parts};
+    const cuuint64_t strides[2] = {(cuuint64_t)(stride * size), (cuuint64_t)(part_stride * size)};
+    const cuuint32_t box[3] = {(cuuint32_t)width, 32, 1}, one[3] = {1, 1, 1};
+    const CUresult rc = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(fn)(
+        map,
+        type == PSS_F32    ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
+        : type == PSS_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
+                           : CU_TENSOR_MAP_DATA_TYPE_FLOAT16,
+        3, data, dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+        CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return rc == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+
 template <int BN, bool PAIR, typename T>
 cudaError_t launch(const Product& p, int type, unsigned long long* status, cudaStream_t st) {
     using R = Ring<BN, PAIR>;
-    CUtensorMap ma, mb;
+    CUtensorMap ma, mb, my = {}, mz = {};
     cudaError_t e = operand_map(&ma, p.a, 128, type);
     if (e == cudaSuccess) e = operand_map(&mb, p.b, R::kRows, type);
+    Finish f = p.f;
+    const bool split = p.splits > 1;
+    f.tiles = !f.swapped && (split || f.tiles);
+    if (f.tiles && e == cudaSuccess) {
+        const int width = 64;   // 128 bytes, also where BN = 32 is all there is
+        if (split)
+            e = result_map(&my, p.partial, p.n, p.m, p.splits, p.ld, (int64_t)p.m * p.ld, 32, PSS_F32);
+        else
+            e = result_map(&my, f.y, p.n, p.m, 1, f.y_stride, (int64_t)p.m * f.y_stride,
+                           f.y_f32 ? 32 : width, f.y_f32 ? PSS_F32 : type);
+        if (!split && f.z && !f.y_f32 && e == cudaSuccess)
+            e = result_map(&mz, f.z, p.n, p.m, 1, f.z_stride, (int64_t)p.m * f.z_stride, width, type);
+    }
     if (e != cudaSuccess) return e;
     auto* k = k_linear_product<BN, PAIR, T>;
     static std::atomic<uint64_t> ready{0};
     e = allow_smem(k, R::kSmem, &ready);
     if (e != cudaSuccess) return e;
     const int units = p.m_tiles * p.n_tiles * p.splits, fit = sm_count() / (PAIR ? 2 : 1);
-    const Args a{p.f, p.splits > 1 ? p.partial : nullptr, p.ld, p.m, p.n, p.blocks, p.m_tiles,
+    const Args a{f, split ? p.partial : nullptr, p.ld, p.m, p.n, p.blocks, p.m_tiles,
                  p.n_tiles, p.splits, units, p.a.across, p.b.across, status};
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)((units < fit ? units : fit) * (PAIR ? 2 : 1)));
@@ -567,7 +710,7 @@ cudaError_t launch(const Product& p, int type, unsigned long long* status, cudaS
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = PAIR ? 2 : 1;
-    e = cudaLaunchKernelEx(&cfg, k, ma, mb, a);
+    e = cudaLaunchKernelEx(&cfg, k, ma, mb, my, mz, a);
     if (e != cudaSuccess || p.splits == 1) return e;
     const int64_t rows = p.f.swapped ? p.n : p.m, threads = rows * (p.ld / 8);
     return launch_k(k_linear_join<T>, dim3((unsigned)((threads + kThreads - 1) / kThreads)),
@@ -622,7 +765,7 @@ void plan_product(Product* p) {
         int bn, cycles;
         bool pair;
     };
-    const Kind kinds[] = {{256, 530, true}, {256, 560, false}, {128, 330, false}, {64, 250, false},
+    const Kind kinds[] = {{256, 530, true}, {128, 330, false}, {64, 250, false},
                           {32, 220, false}};
     double best = 0;
     p->bn = 0;
@@ -660,9 +803,7 @@ cudaError_t launch_product(const Product& p, int type, unsigned long long* statu
     auto go = [&](auto t) {
         using T = decltype(t);
         switch (p.bn) {
-            case 256:
-                return p.pair ? launch<256, true, T>(p, type, status, st)
-                              : launch<256, false, T>(p, type, status, st);
+            case 256: return launch<256, true, T>(p, type, status, st);
             case 128: return launch<128, false, T>(p, type, status, st);
             case 64: return launch<64, false, T>(p, type, status, st);
             default: return launch<32, false, T>(p, type, status, st);
