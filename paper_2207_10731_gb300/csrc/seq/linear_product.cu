@@ -27,8 +27,7 @@ namespace {
 constexpr int kBlock = 64;                   // of the contraction: 128 bytes
 constexpr int kFinishers = 8;                // warps
 constexpr int kProductThreads = 128 + 32 * kFinishers;
-constexpr int kStaged = 8192;                // a finishing warp's: two tiles of 32 rows x 128 bytes
-constexpr int kPad = 33;                     // or 32 rows of 32 fp32 values
+constexpr int kStaged = 4096;                // a finishing warp's tile: 32 rows of 128 bytes
 
 // PAIR: two CTAs of a cluster, on neighbouring SMs, make a tile of 256 x BN: each loads its 128
 // rows of A and half of B's, one thread of the first issues products that read both, and
@@ -38,7 +37,8 @@ template <int BN, bool PAIR>
 struct Ring {
     static constexpr int kA = 128 * kBlock * 2, kRows = PAIR ? BN / 2 : BN, kB = kRows * kBlock * 2;
     static constexpr int kStage = kA + kB;
-    static constexpr int kStages = PAIR || BN == 128 ? 5 : BN == 64 ? 6 : 8;
+    // (pairs, 16384 x 4096 x 4096: 3 stages 399 us, 4 335, 5 311, 6 310)
+    static constexpr int kStages = PAIR || BN == 128 ? 6 : 8;
     static constexpr int kSmem = kStages * kStage + kFinishers * kStaged;
     static constexpr int kCols = 2 * BN;     // tensor-memory columns: two accumulators
 };
@@ -286,29 +286,73 @@ __device__ __forceinline__ void add_bias(const Finish& f, float (&v)[32], int c,
 // A finishing warp's part of a tile, rows row0 .. +32 and columns col .. of the accumulator at d:
 // tiles of 128 bytes' width (64 columns of 16 bits, 32 of fp32) are made in shared memory,
 // over the residual's where there is one, and stored by TMA, which leaves out what lies outside.
-// wait(): until the accumulator is there; asked for after the first residual.
+// z goes first, and y from the accumulator again.  wait(): until the accumulator is there;
+// asked for after the first residual.
 template <int BN, typename T, typename TY, typename W>
 __device__ __forceinline__ bool finish_tiles(const Args& a, const CUtensorMap* my,
-                                             const CUtensorMap* mz, uint32_t staged, uint32_t d,
+                                             const CUtensorMap* mz, uint32_t tile, uint32_t d,
                                              int row0, int col0, int half, int split, W wait) {
     const Finish& f = a.f;
     constexpr int kWide = 128 / sizeof(TY) < BN ? 128 / sizeof(TY) : BN;   // columns of a tile
     const int lane = threadIdx.x & 31;
     const bool partial = a.partial != nullptr;
-    const uint32_t y_tile = staged, z_tile = staged + 4096;
     bool waited = false;
+    // the tile's last store has read it (two tiles in turns: no faster)
+    auto tile_free = [&] {
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+        __syncwarp();
+    };
+    auto store = [&](const CUtensorMap* map, int col, int part) {
+        fence_async();
+        __syncwarp();
+        if (lane == 0) {
+            tma_store(map, tile, col, row0, part);
+            asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+        }
+    };
+    auto sums = [&](float (&v)[32], int c, int col) {
+        tmem_load32(d + c, v);
+        tmem_wait_load();
+        tmem_loaded(v);
+        if (f.bias && !partial) add_bias<T>(f, v, col, a.n);
+    };
     for (int c = half * kWide; c < BN; c += 2 * kWide) {
         const int col = col0 + c;
         if (col >= a.n || row0 >= a.m) break;
-        if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
-        __syncwarp();
-        const bool more = f.residual && !partial;
-        if (more)
-            fetch_tile(y_tile, static_cast<const TY*>(f.residual) + (int64_t)row0 * f.residual_stride + col,
+        const bool more = f.residual && !partial, first_z = f.z && !partial;
+        auto fetch = [&] {
+            fetch_tile(tile, static_cast<const TY*>(f.residual) + (int64_t)row0 * f.residual_stride + col,
                        f.residual_stride, a.m - row0, a.n - col);
+        };
+        tile_free();
+        if (more && !first_z) fetch();
         if (!waited) {
             if (!wait()) return false;
             waited = true;
+        }
+        if (first_z) {
+#pragma unroll
+            for (int h = 0; h < kWide; h += 32) {
+                float v[32];
+                sums(v, c + h, col + h);
+                if (sizeof(TY) == 2) {
+                    put32(tile, lane, h / 8, v, T());
+                } else if (row0 + lane < a.m) {   // half a tile's width: as it is
+#pragma unroll
+                    for (int i = 0; i < 32; i += 8) {
+                        float x[8];
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) x[e] = v[i + e];
+                        T* to = static_cast<T*>(f.z) + (int64_t)(row0 + lane) * f.z_stride;
+                        store_part(to, col + i, a.n, x);
+                    }
+                }
+            }
+            if (sizeof(TY) == 2) {
+                store(mz, col, 0);
+                tile_free();
+            }
+            if (more) fetch();
         }
         if (more) {
             asm volatile("cp.async.wait_all;" ::: "memory");
@@ -317,40 +361,17 @@ __device__ __forceinline__ bool finish_tiles(const Args& a, const CUtensorMap* m
 #pragma unroll
         for (int h = 0; h < kWide; h += 32) {
             float v[32];
-            tmem_load32(d + c + h, v);
-            tmem_wait_load();
-            tmem_loaded(v);
+            sums(v, c + h, col + h);
             if (!partial) {
-                if (f.bias) add_bias<T>(f, v, col + h, a.n);
-                if (f.z) {
-                    if (sizeof(TY) == 2) {
-                        put32(z_tile, lane, h / 8, v, T());
-                    } else if (row0 + lane < a.m) {   // half a tile's width: as it is
-#pragma unroll
-                        for (int i = 0; i < 32; i += 8) {
-                            float x[8];
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) x[e] = v[i + e];
-                            T* to = static_cast<T*>(f.z) + (int64_t)(row0 + lane) * f.z_stride;
-                            store_part(to, col + i, a.n, x);
-                        }
-                    }
-                }
                 with_activation(f.activation, [&](auto act) {
 #pragma unroll
                     for (int i = 0; i < 32; ++i) v[i] = activate<decltype(act)::value>(v[i]);
                 });
-                if (more) add32(y_tile, lane, h / (16 / (int)sizeof(TY)), v, TY());
+                if (more) add32(tile, lane, h / (16 / (int)sizeof(TY)), v, TY());
             }
-            put32(y_tile, lane, h / (16 / (int)sizeof(TY)), v, TY());
+            put32(tile, lane, h / (16 / (int)sizeof(TY)), v, TY());
         }
-        fence_async();
-        __syncwarp();
-        if (lane == 0) {
-            if (f.z && !partial && sizeof(TY) == 2) tma_store(mz, z_tile, col, row0, 0);
-            tma_store(my, y_tile, col, row0, partial ? split : 0);
-            asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-        }
+        store(my, col, partial ? split : 0);
     }
     return waited || wait();
 }
@@ -461,10 +482,11 @@ k_linear_product(const __grid_constant__ CUtensorMap ma, const __grid_constant__
             };
             int s = 0, i = 0;
             bool ok = true;
-            // a unit's blocks are counted while the one before is worked on: divisions between
-            // two units' products leave the tensor core idle
+            // a unit's blocks are counted before the one in front of it is worked on: divisions
+            // between two units' products leave the tensor core idle
             int blocks = first_unit < a.units ? blocks_of(a, first_unit) : 0, next = 0;
             for (int u = first_unit; ok && u < a.units; u += step, ++i, blocks = next) {
+                next = blocks_of(a, u + step);
                 const uint32_t d = tmem + (i & 1) * BN;
                 if (i > 1)
                     ok = PAIR ? bar_wait_cluster(&free_[i & 1], ((i >> 1) - 1) & 1, &stop)
@@ -485,7 +507,6 @@ k_linear_product(const __grid_constant__ CUtensorMap ma, const __grid_constant__
                             mma_ss(d, x, y, desc, k > 0 || j > 0);
                     }
                     commit(&empty[slot]);
-                    if (k == 0) next = blocks_of(a, u + step);
                 }
                 if (ok) commit(&done[i & 1]);
             }
@@ -499,6 +520,7 @@ k_linear_product(const __grid_constant__ CUtensorMap ma, const __grid_constant__
         const int quarter = warp & 3, half = (warp - 4) >> 2;
         uint8_t* staged = smem + R::kStages * R::kStage + (warp - 4) * kStaged;
         const Finish& f = a.f;
+        const uint32_t tile = smem_addr(staged);
         int i = 0;
         for (int u = first_unit; u < a.units; u += step, ++i) {
             const Unit w = unit_of(a, u);
@@ -512,9 +534,9 @@ k_linear_product(const __grid_constant__ CUtensorMap ma, const __grid_constant__
             if (f.tiles) {
                 const bool ok =
                     a.partial || f.y_f32
-                        ? finish_tiles<BN, T, float>(a, &my, &mz, smem_addr(staged), d, row0, w.n * BN,
+                        ? finish_tiles<BN, T, float>(a, &my, &mz, tile, d, row0, w.n * BN,
                                                      half, w.split, wait)
-                        : finish_tiles<BN, T, T>(a, &my, &mz, smem_addr(staged), d, row0, w.n * BN,
+                        : finish_tiles<BN, T, T>(a, &my, &mz, tile, d, row0, w.n * BN,
                                                  half, w.split, wait);
                 if (!ok) break;
             } else {
@@ -546,7 +568,7 @@ k_linear_product(const __grid_constant__ CUtensorMap ma, const __grid_constant__
                         float* values = reinterpret_cast<float*>(staged);
                         __syncwarp();
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) values[lane * kPad + j] = v[j];
+                        for (int j = 0; j < 32; ++j) values[lane * 32 + (j ^ lane)] = v[j];
                         __syncwarp();
                         if (col + lane < a.n) {
                             const float bias = f.bias ? f.bias[col + lane] : 0.f;
@@ -561,8 +583,8 @@ k_linear_product(const __grid_constant__ CUtensorMap ma, const __grid_constant__
 #pragma unroll
                                 for (int e = 0; e < 8; ++e)
                                     if (j + e < last)
-                                        finish_one<T>(f, values[(j + e) * kPad + lane], row0 + j + e,
-                                                      col + lane, bias, more[e]);
+                                        finish_one<T>(f, values[(j + e) * 32 + (lane ^ (j + e))],
+                                                      row0 + j + e, col + lane, bias, more[e]);
                             }
                         }
                     }
