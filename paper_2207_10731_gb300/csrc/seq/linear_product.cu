@@ -132,7 +132,7 @@ struct Args {
     Finish f;
     float* partial;
     int64_t ld;
-    int m, n, blocks, m_tiles, n_tiles, splits, units;
+    int m, n, bn, blocks, m_tiles, n_tiles, splits, units;
     bool a_across, b_across;
     unsigned long long* status;
 };
@@ -283,6 +283,32 @@ __device__ __forceinline__ void add_bias(const Finish& f, float (&v)[32], int c,
     }
 }
 
+// 32 values of row t from column c of n on, with their bias, as they lie.
+template <typename T, typename TY>
+__device__ __forceinline__ void finish_row(const Finish& f, float (&v)[32], int64_t t, int c, int n) {
+    auto put = [&](auto* row) {
+#pragma unroll
+        for (int i = 0; i < 32; i += 8) {
+            float x[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = v[i + e];
+            if (c + i < n) store_part(row, c + i, n, x);
+        }
+    };
+    if (f.z) put(static_cast<T*>(f.z) + t * f.z_stride);
+    with_activation(f.activation, [&](auto act) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) v[i] = activate<decltype(act)::value>(v[i]);
+    });
+    if (f.residual) {
+        const TY* row = static_cast<const TY*>(f.residual) + t * f.residual_stride;
+#pragma unroll
+        for (int i = 0; i < 32; ++i)
+            if (c + i < n) v[i] += load_f32(row[c + i]);
+    }
+    put(static_cast<TY*>(f.y) + t * f.y_stride);
+}
+
 // A finishing warp's part of a tile, rows row0 .. +32 and columns col .. of the accumulator at d:
 // tiles of 128 bytes' width (64 columns of 16 bits, 32 of fp32) are made in shared memory,
 // over the residual's where there is one, and stored by TMA, which leaves out what lies outside.
@@ -316,9 +342,18 @@ __device__ __forceinline__ bool finish_tiles(const Args& a, const CUtensorMap* m
         tmem_loaded(v);
         if (f.bias && !partial) add_bias<T>(f, v, col, a.n);
     };
-    for (int c = half * kWide; c < BN; c += 2 * kWide) {
+    for (int c = half * kWide; c < a.bn; c += 2 * kWide) {
         const int col = col0 + c;
         if (col >= a.n || row0 >= a.m) break;
+        if (c + kWide > a.bn) {
+            // 32 columns are left of the tile, and the next 32 another's: a row to a lane
+            if (!waited && !wait()) return false;
+            waited = true;
+            float v[32];
+            sums(v, c, col);
+            if (row0 + lane < a.m) finish_row<T, TY>(f, v, row0 + lane, col, a.n);
+            break;
+        }
         const bool more = f.residual && !partial, first_z = f.z && !partial;
         auto fetch = [&] {
             fetch_tile(tile, static_cast<const TY*>(f.residual) + (int64_t)row0 * f.residual_stride + col,
@@ -344,7 +379,7 @@ __device__ __forceinline__ bool finish_tiles(const Args& a, const CUtensorMap* m
 #pragma unroll
                         for (int e = 0; e < 8; ++e) x[e] = v[i + e];
                         T* to = static_cast<T*>(f.z) + (int64_t)(row0 + lane) * f.z_stride;
-                        store_part(to, col + i, a.n, x);
+                        if (col + i < a.n) store_part(to, col + i, a.n, x);
                     }
                 }
             }
@@ -421,11 +456,15 @@ k_linear_product(const __grid_constant__ CUtensorMap ma, const __grid_constant__
     if (warp == 0) {
         // ---- loads ----
         if (lane == 0) {
+            // the CTA's rows of B; across the contraction they come in boxes of 64
+            const int b_rows = a.bn / kCtas, b_boxes = (b_rows + 63) / 64;
+            const uint32_t bytes =
+                kCtas * (R::kA + (a.b_across ? b_boxes * 64 : b_rows) * kBlock * 2);
             int s = 0;
             bool ok = true;
             for (int u = first_unit; ok && u < a.units; u += step) {
                 const Unit w = unit_of(a, u);
-                const int row = (w.m * kCtas + rank) * 128, col = w.n * BN + rank * R::kRows;
+                const int row = (w.m * kCtas + rank) * 128, col = w.n * a.bn + rank * b_rows;
                 for (int k = w.k0; k < w.k1; ++k, ++s) {
                     const int slot = s % R::kStages, turn = s / R::kStages;
                     if (turn > 0 && !bar_wait(&empty[slot], (turn - 1) & 1, &stop)) {
@@ -433,7 +472,7 @@ k_linear_product(const __grid_constant__ CUtensorMap ma, const __grid_constant__
                         break;
                     }
                     uint8_t* at = smem + slot * R::kStage;
-                    if (rank == 0) bar_expect(&full[slot], kCtas * R::kStage);
+                    if (rank == 0) bar_expect(&full[slot], bytes);
                     const uint32_t bar = PAIR ? first_cta(&full[slot]) : 0;
                     auto load = [&](uint8_t* to, const CUtensorMap* map, int c0, int c1) {
                         if (PAIR)
@@ -449,7 +488,7 @@ k_linear_product(const __grid_constant__ CUtensorMap ma, const __grid_constant__
                     }
                     at += R::kA;
                     if (a.b_across) {
-                        for (int i = 0; i < R::kRows / 64; ++i)
+                        for (int i = 0; i < b_boxes; ++i)
                             load(at + i * 8192, &mb, col + i * 64, k * kBlock);
                     } else {
                         load(at, &mb, k * kBlock, col);
@@ -470,7 +509,7 @@ k_linear_product(const __grid_constant__ CUtensorMap ma, const __grid_constant__
         // ---- products ----
         if (lane == 0 && rank == 0) {
             const uint32_t desc =
-                product_desc(128 * kCtas, BN, std::is_same<T, f16>::value, a.a_across, a.b_across);
+                product_desc(128 * kCtas, a.bn, std::is_same<T, f16>::value, a.a_across, a.b_across);
             const uint32_t base = smem_addr(smem);
             const uint32_t a_lead = a.a_across ? 8192 : 16, b_lead = a.b_across ? 8192 : 16;
             const uint32_t a_step = a.a_across ? 2048 : 32, b_step = a.b_across ? 2048 : 32;
@@ -534,16 +573,16 @@ k_linear_product(const __grid_constant__ CUtensorMap ma, const __grid_constant__
             if (f.tiles) {
                 const bool ok =
                     a.partial || f.y_f32
-                        ? finish_tiles<BN, T, float>(a, &my, &mz, tile, d, row0, w.n * BN,
+                        ? finish_tiles<BN, T, float>(a, &my, &mz, tile, d, row0, w.n * a.bn,
                                                      half, w.split, wait)
-                        : finish_tiles<BN, T, T>(a, &my, &mz, tile, d, row0, w.n * BN,
+                        : finish_tiles<BN, T, T>(a, &my, &mz, tile, d, row0, w.n * a.bn,
                                                  half, w.split, wait);
                 if (!ok) break;
             } else {
                 if (!wait()) break;
                 float* partial = a.partial ? a.partial + (int64_t)w.split * a.n * a.ld : nullptr;
-                for (int c = half; c < BN / 32; c += 2) {
-                    const int col = w.n * BN + c * 32;
+                for (int c = half; c < a.bn / 32; c += 2) {
+                    const int col = w.n * a.bn + c * 32;
                     if (col >= a.n) break;
                     float v[32];
                     tmem_load32(d + c * 32, v);
@@ -697,7 +736,7 @@ cudaError_t launch(const Product& p, int type, unsigned long long* status, cudaS
     using R = Ring<BN, PAIR>;
     CUtensorMap ma, mb, my = {}, mz = {};
     cudaError_t e = operand_map(&ma, p.a, 128, type);
-    if (e == cudaSuccess) e = operand_map(&mb, p.b, R::kRows, type);
+    if (e == cudaSuccess) e = operand_map(&mb, p.b, p.bn / (PAIR ? 2 : 1), type);
     Finish f = p.f;
     const bool split = p.splits > 1;
     f.tiles = !f.swapped && (split || f.tiles);
@@ -717,7 +756,7 @@ cudaError_t launch(const Product& p, int type, unsigned long long* status, cudaS
     e = allow_smem(k, R::kSmem, &ready);
     if (e != cudaSuccess) return e;
     const int units = p.m_tiles * p.n_tiles * p.splits, fit = sm_count() / (PAIR ? 2 : 1);
-    const Args a{f, split ? p.partial : nullptr, p.ld, p.m, p.n, p.blocks, p.m_tiles,
+    const Args a{f, split ? p.partial : nullptr, p.ld, p.m, p.n, p.bn, p.blocks, p.m_tiles,
                  p.n_tiles, p.splits, units, p.a.across, p.b.across, status};
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)((units < fit ? units : fit) * (PAIR ? 2 : 1)));
@@ -787,8 +826,8 @@ void plan_product(Product* p) {
         int bn, cycles;
         bool pair;
     };
-    const Kind kinds[] = {{256, 530, true}, {128, 330, false}, {64, 250, false},
-                          {32, 220, false}};
+    const Kind kinds[] = {{256, 540, true},  {224, 480, true}, {192, 440, true},  {160, 400, true},
+                          {128, 330, false}, {64, 250, false}, {32, 220, false}};
     double best = 0;
     p->bn = 0;
     for (const Kind& kind : kinds) {
@@ -825,10 +864,10 @@ cudaError_t launch_product(const Product& p, int type, unsigned long long* statu
     auto go = [&](auto t) {
         using T = decltype(t);
         switch (p.bn) {
-            case 256: return launch<256, true, T>(p, type, status, st);
             case 128: return launch<128, false, T>(p, type, status, st);
             case 64: return launch<64, false, T>(p, type, status, st);
-            default: return launch<32, false, T>(p, type, status, st);
+            case 32: return launch<32, false, T>(p, type, status, st);
+            default: return launch<256, true, T>(p, type, status, st);
         }
     };
     return type == PSS_BF16 ? go(bf16()) : go(f16());

@@ -95,6 +95,9 @@ CASES = [
     (129, 63, 65, "bf16", "relu", 1, 1, 1), (300, 16, 8, "bf16", "gelu", 0, 1, 0), (1000, 200, 300, "f16", "silu", 1, 1, 1),
     (2000, 8, 777, "bf16", None, 1, 1, 0), (513, 1025, 511, "bf16", "gelu", 1, 1, 0), (4097, 320, 96, "f16", "relu", 1, 0, 0),
     (3000, 256, 1024, "bf16", None, 0, 0, 0), (20000, 64, 64, "bf16", "gelu", 1, 0, 0), (257, 2048, 3, "f16", None, 1, 1, 0),
+    # tiles of 192, 160 and 224 columns, whose last 32 go another way
+    (1500, 64, 2096, "bf16", "gelu", 1, 1, 0), (3620, 48, 712, "f16", "silu", 1, 1, 0), (2233, 72, 1648, "bf16", None, 1, 1, 1),
+    (2233, 72, 1648, "f16", "relu", 1, 0, 0), (1000, 1024, 4096, "bf16", None, 1, 0, 0),
 ]
 
 
