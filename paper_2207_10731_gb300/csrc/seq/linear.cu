@@ -15,8 +15,9 @@ namespace {
 constexpr int kSlopeCols = 256;   // columns of a CTA: 32 lanes x 8
 
 // dz, rounded as an operand of both products, and the sums of the unrounded ones over the
-// rows of a part: a warp to every eighth row, four rows' loads in flight, the warps' sums
-// added in a fixed order.  Bound by memory, but for gelu's slope.
+// rows of a part: a warp to every eighth row, three rows' loads in flight (16384 x 4096 through
+// gelu: four 72 us, of fewer warps an SM, three 69, two 81), the warps' sums added in a
+// fixed order.  Bound by memory, but for gelu's slope, whose instructions take about as long.
 template <typename T, typename TG, bool VECTOR>
 __global__ void __launch_bounds__(kThreads)
 k_linear_slope(const __grid_constant__ Slope s, int parts) {
@@ -28,7 +29,7 @@ k_linear_slope(const __grid_constant__ Slope s, int parts) {
     const TG* grad = static_cast<const TG*>(s.grad);
     const T* z = static_cast<const T*>(s.z);
     float sum[8] = {};
-    constexpr int U = 4;
+    constexpr int U = 3;
     if (c < s.cols) {
         with_activation(s.activation, [&](auto act) {
             constexpr int kAct = decltype(act)::value;
@@ -301,8 +302,7 @@ extern "C" pss_status pss_linear_forward(const pss_linear_forward_args* a, void*
     if (rc != PSS_OK || a->tokens == 0) return rc;
     cudaError_t e = cudaSuccess;
     Operand *x = c.p.f.swapped ? &c.p.b : &c.p.a, *w = c.p.f.swapped ? &c.p.a : &c.p.b;
-    if (c.x_copy) e = copy_matrix(&x->matrix, c.x_copy, st);
-    if (e == cudaSuccess && c.w_copy) e = copy_matrix(&w->matrix, c.w_copy, st);
+    if (c.x_copy || c.w_copy) e = copy_matrices(&x->matrix, c.x_copy, &w->matrix, c.w_copy, st);
     if (e == cudaSuccess)
         e = launch_product(c.p, a->type, reinterpret_cast<unsigned long long*>(status), st);
     return status_of(e);
@@ -349,13 +349,10 @@ extern "C" pss_status pss_linear_backward(const pss_linear_backward_args* a, voi
         e = launch_slope(s, a->type, st);
     }
     unsigned long long* word = reinterpret_cast<unsigned long long*>(status);
-    if (e == cudaSuccess && a->dx) {
-        if (c.w_copy) e = copy_matrix(c.dx.f.swapped ? &c.dx.a.matrix : &c.dx.b.matrix, c.w_copy, st);
-        if (e == cudaSuccess) e = launch_product(c.dx, a->type, word, st);
-    }
-    if (e == cudaSuccess && a->dweight) {
-        if (c.x_copy) e = copy_matrix(c.dw_along_out ? &c.dw.a.matrix : &c.dw.b.matrix, c.x_copy, st);
-        if (e == cudaSuccess) e = launch_product(c.dw, a->type, word, st);
-    }
+    Matrix* w = &(c.dx.f.swapped ? c.dx.a : c.dx.b).matrix;
+    Matrix* x = &(c.dw_along_out ? c.dw.a : c.dw.b).matrix;
+    if (e == cudaSuccess && (c.w_copy || c.x_copy)) e = copy_matrices(w, c.w_copy, x, c.x_copy, st);
+    if (e == cudaSuccess && a->dx) e = launch_product(c.dx, a->type, word, st);
+    if (e == cudaSuccess && a->dweight) e = launch_product(c.dw, a->type, word, st);
     return status_of(e);
 }

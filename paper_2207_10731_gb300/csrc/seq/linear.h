@@ -59,7 +59,8 @@ cudaError_t launch_product(const Product& p, int type, unsigned long long* statu
 // Rows off the 16-byte grid are copied into rows that are on it before they are an operand.
 bool on_grid(const Matrix& x);
 int64_t copy_bytes(const Matrix& x);
-cudaError_t copy_matrix(Matrix* x, void* to, cudaStream_t st);
+// Both at once; a null place: not that one.
+cudaError_t copy_matrices(Matrix* x, void* to_x, Matrix* y, void* to_y, cudaStream_t st);
 
 // dz = grad * act'(z) in 16 bits (null: not wanted) and its column sums in fp32 (dbias).
 struct Slope {

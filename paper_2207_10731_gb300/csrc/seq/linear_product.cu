@@ -560,6 +560,7 @@ k_linear_product(const __grid_constant__ CUtensorMap ma, const __grid_constant__
         uint8_t* staged = smem + R::kStages * R::kStage + (warp - 4) * kStaged;
         const Finish& f = a.f;
         const uint32_t tile = smem_addr(staged);
+        bool stopped = false;
         int i = 0;
         for (int u = first_unit; u < a.units; u += step, ++i) {
             const Unit w = unit_of(a, u);
@@ -577,13 +578,29 @@ k_linear_product(const __grid_constant__ CUtensorMap ma, const __grid_constant__
                                                      half, w.split, wait)
                         : finish_tiles<BN, T, T>(a, &my, &mz, tile, d, row0, w.n * a.bn,
                                                  half, w.split, wait);
-                if (!ok) break;
+                stopped = !ok;
             } else {
-                if (!wait()) break;
                 float* partial = a.partial ? a.partial + (int64_t)w.split * a.n * a.ld : nullptr;
-                for (int c = half; c < a.bn / 32; c += 2) {
+                bool waited = false;
+                for (int c = half; c < a.bn / 32 && !stopped; c += 2) {
                     const int col = w.n * a.bn + c * 32;
                     if (col >= a.n) break;
+                    // a column's residuals, asked for before the sums are waited for
+                    float more[32], bias = 0.f;
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) more[j] = 0.f;
+                    if (!f.swapped && col + lane < a.n) {
+                        if (f.bias) bias = f.bias[col + lane];
+                        if (f.residual)
+#pragma unroll
+                            for (int j = 0; j < 32; ++j)
+                                if (row0 + j < a.m) more[j] = residual_at<T>(f, row0 + j, col + lane);
+                    }
+                    if (!waited && !wait()) {
+                        stopped = true;
+                        break;
+                    }
+                    waited = true;
                     float v[32];
                     tmem_load32(d + c * 32, v);
                     tmem_wait_load();
@@ -591,7 +608,7 @@ k_linear_product(const __grid_constant__ CUtensorMap ma, const __grid_constant__
                     if (f.swapped) {
                         // lanes are neighbours in memory already
                         if (row < a.m) {
-                            const float bias = !partial && f.bias ? f.bias[row] : 0.f;
+                            if (!partial && f.bias) bias = f.bias[row];
 #pragma unroll
                             for (int j = 0; j < 32; ++j) {
                                 if (col + j >= a.n) break;
@@ -610,25 +627,17 @@ k_linear_product(const __grid_constant__ CUtensorMap ma, const __grid_constant__
                         for (int j = 0; j < 32; ++j) values[lane * 32 + (j ^ lane)] = v[j];
                         __syncwarp();
                         if (col + lane < a.n) {
-                            const float bias = f.bias ? f.bias[col + lane] : 0.f;
-                            const int last = min(32, a.m - row0);
-                            // eight rows' residuals are asked for before the first is waited for
-                            for (int j = 0; j < last; j += 8) {
-                                float more[8];
 #pragma unroll
-                                for (int e = 0; e < 8; ++e)
-                                    more[e] = f.residual && j + e < last
-                                                  ? residual_at<T>(f, row0 + j + e, col + lane) : 0.f;
-#pragma unroll
-                                for (int e = 0; e < 8; ++e)
-                                    if (j + e < last)
-                                        finish_one<T>(f, values[(j + e) * 32 + (lane ^ (j + e))],
-                                                      row0 + j + e, col + lane, bias, more[e]);
-                            }
+                            for (int j = 0; j < 32; ++j)
+                                if (row0 + j < a.m)
+                                    finish_one<T>(f, values[j * 32 + (lane ^ j)], row0 + j, col + lane,
+                                                  bias, more[j]);
                         }
                     }
                 }
+                if (!waited && !stopped) stopped = !wait();
             }
+            if (stopped) break;
             tc_before_sync();
             __syncwarp();
             if (lane == 0) {
@@ -779,19 +788,26 @@ cudaError_t launch(const Product& p, int type, unsigned long long* status, cudaS
                     p.f.swapped ? p.m : p.n, p.ld, p.f);
 }
 
-template <typename T>
+// Rows into rows of `ld` values, 8 to a thread, zeros behind a row's end.  The values are moved
+// as they are, whichever 16-bit type they have.
+struct Copy {
+    const uint16_t* from;
+    uint16_t* to;
+    int64_t stride, rows, cols, ld;
+};
 __global__ void __launch_bounds__(kThreads)
-k_linear_copy(const T* __restrict__ from, int64_t stride, int64_t rows, int64_t cols, T* to,
-              int64_t ld) {
+k_linear_copy(const __grid_constant__ Copy x, const __grid_constant__ Copy y, unsigned x_ctas) {
     pdl_prologue();
-    const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x, vecs = ld / 8;
-    const int64_t r = i / vecs, c = (i - r * vecs) * 8;
-    if (r >= rows) return;
-    Raw8<T> v;
+    const Copy& c = blockIdx.x < x_ctas ? x : y;
+    const int64_t cta = blockIdx.x < x_ctas ? blockIdx.x : blockIdx.x - x_ctas;
+    const int64_t i = cta * kThreads + threadIdx.x, vecs = c.ld / 8;
+    const int64_t r = i / vecs, col = (i - r * vecs) * 8;
+    if (r >= c.rows) return;
+    uint32_t v[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-        set_raw(v, e, c + e < cols ? from[r * stride + c + e] : round_to<T>(0.f));
-    *reinterpret_cast<uint4*>(to + r * ld + c) = make_uint4(v.w[0], v.w[1], v.w[2], v.w[3]);
+    for (int e = 0; e < 8; ++e) v[e] = col + e < c.cols ? c.from[r * c.stride + col + e] : 0;
+    *reinterpret_cast<uint4*>(c.to + r * c.ld + col) =
+        make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
 }
 
 }  // namespace
@@ -802,15 +818,24 @@ bool on_grid(const Matrix& x) {
 
 int64_t copy_bytes(const Matrix& x) { return x.outer * ((x.inner + 7) / 8 * 8) * 2; }
 
-cudaError_t copy_matrix(Matrix* x, void* to, cudaStream_t st) {
-    const int64_t ld = (x->inner + 7) / 8 * 8, threads = x->outer * (ld / 8);
-    // the values are moved as they are, whichever 16-bit type they have
-    const cudaError_t e = launch_k(
-        k_linear_copy<f16>, dim3((unsigned)((threads + kThreads - 1) / kThreads)), dim3(kThreads), 0,
-        st, static_cast<const f16*>(x->data), x->stride, x->outer, x->inner, static_cast<f16*>(to), ld);
-    x->data = to;
-    x->stride = ld;
-    return e;
+cudaError_t copy_matrices(Matrix* x, void* to_x, Matrix* y, void* to_y, cudaStream_t st) {
+    unsigned ctas[2];
+    Copy copies[2];
+    Matrix* const from[2] = {x, y};
+    void* const to[2] = {to_x, to_y};
+    for (int i = 0; i < 2; ++i) {
+        Matrix& m = *from[i];
+        const int64_t ld = (m.inner + 7) / 8 * 8;
+        copies[i] = Copy{static_cast<const uint16_t*>(m.data), static_cast<uint16_t*>(to[i]), m.stride,
+                         to[i] ? m.outer : 0, m.inner, ld};
+        ctas[i] = to[i] ? (unsigned)((m.outer * (ld / 8) + kThreads - 1) / kThreads) : 0;
+        if (to[i]) {
+            m.data = to[i];
+            m.stride = ld;
+        }
+    }
+    return launch_k(k_linear_copy, dim3(ctas[0] + ctas[1]), dim3(kThreads), 0, st, copies[0],
+                    copies[1], ctas[0]);
 }
 
 // The width of the tiles and the parts of the contraction: the pair that leaves the fullest SM
@@ -837,9 +862,11 @@ void plan_product(Product* p) {
         if (kind.pair && p->m <= 128) continue;
         const int m_tiles = (p->m + rows - 1) / rows, n_tiles = (p->n + bn - 1) / bn;
         const int64_t tiles = (int64_t)m_tiles * n_tiles;
+        // across the contraction B comes in boxes of 64, two to a CTA of any of these pairs
+        const int cycles = kind.pair && p->b.across ? 540 : kind.cycles;
         for (int s = 1; s <= 64 && s <= p->blocks; ++s) {
             const int64_t rounds = (tiles * s + fit - 1) / fit;
-            double cost = 2000. + (double)rounds * ((p->blocks + s - 1) / s * kind.cycles + 300.);
+            double cost = 2000. + (double)rounds * ((p->blocks + s - 1) / s * cycles + 300.);
             // written and read at some 1800 bytes a cycle each, and a launch
             if (s > 1) cost += 4000. + (double)p->m * p->n * s * 8 / 1800;
             if (p->bn == 0 || cost < best) {
