@@ -24,7 +24,7 @@ constexpr int kPer = 8;          // values of a row that a thread holds
 constexpr int kChunk = 32;       // sorted places of a piece
 constexpr int kPieces = 64;      // pieces of a large piece
 constexpr int kLarge = kChunk * kPieces;
-constexpr int kRows = 8;         // rows of the table that a group sums
+constexpr int kRows = 8;         // rows of the table that a group sums, at most
 constexpr int kSmall = 8192;     // tokens that are ranked instead of sorted
 constexpr uint32_t kNone = 0xffffffffu;
 
@@ -270,11 +270,10 @@ __device__ __forceinline__ int first_place(const unsigned long long* __restrict_
     return lo;
 }
 
-// The same in all of the list, by a warp: 32 places a step.
+// The same by a warp: 32 places a step.
 __device__ __forceinline__ int first_place_warp(const unsigned long long* __restrict__ sorted,
-                                                int n, int64_t v) {
+                                                int lo, int hi, int64_t v) {
     const int lane = threadIdx.x & 31;
-    int lo = 0, hi = n;
     while (lo < hi) {
         // places lo + step, lo + 2 step ..: the answer lies behind the last smaller key
         const int step = (hi - lo + 32) / 33, at = lo + (lane + 1) * step - 1;
@@ -293,98 +292,201 @@ __device__ __forceinline__ bool is_long(int from, int to) {
 }
 
 // The sums of the table's rows.  CTAs up to long_ctas: a group to a piece, which answers for
-// its row where it is the first whole piece of the run: head, pieces (kPieces of them at
-// once where these were summed) and tail.  The others: a group to kRows rows, whose places its
-// lanes find by bisection; then one pass over the short runs, U entries' loads in flight
-// whichever rows these belong to.  (All runs in that pass: 943 us for the popular ids of a
-// batch of 1.7 M x 128, the chains of a few groups.)
+// its row where it is the first whole piece of the run: head, pieces and tail.  Runs of more than
+// kAlone pieces are the CTA's, a part of the pieces to each group (kPieces of them at once where
+// these were summed).  The other CTAs: a group to `per` rows, whose places its lanes find by
+// bisection; then one pass over the short runs, U entries' loads in flight whichever rows
+// these belong to.  (All runs in that pass: 943 us for the popular ids of a batch of
+// 1.7 M x 128, the chains of a few groups; now 230, 82 % of the copy bandwidth.  Pieces of 16
+// entries: 394 instead of 369 us for all of that call; two CTAs an SM 470, four 365.)
+constexpr int kAlone = 16;
 template <typename TG, typename TO, bool VECTOR>
-__global__ void __launch_bounds__(kThreads, 3)
+__global__ void __launch_bounds__(kThreads, 4)
 k_embedding_rows(const TG* __restrict__ grad, int64_t gs,
                  const unsigned long long* __restrict__ sorted,
                  const unsigned long long* __restrict__ count, const float* __restrict__ sums,
                  const float* __restrict__ large, int64_t sums_stride, float scale, TO* out,
-                 int64_t os, int64_t rows, unsigned long_ctas, Spread s) {
+                 int64_t os, int64_t rows, int per, unsigned long_ctas, Spread s) {
     pdl_prologue();
-    constexpr int U = 16 / sizeof(TG);
-    __shared__ int places[kThreads][kRows + 1], ends[2];
+    constexpr int U = 4;
+    __shared__ union {
+        int places[kThreads][kRows + 1];
+        float parts[kThreads][kPer + 1];
+    } shared;
+    __shared__ int ends[2], listed, list[kThreads][2];
     const int n = (int)*count;
+    const int groups = kThreads >> s.log2_lanes, group = threadIdx.x >> s.log2_lanes;
+    const int lanes = 1 << s.log2_lanes, lane = threadIdx.x & (lanes - 1);
     float sum[kPer] = {};
     int block;
     if (blockIdx.x < long_ctas) {
         const int64_t c64 = group_of(s, blockIdx.x, &block);
-        const Piece<VECTOR> piece(s, block);
-        if (!piece.any() || (c64 + 1) * kChunk > n) return;
-        const int c = (int)c64, at = c * kChunk;
-        const uint32_t k = key_of(sorted[at]);
-        if (k != key_of(sorted[at + kChunk - 1]) ||
-            (at > 0 && key_of(sorted[at - kChunk]) == k))
-            return;
-        const int begin = first_place(sorted, at > 0 ? at - kChunk + 1 : 0, at, k);
-        const int end = first_place(sorted, at + kChunk, n, (int64_t)k + 1), last = end / kChunk;
-        auto add = [&](int from, int to, auto load) {
-            for (int i = from; i < to; i += U) {
-                decltype(load(i)) raw[U];
+        if (threadIdx.x == 0) listed = 0;
+        __syncthreads();
+        // what this group sums: whole pieces first .. last of a run, entries head .. in front
+        // of them and .. tail behind
+        int head = 0, first = 0, last = 0, tail = 0;
+        uint32_t k = 0;
+        bool alone = false;
+        if ((c64 + 1) * kChunk <= n) {
+            const int c = (int)c64, at = c * kChunk;
+            k = key_of(sorted[at]);
+            if (k == key_of(sorted[at + kChunk - 1]) &&
+                (at == 0 || key_of(sorted[at - kChunk]) != k)) {
+                // the whole pieces behind it, all looked at at once
+                unsigned whole = 0;
 #pragma unroll
-                for (int u = 0; u < U; ++u)
-                    if (i + u < to) raw[u] = load(i + u);
-#pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    if (i + u >= to) break;
-                    float v[kPer];
-                    unpack(raw[u], v);
-                    add_to(sum, v);
+                for (int j = 0; j < kAlone; ++j) {
+                    const int64_t to = at + (int64_t)(j + 2) * kChunk;
+                    if (to <= n && key_of(sorted[to - 1]) == k) whole |= 1u << j;
+                }
+                const int more = __ffs(~whole) - 1;
+                if (more == kAlone) {
+                    if (lane == 0) {
+                        const int i = atomicAdd(&listed, 1);
+                        list[i][0] = c;
+                        list[i][1] = block;
+                    }
+                } else {
+                    alone = true;
+                    first = c;
+                    last = c + 1 + more;
+                    head = first_place(sorted, at > 0 ? at - kChunk + 1 : 0, at, k);
+                    tail = first_place(sorted, last * kChunk, min(n, last * kChunk + kChunk),
+                                       (int64_t)k + 1);
                 }
             }
-        };
-        auto entry = [&](int i) { return piece.load(grad + (uint32_t)sorted[i] * gs); };
-        auto of_piece = [&](int i) { return piece.load(sums + i * sums_stride); };
-        auto of_large = [&](int i) { return piece.load(large + i * sums_stride); };
-        const int l0 = (c + kPieces - 1) / kPieces, l1 = last / kPieces;
-        add(begin, at, entry);
-        if (l1 > l0) {
-            add(c, l0 * kPieces, of_piece);
-            add(l0, l1, of_large);
-            add(l1 * kPieces, last, of_piece);
-        } else {
-            add(c, last, of_piece);
         }
-        add(last * kChunk, end, entry);
+        __syncthreads();
+        // its own run first, then the CTA's, whose order does not matter: each is a row of its own
+        for (int x = -1; x < listed; ++x) {
+            if (x >= 0) {
+                const int c = list[x][0];
+                block = list[x][1];
+                k = key_of(sorted[c * kChunk]);
+                const int end = first_place_warp(sorted, (c + kAlone) * kChunk, n, (int64_t)k + 1);
+                const int pieces = end / kChunk - c;
+                first = c + (int)((int64_t)pieces * group / groups);
+                last = c + (int)((int64_t)pieces * (group + 1) / groups);
+                head = group > 0 ? first * kChunk
+                                 : first_place(sorted, c > 0 ? c * kChunk - kChunk + 1 : 0, c * kChunk, k);
+                tail = group < groups - 1 ? last * kChunk : end;
 #pragma unroll
-        for (int e = 0; e < kPer; ++e) sum[e] *= scale;
-        piece.store(out + (int64_t)k * os, sum);
+                for (int e = 0; e < kPer; ++e) sum[e] = 0.f;
+            }
+            const Piece<VECTOR> piece(s, block);
+            const bool work = (x >= 0 || alone) && piece.any();
+            if (work) {
+                int l0 = (first + kPieces - 1) / kPieces, l1 = last / kPieces;
+                if (l1 <= l0) l0 = l1 = 0;
+                for (int y = 0; y < 3; ++y) {   // pieces, large pieces, pieces
+                    const float* from = y == 1 ? large : sums;
+                    int i = y == 0 ? first : y == 1 ? l0 : l1 * kPieces;
+                    int to = y == 0 ? l0 * kPieces : y == 1 ? l1 : last;
+                    if (l1 == 0) i = first, to = y == 0 ? last : first;
+                    constexpr int V = 4;
+                    for (; i < to; i += V) {
+                        Raw8<float> raw[V];
+#pragma unroll
+                        for (int u = 0; u < V; ++u)
+                            raw[u] = i + u < to ? piece.load(from + (i + u) * sums_stride) : Raw8<float>{};
+#pragma unroll
+                        for (int u = 0; u < V; ++u) {
+                            float v[kPer];
+                            unpack(raw[u], v);
+                            add_to(sum, v);
+                        }
+                    }
+                }
+                for (int y = 0; y < 2; ++y) {   // head, tail
+                    const int to = y == 0 ? first * kChunk : tail;
+                    for (int i = y == 0 ? head : last * kChunk; i < to; i += U) {
+                        uint32_t t[U];
+                        Raw8<TG> raw[U];
+#pragma unroll
+                        for (int u = 0; u < U; ++u) t[u] = i + u < to ? (uint32_t)sorted[i + u] : 0u;
+#pragma unroll
+                        for (int u = 0; u < U; ++u)
+                            raw[u] = i + u < to ? piece.load(grad + t[u] * gs) : Raw8<TG>{};
+#pragma unroll
+                        for (int u = 0; u < U; ++u) {
+                            float v[kPer];
+                            unpack(raw[u], v);
+                            add_to(sum, v);
+                        }
+                    }
+                }
+            }
+            if (x >= 0) {
+                // the groups' parts, in their order
+#pragma unroll
+                for (int e = 0; e < kPer; ++e) shared.parts[threadIdx.x][e] = sum[e];
+                __syncthreads();
+                if (group == 0 && work)
+                    for (int g = 1; g < groups; ++g)
+#pragma unroll
+                        for (int e = 0; e < kPer; ++e) sum[e] += shared.parts[g * lanes + lane][e];
+                __syncthreads();
+            }
+            if (work && (x < 0 || group == 0)) {
+                float v[kPer];
+#pragma unroll
+                for (int e = 0; e < kPer; ++e) v[e] = sum[e] * scale;
+                piece.store(out + (int64_t)k * os, v);
+            }
+        }
         return;
     }
-    const int64_t v0 = group_of(s, blockIdx.x - long_ctas, &block) * kRows;
+    int64_t v0 = group_of(s, blockIdx.x - long_ctas, &block) * per;
     const Piece<VECTOR> piece(s, block);
-    const int lanes = 1 << s.log2_lanes, lane = threadIdx.x & (lanes - 1);
-    const int some = rows - v0 < kRows ? (int)(rows - v0) : kRows;   // may be below 1
-    int* place = places[threadIdx.x >> s.log2_lanes];
+    const int some = rows - v0 < per ? (int)(rows - v0) : per;   // may be below 1
+    int* place = shared.places[group];
     // the CTA's rows lie side by side: two warps find their ends in the list, and each row is
     // looked for between these (all in the whole list: 20 steps a row, 317 instead of 240 us for a
     // million rows; the runs' ends noted in a table beforehand: 233, and two launches more)
     {
-        const int64_t cta = blockIdx.x - long_ctas, per = kThreads >> s.log2_lanes;
-        const int64_t first = cta * per / s.blocks * kRows;
-        const int64_t last = (((cta + 1) * per - 1) / s.blocks + 1) * kRows;
+        const int64_t cta = blockIdx.x - long_ctas;
+        const int64_t first = cta * groups / s.blocks * per;
+        const int64_t last = (((cta + 1) * groups - 1) / s.blocks + 1) * per;
         const int warp = threadIdx.x >> 5;
         if (warp < 2) {
-            const int at = first_place_warp(sorted, n, warp == 0 ? first : last);
+            const int at = first_place_warp(sorted, 0, n, warp == 0 ? first : last);
             if ((threadIdx.x & 31) == 0) ends[warp] = at;
         }
     }
     __syncthreads();
     for (int j = lane; j <= some; j += lanes) place[j] = first_place(sorted, ends[0], ends[1], v0 + j);
-    __syncwarp();
-    if (!piece.any() || some < 1) return;
+    __syncthreads();
+    // Rows of one block that are dense are dealt out instead: neighbours' runs are as long as
+    // each other's, and a group's would add up.
+    int step = 1, at = group;   // row r of the group is row at % per of group at / per, r by r
+    if (s.blocks == 1 && per > 1 && ends[1] - ends[0] > 2 * groups * per) {
+        step = groups;
+    } else {
+        at = group * per;
+    }
+    if (!piece.any()) return;
+    const int64_t cta_v0 = (int64_t)(blockIdx.x - long_ctas) * groups * per;
     const float none[kPer] = {};
-    for (int r = 0; r < some; ++r) {
-        if (is_long(place[r], place[r + 1])) continue;
-        int to = r;   // rows r .. to are short
-        while (to + 1 < some && !is_long(place[to + 1], place[to + 2])) ++to;
-        int i = place[r];
-        const int end = place[to + 1];
-        int64_t row = v0 + r;
+    const int count_rows = step == 1 ? some : per;
+    for (int r = 0; r < count_rows; ++r) {
+        int64_t row;
+        int i, end, to = r;   // rows r .. to are short
+        if (step == 1) {
+            if (is_long(place[r], place[r + 1])) continue;
+            while (to + 1 < some && !is_long(place[to + 1], place[to + 2])) ++to;
+            i = place[r];
+            end = place[to + 1];
+            row = v0 + r;
+        } else {
+            const int x = at + r * step, g = x / per, y = x - g * per;
+            row = cta_v0 + x;
+            if (row >= rows) break;
+            i = shared.places[g][y];
+            end = shared.places[g][y + 1];
+            if (is_long(i, end)) continue;
+        }
+        const int64_t behind = row + (to - r) + 1;
         auto leave = [&](int64_t next) {   // store the row, and zeros up to the next
             float v[kPer];
 #pragma unroll
@@ -413,7 +515,7 @@ k_embedding_rows(const TG* __restrict__ grad, int64_t gs,
             }
             i += U;
         }
-        leave(v0 + to + 1);
+        leave(behind);
         r = to;
     }
 }
@@ -574,7 +676,10 @@ extern "C" pss_status pss_embedding_backward(const void* grad, pss_dtype grad_ty
     if (tokens > 0 && (!device_ptr(ids) || !aligned_to(ids, 8))) return PSS_ERR_INVALID_ARG;
     const bool some = rows > 0 && cols > 0;
     const Spread s = spread(cols > 0 ? cols : 1);
-    const unsigned n = ctas((rows + kRows - 1) / kRows, s), pieces = ctas(tokens / kChunk, s);
+    // as many rows to a group as have some 32 tokens, were these spread evenly
+    int per = kRows;
+    while (per > 1 && (int64_t)per * tokens > 32 * rows) per /= 2;
+    const unsigned n = ctas((rows + per - 1) / per, s), pieces = ctas(tokens / kChunk, s);
     if (some) {
         if (!device_ptr(dweight) || !aligned_to(dweight, dtype_size(dweight_type)))
             return PSS_ERR_INVALID_ARG;
@@ -619,7 +724,7 @@ extern "C" pss_status pss_embedding_backward(const void* grad, pss_dtype grad_ty
             auto* k = vector ? k_embedding_rows<TG, TO, true> : k_embedding_rows<TG, TO, false>;
             return launch_k(k, dim3(n + pieces), dim3(kThreads), 0, st, g, grad_stride, w.sorted,
                             w.count, w.sums, w.large, w.stride, scale, static_cast<TO*>(dweight),
-                            dweight_stride, rows, pieces, s);
+                            dweight_stride, rows, per, pieces, s);
         });
     }));
 }

@@ -42,6 +42,29 @@ k_residual_norm_forward(const __grid_constant__ Forward<T, R> a) {
 #pragma unroll
     for (int c = 0; c < CH; ++c) in[c] = place.at(sh, c) < sh.cols;
     const int64_t step = (int64_t)gridDim.x * sh.groups;
+    // A ragged row's weights are no vectors: they are laid out once in shared memory, 16-byte
+    // pieces of a thread, since its columns are the same in all of its rows.
+    constexpr bool kLaid = MODE == RAGGED && F::kAhead;
+    extern __shared__ __align__(16) float4 laid[];
+    if constexpr (kLaid) {
+        for (int k = 0; k < 2; ++k) {
+            float w[8] = {};
+            const float* from = k == 0 ? a.post : a.pre;
+            if (from) load_weight<VEC, MODE>(from, place.at(sh, 0), sh.cols, in[0], w);
+            laid[2 * k * blockDim.x + threadIdx.x] = make_float4(w[0], w[1], w[2], w[3]);
+            laid[(2 * k + 1) * blockDim.x + threadIdx.x] = make_float4(w[4], w[5], w[6], w[7]);
+        }
+    }
+    auto weights = [&](int k, int c, float (&w)[VEC]) {
+        if constexpr (kLaid) {
+            const float4 x = laid[2 * k * blockDim.x + threadIdx.x];
+            const float4 y = laid[(2 * k + 1) * blockDim.x + threadIdx.x];
+            w[0] = x.x, w[1] = x.y, w[2] = x.z, w[3] = x.w;
+            w[4] = y.x, w[5] = y.y, w[6] = y.z, w[7] = y.w;
+        } else {
+            load_weight<VEC, MODE>(k == 0 ? a.post : a.pre, place.at(sh, c), sh.cols, in[c], w);
+        }
+    };
     // The next row's loads are under way in registers, which reach here (in shared memory, as
     // backward: 350 instead of 300 us for 131072 x 1024 with an fp32 stream).
     Part<T, VEC, CH> next_x, next_g;
@@ -82,7 +105,7 @@ k_residual_norm_forward(const __grid_constant__ Forward<T, R> a) {
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
                 float w[VEC];
-                load_weight<VEC, MODE>(a.post, place.at(sh, c), sh.cols, in[c], w);
+                weights(0, c, w);
                 mul(v[c], v[c], rstd);
                 mul(v[c], v[c], w);
             }
@@ -117,7 +140,7 @@ k_residual_norm_forward(const __grid_constant__ Forward<T, R> a) {
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
                 float w[VEC];
-                load_weight<VEC, MODE>(a.pre, place.at(sh, c), sh.cols, in[c], w);
+                weights(1, c, w);
                 mul(v[c], v[c], rstd);
                 mul(v[c], v[c], w);
                 if (live && in[c]) store_part(a.y + r * a.ys, place.at(sh, c), sh.cols, v[c]);
@@ -169,13 +192,16 @@ extern "C" pss_status pss_residual_norm_forward(
         auto launch = [&](auto vec, auto k, auto mode, auto full) -> cudaError_t {
             auto* kernel = k_residual_norm_forward<T, R, decltype(vec)::value, decltype(k)::value,
                                                    decltype(mode)::value, decltype(full)::value>;
-            const int n = ctas_of(rows, s, [&] { return resident(kernel, s.threads, 0, 32); },
+            constexpr bool kLaid = decltype(mode)::value == RAGGED &&
+                                   Fit<decltype(vec)::value, decltype(k)::value>::kAhead;
+            const size_t smem = kLaid ? 64 * s.threads : 0;   // at most 32 KB
+            const int n = ctas_of(rows, s, [&] { return resident(kernel, s.threads, smem, 32); },
                                   decltype(mode)::value);
-            return launch_k(kernel, dim3(n), dim3(s.threads), 0, st, f);
+            return launch_k(kernel, dim3(n), dim3(s.threads), smem, st, f);
         };
         auto with = [&](auto vec, auto k, auto mode) -> cudaError_t {
-            if constexpr (decltype(vec)::value == 8 && decltype(mode)::value == ALIGNED &&
-                          decltype(k)::value <= WIDE) {
+            if constexpr (decltype(vec)::value == 8 &&
+                          decltype(k)::value <= (decltype(mode)::value == ALIGNED ? WIDE : MIDDLE)) {
                 if (post_weight && pre_weight)
                     return gates == NO_GATE    ? launch(vec, k, mode, Int<NO_GATE>())
                            : gates == ROW_GATE ? launch(vec, k, mode, Int<ROW_GATE>())

@@ -1,9 +1,9 @@
 """Rows of a dense table by id and their gradient, against the definition in 64 bits.
 
 Tolerances: forward, one product and one rounding.  Backward, a row's n gradients are
-added in fp32 along at most 64 + 64 + 64 + n / 4096 additions (head, pieces, tail and
-large pieces of the sorted run), each off by half a unit of a partial sum that is at
-most sum |grad|; then the product with the scale and the last rounding."""
+added in fp32 along at most 32 + 32 + 32 + 64 + 64 + n / 2048 + 256 additions (head, a piece,
+tail, pieces on both sides of the large ones, these, and the groups' parts), each off by half
+a unit of a partial sum that is at most sum |grad|; then the product with the scale and the last rounding."""
 import pytest
 import torch
 
@@ -42,7 +42,7 @@ def backward(grad, ids, rows, scale):
     want = zero.index_add(0, ids[inside], g[inside]) * scale
     size = zero.index_add(0, ids[inside], g[inside].abs()) * abs(scale)
     n = torch.bincount(ids[inside], minlength=rows).double()
-    depth = torch.minimum(n, 192 + n / 4096) + 2
+    depth = torch.minimum(n, 480 + n / 2048) + 2
     return want, depth[:, None] * U32 * size
 
 
@@ -63,6 +63,10 @@ CASES = [
     (20000, 50, 129, "popular", "f32", "f16"),
     (70001, 3, 64, "popular", "bf16", "f32"),
     (300, 20, 1024, "popular", "bf16", "f32"),
+    (3197, 839, 64, "popular", "f32", "bf16"),
+    (8192, 300, 520, "popular", "bf16", "f32"),
+    (8193, 4000, 8, "popular", "f16", "f32"),
+    (60000, 700, 256, "popular", "f32", "f32"),
     (33, 9, 2056, "padded", "f32", "bf16"),
 ]
 
