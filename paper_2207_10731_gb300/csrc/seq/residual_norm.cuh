@@ -28,24 +28,26 @@ inline int norm_per_sm(int64_t cols) {
 }
 
 // Rows up to 32 lanes' vectors: several to a CTA of 256 threads, within shuffles.  Up to 256
-// threads' (three CTAs an SM) or 512: a CTA to a row.  These with the next row's loads ahead.  Above:
-// two vectors to a thread, 1024 threads at most, for which there is no room for a second row.
+// threads' (three CTAs an SM) or 512: a CTA to a row.  These with the next row's loads ahead.  Up to
+// 1024 threads', and above with two vectors to a thread: without, for want of room.  (Forward in
+// vectors the latter is faster from 512 on, half the warps to a barrier: 8000 x 8192 bf16 on an
+// fp32 stream 135 instead of 190 us; backward 370 instead of 322.)
 // (Two vectors to a thread for shorter rows too: 495 instead of 434 us for the gradients of
 // 65536 x 2048, half the warps.)
-enum { NARROW, MIDDLE, WIDE, WIDEST };
+enum { NARROW, MIDDLE, WIDE, WIDER, WIDEST };
 template <int VEC, int KIND>
 struct Fit {
     static constexpr int kVectors = (VEC == 8 ? 1 : 8) * (KIND == WIDEST ? 2 : 1);
     static constexpr int kMost = KIND <= MIDDLE ? 256 : KIND == WIDE ? 512 : 1024;
     static constexpr int kLeast = KIND == MIDDLE && VEC == 8 ? 3 : 1;   // CTAs an SM
-    static constexpr bool kAhead = VEC == 8 && KIND != WIDEST;
+    static constexpr bool kAhead = VEC == 8 && KIND <= WIDE;
 };
 // What is there of norms and gates is known to the kernel where both norms are and rows are
 // aligned: FULL is the kind of gate then.  ANY asks at every turn.
 enum { ANY = -1 };
 
-// extra: elements that a ragged row's first vector may hold in front of it.
-inline Split norm_split(int cols, int extra, int* kind) {
+// extra: elements that a ragged row's first vector may hold in front of it; wider: see above.
+inline Split norm_split(int cols, int extra, bool wider, int* kind) {
     Split s;
     const int units = (cols + extra + 7) / 8;   // of 8 elements, VEC = 8 or 1
     s.ch = 0;
@@ -58,7 +60,7 @@ inline Split norm_split(int cols, int extra, int* kind) {
         s.groups = 256 / s.lanes;
         return s;
     }
-    *kind = units <= 256 ? MIDDLE : units <= 512 ? WIDE : WIDEST;
+    *kind = units <= 256 ? MIDDLE : units <= 512 ? WIDE : units <= 1024 && wider ? WIDER : WIDEST;
     s.lanes = ((*kind == WIDEST ? (units + 1) / 2 : units) + 31) / 32 * 32;
     s.threads = s.lanes;
     s.groups = 1;
@@ -93,7 +95,7 @@ __device__ __forceinline__ V row_sums(V v, int lanes, float2 (*slots)[32], int& 
         constexpr int kFirst = KIND == MIDDLE ? 4 : KIND == WIDE ? 8 : 16;
 #pragma unroll
         for (int m = kFirst; m > 0; m >>= 1) v = add_pair(v, shuffled(v, m));
-        if (KIND != WIDEST) {
+        if (KIND <= WIDE) {
             // the lanes behind these hold the sum of nothing: take the first one's
             if constexpr (sizeof(V) == 4) {
                 v = __shfl_sync(0xffffffffu, v, 0);

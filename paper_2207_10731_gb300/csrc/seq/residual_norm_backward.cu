@@ -365,7 +365,7 @@ extern "C" pss_status pss_residual_norm_backward(
                          post_rstd, pre_rstd, scale, gates, reads_x, nullptr, Shape{}};
         const bool ragged = lie.how == SHIFTED && cols <= kNormMaxCols - 8;
         int kind;
-        const Split s = norm_split((int)cols, ragged ? 7 : 0, &kind);
+        const Split s = norm_split((int)cols, ragged ? 7 : 0, true, &kind);
         f.sh = Shape{rows, (int)cols, s.lanes, s.log2_lanes, s.groups, lie.shift0, lie.step};
         f.partial = static_cast<float*>(workspace);
         auto launch = [&](auto vec, auto k, auto mode, auto full) -> cudaError_t {
@@ -412,6 +412,7 @@ extern "C" pss_status pss_residual_norm_backward(
             return kind == NARROW   ? with(vec, Int<NARROW>(), mode)
                    : kind == MIDDLE ? with(vec, Int<MIDDLE>(), mode)
                    : kind == WIDE   ? with(vec, Int<WIDE>(), mode)
+                   : kind == WIDER  ? with(vec, Int<WIDER>(), mode)
                                     : with(vec, Int<WIDEST>(), mode);
         };
         return lie.how == VECTORS ? wide(Int<8>(), Int<ALIGNED>())

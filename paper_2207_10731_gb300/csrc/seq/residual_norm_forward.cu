@@ -187,7 +187,7 @@ extern "C" pss_status pss_residual_norm_forward(
                         post_weight, pre_weight, post_rstd, pre_rstd, scale, eps, gates, Shape{}};
         const bool ragged = lie.how == SHIFTED && cols <= kNormMaxCols - 8;
         int kind;
-        const Split s = norm_split((int)cols, ragged ? 7 : 0, &kind);
+        const Split s = norm_split((int)cols, ragged ? 7 : 0, lie.how != VECTORS && !ragged, &kind);
         f.sh = Shape{rows, (int)cols, s.lanes, s.log2_lanes, s.groups, lie.shift0, lie.step};
         auto launch = [&](auto vec, auto k, auto mode, auto full) -> cudaError_t {
             auto* kernel = k_residual_norm_forward<T, R, decltype(vec)::value, decltype(k)::value,
@@ -213,6 +213,7 @@ extern "C" pss_status pss_residual_norm_forward(
             return kind == NARROW   ? with(vec, Int<NARROW>(), mode)
                    : kind == MIDDLE ? with(vec, Int<MIDDLE>(), mode)
                    : kind == WIDE   ? with(vec, Int<WIDE>(), mode)
+                   : kind == WIDER  ? with(vec, Int<decltype(vec)::value == 1 ? WIDER : WIDEST>(), mode)
                                     : with(vec, Int<WIDEST>(), mode);
         };
         return lie.how == VECTORS ? wide(Int<8>(), Int<ALIGNED>())
