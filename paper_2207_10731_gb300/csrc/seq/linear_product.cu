@@ -144,7 +144,7 @@ struct Unit {
 };
 // blocks < 2^25, splits <= 64
 __device__ __forceinline__ int part_start(const Args& a, int split) {
-    return a.splits == 1 ? split * a.blocks : (int)((unsigned)(a.blocks * split) / (unsigned)a.splits);
+    return a.splits == 1 ? split * a.blocks : (int)((unsigned)a.blocks * (unsigned)split / (unsigned)a.splits);
 }
 __device__ __forceinline__ Unit unit_of(const Args& a, int u) {
     constexpr int kBand = 16;
@@ -167,8 +167,8 @@ __device__ __forceinline__ int blocks_of(const Args& a, int u) {
 
 // ---- finishing through shared memory -------------------------------------------
 // A warp's tile: 32 rows of 128 bytes, the 16-byte piece p of row r in the 128-byte swizzle, as
-// TMA stores it.  (32-byte stores of a row a lane, 32 lines an instruction: 7400 cycles a tile
-// of 128 x 256 instead of PLAIN.)
+// TMA stores it.  (32-byte stores of a row a lane, 32 lines an instruction: 55 instead of 42 us for
+// 16384 x 64 x 4096, where finishing is nearly all there is to do.)
 
 __device__ __forceinline__ uint32_t piece_at(uint32_t tile, int row, int p) {
     return tile + row * 128 + ((p ^ (row & 7)) << 4);
@@ -266,7 +266,6 @@ __device__ __forceinline__ void finish_one(const Finish& f, float v, int64_t t, 
         static_cast<T*>(f.y)[at] = round_to<T>(v);
 }
 
-template <typename T>
 __device__ __forceinline__ void add_bias(const Finish& f, float (&v)[32], int c, int n) {
     if (f.bias_vectors && c + 32 <= n) {
 #pragma unroll
@@ -340,7 +339,7 @@ __device__ __forceinline__ bool finish_tiles(const Args& a, const CUtensorMap* m
         tmem_load32(d + c, v);
         tmem_wait_load();
         tmem_loaded(v);
-        if (f.bias && !partial) add_bias<T>(f, v, col, a.n);
+        if (f.bias && !partial) add_bias(f, v, col, a.n);
     };
     for (int c = half * kWide; c < a.bn; c += 2 * kWide) {
         const int col = col0 + c;
