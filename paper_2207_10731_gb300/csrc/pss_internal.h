@@ -76,7 +76,10 @@ struct RadixPlan {
 // Plan for buckets in [0, R): digit_bits 0 picks at most kRadixMaxBits bits per
 // pass, as few passes as that allows, split evenly; 4 .. 11 forces that many.
 RadixPlan radix_plan(uint64_t R, int digit_bits);
-int64_t radix_tiles(int64_t npairs);   // tiles of one pass
+// Entries per thread of a tile: 32, or 12 for lists that would not fill the GPU with such tiles
+// (whose cnt has to be as large as radix_tiles says).
+constexpr int kRadixTile = 32, kRadixSmallTile = 12;
+int64_t radix_tiles(int64_t npairs, int per = kRadixTile);   // tiles of one pass
 
 // Buffers of the sorted backward path (see pss_sorted.cu).
 struct SortedBuffers {
@@ -114,7 +117,7 @@ cudaError_t launch_sorted_scatter(const SortedBuffers& sb, int64_t npairs, int J
 // Stable radix sort of the forward's pairs by bucket into sorted_e (three
 // kernels per pass; see pss_sorted.cu): entries of one bucket in pair order.
 cudaError_t launch_radix_sort(const SortedBuffers& sb, int64_t npairs, int J, uint32_t smask,
-                              const RadixPlan& plan, cudaStream_t st);
+                              const RadixPlan& plan, cudaStream_t st, int per = kRadixTile);
 // Touched bitmap / list of the buckets of the forward's pairs.
 cudaError_t launch_mark_pairs(const SortedBuffers& sb, int64_t npairs, uint32_t smask,
                               const Touched& touched, int sm_count, cudaStream_t st);

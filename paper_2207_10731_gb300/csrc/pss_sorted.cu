@@ -447,7 +447,7 @@ k_sort_local(const uint32_t* __restrict__ pair_x, int64_t npairs,
 // valid pairs to stats[0], which the later passes and the reduce read.
 constexpr int kRThreads = 256;
 constexpr int kRWarps = kRThreads / 32;
-constexpr int kRPer = 32;                        // entries per thread and tile
+constexpr int kRPer = kRadixTile;                // entries per thread and tile
 constexpr int kRWarpKeys = 32 * kRPer;           // entries per warp and tile
 constexpr int kRTile = kRThreads * kRPer;        // entries per tile
 constexpr int kRMaxDigits = 1 << kRadixMaxBits;
@@ -505,7 +505,7 @@ __device__ __forceinline__ int64_t radix_count(int64_t npairs,
 
 // up: cnt[d][tile] = entries of the tile with digit d (every tile writes all
 // of its nd counts, zeros included).
-template <bool FIRST, bool SG>
+template <bool FIRST, bool SG, int PER = kRPer>
 __global__ void __launch_bounds__(kRThreads)
 k_radix_up(const uint32_t* __restrict__ pair_x, const unsigned long long* __restrict__ in_e,
            int64_t npairs, const unsigned long long* __restrict__ stats, int shift, int bits,
@@ -517,10 +517,10 @@ k_radix_up(const uint32_t* __restrict__ pair_x, const unsigned long long* __rest
     for (int d = threadIdx.x; d < nd; d += kRThreads) s_c[d] = 0u;
     __syncthreads();
     const int64_t n = radix_count<FIRST>(npairs, stats);
-    const int64_t t0 = (int64_t)blockIdx.x * kRTile;
-    uint32_t hi[kRPer];
+    const int64_t t0 = (int64_t)blockIdx.x * kRThreads * PER;
+    uint32_t hi[PER];
 #pragma unroll
-    for (int i = 0; i < kRPer; ++i) {
+    for (int i = 0; i < PER; ++i) {
         const int64_t p = t0 + (int64_t)i * kRThreads + threadIdx.x;
         if (FIRST) {
             hi[i] = (p < n) ? __ldg(pair_x + p) : kBad;
@@ -530,7 +530,7 @@ k_radix_up(const uint32_t* __restrict__ pair_x, const unsigned long long* __rest
         }
     }
 #pragma unroll
-    for (int i = 0; i < kRPer; ++i)
+    for (int i = 0; i < PER; ++i)
         if (hi[i] != kBad) atomicAdd(&s_c[(hi[i] >> shift) & dmask], 1u);
     __syncthreads();
     for (int d = threadIdx.x; d < nd; d += kRThreads) cnt[(size_t)d * ntiles + blockIdx.x] = s_c[d];
@@ -616,12 +616,12 @@ k_radix_colscan(uint32_t* __restrict__ cnt, int ntiles, int bits, uint32_t* __re
 }
 
 // Shared memory of the down kernel with 2^bits digits.
-__host__ __device__ constexpr size_t radix_down_smem(int nd) {
-    return sizeof(unsigned long long) * kRTile + (sizeof(uint16_t) * kRWarps + 8) * (size_t)nd;
+__host__ __device__ constexpr size_t radix_down_smem(int nd, int per = kRPer) {
+    return sizeof(unsigned long long) * kRThreads * per + (sizeof(uint16_t) * kRWarps + 8) * (size_t)nd;
 }
 
 // down: one tile per CTA (see the section comment).
-template <bool FIRST, bool SG>
+template <bool FIRST, bool SG, int PER = kRPer>
 __global__ void __launch_bounds__(kRThreads, 2)
 k_radix_down(const uint32_t* __restrict__ pair_x, const uint32_t* __restrict__ q_row,
              const unsigned long long* __restrict__ in_e, unsigned long long* __restrict__ out_e,
@@ -629,10 +629,11 @@ k_radix_down(const uint32_t* __restrict__ pair_x, const uint32_t* __restrict__ q
              int shift, int bits, int ntiles, const uint32_t* __restrict__ cnt,
              const uint32_t* __restrict__ dstart) {
     pdl_prologue();
+    constexpr int kTile = kRThreads * PER;
     extern __shared__ __align__(16) unsigned char r_smem[];
     const int nd = 1 << bits;
-    unsigned long long* s_tile = reinterpret_cast<unsigned long long*>(r_smem);   // [kRTile]
-    uint16_t* s_hist = reinterpret_cast<uint16_t*>(s_tile + kRTile);               // [kRWarps][nd]
+    unsigned long long* s_tile = reinterpret_cast<unsigned long long*>(r_smem);   // [kTile]
+    uint16_t* s_hist = reinterpret_cast<uint16_t*>(s_tile + kTile);               // [kRWarps][nd]
     uint32_t* s_lst = reinterpret_cast<uint32_t*>(s_hist + kRWarps * nd);          // [nd]
     uint32_t* s_base = s_lst + nd;                                                 // [nd]
     __shared__ uint32_t s_w[kRWarps];
@@ -640,36 +641,36 @@ k_radix_down(const uint32_t* __restrict__ pair_x, const uint32_t* __restrict__ q
     const int lane = threadIdx.x & 31;
     const int warp = threadIdx.x >> 5;
     const int64_t n = radix_count<FIRST>(npairs, stats);
-    const int64_t t0 = (int64_t)blockIdx.x * kRTile;
+    const int64_t t0 = (int64_t)blockIdx.x * kTile;
     if (t0 >= n) return;
     {
         uint32_t* z = reinterpret_cast<uint32_t*>(s_hist);
         for (int i = threadIdx.x; i < kRWarps * nd / 2; i += kRThreads) z[i] = 0u;
     }
-    // load, warp w taking entries t0 + w*kRWarpKeys + i*32 + lane (i in order)
-    unsigned long long e[kRPer];
+    // load, warp w taking entries t0 + w*32*PER + i*32 + lane (i in order)
+    unsigned long long e[PER];
     {
-        const int64_t wb = t0 + (int64_t)warp * kRWarpKeys + lane;
+        const int64_t wb = t0 + (int64_t)warp * (32 * PER) + lane;
         if (FIRST) {
             // every load is issued before any is used: buckets, then id rows
-            uint32_t x[kRPer], row[kRPer];
+            uint32_t x[PER], row[PER];
 #pragma unroll
-            for (int i = 0; i < kRPer; ++i) {
+            for (int i = 0; i < PER; ++i) {
                 const int64_t p = wb + i * 32;
                 x[i] = (p < n) ? __ldg(pair_x + p) : kBad;
             }
 #pragma unroll
-            for (int i = 0; i < kRPer; ++i) {
+            for (int i = 0; i < PER; ++i) {
                 const uint32_t pp = (uint32_t)(wb + i * 32);   // npairs < 2^32 here
                 const uint32_t q = (log2J >= 0) ? (pp >> log2J) : pp / (uint32_t)J;
                 row[i] = (wb + i * 32 < n) ? __ldg(q_row + q) : 0u;
             }
 #pragma unroll
-            for (int i = 0; i < kRPer; ++i)
+            for (int i = 0; i < PER; ++i)
                 e[i] = radix_pair_entry<SG>(x[i], row[i], (uint32_t)(wb + i * 32), J, log2J);
         } else {
 #pragma unroll
-            for (int i = 0; i < kRPer; ++i) {
+            for (int i = 0; i < PER; ++i) {
                 const int64_t p = wb + i * 32;
                 e[i] = (p < n) ? __ldcs(in_e + p) : ~0ull;
             }
@@ -677,12 +678,12 @@ k_radix_down(const uint32_t* __restrict__ pair_x, const uint32_t* __restrict__ q
     }
     __syncthreads();
     // rank each entry among the warp's entries of its digit, in input order
-    uint32_t rank[kRPer];
+    uint32_t rank[PER];
     {
         uint16_t* hw = s_hist + warp * nd;
         const uint32_t lt = (1u << lane) - 1u;
 #pragma unroll
-        for (int i = 0; i < kRPer; ++i) {
+        for (int i = 0; i < PER; ++i) {
             const bool valid = e[i] != ~0ull;
             const uint32_t dg = valid ? ((uint32_t)(e[i] >> (32 + shift)) & dmask) : 0xffffffffu;
             const uint32_t peers = __match_any_sync(0xffffffffu, dg);
@@ -735,7 +736,7 @@ k_radix_down(const uint32_t* __restrict__ pair_x, const uint32_t* __restrict__ q
     __syncthreads();
     // stage the tile in digit order
 #pragma unroll
-    for (int i = 0; i < kRPer; ++i) {
+    for (int i = 0; i < PER; ++i) {
         if (e[i] == ~0ull) continue;
         const uint32_t dg = (uint32_t)(e[i] >> (32 + shift)) & dmask;
         s_tile[s_lst[dg] + s_hist[warp * nd + dg] + rank[i]] = e[i];
@@ -1426,35 +1427,36 @@ RadixPlan radix_plan(uint64_t R, int digit_bits) {
     return pl;
 }
 
-int64_t radix_tiles(int64_t npairs) {
-    const int64_t t = (npairs + kRTile - 1) / kRTile;
+int64_t radix_tiles(int64_t npairs, int per) {
+    const int64_t tile = (int64_t)kRThreads * per, t = (npairs + tile - 1) / tile;
     return t < 1 ? 1 : t;
 }
 
-template <bool FIRST, bool SG>
+template <bool FIRST, bool SG, int PER>
 cudaError_t radix_pass(const SortedBuffers& sb, const unsigned long long* in,
                        unsigned long long* out, int64_t npairs, int J, int log2J,
                        const RadixPlan& plan, int k, cudaStream_t st) {
-    const int ntiles = (int)radix_tiles(npairs);
+    const int ntiles = (int)radix_tiles(npairs, PER);
     const int bits = plan.bits[k], shift = plan.shift[k];
     const int nd = 1 << bits;
-    cudaError_t e = launch_k(k_radix_up<FIRST, SG>, dim3(ntiles), dim3(kRThreads), 0, st,
+    cudaError_t e = launch_k(k_radix_up<FIRST, SG, PER>, dim3(ntiles), dim3(kRThreads), 0, st,
                              sb.pair_x, in, npairs, sb.stats, shift, bits, ntiles, sb.cnt);
     if (e != cudaSuccess) return e;
     e = launch_k(k_radix_colscan<FIRST>, dim3((nd + kRWarps - 1) / kRWarps), dim3(kRThreads), 0,
                  st, sb.cnt, ntiles, bits, sb.tot, sb.dstart, sb.done, sb.stats);
     if (e != cudaSuccess) return e;
-    const size_t smem = radix_down_smem(nd);
-    e = cudaFuncSetAttribute(k_radix_down<FIRST, SG>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+    const size_t smem = radix_down_smem(nd, PER);
+    e = cudaFuncSetAttribute(k_radix_down<FIRST, SG, PER>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                              (int)smem);
     if (e != cudaSuccess) return e;
-    return launch_k(k_radix_down<FIRST, SG>, dim3(ntiles), dim3(kRThreads), smem, st, sb.pair_x,
+    return launch_k(k_radix_down<FIRST, SG, PER>, dim3(ntiles), dim3(kRThreads), smem, st, sb.pair_x,
                     sb.q_row, in, out, npairs, sb.stats, J, log2J, shift, bits, ntiles, sb.cnt,
                     sb.dstart);
 }
 
-cudaError_t launch_radix_sort(const SortedBuffers& sb, int64_t npairs, int J, uint32_t smask,
-                              const RadixPlan& plan, cudaStream_t st) {
+template <int PER>
+cudaError_t radix_sort(const SortedBuffers& sb, int64_t npairs, int J, uint32_t smask,
+                       const RadixPlan& plan, cudaStream_t st) {
     const int log2J = (J & (J - 1)) == 0 ? ceil_log2(J) : -1;
     const unsigned long long* in = nullptr;
     for (int k = 0; k < plan.passes; ++k) {
@@ -1462,14 +1464,20 @@ cudaError_t launch_radix_sort(const SortedBuffers& sb, int64_t npairs, int J, ui
         unsigned long long* out = ((plan.passes - 1 - k) % 2 == 0) ? sb.sorted_e : sb.tmp_e;
         cudaError_t e;
         if (k == 0)
-            e = smask ? radix_pass<true, true>(sb, in, out, npairs, J, log2J, plan, k, st)
-                      : radix_pass<true, false>(sb, in, out, npairs, J, log2J, plan, k, st);
+            e = smask ? radix_pass<true, true, PER>(sb, in, out, npairs, J, log2J, plan, k, st)
+                      : radix_pass<true, false, PER>(sb, in, out, npairs, J, log2J, plan, k, st);
         else
-            e = radix_pass<false, false>(sb, in, out, npairs, J, log2J, plan, k, st);
+            e = radix_pass<false, false, PER>(sb, in, out, npairs, J, log2J, plan, k, st);
         if (e != cudaSuccess) return e;
         in = out;
     }
     return cudaSuccess;
+}
+
+cudaError_t launch_radix_sort(const SortedBuffers& sb, int64_t npairs, int J, uint32_t smask,
+                              const RadixPlan& plan, cudaStream_t st, int per) {
+    return per == kRadixSmallTile ? radix_sort<kRadixSmallTile>(sb, npairs, J, smask, plan, st)
+                                  : radix_sort<kRPer>(sb, npairs, J, smask, plan, st);
 }
 
 int64_t sorted_scan_blocks(int64_t R) { return (R + kScanChunk - 1) / kScanChunk; }

@@ -81,7 +81,7 @@ k_linear_slope(const __grid_constant__ Slope s, int parts) {
     float v = 0.f;
 #pragma unroll
     for (int w = 0; w < kWarps; ++w) v += sums[w][threadIdx.x];
-    s.partial[(int64_t)part * s.cols + col] = v;
+    (parts == 1 ? s.dbias : s.partial)[(int64_t)part * s.cols + col] = v;
 }
 
 // Parts of the rows: the GPU filled four CTAs an SM, of 32 rows each at least.
@@ -110,7 +110,7 @@ cudaError_t launch_slope(const Slope& s, int type, cudaStream_t st) {
                           : go(k_linear_slope<T, T, false>);
     };
     const cudaError_t e = type == PSS_BF16 ? typed(bf16()) : typed(f16());
-    if (e != cudaSuccess || !s.dbias) return e;
+    if (e != cudaSuccess || !s.dbias || parts == 1) return e;
     return launch_k(k_row_columns, dim3((unsigned)((s.cols + 31) / 32)), dim3(1024), 0, st,
                     static_cast<const float*>(s.partial), parts, s.cols, s.cols, 0, s.cols, s.dbias,
                     static_cast<float*>(nullptr));
