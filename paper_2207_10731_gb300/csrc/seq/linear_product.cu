@@ -459,20 +459,21 @@ k_linear_product(const __grid_constant__ CUtensorMap ma, const __grid_constant__
             const int b_rows = a.bn / kCtas, b_boxes = (b_rows + 63) / 64;
             const uint32_t bytes =
                 kCtas * (R::kA + (a.b_across ? b_boxes * 64 : b_rows) * kBlock * 2);
-            int s = 0;
+            const uint32_t first_full = PAIR ? first_cta(&full[0]) : 0;
+            int s = 0, slot = 0;
+            uint32_t turn = 1;   // a stage's first use waits for nobody
             bool ok = true;
             for (int u = first_unit; ok && u < a.units; u += step) {
                 const Unit w = unit_of(a, u);
                 const int row = (w.m * kCtas + rank) * 128, col = w.n * a.bn + rank * b_rows;
                 for (int k = w.k0; k < w.k1; ++k, ++s) {
-                    const int slot = s % R::kStages, turn = s / R::kStages;
-                    if (turn > 0 && !bar_wait(&empty[slot], (turn - 1) & 1, &stop)) {
+                    if (s >= R::kStages && !bar_wait(&empty[slot], turn, &stop)) {
                         ok = false;
                         break;
                     }
                     uint8_t* at = smem + slot * R::kStage;
                     if (rank == 0) bar_expect(&full[slot], bytes);
-                    const uint32_t bar = PAIR ? first_cta(&full[slot]) : 0;
+                    const uint32_t bar = first_full + 8 * slot;
                     auto load = [&](uint8_t* to, const CUtensorMap* map, int c0, int c1) {
                         if (PAIR)
                             tma_load2_pair(to, map, c0, c1, bar);
@@ -492,6 +493,7 @@ k_linear_product(const __grid_constant__ CUtensorMap ma, const __grid_constant__
                     } else {
                         load(at, &mb, k * kBlock, col);
                     }
+                    if (++slot == R::kStages) slot = 0, turn ^= 1;
                 }
             }
             // The loads must land before the CTA ends, also where nobody waits for them.  A pair's
@@ -509,16 +511,24 @@ k_linear_product(const __grid_constant__ CUtensorMap ma, const __grid_constant__
         if (lane == 0 && rank == 0) {
             const uint32_t desc =
                 product_desc(128 * kCtas, a.bn, std::is_same<T, f16>::value, a.a_across, a.b_across);
+            // A product of 16 along the contraction takes the tensor core 128 cycles (256 columns), and
+            // what this one thread does for it has to be less: descriptors differ in the low word's
+            // address alone, stages and their turns are counted, not divided for.
             const uint32_t base = smem_addr(smem);
-            const uint32_t a_lead = a.a_across ? 8192 : 16, b_lead = a.b_across ? 8192 : 16;
-            const uint32_t a_step = a.a_across ? 2048 : 32, b_step = a.b_across ? 2048 : 32;
+            const uint64_t a0 = smem_desc(base, a.a_across ? 8192 : 16);
+            const uint64_t b0 = smem_desc(base + R::kA, a.b_across ? 8192 : 16);
+            const uint32_t a_step = (a.a_across ? 2048 : 32) >> 4, b_step = (a.b_across ? 2048 : 32) >> 4;
             auto commit = [&](uint64_t* bar) {
                 if (PAIR)
                     tc_commit_pair(bar);
                 else
                     tc_commit(bar);
             };
-            int s = 0, i = 0;
+            auto at = [](uint64_t desc, uint32_t offset) {
+                return (desc & 0xffffffff00000000ull) | ((uint32_t)desc + offset);
+            };
+            int i = 0;
+            uint32_t slot = 0, turn = 0, from = 0;   // from: the stage's place, in 16 bytes
             bool ok = true;
             // a unit's blocks are counted before the one in front of it is worked on: divisions
             // between two units' products leave the tensor core idle
@@ -529,22 +539,23 @@ k_linear_product(const __grid_constant__ CUtensorMap ma, const __grid_constant__
                 if (i > 1)
                     ok = PAIR ? bar_wait_cluster(&free_[i & 1], ((i >> 1) - 1) & 1, &stop)
                               : bar_wait(&free_[i & 1], ((i >> 1) - 1) & 1, &stop);
-                for (int k = 0; ok && k < blocks; ++k, ++s) {
-                    const int slot = s % R::kStages;
-                    ok = bar_wait(&full[slot], (s / R::kStages) & 1, &stop);
+                bool add = false;
+                for (int k = 0; ok && k < blocks; ++k) {
+                    ok = bar_wait(&full[slot], turn, &stop);
                     if (!ok) break;
                     tc_after_sync();
-                    const uint32_t a_at = base + slot * R::kStage, b_at = a_at + R::kA;
 #pragma unroll
                     for (int j = 0; j < kBlock / 16; ++j) {
-                        const uint64_t x = smem_desc(a_at + j * a_step, a_lead);
-                        const uint64_t y = smem_desc(b_at + j * b_step, b_lead);
+                        const uint64_t x = at(a0, from + j * a_step), y = at(b0, from + j * b_step);
                         if (PAIR)
-                            mma_pair(d, x, y, desc, k > 0 || j > 0);
+                            mma_pair(d, x, y, desc, add || j > 0);
                         else
-                            mma_ss(d, x, y, desc, k > 0 || j > 0);
+                            mma_ss(d, x, y, desc, add || j > 0);
                     }
                     commit(&empty[slot]);
+                    add = true;
+                    from += R::kStage >> 4;
+                    if (++slot == R::kStages) slot = 0, from = 0, turn ^= 1;
                 }
                 if (ok) commit(&done[i & 1]);
             }

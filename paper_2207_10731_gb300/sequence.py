@@ -1,6 +1,8 @@
 """Operators of a sequence encoder over the pooled embeddings: layer norm,
-dropout and attention over packed sequences (argument marshalling only, like
-``binding``; the kernels are in libpss.so, their contracts in include/pss.h).
+dropout, attention over packed sequences, rows of a dense table, norms between
+blocks with gate and residual, and products with bias, activation and residual
+(argument marshalling only, like ``binding``; the kernels are in libpss.so, their
+contracts in include/pss.h).
 
 All tensors are CUDA tensors of the current device; calls are asynchronous on
 ``stream`` (a keyword of each; default: the current stream), to which the
