@@ -76,6 +76,13 @@ __device__ __forceinline__ void tma_load2_pair(void* dst, const CUtensorMap* map
         " [%0], [%1, {%2, %3}], [%4];"
         :: "r"(smem_addr(dst)), "l"(map), "r"(c0), "r"(c1), "r"(bar) : "memory");
 }
+__device__ __forceinline__ void tma_load3_pair(void* dst, const CUtensorMap* map, int c0, int c1,
+                                               int c2, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+        " [%0], [%1, {%2, %3, %4}], [%5];"
+        :: "r"(smem_addr(dst)), "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(bar) : "memory");
+}
 __device__ __forceinline__ void tmem_alloc_pair(uint32_t* at, uint32_t cols) {
     asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;"
                  :: "r"(smem_addr(at)), "r"(cols) : "memory");
@@ -134,6 +141,7 @@ struct Args {
     int64_t ld;
     int m, n, bn, blocks, m_tiles, n_tiles, splits, units;
     bool a_across, b_across;
+    bool a_boxes, b_boxes;   // across: in pairs of boxes of 64 (operand_map)
     unsigned long long* status;
 };
 
@@ -480,14 +488,24 @@ k_linear_product(const __grid_constant__ CUtensorMap ma, const __grid_constant__
                         else
                             tma_load2(to, map, c0, c1, &full[slot]);
                     };
-                    if (a.a_across) {
+                    auto load_pair = [&](uint8_t* to, const CUtensorMap* map, int c0, int c1) {
+                        if (PAIR)
+                            tma_load3_pair(to, map, 0, c1, c0 / 64, bar);
+                        else
+                            tma_load3(to, map, 0, c1, c0 / 64, &full[slot]);
+                    };
+                    if (a.a_boxes) {
+                        load_pair(at, &ma, row, k * kBlock);
+                    } else if (a.a_across) {
                         for (int i = 0; i < 2; ++i)
                             load(at + i * 8192, &ma, row + i * 64, k * kBlock);
                     } else {
                         load(at, &ma, k * kBlock, row);
                     }
                     at += R::kA;
-                    if (a.b_across) {
+                    if (a.b_boxes) {
+                        load_pair(at, &mb, col, k * kBlock);
+                    } else if (a.b_across) {
                         for (int i = 0; i < b_boxes; ++i)
                             load(at + i * 8192, &mb, col + i * 64, k * kBlock);
                     } else {
@@ -706,8 +724,15 @@ k_linear_join(const float* __restrict__ partial, int splits, int64_t rows, int c
                           f.residual ? residual_at<T>(f, t, c + e) : 0.f);
 }
 
-// Boxes of 64 along the dense dimension and `box` (at most 256) along the other.
-cudaError_t operand_map(CUtensorMap* map, const Operand& o, int box, int type) {
+// Whether an operand across the contraction may be loaded two boxes of 64 at a time: its rows are
+// seen as boxes beside each other then, all of them whole.
+bool in_boxes(const Operand& o, int rows) {
+    return o.across && rows > 64 && o.matrix.inner % 64 == 0;
+}
+
+// Boxes of 64 along the dense dimension and `box` (at most 256) along the other; or, across and
+// `boxes`, two boxes of 64 x 64 side by side.
+cudaError_t operand_map(CUtensorMap* map, const Operand& o, int box, bool boxes, int type) {
     static std::atomic<void*> found{nullptr};
     void* fn = driver_call("cuTensorMapEncodeTiled", &found);
     if (!fn) return cudaErrorNotSupported;
@@ -716,13 +741,14 @@ cudaError_t operand_map(CUtensorMap* map, const Operand& o, int box, int type) {
     const Matrix& x = o.matrix;
     // the stride over a single row is free, but the encoder checks it
     const int64_t stride = x.outer > 1 ? x.stride : (x.inner + 7) / 8 * 8;
-    const cuuint64_t dims[2] = {(cuuint64_t)x.inner, (cuuint64_t)x.outer};
-    const cuuint64_t strides[1] = {(cuuint64_t)stride * 2};
-    const cuuint32_t sizes[2] = {64, (cuuint32_t)(o.across ? kBlock : box)};
-    const cuuint32_t one[2] = {1, 1};
+    const cuuint64_t dims[3] = {boxes ? 64 : (cuuint64_t)x.inner, (cuuint64_t)x.outer,
+                                (cuuint64_t)(x.inner / 64)};
+    const cuuint64_t strides[2] = {(cuuint64_t)stride * 2, 128};
+    const cuuint32_t sizes[3] = {64, (cuuint32_t)(o.across ? kBlock : box), 2};
+    const cuuint32_t one[3] = {1, 1, 1};
     const CUresult rc = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(fn)(
-        map, type == PSS_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2,
-        const_cast<void*>(x.data), dims, strides, sizes, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+        map, type == PSS_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16,
+        boxes ? 3 : 2, const_cast<void*>(x.data), dims, strides, sizes, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
         CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
         CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return rc == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
@@ -754,8 +780,10 @@ template <int BN, bool PAIR, typename T>
 cudaError_t launch(const Product& p, int type, unsigned long long* status, cudaStream_t st) {
     using R = Ring<BN, PAIR>;
     CUtensorMap ma, mb, my = {}, mz = {};
-    cudaError_t e = operand_map(&ma, p.a, 128, type);
-    if (e == cudaSuccess) e = operand_map(&mb, p.b, p.bn / (PAIR ? 2 : 1), type);
+    const int b_rows = p.bn / (PAIR ? 2 : 1);
+    const bool a_boxes = in_boxes(p.a, 128), b_boxes = in_boxes(p.b, b_rows);
+    cudaError_t e = operand_map(&ma, p.a, 128, a_boxes, type);
+    if (e == cudaSuccess) e = operand_map(&mb, p.b, b_rows, b_boxes, type);
     Finish f = p.f;
     const bool split = p.splits > 1;
     f.tiles = !f.swapped && (split || f.tiles);
@@ -776,7 +804,7 @@ cudaError_t launch(const Product& p, int type, unsigned long long* status, cudaS
     if (e != cudaSuccess) return e;
     const int units = p.m_tiles * p.n_tiles * p.splits, fit = sm_count() / (PAIR ? 2 : 1);
     const Args a{f, split ? p.partial : nullptr, p.ld, p.m, p.n, p.bn, p.blocks, p.m_tiles,
-                 p.n_tiles, p.splits, units, p.a.across, p.b.across, status};
+                 p.n_tiles, p.splits, units, p.a.across, p.b.across, a_boxes, b_boxes, status};
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)((units < fit ? units : fit) * (PAIR ? 2 : 1)));
     cfg.blockDim = dim3(kProductThreads);
