@@ -617,13 +617,10 @@ k_linear_product(const __grid_constant__ CUtensorMap ma, const __grid_constant__
                     float more[32], bias = 0.f;
 #pragma unroll
                     for (int j = 0; j < 32; ++j) more[j] = 0.f;
-                    if (!f.swapped && col + lane < a.n) {
-                        if (f.bias) bias = f.bias[col + lane];
-                        if (f.residual)
+                    if (!f.swapped && f.residual && col + lane < a.n)
 #pragma unroll
-                            for (int j = 0; j < 32; ++j)
-                                if (row0 + j < a.m) more[j] = residual_at<T>(f, row0 + j, col + lane);
-                    }
+                        for (int j = 0; j < 32; ++j)
+                            if (row0 + j < a.m) more[j] = residual_at<T>(f, row0 + j, col + lane);
                     if (!waited && !wait()) {
                         stopped = true;
                         break;
@@ -648,19 +645,35 @@ k_linear_product(const __grid_constant__ CUtensorMap ma, const __grid_constant__
                             }
                         }
                     } else {
-                        // through shared memory: a row at a time, a lane to a column
+                        // bias and activation a lane to a row, where bias and code are the warp's; then
+                        // through shared memory, a row at a time and a lane to a column
                         float* values = reinterpret_cast<float*>(staged);
-                        __syncwarp();
+                        const bool mine = col + lane < a.n;
+                        const int last = min(32, a.m - row0);
+                        auto spread = [&](auto* to, int64_t stride, bool add) {
+                            using TO = typename std::remove_pointer<decltype(to)>::type;
+                            __syncwarp();
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) values[lane * 32 + (j ^ lane)] = v[j];
-                        __syncwarp();
-                        if (col + lane < a.n) {
+                            for (int j = 0; j < 32; ++j) values[lane * 32 + (j ^ lane)] = v[j];
+                            __syncwarp();
+                            if (!mine) return;
+                            TO* at = to + (int64_t)row0 * stride + col + lane;
 #pragma unroll
-                            for (int j = 0; j < 32; ++j)
-                                if (row0 + j < a.m)
-                                    finish_one<T>(f, values[j * 32 + (lane ^ j)], row0 + j, col + lane,
-                                                  bias, more[j]);
-                        }
+                            for (int j = 0; j < 32; ++j, at += stride)
+                                if (j < last)
+                                    *at = round_to<TO>(values[j * 32 + (lane ^ j)] +
+                                                       (add ? more[j] : 0.f));
+                        };
+                        if (f.bias) add_bias(f, v, col, a.n);
+                        if (f.z) spread(static_cast<T*>(f.z), f.z_stride, false);
+                        with_activation(f.activation, [&](auto act) {
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) v[j] = activate<decltype(act)::value>(v[j]);
+                        });
+                        if (f.y_f32)
+                            spread(static_cast<float*>(f.y), f.y_stride, f.residual != nullptr);
+                        else
+                            spread(static_cast<T*>(f.y), f.y_stride, f.residual != nullptr);
                     }
                 }
                 if (!waited && !stopped) stopped = !wait();
