@@ -86,7 +86,8 @@ __device__ __forceinline__ void note_outside(unsigned long long* status, int64_t
     if (status) atomicMin(status, (unsigned long long)t);
 }
 
-// U tokens to a group, all their loads in flight.
+// U tokens to a group, all their loads in flight (four in vectors: two 162 us and eight 197 for
+// 1.7 M x 128; value by value two, 53 instead of 59 us for 100000 x 333).
 template <typename TW, typename TO, bool VECTOR, int U>
 __global__ void __launch_bounds__(kThreads)
 k_embedding_forward(const TW* __restrict__ weight, int64_t ws, int64_t rows,
@@ -636,13 +637,14 @@ extern "C" pss_status pss_embedding_forward(const void* weight, pss_dtype weight
     // one token to a group while these do not fill the GPU
     const int64_t fill = (int64_t)sm_count() * 4 * (kThreads >> s.log2_lanes);
     const bool one = tokens * s.blocks <= fill;
-    const unsigned n = ctas(one ? tokens : (tokens + 3) / 4, s);
+    const bool vector = cols % 8 == 0 && aligned8(out, out_stride, dtype_size(out_type)) &&
+                        aligned8(weight, weight_stride, dtype_size(weight_type));
+    const int at_once = one ? 1 : vector ? 4 : 2;
+    const unsigned n = ctas((tokens + at_once - 1) / at_once, s);
     if (some && n == 0) return PSS_ERR_UNSUPPORTED;
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     const pss_status rc = clear_status(status, st);
     if (rc != PSS_OK || !some) return rc;
-    const bool vector = cols % 8 == 0 && aligned8(out, out_stride, dtype_size(out_type)) &&
-                        aligned8(weight, weight_stride, dtype_size(weight_type));
     return status_of(with_type(weight_type, [&](auto tw) {
         return with_type(out_type, [&](auto to) {
             using TW = decltype(tw);
@@ -655,7 +657,7 @@ extern "C" pss_status pss_embedding_forward(const void* weight, pss_dtype weight
             return vector ? one ? go(k_embedding_forward<TW, TO, true, 1>)
                                 : go(k_embedding_forward<TW, TO, true, 4>)
                    : one  ? go(k_embedding_forward<TW, TO, false, 1>)
-                          : go(k_embedding_forward<TW, TO, false, 4>);
+                          : go(k_embedding_forward<TW, TO, false, 2>);
         });
     }));
 }

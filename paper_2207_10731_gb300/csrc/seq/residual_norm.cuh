@@ -27,23 +27,27 @@ inline int norm_per_sm(int64_t cols) {
     return (int)(1536 / threads);
 }
 
-// Rows up to 32 lanes' vectors: several to a CTA of 256 threads, within shuffles.  Up to 256
+// Rows up to 32 lanes' vectors, several to a CTA of 256 threads, or with two to a lane twice that, four
+// to a CTA of 128: within shuffles.  (40001 x 333 bf16 backward 96 us; by CTAs of two warps to a row
+// 146, by eight rows to a CTA 97, on an fp32 stream 119 for want of shared memory.)  Up to 256
 // threads' (three CTAs an SM) or 512: a CTA to a row.  These with the next row's loads ahead.  Up to
 // 1024 threads', and above with two vectors to a thread: without, for want of room.  (Forward in
 // vectors the latter is faster from 512 on, half the warps to a barrier: 8000 x 8192 bf16 on an
 // fp32 stream 135 instead of 190 us; backward 370 instead of 322.)
 // (Two vectors to a thread for shorter rows too: 495 instead of 434 us for the gradients of
 // 65536 x 2048, half the warps.)
-enum { NARROW, MIDDLE, WIDE, WIDER, WIDEST };
+enum { NARROW, DOUBLE, MIDDLE, WIDE, WIDER, WIDEST };
 template <int VEC, int KIND>
 struct Fit {
-    static constexpr int kVectors = (VEC == 8 ? 1 : 8) * (KIND == WIDEST ? 2 : 1);
+    static constexpr int kVectors = (VEC == 8 ? 1 : 8) * (KIND == WIDEST || KIND == DOUBLE ? 2 : 1);
+    static constexpr bool kWarp = KIND <= DOUBLE;   // a row is a warp's
     static constexpr int kMost = KIND <= MIDDLE ? 256 : KIND == WIDE ? 512 : 1024;
-    static constexpr int kLeast = KIND == MIDDLE && VEC == 8 ? 3 : 1;   // CTAs an SM
+    static constexpr int kLeast = KIND == MIDDLE && VEC == 8 ? 3 : KIND == DOUBLE ? 2 : 1;   // CTAs an SM
     static constexpr bool kAhead = VEC == 8 && KIND <= WIDE;
 };
-// What is there of norms and gates is known to the kernel where both norms are and rows are
-// aligned: FULL is the kind of gate then.  ANY asks at every turn.
+// What is there of norms and gates is known to the kernel where both norms are and rows go in
+// vectors (up to 512 threads' aligned ones, 256 threads' others): FULL is the kind of gate then.  ANY
+// asks at every turn.
 enum { ANY = -1 };
 
 // extra: elements that a ragged row's first vector may hold in front of it; wider: see above.
@@ -58,6 +62,14 @@ inline Split norm_split(int cols, int extra, bool wider, int* kind) {
         while (s.lanes < units) s.lanes *= 2, ++s.log2_lanes;
         s.threads = 256;
         s.groups = 256 / s.lanes;
+        return s;
+    }
+    if (units <= 64) {
+        *kind = DOUBLE;
+        s.lanes = 32;
+        s.log2_lanes = 5;
+        s.threads = 128;
+        s.groups = 4;
         return s;
     }
     *kind = units <= 256 ? MIDDLE : units <= 512 ? WIDE : units <= 1024 && wider ? WIDER : WIDEST;
@@ -78,7 +90,7 @@ __device__ __forceinline__ float shuffled(float a, int m) { return __shfl_xor_sy
 // the next but one call, so that one barrier a call is enough: `turn` counts.
 template <int KIND, typename V>
 __device__ __forceinline__ V row_sums(V v, int lanes, float2 (*slots)[32], int& turn) {
-    if constexpr (KIND == NARROW) {
+    if constexpr (KIND <= DOUBLE) {
         for (int m = lanes >> 1; m > 0; m >>= 1) v = add_pair(v, shuffled(v, m));
         return v;
     } else {

@@ -43,7 +43,7 @@ k_residual_norm_backward(const __grid_constant__ Backward<T, R> a) {
     const bool grad_total = FULL != ANY || a.grad_total, reads_x = FULL != ANY || a.reads_x;
     using F = Fit<VEC, KIND>;
     constexpr int CH = F::kVectors;
-    constexpr bool kShared = KIND != NARROW;
+    constexpr bool kShared = !F::kWarp;
     constexpr int kDirty = F::kAhead ? ALIGNED : MODE;   // whether a vector may hold a neighbour's values
     extern __shared__ __align__(16) float sums[];
     __shared__ float2 slots[2][32];
@@ -98,16 +98,18 @@ k_residual_norm_backward(const __grid_constant__ Backward<T, R> a) {
     uint32_t laid = 0;
     if constexpr (kLaid) {
         laid = at + threadIdx.x * 16;
-        for (int k = 0; k < 2; ++k) {
-            float w[8] = {};
-            const float* from = k == 0 ? a.post : a.pre;
-            if (from) load_weight<VEC, MODE>(from, place.at(sh, 0), sh.cols, in[0], w);
+        for (int k = 0; k < 2; ++k)
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
-                asm volatile("st.shared.v4.f32 [%0], {%1,%2,%3,%4};"
-                             :: "r"(laid + (2 * k + h) * blockDim.x * 16), "f"(w[4 * h]),
-                                "f"(w[4 * h + 1]), "f"(w[4 * h + 2]), "f"(w[4 * h + 3]) : "memory");
-        }
+            for (int c = 0; c < CH; ++c) {
+                float w[8] = {};
+                const float* from = k == 0 ? a.post : a.pre;
+                if (from) load_weight<VEC, MODE>(from, place.at(sh, c), sh.cols, in[c], w);
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+                    asm volatile("st.shared.v4.f32 [%0], {%1,%2,%3,%4};"
+                                 :: "r"(laid + (2 * (k * CH + c) + h) * blockDim.x * 16), "f"(w[4 * h]),
+                                    "f"(w[4 * h + 1]), "f"(w[4 * h + 2]), "f"(w[4 * h + 3]) : "memory");
+            }
     }
     auto weights = [&](int k, int c, float (&w)[VEC]) {
         if constexpr (kLaid) {
@@ -115,14 +117,14 @@ k_residual_norm_backward(const __grid_constant__ Backward<T, R> a) {
             for (int h = 0; h < 2; ++h)
                 asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];"
                              : "=f"(w[4 * h]), "=f"(w[4 * h + 1]), "=f"(w[4 * h + 2]), "=f"(w[4 * h + 3])
-                             : "r"(laid + (2 * k + h) * blockDim.x * 16) : "memory");
+                             : "r"(laid + (2 * (k * CH + c) + h) * blockDim.x * 16) : "memory");
         } else {
             load_weight<VEC, MODE>(k == 0 ? a.post : a.pre, place.at(sh, c), sh.cols, in[c], w);
         }
     };
     float next_gate = 0.f, next_post = 0.f, next_pre = 0.f;
     auto fetch = [&](int stage, int64_t r) {
-        const bool live = KIND != NARROW || r < sh.rows;
+        const bool live = !F::kWarp || r < sh.rows;
         auto whole = [&](int64_t stride) { return MODE == ALIGNED || inner(sh, r, stride); };
         if (pre) {
             held_t.fetch(stage, a.total + r * a.ts, live, whole(a.ts), in, place, sh);
@@ -142,7 +144,7 @@ k_residual_norm_backward(const __grid_constant__ Backward<T, R> a) {
     int turn = 0, stage = 0;
     for (int64_t r0 = (int64_t)blockIdx.x * sh.groups; r0 < sh.rows; r0 += step, stage ^= 1) {
         const int64_t r = r0 + place.group;
-        const bool live = KIND != NARROW || r < sh.rows;
+        const bool live = !F::kWarp || r < sh.rows;
         if (!F::kAhead) fetch(0, r);
         const float row_gate = next_gate, post_rstd = next_post, pre_rstd = next_pre;
         if (F::kAhead) {
@@ -374,13 +376,13 @@ extern "C" pss_status pss_residual_norm_backward(
             using F = Fit<decltype(vec)::value, decltype(k)::value>;
             constexpr int kT = held_bytes<T, F::kVectors>(), kR = held_bytes<R, F::kVectors>();
             const size_t ahead =
-                F::kAhead ? s.threads * (size_t)((decltype(mode)::value == RAGGED ? 64 : 0) +
+                F::kAhead ? s.threads * (size_t)((decltype(mode)::value == RAGGED ? 64 * F::kVectors : 0) +
                                                  (grad_total ? kR : 0) + (pre_weight ? kR + kT : 0) +
                                                  (reads_x ? kT : 0) + (values ? kT : 0))
                           : 0;
             // rows of a warp: at the end, the groups' sums instead
             const size_t smem =
-                kind == NARROW ? std::max(ahead, (size_t)s.groups * 8 * cols)
+                kind <= DOUBLE ? std::max(ahead, (size_t)s.groups * 8 * cols)
                               : ahead + (size_t)8 * F::kVectors * decltype(vec)::value * s.threads;
             cudaError_t e = cudaSuccess;
             if (smem + 1024 > 48 * 1024)   // 48 KB with the kernel's own
@@ -410,6 +412,7 @@ extern "C" pss_status pss_residual_norm_backward(
         };
         auto wide = [&](auto vec, auto mode) {
             return kind == NARROW   ? with(vec, Int<NARROW>(), mode)
+                   : kind == DOUBLE ? with(vec, Int<DOUBLE>(), mode)
                    : kind == MIDDLE ? with(vec, Int<MIDDLE>(), mode)
                    : kind == WIDE   ? with(vec, Int<WIDE>(), mode)
                    : kind == WIDER  ? with(vec, Int<WIDER>(), mode)

@@ -47,18 +47,21 @@ k_residual_norm_forward(const __grid_constant__ Forward<T, R> a) {
     constexpr bool kLaid = MODE == RAGGED && F::kAhead;
     extern __shared__ __align__(16) float4 laid[];
     if constexpr (kLaid) {
-        for (int k = 0; k < 2; ++k) {
-            float w[8] = {};
-            const float* from = k == 0 ? a.post : a.pre;
-            if (from) load_weight<VEC, MODE>(from, place.at(sh, 0), sh.cols, in[0], w);
-            laid[2 * k * blockDim.x + threadIdx.x] = make_float4(w[0], w[1], w[2], w[3]);
-            laid[(2 * k + 1) * blockDim.x + threadIdx.x] = make_float4(w[4], w[5], w[6], w[7]);
-        }
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int c = 0; c < CH; ++c) {
+                float w[8] = {};
+                const float* from = k == 0 ? a.post : a.pre;
+                if (from) load_weight<VEC, MODE>(from, place.at(sh, c), sh.cols, in[c], w);
+                float4* to = laid + 2 * (k * CH + c) * blockDim.x + threadIdx.x;
+                to[0] = make_float4(w[0], w[1], w[2], w[3]);
+                to[blockDim.x] = make_float4(w[4], w[5], w[6], w[7]);
+            }
     }
     auto weights = [&](int k, int c, float (&w)[VEC]) {
         if constexpr (kLaid) {
-            const float4 x = laid[2 * k * blockDim.x + threadIdx.x];
-            const float4 y = laid[(2 * k + 1) * blockDim.x + threadIdx.x];
+            const float4* from = laid + 2 * (k * CH + c) * blockDim.x + threadIdx.x;
+            const float4 x = from[0], y = from[blockDim.x];
             w[0] = x.x, w[1] = x.y, w[2] = x.z, w[3] = x.w;
             w[4] = y.x, w[5] = y.y, w[6] = y.z, w[7] = y.w;
         } else {
@@ -71,7 +74,7 @@ k_residual_norm_forward(const __grid_constant__ Forward<T, R> a) {
     Part<R, VEC, CH> next_r;
     float next_gate = 0.f;
     auto fetch = [&](int64_t r) {
-        const bool live = KIND != NARROW || r < sh.rows;
+        const bool live = !F::kWarp || r < sh.rows;
         auto whole = [&](int64_t stride) { return MODE == ALIGNED || inner(sh, r, stride); };
         next_x.load(a.x + r * a.xs, live, whole(a.xs), in, place, sh);
         next_r.load(a.residual + r * a.rs, live, whole(a.rs), in, place, sh);
@@ -85,7 +88,7 @@ k_residual_norm_forward(const __grid_constant__ Forward<T, R> a) {
     // rows past the end are computed from zeros and dropped
     for (int64_t r0 = (int64_t)blockIdx.x * sh.groups; r0 < sh.rows; r0 += step) {
         const int64_t r = r0 + place.group;
-        const bool live = KIND != NARROW || r < sh.rows;
+        const bool live = !F::kWarp || r < sh.rows;
         if (!F::kAhead) fetch(r);
         const Part<T, VEC, CH> part_x = next_x, part_g = next_g;
         const Part<R, VEC, CH> part_r = next_r;
@@ -192,9 +195,9 @@ extern "C" pss_status pss_residual_norm_forward(
         auto launch = [&](auto vec, auto k, auto mode, auto full) -> cudaError_t {
             auto* kernel = k_residual_norm_forward<T, R, decltype(vec)::value, decltype(k)::value,
                                                    decltype(mode)::value, decltype(full)::value>;
-            constexpr bool kLaid = decltype(mode)::value == RAGGED &&
-                                   Fit<decltype(vec)::value, decltype(k)::value>::kAhead;
-            const size_t smem = kLaid ? 64 * s.threads : 0;   // at most 32 KB
+            using F = Fit<decltype(vec)::value, decltype(k)::value>;
+            constexpr bool kLaid = decltype(mode)::value == RAGGED && F::kAhead;
+            const size_t smem = kLaid ? 64 * F::kVectors * s.threads : 0;   // at most 32 KB
             const int n = ctas_of(rows, s, [&] { return resident(kernel, s.threads, smem, 32); },
                                   decltype(mode)::value);
             return launch_k(kernel, dim3(n), dim3(s.threads), smem, st, f);
@@ -211,6 +214,7 @@ extern "C" pss_status pss_residual_norm_forward(
         };
         auto wide = [&](auto vec, auto mode) {
             return kind == NARROW   ? with(vec, Int<NARROW>(), mode)
+                   : kind == DOUBLE ? with(vec, Int<DOUBLE>(), mode)
                    : kind == MIDDLE ? with(vec, Int<MIDDLE>(), mode)
                    : kind == WIDE   ? with(vec, Int<WIDE>(), mode)
                    : kind == WIDER  ? with(vec, Int<decltype(vec)::value == 1 ? WIDER : WIDEST>(), mode)

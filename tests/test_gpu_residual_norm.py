@@ -134,6 +134,7 @@ CASES = [
     (41, 1001, "f32", "f32", 0, 1, 1), (700, 2048, "bf16", "bf16", 1, 1, 2), (19, 4096, "bf16", "f32", 1, 1, 2),
     (19, 4104, "f16", "f32", 1, 1, 2), (23, 5001, "bf16", "bf16", 1, 1, 1), (5, 8192, "f32", "f32", 1, 1, 2),
     (7, 16384, "bf16", "f32", 1, 1, 2), (6, 16381, "f16", "f16", 1, 1, 2), (50, 48, "f32", "f32", 0, 0, 0),
+    (501, 505, "bf16", "bf16", 1, 1, 2), (501, 300, "f16", "f32", 1, 1, 1), (130, 512, "bf16", "bf16", 1, 1, 2),
 ]
 
 
