@@ -515,13 +515,16 @@ k_linear_product(const __grid_constant__ CUtensorMap ma, const __grid_constant__
                 }
             }
             // The loads must land before the CTA ends, also where nobody waits for them.  A pair's
-            // second CTA cannot see them land: the first one's wait ends after them, and both
-            // CTAs end together.
+            // second CTA cannot see them land, but its stages are free again only after they have
+            // been multiplied.  The products' arrivals must be there too: one still on its way to
+            // this CTA's barriers would reach the shared memory of whichever CTA comes next.
             int never = 0;
             if (rank == 0)
                 for (int w = max(0, s - R::kStages); w < s; ++w)
                     bar_wait(&full[w % R::kStages], (w / R::kStages) & 1, &never);
-            else if (!ok)
+            for (int w = max(0, s - R::kStages); ok && w < s; ++w)
+                ok = bar_wait(&empty[w % R::kStages], (w / R::kStages) & 1, &stop);
+            if (rank != 0 && !ok)
                 for (const uint64_t t = now_ns(); now_ns() - t < 10000000ull;) __nanosleep(1000);
         }
     } else if (warp == 1) {
@@ -581,6 +584,10 @@ k_linear_product(const __grid_constant__ CUtensorMap ma, const __grid_constant__
             int never = 0;
             commit(&drained);
             bar_wait(&drained, 0, &never);
+        } else if (lane == 0) {
+            // the pair's last commit arrives here as well, and must not come after the CTA's end
+            int never = 0;
+            bar_wait_cluster(&drained, 0, &never);
         }
     } else if (warp >= 4) {
         // ---- finishing: a thread to a row of the tile, two warps to 32 rows ----
