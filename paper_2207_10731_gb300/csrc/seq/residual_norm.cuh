@@ -240,9 +240,11 @@ struct Held<T, 8, CH, true> {
                         asm volatile("cp.async.cg.shared.global [%0], [%1], 16;"
                                      :: "r"(slot(stage, c, h)), "l"(from) : "memory");
                     } else {
+                        // no bytes at all are copied from the vector's own start: the row's may
+                        // lie off the 16-byte grid, which no copy's source may
                         const int left = (sh.cols - at) * (int)sizeof(T) - 16 * h;
                         asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;"
-                                     :: "r"(slot(stage, c, h)), "l"(left > 0 ? from : row),
+                                     :: "r"(slot(stage, c, h)), "l"(left > 0 ? from : row + at),
                                         "r"(min(max(left, 0), 16)) : "memory");
                     }
                 }
