@@ -101,27 +101,21 @@ int64_t lay_out(const pss_attention_shape& s, bool backward, void* base, Plan* p
     p->per_item = !backward && ctas >= 8 * sms && s.q_tokens >= 512 * s.sequences ? 2 : 1;
     p->keys = backward ? backward_columns(s) : kTile;
     p->key_tokens = backward_columns(s) / group;
-    int64_t at = 0;
-    char* b = static_cast<char*>(base);
-    auto take = [&](int64_t bytes) {
-        char* q = b + at;
-        at += (bytes + 255) / 256 * 256;
-        return q;
-    };
+    Take take(base);
     p->most_items = (int)((p->tiles + p->per_item - 1) / p->per_item + slots);
     p->most_slots = (int)slots;
-    p->head = reinterpret_cast<PlanHead*>(take(sizeof(PlanHead)));
-    p->items = reinterpret_cast<Item*>(take(p->most_items * sizeof(Item)));
-    p->q_range = reinterpret_cast<Range*>(take(s.q_tokens * sizeof(Range)));
+    p->head = static_cast<PlanHead*>(take(sizeof(PlanHead)));
+    p->items = static_cast<Item*>(take(p->most_items * sizeof(Item)));
+    p->q_range = static_cast<Range*>(take(s.q_tokens * sizeof(Range)));
     if (backward) {
-        p->key_items = reinterpret_cast<Item*>(take(p->key_tiles * sizeof(Item)));
-        p->k_range = reinterpret_cast<Range*>(take(s.k_tokens * sizeof(Range)));
-        p->stats = reinterpret_cast<float2*>(take(s.q_tokens * s.heads * 8));
+        p->key_items = static_cast<Item*>(take(p->key_tiles * sizeof(Item)));
+        p->k_range = static_cast<Range*>(take(s.k_tokens * sizeof(Range)));
+        p->stats = static_cast<float2*>(take(s.q_tokens * s.heads * 8));
     }
-    p->joins = reinterpret_cast<Join*>(take(slots / 2 * sizeof(Join)));
-    p->partial = reinterpret_cast<float*>(take(slots * s.kv_heads * kTile * s.dim * 4));
-    p->partial_lse = reinterpret_cast<float*>(take(slots * s.kv_heads * kTile * 4));
-    return at;
+    p->joins = static_cast<Join*>(take(slots / 2 * sizeof(Join)));
+    p->partial = static_cast<float*>(take(slots * s.kv_heads * kTile * s.dim * 4));
+    p->partial_lse = static_cast<float*>(take(slots * s.kv_heads * kTile * 4));
+    return take.bytes();
 }
 
 // Nothing to do but to say so.

@@ -554,30 +554,24 @@ struct Work {
 };
 // Where each part of the workspace lies; returns the bytes.
 int64_t lay_out(int64_t tokens, int64_t rows, int64_t cols, void* base, Work* w) {
-    int64_t at = 0;
-    char* b = static_cast<char*>(base);
-    auto take = [&](int64_t bytes) {
-        char* q = b + at;
-        at += (bytes + 255) / 256 * 256;
-        return q;
-    };
+    Take take(base);
     *w = Work{};
     w->stride = (cols + kPer - 1) / kPer * kPer;
-    w->count = reinterpret_cast<unsigned long long*>(take(16));
-    w->done = reinterpret_cast<uint32_t*>(take(4));
-    w->sorted = reinterpret_cast<unsigned long long*>(take(8 * tokens));
-    w->sums = reinterpret_cast<float*>(take(tokens / kChunk * w->stride * 4));
-    w->large = reinterpret_cast<float*>(take(tokens / kLarge * w->stride * 4));
+    w->count = static_cast<unsigned long long*>(take(16));
+    w->done = static_cast<uint32_t*>(take(4));
+    w->sorted = static_cast<unsigned long long*>(take(8 * tokens));
+    w->sums = static_cast<float*>(take(tokens / kChunk * w->stride * 4));
+    w->large = static_cast<float*>(take(tokens / kLarge * w->stride * 4));
     if (tokens > kSmall) {
         const RadixPlan plan = radix_plan((uint64_t)(rows > 0 ? rows : 1), 0);
-        w->other = reinterpret_cast<unsigned long long*>(take(8 * tokens));
-        w->keys = reinterpret_cast<uint32_t*>(take(4 * tokens));
-        w->places = reinterpret_cast<uint32_t*>(take(4 * tokens));
-        w->cnt = reinterpret_cast<uint32_t*>(take(4 * radix_tiles(tokens, sort_tile(tokens)) << plan.bits[0]));
-        w->tot = reinterpret_cast<uint32_t*>(take(4 << kRadixMaxBits));
-        w->dstart = reinterpret_cast<uint32_t*>(take(4 << kRadixMaxBits));
+        w->other = static_cast<unsigned long long*>(take(8 * tokens));
+        w->keys = static_cast<uint32_t*>(take(4 * tokens));
+        w->places = static_cast<uint32_t*>(take(4 * tokens));
+        w->cnt = static_cast<uint32_t*>(take(4 * radix_tiles(tokens, sort_tile(tokens)) << plan.bits[0]));
+        w->tot = static_cast<uint32_t*>(take(4 << kRadixMaxBits));
+        w->dstart = static_cast<uint32_t*>(take(4 << kRadixMaxBits));
     }
-    return at;
+    return take.bytes();
 }
 
 cudaError_t sort_tokens(const int64_t* ids, int64_t tokens, int64_t rows, const Work& w,

@@ -121,16 +121,6 @@ namespace {
 constexpr int64_t kMost = (int64_t(1) << 31) - 1024;
 constexpr int kFewTokens = 64;   // up to here the tokens are the product's columns
 
-struct Take {
-    char* base;
-    int64_t at = 0;
-    void* operator()(int64_t bytes) {
-        char* p = base + at;
-        at += (bytes + 255) / 256 * 256;
-        return p;
-    }
-};
-
 bool types_ok(int32_t type, int32_t wide) {
     return (type == PSS_BF16 || type == PSS_F16) && (wide == type || wide == PSS_F32);
 }
@@ -190,7 +180,7 @@ int64_t lay_out(const pss_linear_forward_args* a, void* base, ForwardCall* c) {
         return -1;
     c->x = Matrix{a->x, a->tokens, a->in, a->x_stride};
     if (a->tokens == 0) return 0;
-    Take take{static_cast<char*>(base)};
+    Take take(base);
     if (!on_grid(c->x)) c->x_copy = take(copy_bytes(c->x));
     if (!on_grid(c->w)) c->w_copy = take(copy_bytes(c->w));
     c->p.f = Finish{a->bias, a->residual, a->z, a->y, a->residual_stride, a->z_stride, a->y_stride,
@@ -200,7 +190,7 @@ int64_t lay_out(const pss_linear_forward_args* a, void* base, ForwardCall* c) {
                      rows16(a->residual, a->residual_stride, size);
     orient(&c->p, Operand{c->x, false}, Operand{c->w, c->w_along_out});
     c->p.partial = static_cast<float*>(take(partial_values(c->p) * 4));
-    return take.at;
+    return take.bytes();
 }
 
 struct BackwardCall {
@@ -226,7 +216,7 @@ int64_t lay_out(const pss_linear_backward_args* a, void* base, BackwardCall* c) 
                                      a->dweight_out_stride, &dw, &c->dw_along_out))
         return -1;
     if (a->tokens == 0) return 0;
-    Take take{static_cast<char*>(base)};
+    Take take(base);
     c->x = Matrix{a->x, a->tokens, a->in, a->x_stride};
     c->dz = Matrix{a->grad, a->tokens, a->out, a->grad_stride};
     c->needs_dz = (a->dx || a->dweight) &&
@@ -256,7 +246,7 @@ int64_t lay_out(const pss_linear_backward_args* a, void* base, BackwardCall* c) 
         shared = std::max(shared, partial_values(c->dw));
     }
     c->dx.partial = c->dw.partial = static_cast<float*>(take(shared * 4));
-    return take.at;
+    return take.bytes();
 }
 
 pss_status clear_status(int64_t* status, cudaStream_t st) {

@@ -163,6 +163,22 @@ inline bool aligned8(const void* p, int64_t stride, size_t size) {
 inline int past8(const void* p, size_t size) { return (int)((uintptr_t)p / size % 8); }
 inline bool aligned_to(const void* p, size_t n) { return ((uintptr_t)p % n) == 0; }
 
+// Hands out the parts of a workspace, each a multiple of 256 bytes behind the first.  A workspace
+// need only be 16-byte aligned, but fp32 values are moved 32 bytes at a time, so the first
+// part lies at the workspace's first multiple of 32, for which bytes() has room.
+struct Take {
+    char* base;
+    int64_t at = 0;
+    explicit Take(void* workspace)
+        : base(reinterpret_cast<char*>(((uintptr_t)workspace + 31) / 32 * 32)) {}
+    void* operator()(int64_t bytes) {
+        char* p = base + at;
+        at += (bytes + 255) / 256 * 256;
+        return p;
+    }
+    int64_t bytes() const { return at > 0 ? at + 16 : 0; }
+};
+
 inline int sm_count() {
     static int cached[64] = {};
     int dev = 0;
