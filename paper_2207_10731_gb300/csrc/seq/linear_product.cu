@@ -191,6 +191,12 @@ __device__ __forceinline__ uint4 get_piece(uint32_t at) {
                  : "=r"(w.x), "=r"(w.y), "=r"(w.z), "=r"(w.w) : "r"(at) : "memory");
     return w;
 }
+// The word w as it is, or its half h.
+__device__ __forceinline__ void put_raw(float* to, uint32_t w, int) { *to = __uint_as_float(w); }
+template <typename T>
+__device__ __forceinline__ void put_raw(T* to, uint32_t w, int h) {
+    *reinterpret_cast<uint16_t*>(to) = (uint16_t)(w >> (16 * h));
+}
 // 32 values of row `row`, from its piece p on.
 template <typename T>
 __device__ __forceinline__ void put32(uint32_t tile, int row, int p, const float (&v)[32], T) {
@@ -318,7 +324,9 @@ __device__ __forceinline__ void finish_row(const Finish& f, float (&v)[32], int6
 
 // A finishing warp's part of a tile, rows row0 .. +32 and columns col .. of the accumulator at d:
 // tiles of 128 bytes' width (64 columns of 16 bits, 32 of fp32) are made in shared memory,
-// over the residual's where there is one, and stored by TMA, which leaves out what lies outside.
+// over the residual's where there is one, and stored by TMA, which leaves out what lies outside, but
+// writes whole 16-byte pieces: its maps end with the last whole one (launch), and what a row has
+// behind that, its lane stores value by value.
 // z goes first, and y from the accumulator again.  wait(): until the accumulator is there;
 // asked for after the first residual.
 template <int BN, typename T, typename TY, typename W>
@@ -335,12 +343,22 @@ __device__ __forceinline__ bool finish_tiles(const Args& a, const CUtensorMap* m
         if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
         __syncwarp();
     };
-    auto store = [&](const CUtensorMap* map, int col, int part) {
+    constexpr int kValues = 16 / sizeof(TY);
+    const int whole = partial ? a.n : a.n / kValues * kValues;
+    auto store = [&](const CUtensorMap* map, TY* to, int64_t stride, int col, int part) {
         fence_async();
         __syncwarp();
-        if (lane == 0) {
+        if (lane == 0 && col < whole) {
             tma_store(map, tile, col, row0, part);
             asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+        }
+        if (whole < a.n && whole < col + kWide && row0 + lane < a.m) {
+            const uint4 w = get_piece(piece_at(tile, lane, (whole - col) / kValues));
+            const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+            TY* row = to + (row0 + lane) * stride + whole;
+#pragma unroll
+            for (int i = 0; i < kValues - 1; ++i)
+                if (whole + i < a.n) put_raw(row + i, x[i / (kValues / 4)], i % (kValues / 4));
         }
     };
     auto sums = [&](float (&v)[32], int c, int col) {
@@ -391,7 +409,7 @@ __device__ __forceinline__ bool finish_tiles(const Args& a, const CUtensorMap* m
                 }
             }
             if (sizeof(TY) == 2) {
-                store(mz, col, 0);
+                store(mz, static_cast<TY*>(f.z), f.z_stride, col, 0);
                 tile_free();
             }
             if (more) fetch();
@@ -413,7 +431,7 @@ __device__ __forceinline__ bool finish_tiles(const Args& a, const CUtensorMap* m
             }
             put32(tile, lane, h / (16 / (int)sizeof(TY)), v, TY());
         }
-        store(my, col, partial ? split : 0);
+        store(my, static_cast<TY*>(f.y), f.y_stride, col, partial ? split : 0);
     }
     return waited || wait();
 }
@@ -775,12 +793,16 @@ cudaError_t operand_map(CUtensorMap* map, const Operand& o, int box, bool boxes,
 }
 
 // Results [parts][rows][cols], stored in boxes of `width` columns (at most 128 bytes) x 32 rows.
+// TMA leaves out what lies outside the tensor by 16-byte pieces only: a store to 517 columns of
+// 16 bits writes 520.  What is behind a row's last whole piece is not TMA's, then, unless the rows
+// have room for it (`padded`).
 cudaError_t result_map(CUtensorMap* map, void* data, int64_t cols, int64_t rows, int64_t parts,
-                       int64_t stride, int64_t part_stride, int width, int type) {
+                       int64_t stride, int64_t part_stride, int width, int type, bool padded) {
     static std::atomic<void*> found{nullptr};
     void* fn = driver_call("cuTensorMapEncodeTiled", &found);
     if (!fn) return cudaErrorNotSupported;
     const int64_t size = type == PSS_F32 ? 4 : 2, grid = 16 / size;
+    if (!padded) cols = cols < grid ? grid : cols / grid * grid;   // (of less than a piece: never used)
     if (rows <= 1) stride = (cols + grid - 1) / grid * grid;       // free, but checked
     if (parts <= 1) part_stride = stride;
     const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)parts};
@@ -810,12 +832,14 @@ cudaError_t launch(const Product& p, int type, unsigned long long* status, cudaS
     if (f.tiles && e == cudaSuccess) {
         const int width = 64;   // 128 bytes, also where BN = 32 is all there is
         if (split)
-            e = result_map(&my, p.partial, p.n, p.m, p.splits, p.ld, (int64_t)p.m * p.ld, 32, PSS_F32);
+            e = result_map(&my, p.partial, p.n, p.m, p.splits, p.ld, (int64_t)p.m * p.ld, 32, PSS_F32,
+                           true);
         else
             e = result_map(&my, f.y, p.n, p.m, 1, f.y_stride, (int64_t)p.m * f.y_stride,
-                           f.y_f32 ? 32 : width, f.y_f32 ? PSS_F32 : type);
+                           f.y_f32 ? 32 : width, f.y_f32 ? PSS_F32 : type, false);
         if (!split && f.z && !f.y_f32 && e == cudaSuccess)
-            e = result_map(&mz, f.z, p.n, p.m, 1, f.z_stride, (int64_t)p.m * f.z_stride, width, type);
+            e = result_map(&mz, f.z, p.n, p.m, 1, f.z_stride, (int64_t)p.m * f.z_stride, width, type,
+                           false);
     }
     if (e != cudaSuccess) return e;
     auto* k = k_linear_product<BN, PAIR, T>;
