@@ -38,8 +38,9 @@ template <int ACT>
 __device__ __forceinline__ float activate(float z) {
     if (ACT == ACT_RELU) return z < 0.f ? 0.f : z;   // NaN stays
     if (ACT == ACT_GELU) {
+        // q is zero from 15 on: from there z itself, also where it is infinite and z q is not a number
         const float q = normal_below(fabsf(z), __expf(-0.5f * z * z));
-        return z < 0.f ? z * q : z - z * q;
+        return z < 0.f ? z * q : z - fminf(z, 128.f) * q;
     }
     if (ACT == ACT_SILU) {
         const float e = __expf(-fabsf(z)), inv = z * reciprocal(1.f + e);
