@@ -948,7 +948,8 @@ void plan_product(Product* p) {
         const int cycles = kind.pair && p->b.across ? 540 : kind.cycles;
         for (int s = 1; s <= 64 && s <= p->blocks; ++s) {
             const int64_t rounds = (tiles * s + fit - 1) / fit;
-            double cost = 2000. + (double)rounds * ((p->blocks + s - 1) / s * cycles + 300.);
+            const double most = (p->blocks + s - 1) / s;   // blocks of a unit, below 2^25
+            double cost = 2000. + (double)rounds * (most * cycles + 300.);
             // written and read at some 1800 bytes a cycle each, and a launch
             if (s > 1) cost += 4000. + (double)p->m * p->n * s * 8 / 1800;
             if (p->bn == 0 || cost < best) {

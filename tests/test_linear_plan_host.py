@@ -1,0 +1,24 @@
+"""How products are dealt out, without a GPU: what the sizes of workspaces say of it."""
+import pytest
+
+from paper_2207_10731_gb300 import binding, build, sequence
+
+
+@pytest.fixture(scope="module")
+def lib():
+    build.build()
+    return binding.load_library()
+
+
+def weight_gradient(lib, tokens, n=8, m=8):
+    """Bytes of the parts of dweight alone, [n, m] in bf16."""
+    at = sequence._packed(sequence._BACKWARD, tokens, n, m, 4096, m, 4096, n, 4096, m, 1, 0, m, 0, n,
+                          4096, m, 1, 0, 1, 1, 1, 0)
+    return lib.pss_linear_backward_workspace(at)
+
+
+@pytest.mark.parametrize("tokens", [10 ** 7, 10 ** 8, 440 * 10 ** 6, 550 * 10 ** 6, 10 ** 9, 2 ** 31 - 1025])
+def test_long_contractions_are_split(lib, tokens):
+    # one tile: its contraction is dealt out to as many CTAs as ten million tokens are, and more
+    # tokens change nothing
+    assert weight_gradient(lib, tokens) == weight_gradient(lib, 10 ** 6) > 0
