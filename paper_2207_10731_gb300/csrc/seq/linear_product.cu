@@ -763,9 +763,9 @@ k_linear_join(const float* __restrict__ partial, int splits, int64_t rows, int c
 }
 
 // Whether an operand across the contraction may be loaded two boxes of 64 at a time: its rows are
-// seen as boxes beside each other then, all of them whole.
+// seen as boxes beside each other then, all of them whole, and each CTA's begin with one.
 bool in_boxes(const Operand& o, int rows) {
-    return o.across && rows > 64 && o.matrix.inner % 64 == 0;
+    return o.across && rows == 128 && o.matrix.inner % 64 == 0;
 }
 
 // Boxes of 64 along the dense dimension and `box` (at most 256) along the other; or, across and
@@ -944,7 +944,8 @@ void plan_product(Product* p) {
         if (kind.pair && p->m <= 128) continue;
         const int m_tiles = (p->m + rows - 1) / rows, n_tiles = (p->n + bn - 1) / bn;
         const int64_t tiles = (int64_t)m_tiles * n_tiles;
-        // across the contraction B comes in boxes of 64, two to a CTA of any of these pairs
+        // across the contraction B comes in boxes of 64, two to a CTA of any of these pairs: none is
+        // cheaper than 256 columns
         const int cycles = kind.pair && p->b.across ? 540 : kind.cycles;
         for (int s = 1; s <= 64 && s <= p->blocks; ++s) {
             const int64_t rounds = (tiles * s + fit - 1) / fit;
