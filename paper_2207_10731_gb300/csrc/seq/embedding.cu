@@ -86,6 +86,15 @@ __device__ __forceinline__ void note_outside(unsigned long long* status, int64_t
     if (status) atomicMin(status, (unsigned long long)t);
 }
 
+// The status of a call that has no value to read or write.
+__global__ void __launch_bounds__(kThreads)
+k_embedding_check(const int64_t* __restrict__ ids, int64_t tokens, int64_t rows,
+                  unsigned long long* status) {
+    pdl_prologue();
+    const int64_t t = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    if (t < tokens && (uint64_t)ids[t] >= (uint64_t)rows) note_outside(status, t);
+}
+
 // U tokens to a group, all their loads in flight (four in vectors: two 162 us and eight 197 for
 // 1.7 M x 128; value by value two, 53 instead of 59 us for 100000 x 333).
 template <typename TW, typename TO, bool VECTOR, int U>
@@ -607,6 +616,15 @@ pss_status clear_status(int64_t* status, cudaStream_t st) {
     return status ? status_of(cudaMemsetAsync(status, 0xff, 8, st)) : PSS_OK;
 }
 
+// For tables without rows or columns: the ids are looked at for the status alone.
+pss_status check_only(const int64_t* ids, int64_t tokens, int64_t rows, int64_t* status,
+                      cudaStream_t st) {
+    if (!status || tokens == 0) return PSS_OK;
+    return status_of(launch_k(k_embedding_check, dim3((unsigned)((tokens + kThreads - 1) / kThreads)),
+                              dim3(kThreads), 0, st, ids, tokens, rows,
+                              reinterpret_cast<unsigned long long*>(status)));
+}
+
 }  // namespace
 
 extern "C" pss_status pss_embedding_forward(const void* weight, pss_dtype weight_type,
@@ -620,10 +638,10 @@ extern "C" pss_status pss_embedding_forward(const void* weight, pss_dtype weight
     if (cols > kMostCols) return PSS_ERR_UNSUPPORTED;
     if (status && !(device_ptr(status) && aligned_to(status, 8))) return PSS_ERR_INVALID_ARG;
     const bool some = tokens > 0 && cols > 0;
+    if ((some || (status && tokens > 0)) && (!device_ptr(ids) || !aligned_to(ids, 8)))
+        return PSS_ERR_INVALID_ARG;
     if (some) {
-        if (!device_ptr(ids) || !aligned_to(ids, 8) || !device_ptr(out) ||
-            !aligned_to(out, dtype_size(out_type)))
-            return PSS_ERR_INVALID_ARG;
+        if (!device_ptr(out) || !aligned_to(out, dtype_size(out_type))) return PSS_ERR_INVALID_ARG;
         if (rows > 0 && (!device_ptr(weight) || !aligned_to(weight, dtype_size(weight_type))))
             return PSS_ERR_INVALID_ARG;
     }
@@ -638,7 +656,8 @@ extern "C" pss_status pss_embedding_forward(const void* weight, pss_dtype weight
     if (some && n == 0) return PSS_ERR_UNSUPPORTED;
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     const pss_status rc = clear_status(status, st);
-    if (rc != PSS_OK || !some) return rc;
+    if (rc != PSS_OK) return rc;
+    if (!some) return check_only(ids, tokens, rows, status, st);
     return status_of(with_type(weight_type, [&](auto tw) {
         return with_type(out_type, [&](auto to) {
             using TW = decltype(tw);
@@ -695,7 +714,8 @@ extern "C" pss_status pss_embedding_backward(const void* grad, pss_dtype grad_ty
     }
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     const pss_status rc = clear_status(status, st);
-    if (rc != PSS_OK || !some) return rc;
+    if (rc != PSS_OK) return rc;
+    if (!some) return check_only(ids, tokens, rows, status, st);
     if (tokens == 0)
         return status_of(cudaMemset2DAsync(dweight, dweight_stride * dtype_size(dweight_type), 0,
                                            cols * dtype_size(dweight_type), rows, st));
