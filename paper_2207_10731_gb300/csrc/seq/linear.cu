@@ -130,10 +130,12 @@ bool sizes_ok(int64_t tokens, int64_t in, int64_t out) {
 bool ok(const void* p, size_t size) { return device_ptr(p) && aligned_to(p, size); }
 
 // A matrix [in][out] with one dense dimension; the stride over a single row or column is
-// free.
+// free.  A dense column is one row of `in` values, not `in` rows of one value (which would
+// lie off the 16-byte grid and be copied).
 bool weight_matrix(const void* data, int64_t in, int64_t out, int64_t in_stride,
                    int64_t out_stride, Matrix* m, bool* along_out) {
-    if ((out == 1 || out_stride == 1) && (in == 1 || in_stride >= out)) {
+    const bool column = out == 1 && in > 1 && in_stride == 1;
+    if (!column && (out == 1 || out_stride == 1) && (in == 1 || in_stride >= out)) {
         *m = Matrix{data, in, out, in_stride};
         *along_out = true;
         return true;

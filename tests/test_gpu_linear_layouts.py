@@ -88,3 +88,26 @@ def test_weight_gradients_of_every_tile_width(out, tokens):
         check(dw, x.double().t() @ g.double(), size * 2 * (tokens + 2) * 2.0 ** -24, "dweight")
         _, dw, _ = sequence.linear_backward(g, x, w.t().contiguous().t(), dx=False, dbias=False)
         check(dw, x.double().t() @ g.double(), size * 2 * (tokens + 2) * 2.0 ** -24, "dweight, in dense")
+
+
+@pytest.mark.parametrize("tokens", [1, 40, 300, 5000])
+@pytest.mark.parametrize("n", [1, 60, 333, 1024])
+@pytest.mark.parametrize("strides", ["dense", "other stride", "row apart", "off the grid"])
+def test_single_columns(tokens, n, strides):
+    """A weight [n, 1], as a gate's, however its n values lie."""
+    kind = torch.bfloat16
+    whole = normal(2, 1, n * 8 + 8, dtype=kind, scale=n ** -0.5)[0]
+    at, step, other = {"dense": (0, 1, 1), "other stride": (8, 1, n + 3), "row apart": (0, 8, 1),
+                       "off the grid": (1, 1, 1)}[strides]
+    w = whole.as_strided((n, 1), (step, other), at)
+    x, bias, grad = normal(1, tokens, n, dtype=kind), normal(3, 1), normal(5, tokens, 1, dtype=kind)
+    y = sequence.linear_forward(x, w, bias)
+    check(y, *forward(x, w, bias, None, None)[0], "y")
+    other = torch.full_like(whole, 9.0).as_strided(w.shape, w.stride(), at)
+    for dweight in (True, other):
+        back = sequence.linear_backward(grad, x, w, dweight=dweight)
+        for what, g, v in zip(("dx", "dweight", "dbias"), back, backward(grad, x, w, None, None, None)):
+            check(g, v[0], v[1], what)
+    marks = torch.full_like(whole, 9.0)
+    marks.as_strided(w.shape, w.stride(), at).copy_(other)
+    assert torch.equal(other._base if other._base is not None else other, marks)

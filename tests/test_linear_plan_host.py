@@ -22,3 +22,22 @@ def test_long_contractions_are_split(lib, tokens):
     # one tile: its contraction is dealt out to as many CTAs as ten million tokens are, and more
     # tokens change nothing
     assert weight_gradient(lib, tokens) == weight_gradient(lib, 10 ** 6) > 0
+
+
+@pytest.mark.parametrize("n", [8, 60, 1024])
+def test_a_dense_column_is_read_in_place(lib, n):
+    """A weight [n, 1], as a gate's: neither direction has a copy of it to make."""
+    def forward(w, wi, wo):
+        return lib.pss_linear_forward_workspace(sequence._packed(
+            sequence._FORWARD, 1000, n, 1, 4096, up, w, wi, wo, 0, 0, 1, 4096, 1, 0, 1, 1, 1, 0, 0))
+
+    def backward(w, wi, wo):   # dx alone, with the upstream gradient on the grid
+        return lib.pss_linear_backward_workspace(sequence._packed(
+            sequence._BACKWARD, 1000, n, 1, 4096, 8, 4096, up, w, wi, wo, 0, 1, 4096, n, 0, 1, 1, 0,
+            1, 1, 1, 0))
+    up = -(-n // 8) * 8
+    for call in (forward, backward):
+        rows = call(4096, 8, 1)                 # rows of one value, each on the grid
+        assert call(4096, 1, 1) <= rows         # a dense column
+        assert call(4096, 1, n) <= rows         # its other stride is free
+        assert call(4098, 1, 1) >= rows + -(-n * 2 // 256) * 256   # off the grid: copied
