@@ -1,6 +1,7 @@
 // Device helpers of libpss: the location hash and small memory primitives.
 #pragma once
 
+#include <atomic>
 #include <cstdint>
 #include <cuda_runtime.h>
 
@@ -111,6 +112,29 @@ cudaError_t launch_k(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t sme
     cfg.attrs = attr;
     cfg.numAttrs = 1;
     return cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);
+}
+
+// Lets a kernel have all the dynamic shared memory that there is beside its own, once a device.  The
+// limit is the kernel's, not the call's: set by each call to what that call needs, it would be
+// another thread's too, between that one's setting and its launch (a call in 3000 refused, two
+// threads calling the norms' backward on rows of 2048 and 1536 as fast as they can).
+template <typename K>
+cudaError_t allow_most_smem(K* kernel, std::atomic<uint64_t>* ready) {
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    const uint64_t bit = 1ull << (dev & 63);
+    if (dev < 64 && (ready->load(std::memory_order_acquire) & bit)) return cudaSuccess;
+    int most = 0;
+    e = cudaDeviceGetAttribute(&most, cudaDevAttrMaxSharedMemoryPerBlockOptin, dev);
+    if (e != cudaSuccess) return e;
+    cudaFuncAttributes built;
+    e = cudaFuncGetAttributes(&built, kernel);
+    if (e != cudaSuccess) return e;
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                             most - (int)built.sharedSizeBytes);
+    if (e == cudaSuccess) ready->fetch_or(bit, std::memory_order_release);
+    return e;
 }
 
 inline int ceil_log2(int v) {

@@ -1446,8 +1446,8 @@ cudaError_t radix_pass(const SortedBuffers& sb, const unsigned long long* in,
                  st, sb.cnt, ntiles, bits, sb.tot, sb.dstart, sb.done, sb.stats);
     if (e != cudaSuccess) return e;
     const size_t smem = radix_down_smem(nd, PER);
-    e = cudaFuncSetAttribute(k_radix_down<FIRST, SG, PER>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                             (int)smem);
+    static std::atomic<uint64_t> ready{0};
+    e = allow_most_smem(k_radix_down<FIRST, SG, PER>, &ready);
     if (e != cudaSuccess) return e;
     return launch_k(k_radix_down<FIRST, SG, PER>, dim3(ntiles), dim3(kRThreads), smem, st, sb.pair_x,
                     sb.q_row, in, out, npairs, sb.stats, J, log2J, shift, bits, ntiles, sb.cnt,

@@ -287,8 +287,8 @@ cudaError_t launch_backward(const TG* g, int64_t gs, const TX* x, int64_t xs, co
     const size_t smem =
         SUMS == SHARED ? (size_t)8 * cols : s.lanes <= 32 ? (size_t)s.groups * 8 * cols : 0;
     if (smem > 48 * 1024) {
-        const cudaError_t e =
-            cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        static std::atomic<uint64_t> ready{0};
+        const cudaError_t e = allow_most_smem(k, &ready);
         if (e != cudaSuccess) return e;
     }
     const Shape sh{rows, cols, s.lanes, s.log2_lanes, s.groups, lie.shift0, lie.step};

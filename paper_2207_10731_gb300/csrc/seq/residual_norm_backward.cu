@@ -385,9 +385,8 @@ extern "C" pss_status pss_residual_norm_backward(
                 kind <= DOUBLE ? std::max(ahead, (size_t)s.groups * 8 * cols)
                               : ahead + (size_t)8 * F::kVectors * decltype(vec)::value * s.threads;
             cudaError_t e = cudaSuccess;
-            if (smem + 1024 > 48 * 1024)   // 48 KB with the kernel's own
-                e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                         (int)smem);
+            static std::atomic<uint64_t> ready{0};
+            if (smem + 1024 > 48 * 1024) e = allow_most_smem(kernel, &ready);   // 48 KB with the kernel's own
             if (e != cudaSuccess) return e;
             const int n = ctas_of(
                 rows, s, [&] { return resident(kernel, s.threads, smem, norm_per_sm(cols)); },
