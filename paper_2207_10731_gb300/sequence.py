@@ -378,9 +378,9 @@ def embedding_forward(weight, ids, scale: float = 1.0, out=None, out_dtype=None,
         out = torch.empty((*ids.shape, cols), dtype=out_dtype or weight.dtype, device=weight.device)
         os = cols
     else:
+        _tensor(out, "out", device)
         if out_dtype is not None and out.dtype != out_dtype:
             raise TypeError(f"out must be {out_dtype}, got {out.dtype}")
-        _tensor(out, "out", device)
         if out.shape != (*ids.shape, cols):
             raise ValueError(f"out must have shape {(*ids.shape, cols)}, got {tuple(out.shape)}")
         os = _rows(out, "out", device)[2]
@@ -410,6 +410,7 @@ def embedding_backward(grad, ids, rows: int, scale: float = 1.0, out=None, out_d
         out = torch.empty((rows, cols), dtype=out_dtype or torch.float32, device=grad.device)
         os = cols
     else:
+        _tensor(out, "out", device)
         if out_dtype is not None and out.dtype != out_dtype:
             raise TypeError(f"out must be {out_dtype}, got {out.dtype}")
         os = _table(out, "out", device, rows, cols)
@@ -429,9 +430,9 @@ def _gate(gate, x, name, device):
     """(data, kind, stride) of a gate: one value to each of x's, or one to a row."""
     if gate is None:
         return None, 0, 0
+    _tensor(gate, name, device)
     if gate.shape == x.shape and x.shape[-1] != 1:
         return gate.data_ptr(), 2, _rows(gate, name, device, dtype=x.dtype)[2]
-    _tensor(gate, name, device)
     if gate.shape != (*x.shape[:-1], 1):
         raise ValueError(f"{name} must have shape {tuple(x.shape)} or {(*x.shape[:-1], 1)}, "
                          f"got {tuple(gate.shape)}")
@@ -646,6 +647,8 @@ def linear_forward(x, weight, bias=None, activation=None, residual=None, keep: b
     m = weight.shape[1]
     if weight.shape[0] != n:
         raise ValueError(f"weight must have {n} rows, got {weight.shape[0]}")
+    if out is not None:
+        _tensor(out, "out", device)
     kind = out.dtype if out is not None and out_dtype is None else out_dtype or x.dtype
     if kind != x.dtype and kind != torch.float32:
         raise TypeError(f"out_dtype must be {x.dtype} or torch.float32, got {kind}")
@@ -701,7 +704,8 @@ def linear_backward(grad, x, weight, z=None, activation=None, dx=True, dweight=T
     if act:
         if z is None:
             raise ValueError("z is needed with an activation")
-        pz, zs = z.data_ptr(), _rows(z, "z", device, like=grad, dtype=x.dtype)[2]
+        zs = _rows(z, "z", device, like=grad, dtype=x.dtype)[2]
+        pz = z.data_ptr()
     px = pdw = pb = 0
     dxs, dwi, dwo = n, 0, 0
     kind = weight.dtype
@@ -719,8 +723,10 @@ def linear_backward(grad, x, weight, z=None, activation=None, dx=True, dweight=T
                 dweight = torch.empty((n, m), dtype=kind, device=x.device)
             else:
                 dweight = torch.empty((m, n), dtype=kind, device=x.device).t()
-        elif dweight_dtype is not None and dweight.dtype != dweight_dtype:
-            raise TypeError(f"dweight must be {dweight_dtype}, got {dweight.dtype}")
+        else:
+            _tensor(dweight, "dweight", device)
+            if dweight_dtype is not None and dweight.dtype != dweight_dtype:
+                raise TypeError(f"dweight must be {dweight_dtype}, got {dweight.dtype}")
         pdw, dwi, dwo = _weight(dweight, "dweight", device, (x.dtype, torch.float32), weight.shape)
         kind = dweight.dtype
     if dbias is False or dbias is None:
