@@ -618,7 +618,8 @@ pss_status pss_residual_norm_backward(
  * A product with its bias, activation and residual in one pass over the result:
  *   z = x weight + bias,   y = act(z) + residual,
  * x[tokens][in], weight[in][out], the sums in fp32, z and y rounded once each.
- *   act: PSS_ACT_NONE, RELU, GELU (z Phi(z), the exact form), SILU (z sigmoid(z)).
+ *   act: PSS_ACT_NONE, RELU, GELU (z Phi(z), the exact form), SILU (z sigmoid(z)); the latter two
+ *   are +infinity at +infinity and, infinity times zero, NaN at -infinity.
  */
 typedef enum { PSS_ACT_NONE = 0, PSS_ACT_RELU = 1, PSS_ACT_GELU = 2, PSS_ACT_SILU = 3 } pss_activation;
 typedef struct {
@@ -659,7 +660,8 @@ pss_status pss_linear_forward(const pss_linear_forward_args* args, void* workspa
  * Its gradients, for the upstream gradient of y (the residual's gradient is that one itself):
  *   dz = grad act'(z),  dx = dz weight^T,  dweight = x^T dz,  dbias = sum over tokens of dz.
  * dz enters the two products rounded to `type`; dbias is the sum of the unrounded values.  All
- * sums are fp32, in a fixed order.  Results that are NULL are not computed.
+ * sums are fp32, in a fixed order.  Results that are NULL are not computed.  What results are made
+ * of where they overlap an input or each other is undefined.
  */
 typedef struct {
     int64_t tokens, in, out;

@@ -683,6 +683,7 @@ def linear_backward(grad, x, weight, z=None, activation=None, dx=True, dweight=T
     dx, dweight and dbias is True, False (not wanted: None is returned) or the
     tensor to fill.  dx has x's type and shape; dweight lies in memory as weight does,
     in ``dweight_dtype`` (weight's type, the default, or float32); dbias is float32.
+    They may not overlap the inputs or each other.
     grad * act'(z) enters the products rounded to x's type, and dbias unrounded."""
     if stream is not None:
         return _under(stream, linear_backward, grad, x, weight, z, activation, dx, dweight, dbias,
